@@ -261,20 +261,19 @@ def prepare(case, seed):
 # ---------------------------------------------------------------------------------------------------- plain forms
 
 def _norm_rotate(x, gain, table, pos, axis_pairs, interleaved):
-    """float32, every operation rounded once; the squares are added by folding each block of 32 channels in halves, then the
-    blocks (filled up with zeros to a power of two) in halves"""
+    """float32, every operation rounded once; the squares are added by folding every run of 8 channels in halves, then the runs
+    of the row's two halves pairwise, then these sums (filled up with zeros to a power of two) in halves"""
     x = x.float()
     t, h, dim = x.shape
-    s = (x * x).view(t, h, dim // 32, 32)
-    s = s[..., :16] + s[..., 16:]
-    s = s[..., :8] + s[..., 8:]
+    s = (x * x).view(t, h, dim // 8, 8)
     s = s[..., :4] + s[..., 4:]
     s = s[..., :2] + s[..., 2:]
     s = s[..., 0] + s[..., 1]
-    s = torch.nn.functional.pad(s, (0, 8 - dim // 32))
-    s = s.view(t, h, 8) if dim > 128 else s[..., :4] if dim > 64 else s[..., :2]
-    s = s[..., :4] + s[..., 4:] if dim > 128 else s
-    s = s[..., :2] + s[..., 2:] if dim > 64 else s
+    s = s[..., :dim // 16] + s[..., dim // 16:]
+    s = torch.nn.functional.pad(s, (0, 16 - dim // 16))
+    s = s[..., :8] + s[..., 8:]
+    s = s[..., :4] + s[..., 4:]
+    s = s[..., :2] + s[..., 2:]
     s = s[..., :1] + s[..., 1:]
     r = torch.reciprocal(torch.sqrt(s * float(np.float32(1.0 / dim)) + float(np.float32(EPS))))
     y = (x * r) * gain.float()
