@@ -395,6 +395,122 @@ int fb4_quantize_mxfp8_decomposed(fb4_ctx* ctx, const void* x_bf16, int64_t T, i
 int64_t fb4_mxfp8_scale_bytes(int64_t T, int64_t C, int scale_layout);
 
 /*
+ * Position rotation of the operators below.  Channel pair i (0 <= i < D/2) of a head is rotated by the angle of
+ * its own axis: pairs 0 .. axis_pairs[0]-1 belong to axis 0, the next axis_pairs[1] to axis 1 and so on (one axis for
+ * text; time, height and width for video).  The table holds cos and sin of every pair's angle at every position, so
+ * frequencies, their base and any rescaling of positions are the caller's:
+ *     (a, b) -> (a * cos - b * sin, b * cos + a * sin),   a, b = channels i and i + D/2 (interleaved 0) or 2i and 2i + 1 (1)
+ * A pair that is not to be rotated has cos 1 and sin 0.
+ *   table      : device float32 [n_pos][D/2][2] (cos, sin), 16-byte aligned
+ *   pos        : device int32 [T][n_axes]; a position outside [0, n_pos) counts as position 0 and raises bit 1 of the
+ *                status word (fb4_device_status)
+ *   n_axes     : 1 to 4;  axis_pairs: their pairs, in sum D/2
+ */
+typedef struct {
+  const float* table;
+  int64_t n_pos;
+  const int32_t* pos;
+  int32_t n_axes;
+  int32_t axis_pairs[4];
+  int32_t interleaved;
+} fb4_rope;
+
+/*
+ * RMS norm of every query and key head with the position rotation, in one pass.  Per token and head of D channels,
+ * in float32:
+ *     t = sum(x * x),  r = 1 / sqrt(t * (1/D) + eps),  y[c] = (x[c] * r) * gain[c],
+ * then the rotation as stated at fb4_rope, then one rounding to bfloat16 (nearest even).  Every operation is rounded
+ * once (square root and division correctly, 1/D is the nearest float32), no multiplication is fused with an
+ * addition, and the squares are added in a fixed order: in every run of 8 channels by folding halves (v_i + v_(i+4), then
+ * +2, then +1); run j plus run j + D/16; these D/16 sums, filled up with +0 to a power of two, by folding halves.
+ *   q, k         : device bfloat16, token t's head h at x + t * ld + h * D; 16-byte aligned, ld a multiple of 8 (>= heads * D)
+ *   D            : a multiple of 32, at most 256 (FB4_ERR_SHAPE otherwise)
+ *   q_gain       : device bfloat16 [D], 16-byte aligned; NULL = q is rotated without a norm (k_gain likewise)
+ *   eps          : added to the mean square (>= 0, finite)
+ *   rope         : host struct with device pointers; NULL = no rotation
+ *   q_out, k_out : device bfloat16, laid out like q and k with their own ld; may be q and k themselves (same ld), must not
+ *                  overlap them otherwise
+ * Either side may have 0 heads (its pointers are then ignored).  Works with every context configuration.
+ */
+int fb4_qk_norm_rope(fb4_ctx* ctx, const void* q_bf16, int32_t q_heads, int64_t q_ld, const void* k_bf16, int32_t k_heads,
+                     int64_t k_ld, int64_t T, int32_t D, const void* q_gain, const void* k_gain, float eps,
+                     const fb4_rope* rope, void* q_out, int64_t q_out_ld, void* k_out, int64_t k_out_ld, void* stream);
+
+/*
+ * A paged cache of keys and values in FB4 blocks (4.5 bits per value with 32 channels to a block).  Page p holds
+ * page_tokens tokens of every head:
+ *     codes : uint8  [n_pages][n_heads][page_tokens][D/2],   meta : uint16 [n_pages][n_heads][page_tokens][D/32]
+ * so the rows of a cache read in order are a quantized tensor of n_pages * n_heads * page_tokens tokens and D channels,
+ * which fb4_dequantize and fb4_to_mxfp8 take as it is.  Slot s = page * page_tokens + place in the page.
+ *   n_pages     : >= 1;  page_tokens: a power of two, 16 to 4096;  n_heads: 1 to 1024;
+ *   head_dim    : D, a multiple of 32, at most 256.  All four arrays 16-byte aligned.
+ */
+typedef struct {
+  uint8_t* k_codes;
+  uint16_t* k_meta;
+  uint8_t* v_codes;
+  uint16_t* v_meta;
+  int64_t n_pages;
+  int32_t page_tokens;
+  int32_t n_heads;
+  int32_t head_dim;
+} fb4_cache;
+
+/*
+ * Appends T tokens to the cache: k goes through the norm and the rotation of fb4_qk_norm_rope and, like v, is quantized
+ * from float32 registers as fb4_quantize_f32 quantizes a float32 tensor (no rounding to bfloat16 in between);
+ * token t's blocks are written at slot[t].  q, if given, goes through the norm and the rotation in the same pass and
+ * leaves as bfloat16.  Default configuration only (block 32, 8 groups, two-stage selection, full exponent range):
+ * FB4_ERR_INVALID_ARG otherwise.
+ *   slot   : device int64 [T].  -1 = nothing is cached for this token (a row that pads a batch; its q row is still
+ *            written).  Any other value outside [0, n_pages * page_tokens) is treated as -1 and raises bit 1 of the status
+ *            word.  The slots of one call must differ from one another (precondition: with a slot given twice, the
+ *            codes and the metadata found there may come from different tokens)
+ *   q_heads: 0 = no q (q, q_gain and q_out are ignored)
+ *   other arguments as in fb4_qk_norm_rope; k and v have cache->n_heads heads
+ */
+int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, const void* k_bf16, int64_t k_ld,
+                     const void* v_bf16, int64_t v_ld, int64_t T, const void* k_gain, float eps, const fb4_rope* rope,
+                     const void* q_bf16, int32_t q_heads, int64_t q_ld, const void* q_gain, void* q_out, int64_t q_out_ld,
+                     void* stream);
+
+/*
+ * Attention of new tokens over the cache, whose blocks are decoded on the way:
+ *     out[i][h] = sum_j p_ij v_j,   p_ij = exp(scale * q_i . k_j) / sum over the visible j
+ * for every sequence b: query rows q_start[b] .. q_start[b+1]-1 (n_q of them) and cached tokens 0 .. kv_len[b]-1, token j
+ * at place j mod page_tokens of page page_table[b][j / page_tokens].  The new tokens are in the cache already (append
+ * first): query i stands at position kv_len - n_q + i.  It sees the tokens j < kv_len with
+ *     j <= position (causal 1),   j > position - window (window > 0).
+ * A query that sees nothing gets out = 0 and lse = -infinity.  Query head h reads cache head h / (q_heads / n_heads).
+ * Products are summed in float32, the statistics of the softmax are float32, probabilities enter the second product as
+ * bfloat16 (relative to the row's running maximum; the sum that divides is that of the unrounded ones).
+ *   q          : device bfloat16 [total_q][q_heads][D] with token stride q_ld; 16-byte aligned, q_ld a multiple of 8
+ *   q_heads    : a multiple of cache->n_heads, at most 1024
+ *   page_table : device int32 [n_seqs][max_pages].  A page outside [0, n_pages) that a query would read is left out (its
+ *                tokens count as invisible) and raises bit 1 of the status word
+ *   kv_len     : device int32 [n_seqs], each at most max_kv and max_pages * page_tokens
+ *   q_start    : device int32 [n_seqs + 1], ascending, from >= 0 to <= total_q, steps of at most max_q.  kv_len and q_start
+ *                are clamped to these ranges on the device; a value that was outside raises bit 1 of the status word
+ *   max_q, max_kv : host bounds of the lengths; they fix the launch shape (and only that)
+ *   out        : device [total_q][q_heads][D] with token stride out_ld (elements), out_dtype 0 = float32, 1 = bfloat16,
+ *                2 = IEEE half; 16-byte aligned, out_ld * element size a multiple of 16.  Rows of no sequence are left alone
+ *   lse        : device float32 [total_q][q_heads]: log of the sum of exp(scale * q . k) over the visible tokens; or NULL
+ *   workspace  : device, 256-byte aligned, workspace_bytes >= fb4_cache_attention_workspace(...) of the same arguments
+ *                (FB4_ERR_INVALID_ARG otherwise; NULL when that is 0).  It holds partial results between the launches of one
+ *                call: two calls that may run at the same time need two workspaces
+ * Needs block size 32 (FB4_ERR_INVALID_ARG otherwise); the context's formatbook decodes the cache.
+ */
+int fb4_cache_attention(fb4_ctx* ctx, const void* q_bf16, int64_t q_ld, int32_t q_heads, int64_t total_q,
+                        const fb4_cache* cache, const int32_t* page_table, int32_t max_pages, const int32_t* kv_len,
+                        const int32_t* q_start, int32_t n_seqs, int32_t max_q, int32_t max_kv, float scale, int causal,
+                        int32_t window, void* out, int64_t out_ld, int out_dtype, float* lse, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/* Size in bytes of the workspace of fb4_cache_attention (0 = none needed; -1 for invalid arguments).  Host only. */
+int64_t fb4_cache_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
+                                      int32_t max_q, int32_t max_kv);
+
+/*
  * Host-buffer form of fb4_quantize for callers whose tensors live in host memory:
  * copies x from the host, quantizes, and copies codes and meta back, in row
  * chunks pipelined over the context's own streams, then waits for completion.

@@ -89,6 +89,40 @@ struct DeviceGuard {
   }
 };
 
+// The rows of one tensor of heads: pointer, token stride and gain as fb4_qk_norm_rope wants them.
+int check_heads(const void* x, int64_t heads, int64_t D, int64_t ld) {
+  if (!x) return FB4_ERR_INVALID_ARG;
+  if (ld < heads * D) return FB4_ERR_SHAPE;
+  if (!aligned16(x) || (ld & 7)) return FB4_ERR_ALIGN;
+  return FB4_OK;
+}
+
+int check_rope(const fb4_rope* r, int64_t T, int32_t D) {
+  if (!r) return FB4_OK;
+  if (r->n_axes < 1 || r->n_axes > 4 || (r->interleaved != 0 && r->interleaved != 1)) return FB4_ERR_INVALID_ARG;
+  int64_t pairs = 0;
+  for (int a = 0; a < r->n_axes; ++a) {
+    if (r->axis_pairs[a] < 0) return FB4_ERR_INVALID_ARG;
+    pairs += r->axis_pairs[a];
+  }
+  if (pairs * 2 != D || r->n_pos < 1 || r->n_pos > 0x7fffffffLL) return FB4_ERR_SHAPE;
+  if (T == 0) return FB4_OK;
+  if (!r->table || !r->pos) return FB4_ERR_INVALID_ARG;
+  if (!aligned16(r->table) || (reinterpret_cast<uintptr_t>(r->pos) & 3u)) return FB4_ERR_ALIGN;
+  return FB4_OK;
+}
+
+int check_cache(const fb4_cache* c) {
+  if (!c) return FB4_ERR_INVALID_ARG;
+  if (c->n_pages < 1 || c->page_tokens < 16 || c->page_tokens > 4096 || (c->page_tokens & (c->page_tokens - 1)) != 0 ||
+      c->n_heads < 1 || c->n_heads > 1024 || c->head_dim < 32 || c->head_dim > 256 || c->head_dim % 32 != 0 ||
+      c->n_pages > (1LL << 40) / c->page_tokens)
+    return FB4_ERR_SHAPE;
+  if (!c->k_codes || !c->k_meta || !c->v_codes || !c->v_meta) return FB4_ERR_INVALID_ARG;
+  if (!aligned16(c->k_codes) || !aligned16(c->k_meta) || !aligned16(c->v_codes) || !aligned16(c->v_meta)) return FB4_ERR_ALIGN;
+  return FB4_OK;
+}
+
 int run_quantize(fb4_ctx* ctx, const void* x, int64_t T, int64_t C, int64_t ld, const Fb4RowExtras& ex,
                  uint8_t* codes, uint16_t* meta, cudaStream_t stream) {
   if (T == 0) return FB4_OK;
@@ -179,7 +213,7 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
   }
   size_t fast_bytes = 0;
   if (fb4_fast_build_tables(ctx->host_tables, c.select_mode, &ctx->d_fast_tables, &fast_bytes) &&
-      fb4_fast_prepare_device() == cudaSuccess)
+      fb4_fast_prepare_device() == cudaSuccess && fb4_rope_prepare_device() == cudaSuccess)
     ctx->fast_ok = 1;
   ctx->fast_table_bytes = fast_bytes;
   cudaGetLastError();
@@ -560,6 +594,130 @@ int fb4_to_mxfp8(fb4_ctx* ctx, const uint8_t* codes, const uint16_t* meta, int64
   if (!aligned16(codes) || !aligned16(meta) || !aligned16(e4m3)) return FB4_ERR_ALIGN;
   cudaError_t e = fb4_launch_to_mxfp8(ctx, codes, meta, T, C, e4m3, scales, scale_layout,
                                       static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fb4_set_cuda_error(e);
+  ctx->launches += 1;
+  return FB4_OK;
+}
+
+int fb4_qk_norm_rope(fb4_ctx* ctx, const void* q, int32_t q_heads, int64_t q_ld, const void* k, int32_t k_heads, int64_t k_ld,
+                     int64_t T, int32_t D, const void* q_gain, const void* k_gain, float eps, const fb4_rope* rope,
+                     void* q_out, int64_t q_out_ld, void* k_out, int64_t k_out_ld, void* stream) {
+  if (!ctx) return FB4_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f) || eps > 3.0e38f || q_heads < 0 || k_heads < 0) return FB4_ERR_INVALID_ARG;
+  if (T < 0 || T > 0x7fffffffLL || D < 32 || D > 256 || D % 32 != 0 || q_heads > 1024 || k_heads > 1024) return FB4_ERR_SHAPE;
+  int rc = check_rope(rope, T, D);
+  if (rc != FB4_OK) return rc;
+  if (T == 0 || (q_heads == 0 && k_heads == 0)) return FB4_OK;
+  if (q_heads > 0) {
+    rc = check_heads(q, q_heads, D, q_ld);
+    if (rc == FB4_OK) rc = check_heads(q_out, q_heads, D, q_out_ld);
+    if (rc != FB4_OK) return rc;
+    if (q == q_out && q_ld != q_out_ld) return FB4_ERR_INVALID_ARG;
+    if (!aligned16(q_gain)) return FB4_ERR_ALIGN;
+  }
+  if (k_heads > 0) {
+    rc = check_heads(k, k_heads, D, k_ld);
+    if (rc == FB4_OK) rc = check_heads(k_out, k_heads, D, k_out_ld);
+    if (rc != FB4_OK) return rc;
+    if (k == k_out && k_ld != k_out_ld) return FB4_ERR_INVALID_ARG;
+    if (!aligned16(k_gain)) return FB4_ERR_ALIGN;
+  }
+  const cudaError_t e = fb4_launch_norm_rope(ctx, q, q_heads, q_ld, k, k_heads, k_ld, T, D, q_gain, k_gain, eps, rope, q_out,
+                                             q_out_ld, k_out, k_out_ld, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fb4_set_cuda_error(e);
+  ctx->launches += 1;
+  return FB4_OK;
+}
+
+int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, const void* k, int64_t k_ld, const void* v,
+                     int64_t v_ld, int64_t T, const void* k_gain, float eps, const fb4_rope* rope, const void* q,
+                     int32_t q_heads, int64_t q_ld, const void* q_gain, void* q_out, int64_t q_out_ld, void* stream) {
+  if (!ctx) return FB4_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f) || eps > 3.0e38f || q_heads < 0) return FB4_ERR_INVALID_ARG;
+  const fb4_config& c = ctx->cfg;
+  if (c.block_size != 32 || c.num_groups != 8 || c.select_mode != 0 || c.exp_min != -124 || c.exp_max != 127 || !ctx->fast_ok)
+    return FB4_ERR_INVALID_ARG;
+  int rc = check_cache(cache);
+  if (rc != FB4_OK) return rc;
+  const int32_t D = cache->head_dim;
+  if (T < 0 || T > 0x7fffffffLL || q_heads > 1024) return FB4_ERR_SHAPE;
+  rc = check_rope(rope, T, D);
+  if (rc != FB4_OK) return rc;
+  if (T == 0) return FB4_OK;
+  if (!slot) return FB4_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(slot) & 7u) return FB4_ERR_ALIGN;
+  rc = check_heads(k, cache->n_heads, D, k_ld);
+  if (rc == FB4_OK) rc = check_heads(v, cache->n_heads, D, v_ld);
+  if (rc == FB4_OK && q_heads > 0) rc = check_heads(q, q_heads, D, q_ld);
+  if (rc == FB4_OK && q_heads > 0) rc = check_heads(q_out, q_heads, D, q_out_ld);
+  if (rc != FB4_OK) return rc;
+  if (q_heads > 0 && q == q_out && q_ld != q_out_ld) return FB4_ERR_INVALID_ARG;
+  if (!aligned16(k_gain) || (q_heads > 0 && !aligned16(q_gain))) return FB4_ERR_ALIGN;
+  const cudaError_t e = fb4_launch_cache_append(ctx, q, q_heads, q_ld, k, k_ld, v, v_ld, T, q_gain, k_gain, eps, rope, slot,
+                                                cache, q_out, q_out_ld, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fb4_set_cuda_error(e);
+  ctx->launches += 1;
+  return FB4_OK;
+}
+
+int64_t fb4_cache_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
+                                      int32_t max_q, int32_t max_kv) {
+  if (!ctx || n_heads < 1 || n_heads > 1024 || q_heads < n_heads || q_heads > 1024 || q_heads % n_heads != 0 || head_dim < 32 ||
+      head_dim > 256 || head_dim % 32 != 0 || n_seqs < 0 || max_q < 0 || max_kv < 0)
+    return -1;
+  return 0;
+}
+
+int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_heads, int64_t total_q, const fb4_cache* cache,
+                        const int32_t* page_table, int32_t max_pages, const int32_t* kv_len, const int32_t* q_start,
+                        int32_t n_seqs, int32_t max_q, int32_t max_kv, float scale, int causal, int32_t window, void* out,
+                        int64_t out_ld, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!ctx || ctx->cfg.block_size != 32) return FB4_ERR_INVALID_ARG;
+  if ((causal != 0 && causal != 1) || window < 0 || out_dtype < 0 || out_dtype > 2 || !(scale > -3.0e38f && scale < 3.0e38f))
+    return FB4_ERR_INVALID_ARG;
+  int rc = check_cache(cache);
+  if (rc != FB4_OK) return rc;
+  if (q_heads < 1 || q_heads > 1024 || q_heads % cache->n_heads != 0 || total_q < 0 || total_q > 0x7fffffffLL || n_seqs < 0 ||
+      max_q < 0 || max_kv < 0 || max_pages < 0)
+    return FB4_ERR_SHAPE;
+  if (total_q == 0 || n_seqs == 0 || max_q == 0) return FB4_OK;
+  const int32_t D = cache->head_dim;
+  rc = check_heads(q, q_heads, D, q_ld);
+  if (rc != FB4_OK) return rc;
+  if (!out || !kv_len || !q_start || (!page_table && max_pages > 0)) return FB4_ERR_INVALID_ARG;
+  if (out_ld < (int64_t)q_heads * D) return FB4_ERR_SHAPE;
+  if (!aligned16(out) || (out_ld * (out_dtype == 0 ? 4 : 2)) % 16 != 0) return FB4_ERR_ALIGN;
+  if (((reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(page_table) |
+        reinterpret_cast<uintptr_t>(lse)) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return FB4_ERR_ALIGN;
+  const int64_t need = fb4_cache_attention_workspace(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv);
+  if (need < 0 || workspace_bytes < need || (need > 0 && !workspace)) return FB4_ERR_INVALID_ARG;
+  Fb4Attend a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_ld = q_ld;
+  a.total_q = total_q;
+  a.q_heads = q_heads;
+  a.group = q_heads / cache->n_heads;
+  a.cache = *cache;
+  while ((1 << a.page_shift) < cache->page_tokens) ++a.page_shift;
+  a.page_table = page_table;
+  a.max_pages = max_pages;
+  a.kv_len = kv_len;
+  a.q_start = q_start;
+  a.n_seqs = n_seqs;
+  a.max_q = max_q;
+  a.max_kv = max_kv;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.causal = causal;
+  a.window = window;
+  a.out = out;
+  a.out_ld = out_ld;
+  a.out_dtype = out_dtype;
+  a.lse = lse;
+  a.tables = ctx->d_tables;
+  a.status = ctx->d_status;
+  const cudaError_t e = fb4_launch_attend_generic(ctx, a, static_cast<cudaStream_t>(stream));
+  ctx->last_variant = "generic";
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
   ctx->launches += 1;
   return FB4_OK;

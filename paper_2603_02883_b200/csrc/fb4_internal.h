@@ -114,3 +114,39 @@ cudaError_t fb4_launch_select_salient_topk(const float* score, int64_t T, int64_
                                            cudaStream_t stream);
 cudaError_t fb4_launch_select_salient(const float* score, int64_t T, int32_t tile, int32_t* salient_idx,
                                       cudaStream_t stream);
+
+// per-head norm + rotation, cache append (fb4_rope.cu)
+cudaError_t fb4_rope_prepare_device();
+cudaError_t fb4_launch_norm_rope(const fb4_ctx* ctx, const void* q, int32_t q_heads, int64_t q_ld, const void* k,
+                                 int32_t k_heads, int64_t k_ld, int64_t T, int32_t D, const void* q_gain, const void* k_gain,
+                                 float eps, const fb4_rope* rope, void* q_out, int64_t q_out_ld, void* k_out, int64_t k_out_ld,
+                                 cudaStream_t stream);
+cudaError_t fb4_launch_cache_append(const fb4_ctx* ctx, const void* q, int32_t q_heads, int64_t q_ld, const void* k,
+                                    int64_t k_ld, const void* v, int64_t v_ld, int64_t T, const void* q_gain,
+                                    const void* k_gain, float eps, const fb4_rope* rope, const int64_t* slot,
+                                    const fb4_cache* cache, void* q_out, int64_t q_out_ld, cudaStream_t stream);
+
+// One fb4_cache_attention call as its kernels see it.
+struct Fb4Attend {
+  const uint16_t* q;
+  int64_t q_ld, total_q;
+  int32_t q_heads, group;        // group = q_heads / cache.n_heads
+  fb4_cache cache;
+  int32_t page_shift;
+  const int32_t* page_table;
+  int32_t max_pages;
+  const int32_t* kv_len;
+  const int32_t* q_start;
+  int32_t n_seqs, max_q, max_kv;
+  float scale_log2;              // scale * log2(e)
+  int32_t causal, window;
+  void* out;
+  int64_t out_ld;
+  int32_t out_dtype;
+  float* lse;
+  const Fb4DeviceTables* tables;
+  uint32_t* status;
+  float* partial;                // [split][row] records of the split kernels, NULL with one split
+  int32_t splits;
+};
+cudaError_t fb4_launch_attend_generic(const fb4_ctx* ctx, const Fb4Attend& a, cudaStream_t stream);

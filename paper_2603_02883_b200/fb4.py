@@ -23,13 +23,24 @@ STATIC_MAX_CLUSTERS = 1024
 EXPORTS = [
     "fb4_default_config", "fb4_init", "fb4_destroy", "fb4_get_tables", "fb4_block_tables", "fb4_quantize", "fb4_quantize_f32", "fb4_quantize_affine", "fb4_quantize_affine_mxfp8", "fb4_quantize_layernorm", "fb4_quantize_seda",
     "fb4_build_subformatbook", "fb4_build_subformatbook_static", "fb4_select_salient", "fb4_select_salient_topk", "fb4_quantize_decomposed", "fb4_quantize_decomposed_idx", "fb4_dequantize",
-    "fb4_quantize_weights", "fb4_quantize_mxfp8", "fb4_quantize_mxfp8_decomposed", "fb4_to_mxfp8", "fb4_mxfp8_scale_bytes", "fb4_quantize_host", "fb4_set_kernel_variant", "fb4_device_status", "fb4_launch_count", "fb4_last_variant", "fb4_last_cuda_error", "fb4_strerror",
+    "fb4_quantize_weights", "fb4_qk_norm_rope", "fb4_cache_append", "fb4_cache_attention", "fb4_cache_attention_workspace", "fb4_quantize_mxfp8", "fb4_quantize_mxfp8_decomposed", "fb4_to_mxfp8", "fb4_mxfp8_scale_bytes", "fb4_quantize_host", "fb4_set_kernel_variant", "fb4_device_status", "fb4_launch_count", "fb4_last_variant", "fb4_last_cuda_error", "fb4_strerror",
 ]
 
 
 class Fb4Config(ctypes.Structure):
     _fields_ = [("block_size", ctypes.c_uint32), ("num_groups", ctypes.c_uint32),
                 ("exp_min", ctypes.c_int32), ("exp_max", ctypes.c_int32), ("select_mode", ctypes.c_uint32)]
+
+
+class Fb4Rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_pos", ctypes.c_int64), ("pos", ctypes.c_void_p), ("n_axes", ctypes.c_int32),
+                ("axis_pairs", ctypes.c_int32 * 4), ("interleaved", ctypes.c_int32)]
+
+
+class Fb4Cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_meta", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_meta", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32),
+                ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class Fb4Error(RuntimeError):
@@ -92,6 +103,16 @@ def lib() -> ctypes.CDLL:
     L.fb4_dequantize.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, ci, vp]
     L.fb4_quantize_weights.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp]
     L.fb4_quantize_weights.restype = ci
+    cf, rp, cp = ctypes.c_float, ctypes.POINTER(Fb4Rope), ctypes.POINTER(Fb4Cache)
+    L.fb4_qk_norm_rope.argtypes = [vp, vp, i32, i64, vp, i32, i64, i64, i32, vp, vp, cf, rp, vp, i64, vp, i64, vp]
+    L.fb4_qk_norm_rope.restype = ci
+    L.fb4_cache_append.argtypes = [vp, cp, vp, vp, i64, vp, i64, i64, vp, cf, rp, vp, i32, i64, vp, vp, i64, vp]
+    L.fb4_cache_append.restype = ci
+    L.fb4_cache_attention.argtypes = [vp, vp, i64, i32, i64, cp, vp, i32, vp, vp, i32, i32, i32, cf, ci, i32, vp, i64, ci, vp,
+                                      vp, i64, vp]
+    L.fb4_cache_attention.restype = ci
+    L.fb4_cache_attention_workspace.argtypes = [vp, i32, i32, i32, i32, i32, i32]
+    L.fb4_cache_attention_workspace.restype = i64
     L.fb4_quantize_mxfp8.argtypes = [vp, vp, i64, i64, i64, vp, vp, i32, vp, vp, ci, vp]
     L.fb4_quantize_mxfp8.restype = ci
     L.fb4_quantize_mxfp8_decomposed.argtypes = [vp, vp, i64, i64, i64, vp, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp,
@@ -290,6 +311,33 @@ def fb4_mxfp8_scale_bytes(T, C, scale_layout) -> int:
     return int(lib().fb4_mxfp8_scale_bytes(T, C, scale_layout))
 
 
+def fb4_qk_norm_rope(ctx, q, q_heads, q_ld, k, k_heads, k_ld, T, D, q_gain, k_gain, eps, rope, q_out, q_out_ld, k_out, k_out_ld,
+                     stream=None) -> None:
+    """rope: an Fb4Rope or None"""
+    _check(lib().fb4_qk_norm_rope(ctx, _ptr(q), q_heads, q_ld, _ptr(k), k_heads, k_ld, T, D, _ptr(q_gain), _ptr(k_gain), eps,
+                                  rope, _ptr(q_out), q_out_ld, _ptr(k_out), k_out_ld, _stream(stream)), "fb4_qk_norm_rope")
+
+
+def fb4_cache_append(ctx, cache, slot, k, k_ld, v, v_ld, T, k_gain, eps, rope, q, q_heads, q_ld, q_gain, q_out, q_out_ld,
+                     stream=None) -> None:
+    """cache: an Fb4Cache; rope: an Fb4Rope or None"""
+    _check(lib().fb4_cache_append(ctx, cache, _ptr(slot), _ptr(k), k_ld, _ptr(v), v_ld, T, _ptr(k_gain), eps, rope, _ptr(q),
+                                  q_heads, q_ld, _ptr(q_gain), _ptr(q_out), q_out_ld, _stream(stream)), "fb4_cache_append")
+
+
+def fb4_cache_attention(ctx, q, q_ld, q_heads, total_q, cache, page_table, max_pages, kv_len, q_start, n_seqs, max_q, max_kv,
+                        scale, causal, window, out, out_ld, out_dtype, lse, workspace, workspace_bytes, stream=None) -> None:
+    """cache: an Fb4Cache"""
+    _check(lib().fb4_cache_attention(ctx, _ptr(q), q_ld, q_heads, total_q, cache, _ptr(page_table), max_pages, _ptr(kv_len),
+                                     _ptr(q_start), n_seqs, max_q, max_kv, scale, int(bool(causal)), window, _ptr(out), out_ld,
+                                     out_dtype, _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream)),
+           "fb4_cache_attention")
+
+
+def fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv) -> int:
+    return int(lib().fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv))
+
+
 def fb4_quantize_host(ctx, x_host, T, C, d_x, d_codes, d_meta, codes_host, meta_host) -> None:
     _check(lib().fb4_quantize_host(ctx, _ptr(x_host), T, C, _ptr(d_x), _ptr(d_codes), _ptr(d_meta),
                                    _ptr(codes_host), _ptr(meta_host)), "fb4_quantize_host")
@@ -322,6 +370,25 @@ class Quantized:
     salient_idx: torch.Tensor | None = None  # int32 [n_salient]
     res_codes: torch.Tensor | None = None
     res_meta: torch.Tensor | None = None
+
+
+@dataclass
+class Rope:
+    """Position rotation (see fb4_rope in include/fb4.h): pair i of a head belongs to the axis whose run of `axis_pairs` it
+    lies in and is rotated by the angle that `table` holds for that axis' position"""
+    table: torch.Tensor                      # float32 [n_pos][D/2][2]: cos, sin
+    pos: torch.Tensor                        # int32 [T][n_axes] (or [T] with one axis)
+    axis_pairs: list
+    interleaved: bool = False
+
+
+@dataclass
+class Cache:
+    """Paged FB4 cache (see fb4_cache in include/fb4.h)"""
+    k_codes: torch.Tensor                    # uint8 [n_pages][n_heads][page_tokens][D/2]
+    k_meta: torch.Tensor                     # uint16 bits in an int16 tensor [n_pages][n_heads][page_tokens][D/32]
+    v_codes: torch.Tensor
+    v_meta: torch.Tensor
 
 
 class Fb4:
@@ -497,6 +564,144 @@ class Fb4:
                              device=q.codes.device)
         fb4_to_mxfp8(self.ctx, q.codes, q.meta, T, C, e4m3, scales, scale_layout)
         return e4m3, scales[:fb4_mxfp8_scale_bytes(T, C, scale_layout)]
+
+    # ---- attention side: norm + rotation of q and k, paged cache, attention over it
+
+    def _on(self, *tensors):
+        for t in tensors:
+            if t is not None and (not t.is_cuda or t.device.index != self.device):
+                raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
+
+    @staticmethod
+    def _heads(x):
+        """(T, heads, D, token stride) of a [T][heads][D] bf16 tensor whose heads lie next to one another"""
+        if x.dtype != torch.bfloat16 or x.dim() != 3:
+            raise ValueError("expected a bfloat16 tensor [tokens][heads][D]")
+        T, H, D = x.shape
+        if (D > 1 and x.stride(2) != 1) or (H > 1 and x.stride(1) != D):
+            raise ValueError("the heads of a token must lie next to one another, channels contiguous")
+        return T, H, D, (x.stride(0) if T > 1 else H * D)
+
+    def _rope(self, rope: Rope | None, T: int, D: int):
+        if rope is None:
+            return None
+        self._on(rope.table, rope.pos)
+        pairs = [int(n) for n in rope.axis_pairs]
+        if not 1 <= len(pairs) <= 4:
+            raise ValueError("a rotation has 1 to 4 axes")
+        if rope.table.dtype != torch.float32 or not rope.table.is_contiguous() or tuple(rope.table.shape[1:]) != (D // 2, 2):
+            raise ValueError("rope.table must be a contiguous float32 tensor [n_pos][D/2][2]")
+        if rope.pos.dtype != torch.int32 or not rope.pos.is_contiguous() or rope.pos.numel() != T * len(pairs) or \
+                (T and rope.pos.shape[0] != T):
+            raise ValueError("rope.pos must be a contiguous int32 tensor [T][n_axes]")
+        return Fb4Rope(rope.table.data_ptr(), rope.table.shape[0], rope.pos.data_ptr(), len(pairs),
+                       (ctypes.c_int32 * 4)(*pairs), int(bool(rope.interleaved)))
+
+    @staticmethod
+    def _gain(gain, D):
+        if gain is not None and (gain.dtype != torch.bfloat16 or gain.numel() != D or not gain.is_contiguous()):
+            raise ValueError("a gain must be a contiguous bfloat16 tensor [D]")
+
+    def _cache(self, c: Cache) -> Fb4Cache:
+        self._on(c.k_codes, c.k_meta, c.v_codes, c.v_meta)
+        if c.k_codes.dim() != 4:
+            raise ValueError("cache codes must be [n_pages][n_heads][page_tokens][D/2]")
+        n, h, p, half = c.k_codes.shape
+        for codes, meta in ((c.k_codes, c.k_meta), (c.v_codes, c.v_meta)):
+            if codes.dtype != torch.uint8 or tuple(codes.shape) != (n, h, p, half) or not codes.is_contiguous():
+                raise ValueError("cache codes must be contiguous uint8 [n_pages][n_heads][page_tokens][D/2]")
+            if meta.element_size() != 2 or tuple(meta.shape) != (n, h, p, half // 16) or not meta.is_contiguous():
+                raise ValueError("cache meta must be contiguous 16-bit [n_pages][n_heads][page_tokens][D/32]")
+        return Fb4Cache(c.k_codes.data_ptr(), c.k_meta.data_ptr(), c.v_codes.data_ptr(), c.v_meta.data_ptr(), n, p, h, half * 2)
+
+    def new_cache(self, n_pages: int, page_tokens: int, n_heads: int, head_dim: int) -> Cache:
+        """an empty cache: all zero, so every slot reads as zeros"""
+        dev = torch.device("cuda", self.device)
+        codes = lambda: torch.zeros((n_pages, n_heads, page_tokens, head_dim // 2), dtype=torch.uint8, device=dev)  # noqa: E731
+        meta = lambda: torch.zeros((n_pages, n_heads, page_tokens, head_dim // 32), dtype=torch.int16, device=dev)  # noqa: E731
+        return Cache(codes(), meta(), codes(), meta())
+
+    def qk_norm_rope(self, q, k, q_gain=None, k_gain=None, eps: float = 1e-6, rope: Rope | None = None, out=None):
+        """(q, k) [T][heads][D] after the RMS norm of every head (gain None: no norm) and the rotation; out: (q_out, k_out)
+        to write to, which may be q and k themselves"""
+        T, Hq, D, q_ld = self._heads(q)
+        Tk, Hk, Dk, k_ld = self._heads(k)
+        if (Tk, Dk) != (T, D):
+            raise ValueError("q and k must have the same tokens and head dimension")
+        self._on(q, k, q_gain, k_gain)
+        self._gain(q_gain, D)
+        self._gain(k_gain, D)
+        with torch.cuda.device(self.device):
+            qo, ko = out if out is not None else (torch.empty((T, Hq, D), dtype=q.dtype, device=q.device),
+                                                  torch.empty((T, Hk, D), dtype=k.dtype, device=k.device))
+            self._on(qo, ko)
+            (Ta, Ha, Da, qo_ld), (Tb, Hb, Db, ko_ld) = self._heads(qo), self._heads(ko)
+            if (Ta, Ha, Da) != (T, Hq, D) or (Tb, Hb, Db) != (T, Hk, D):
+                raise ValueError("out must have the shapes of q and k")
+            fb4_qk_norm_rope(self.ctx, q, Hq, q_ld, k, Hk, k_ld, T, D, q_gain, k_gain, eps, self._rope(rope, T, D), qo, qo_ld,
+                             ko, ko_ld)
+        return qo, ko
+
+    def cache_append(self, cache: Cache, slot, k, v, k_gain=None, eps: float = 1e-6, rope: Rope | None = None, q=None,
+                     q_gain=None):
+        """writes the tokens' keys (after norm and rotation) and values to their slots (int64 [T], -1 = none) of the cache;
+        returns q after norm and rotation, if q is given"""
+        T, H, D, k_ld = self._heads(k)
+        Tv, Hv, Dv, v_ld = self._heads(v)
+        c = self._cache(cache)
+        if (Tv, Hv, Dv) != (T, H, D) or H != c.n_heads or D != c.head_dim:
+            raise ValueError("k and v must have the heads and the head dimension of the cache")
+        if slot.dtype != torch.int64 or slot.numel() != T or not slot.is_contiguous():
+            raise ValueError("slot must be a contiguous int64 tensor [T]")
+        self._on(slot, k, v, q, k_gain, q_gain)
+        self._gain(k_gain, D)
+        with torch.cuda.device(self.device):
+            Hq = q_ld = 0
+            qo = None
+            if q is not None:
+                Tq, Hq, Dq, q_ld = self._heads(q)
+                if (Tq, Dq) != (T, D):
+                    raise ValueError("q must have the tokens and the head dimension of k")
+                self._gain(q_gain, D)
+                qo = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+            fb4_cache_append(self.ctx, c, slot, k, k_ld, v, v_ld, T, k_gain, eps, self._rope(rope, T, D), q, Hq, q_ld, q_gain,
+                             qo, Hq * D)
+        return qo
+
+    def cache_attention(self, q, cache: Cache, page_table, kv_len, q_start, max_q: int, max_kv: int, scale: float | None = None,
+                        causal: bool = True, window: int = 0, dtype=torch.bfloat16):
+        """(out [total_q][q_heads][D], lse float32 [total_q][q_heads]) of the queries over their sequences' pages; rows that
+        belong to no sequence are left undefined.  scale None = D ** -0.5"""
+        total, Hq, D, q_ld = self._heads(q)
+        c = self._cache(cache)
+        if D != c.head_dim:
+            raise ValueError("q must have the head dimension of the cache")
+        self._on(q, page_table, kv_len, q_start)
+        n = kv_len.numel()
+        for t, shape in ((page_table, (n, page_table.shape[-1])), (kv_len, (n,)), (q_start, (n + 1,))):
+            if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+                raise ValueError("page_table [n_seqs][max_pages], kv_len [n_seqs] and q_start [n_seqs + 1] must be contiguous int32")
+        with torch.cuda.device(self.device):
+            out = torch.empty((total, Hq, D), dtype=dtype, device=q.device)
+            lse = torch.empty((total, Hq), dtype=torch.float32, device=q.device)
+            need = max(fb4_cache_attention_workspace(self.ctx, Hq, c.n_heads, D, n, max_q, max_kv), 0)
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+            fb4_cache_attention(self.ctx, q, q_ld, Hq, total, c, page_table, page_table.shape[1], kv_len, q_start, n, max_q, max_kv,
+                                D ** -0.5 if scale is None else scale, causal, window, out, Hq * D,
+                                {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[dtype], lse, ws, need)
+        return out, lse
+
+    def cache_values(self, cache: Cache, dtype=torch.float32):
+        """(k, v) [n_pages][n_heads][page_tokens][D]: all that a cache holds, decoded"""
+        c = self._cache(cache)
+        out = []
+        with torch.cuda.device(self.device):
+            for codes, meta in ((cache.k_codes, cache.k_meta), (cache.v_codes, cache.v_meta)):
+                x = torch.empty((*codes.shape[:3], c.head_dim), dtype=dtype, device=codes.device)
+                fb4_dequantize(self.ctx, codes, meta, c.n_pages * c.n_heads * c.page_tokens, c.head_dim, None, 0, None, None, x,
+                               {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[dtype])
+                out.append(x)
+        return tuple(out)
 
     def set_kernel_variant(self, variant: int) -> None:
         fb4_set_kernel_variant(self.ctx, variant)
