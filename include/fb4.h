@@ -491,7 +491,8 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
  *   kv_len     : device int32 [n_seqs], each at most max_kv and max_pages * page_tokens
  *   q_start    : device int32 [n_seqs + 1], ascending, from >= 0 to <= total_q, steps of at most max_q.  kv_len and q_start
  *                are clamped to these ranges on the device; a value that was outside raises bit 1 of the status word
- *   max_q, max_kv : host bounds of the lengths; they fix the launch shape (and only that)
+ *   max_q, max_kv : host bounds of the lengths; they fix the launch shape (and only that).  max_kv <= 2^30,
+ *                n_seqs * max_q * q_heads < 2^31 (FB4_ERR_SHAPE)
  *   out        : device [total_q][q_heads][D] with token stride out_ld (elements), out_dtype 0 = float32, 1 = bfloat16,
  *                2 = IEEE half; 16-byte aligned, out_ld * element size a multiple of 16.  Rows of no sequence are left alone
  *   lse        : device float32 [total_q][q_heads]: log of the sum of exp(scale * q . k) over the visible tokens; or NULL

@@ -215,6 +215,7 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
   if (fb4_fast_build_tables(ctx->host_tables, c.select_mode, &ctx->d_fast_tables, &fast_bytes) &&
       fb4_fast_prepare_device() == cudaSuccess && fb4_rope_prepare_device() == cudaSuccess)
     ctx->fast_ok = 1;
+  ctx->attend_ok = fb4_attend_prepare_device() == cudaSuccess;
   ctx->fast_table_bytes = fast_bytes;
   cudaGetLastError();
   *out = ctx;
@@ -663,9 +664,10 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
 int64_t fb4_cache_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
                                       int32_t max_q, int32_t max_kv) {
   if (!ctx || n_heads < 1 || n_heads > 1024 || q_heads < n_heads || q_heads > 1024 || q_heads % n_heads != 0 || head_dim < 32 ||
-      head_dim > 256 || head_dim % 32 != 0 || n_seqs < 0 || max_q < 0 || max_kv < 0)
+      head_dim > 256 || head_dim % 32 != 0 || n_seqs < 0 || max_q < 0 || max_kv < 0 || max_kv > (1 << 30) ||
+      (int64_t)max_q * q_heads > (1 << 30) || (int64_t)max_q * q_heads * n_seqs > 0x7fffffffLL)
     return -1;
-  return 0;
+  return fb4_attend_plan(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv).workspace;
 }
 
 int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_heads, int64_t total_q, const fb4_cache* cache,
@@ -678,7 +680,8 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
   int rc = check_cache(cache);
   if (rc != FB4_OK) return rc;
   if (q_heads < 1 || q_heads > 1024 || q_heads % cache->n_heads != 0 || total_q < 0 || total_q > 0x7fffffffLL || n_seqs < 0 ||
-      max_q < 0 || max_kv < 0 || max_pages < 0)
+      max_q < 0 || max_kv < 0 || max_pages < 0 || max_kv > (1 << 30) || (int64_t)max_q * q_heads > (1 << 30) ||
+      (int64_t)max_q * q_heads * n_seqs > 0x7fffffffLL)
     return FB4_ERR_SHAPE;
   if (total_q == 0 || n_seqs == 0 || max_q == 0) return FB4_OK;
   const int32_t D = cache->head_dim;
@@ -716,10 +719,17 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
   a.lse = lse;
   a.tables = ctx->d_tables;
   a.status = ctx->d_status;
-  const cudaError_t e = fb4_launch_attend_generic(ctx, a, static_cast<cudaStream_t>(stream));
-  ctx->last_variant = "generic";
+  const Fb4AttendPlan plan = fb4_attend_plan(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv);
+  a.splits = plan.splits;
+  a.split_tiles = plan.split_tiles;
+  a.partial = plan.splits > 1 ? static_cast<float*>(workspace) : nullptr;
+  int launches = 1;
+  cudaError_t e;
+  if (plan.kernel == 0) e = fb4_launch_attend_generic(ctx, a, static_cast<cudaStream_t>(stream));
+  else e = fb4_launch_attend_few(ctx, a, static_cast<cudaStream_t>(stream), &launches);
+  ctx->last_variant = plan.kernel ? "fast" : "generic";
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
-  ctx->launches += 1;
+  ctx->launches += launches;
   return FB4_OK;
 }
 

@@ -1,0 +1,495 @@
+// Attention of few query rows per cache head (single tokens, drafted tokens, small groups) over the paged FB4 cache.
+//
+// Work: a CTA of 4 warps takes one sequence, one cache head, up to 8 * NT query rows (query-major: row r = query r / group,
+// head r mod group) and one run of the cached tokens (a "split"); its warps take that run's tiles of 32 tokens in turn.  Each warp
+// has its own ring of bulk-copied tiles (codes and metadata of K and V), its own running maximum and sum, and its own
+// accumulators; the warps are joined in shared memory at the end, the splits in a second small kernel.
+//
+// The tokens are the long side, so they are the M side of the products: S^T = K Q^T (m = 16 tokens, n = 8 queries),
+// O^T = V^T P^T (m = 16 channels, n = 8 queries), mma.sync m16n8k16: with one query per head 7/8 of the N side is idle, but a
+// step reads every cached value once and costs 16 mma per 16 tokens; tcgen05 would want the decoded tile in shared
+// memory, which costs more than these products.  A lane decodes a quarter of a token's channels from one 16-byte word of
+// codes with one metadata record, straight into the A fragment of the first product (which channel sits at which k is
+// free, as long as Q agrees); V goes through movmatrix once, because there the tokens are the contracted side.
+//
+// Bound: the decode's ALU and FMA instructions (about 2.4 per cached value with everything, against the 3.1 that fit under
+// 0.5625 bytes of traffic), so close to, but not quite, memory-bound.
+#include "fb4_attend.cuh"
+#include "fb4_staging.cuh"
+
+namespace {
+
+using namespace fb4att;
+using fb4stage::bulk_load;
+using fb4stage::kSpinLimit;
+using fb4stage::mbar_expect_tx;
+using fb4stage::mbar_init;
+using fb4stage::mbar_try_wait;
+
+constexpr int kWarpsFew = 4;
+constexpr int kTile = 32;              // tokens of a warp's tile
+
+template <int D>
+struct Few {
+  static constexpr int kStagesFew = D == 128 ? 3 : 6;
+  static constexpr int kCodes = kTile * D / 2, kMeta = kTile * (D / 32) * 2;
+  static constexpr int kStage = 2 * kCodes + 2 * kMeta;
+  static constexpr int kRing = kWarpsFew * kStagesFew * kStage;
+  // the join of the warps reuses the ring: per warp 16 rows of D sums
+  static constexpr int kJoin = kWarpsFew * 16 * D * 4;
+  static constexpr int kBytes = (kRing > kJoin ? kRing : kJoin);
+};
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_few_kernel(const __grid_constant__ Fb4Attend a) {
+  using L = Few<D>;
+  constexpr int NW = D / 32;             // code words of a lane's quarter row
+  constexpr int ST = L::kStagesFew;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint32_t book[64];
+  __shared__ uint64_t bars[kWarpsFew * ST];
+  __shared__ float2 stat[kWarpsFew][8 * NT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int32_t row_tiles = (a.max_q * a.group + 8 * NT - 1) / (8 * NT);
+
+  int64_t id = blockIdx.x;
+  const int32_t split = (int32_t)(id % a.splits);
+  id /= a.splits;
+  const int32_t head = (int32_t)(id % a.cache.n_heads);
+  id /= a.cache.n_heads;
+  const int32_t row0 = (int32_t)(id % row_tiles) * 8 * NT, b = (int32_t)(id / row_tiles);
+
+  const Sequence sq = sequence(a, b, threadIdx.x == 0 && split == 0 && head == 0 && row0 == 0);
+  const int32_t rows = sq.n_q * a.group;
+  if (row0 >= rows) return;
+  const int32_t n_rows = rows - row0 < 8 * NT ? rows - row0 : 8 * NT;
+  // what any of these rows sees, cut into tiles from its first token's multiple of 32
+  const Range first = visible(a, sq, row0 / a.group), last = visible(a, sq, (row0 + n_rows - 1) / a.group);
+  const int32_t base = first.lo & ~(kTile - 1);
+  const int32_t tiles = last.hi > base && last.hi > first.lo ? (last.hi - base + kTile - 1) / kTile : 0;
+  const int32_t tile0 = split * a.split_tiles;
+  const int32_t tile1 = tiles - tile0 < a.split_tiles ? tiles : tile0 + a.split_tiles;
+  const bool empty = tile0 >= tiles;      // this split has nothing; its record says so
+
+  if (threadIdx.x < 64) fill_book(book, a.tables, threadIdx.x);
+  if (lane == 0) {
+    for (int i = 0; i < ST; ++i) mbar_init(fb4blk::smem_u32(bars + warp * ST + i), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  const uint32_t ring = fb4blk::smem_u32(smem) + warp * ST * L::kStage, bar = fb4blk::smem_u32(bars + warp * ST);
+  const uint32_t book_at = fb4blk::smem_u32(book);
+
+  // the pages of this warp's tiles: lane l holds those of tile `batch + l` (two halves of 16 tokens; equal in pages of 32 or more)
+  const int32_t n_mine = empty || tile0 + warp >= tile1 ? 0 : (tile1 - tile0 - warp + kWarpsFew - 1) / kWarpsFew;
+  const int32_t my0 = tile0 + warp;
+  int32_t page_lo = -1, page_hi = -1;
+  bool bad = false;
+  auto fetch_pages = [&](int32_t from) {
+    page_lo = page_hi = -1;
+    if (from + lane < n_mine) {
+      const int32_t j = base + (my0 + (from + lane) * kWarpsFew) * kTile;
+      const int32_t* pt = a.page_table + (int64_t)b * a.max_pages;
+      if (j < sq.kv) page_lo = __ldg(pt + (j >> a.page_shift));
+      if (j + 16 < sq.kv) page_hi = a.page_shift > 4 ? page_lo : __ldg(pt + ((j + 16) >> a.page_shift));
+      if (j < sq.kv && (uint32_t)page_lo >= (uint64_t)a.cache.n_pages) { bad = true; page_lo = -1; }
+      if (j + 16 < sq.kv && (uint32_t)page_hi >= (uint64_t)a.cache.n_pages) { bad = true; page_hi = -1; }
+    }
+  };
+  // requests tile n of this warp into ring stage n mod ST; which of its halves are there goes to `have` (2 bits per stage)
+  uint32_t have = 0;
+  auto request = [&](int32_t n) {
+    if ((n & 31) == 0) fetch_pages(n);
+    const int32_t plo = __shfl_sync(0xffffffffu, page_lo, n & 31), phi = __shfl_sync(0xffffffffu, page_hi, n & 31);
+    const int st = n % ST;
+    have = (have & ~(3u << (2 * st))) | ((plo >= 0 ? 1u : 0u) | (phi >= 0 ? 2u : 0u)) << (2 * st);
+    if (lane == 0) {
+      const uint32_t dst = ring + st * L::kStage, full = bar + 8 * st;
+      const int32_t j = base + (my0 + n * kWarpsFew) * kTile, at = j & ((1 << a.page_shift) - 1);
+      const bool one = a.page_shift > 4 && plo >= 0;               // one page holds the whole tile
+      const uint32_t halves = one ? 2u : (plo >= 0 ? 1u : 0u) + (phi >= 0 ? 1u : 0u);
+      mbar_expect_tx(full, halves * (L::kStage / 2));
+      auto piece = [&](int32_t page, int32_t place, int half, uint32_t n16) {
+        const int64_t row = (((int64_t)page * a.cache.n_heads + head) << a.page_shift) + place;
+        const uint32_t cb = n16 * (L::kCodes / 2), mb = n16 * (L::kMeta / 2);
+        bulk_load(dst + half * (L::kCodes / 2), a.cache.k_codes + row * (D / 2), cb, full);
+        bulk_load(dst + L::kCodes + half * (L::kCodes / 2), a.cache.v_codes + row * (D / 2), cb, full);
+        bulk_load(dst + 2 * L::kCodes + half * (L::kMeta / 2), a.cache.k_meta + row * (D / 32), mb, full);
+        bulk_load(dst + 2 * L::kCodes + L::kMeta + half * (L::kMeta / 2), a.cache.v_meta + row * (D / 32), mb, full);
+      };
+      if (one) piece(plo, at, 0, 2);
+      else {
+        if (plo >= 0) piece(plo, at, 0, 1);
+        if (phi >= 0) piece(phi, 0, 1, 1);
+      }
+    }
+  };
+#pragma unroll
+  for (int n = 0; n < ST - 1; ++n)
+    if (n < n_mine) request(n);
+
+  // Q as the B side of S^T = K Q^T: lane (g, t) holds query row0 + 8 nt + g, channels of quarter t
+  uint32_t qf[NT][NW][4];
+  int32_t lo[NT][2], hi[NT][2];            // what the two queries of this lane's accumulator columns see
+  int32_t lo_max = 0, hi_min = 0x7fffffff;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int32_t r = row0 + 8 * nt + g;
+    const bool on = r < rows;
+    const uint16_t* src = a.q + (int64_t)(sq.q0 + (on ? r / a.group : 0)) * a.q_ld + (int64_t)(head * a.group + (on ? r % a.group : 0)) * D + t * (D / 4);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (on) u = __ldg(reinterpret_cast<const uint4*>(src + 8 * w));
+      qf[nt][w][0] = prmt(u.x, u.y, 0x5410u);
+      qf[nt][w][1] = prmt(u.x, u.y, 0x7632u);
+      qf[nt][w][2] = prmt(u.z, u.w, 0x5410u);
+      qf[nt][w][3] = prmt(u.z, u.w, 0x7632u);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {          // rows behind the last one are computed like the last one and not stored
+      const int32_t rc = row0 + 8 * nt + 2 * t + k < rows ? row0 + 8 * nt + 2 * t + k : rows - 1;
+      const Range v = visible(a, sq, rc / a.group);
+      lo[nt][k] = v.lo;
+      hi[nt][k] = v.hi;
+      lo_max = max(lo_max, v.lo);
+      hi_min = min(hi_min, v.hi);
+    }
+  }
+  lo_max = __reduce_max_sync(0xffffffffu, lo_max);
+  hi_min = __reduce_min_sync(0xffffffffu, hi_min);
+
+  float o[NT][2 * NW][4];
+  float m[NT][2], l[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int i = 0; i < 2 * NW; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[nt][i][k] = 0.0f;
+    m[nt][0] = m[nt][1] = -INFINITY;
+    l[nt][0] = l[nt][1] = 0.0f;
+  }
+
+  int32_t lost = -1;
+  for (int32_t n = 0; n < n_mine; ++n) {
+    if (n + ST - 1 < n_mine) request(n + ST - 1);
+    const int st = n % ST;
+    const uint32_t parity = (uint32_t)(n / ST) & 1u, full = bar + 8 * st;
+    uint32_t tries = 0;
+    bool ready = mbar_try_wait(full, parity);
+    while (!ready && ++tries < kSpinLimit) ready = mbar_try_wait(full, parity);
+    if (!__all_sync(0xffffffffu, ready)) {
+      lost = n;
+      break;
+    }
+    const uint32_t codes = ring + st * L::kStage, meta = codes + 2 * L::kCodes;
+    const int32_t j0 = base + (my0 + n * kWarpsFew) * kTile;
+    const uint32_t here = (have >> (2 * st)) & 3u;
+    const bool whole = j0 >= lo_max && j0 + kTile <= hi_min && here == 3u;      // nothing of the tile is masked for any row
+
+    auto words = [&](uint32_t at, uint32_t (&w)[NW]) {
+      if (NW == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[NW - 2]), "=r"(w[NW - 1]) : "r"(at));
+      else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    };
+    auto record = [&](uint32_t at) -> uint32_t {
+      uint16_t v;
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+      return v;
+    };
+    auto meta_at = [&](int row) -> uint32_t { return (uint32_t)(row * (D / 32) + t / (4 / (D / 32))) * 2u; };
+
+    // ---- S^T = K Q^T for the tile's two halves of 16 tokens
+    float s[2][NT][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[h][nt][k] = 0.0f;
+      const int ra = 16 * h + g, rb = ra + 8;
+      uint32_t wa[NW], wb[NW];
+      words(codes + ra * (D / 2) + t * (D / 8), wa);
+      words(codes + rb * (D / 2) + t * (D / 8), wb);
+      const BlockScale sa = block_scale(record(meta + meta_at(ra)), book_at, true);
+      const BlockScale sb = block_scale(record(meta + meta_at(rb)), book_at, true);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        uint32_t ka[4], kb[4];
+        decode_word(wa[w], sa, ka);
+        decode_word(wb[w], sb, kb);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma_bf16(s[h][nt], ka[0], kb[0], ka[1], kb[1], qf[nt][w][0], qf[nt][w][1]);
+          mma_bf16(s[h][nt], ka[2], kb[2], ka[3], kb[3], qf[nt][w][2], qf[nt][w][3]);
+        }
+      }
+    }
+    // ---- scores in units of log2, masks, running maximum (moved only when it would grow by more than 2^8: the
+    // accumulators are then rescaled, which is rare after the first tiles)
+    bool grow = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float x = s[h][nt][k] * a.scale_log2;
+          if (!whole) {
+            const int32_t j = j0 + 16 * h + g + (k & 2 ? 8 : 0);
+            if (j < lo[nt][k & 1] || j >= hi[nt][k & 1] || !((here >> h) & 1u)) x = -INFINITY;
+          }
+          s[h][nt][k] = x;
+        }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float top = fmaxf(fmaxf(s[0][nt][k], s[0][nt][k + 2]), fmaxf(s[1][nt][k], s[1][nt][k + 2]));
+        grow |= top > m[nt][k] + 8.0f;
+      }
+    }
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float top = fmaxf(fmaxf(s[0][nt][k], s[0][nt][k + 2]), fmaxf(s[1][nt][k], s[1][nt][k + 2]));
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+          const float next = fmaxf(m[nt][k], top);
+          const float f = next == -INFINITY ? 1.0f : exp2_approx(m[nt][k] - next);
+          m[nt][k] = next;
+          l[nt][k] *= f;
+#pragma unroll
+          for (int i = 0; i < 2 * NW; ++i) {
+            o[nt][i][k] *= f;
+            o[nt][i][k + 2] *= f;
+          }
+        }
+    }
+    uint32_t pf[2][NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float m0 = m[nt][0] == -INFINITY ? 0.0f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.0f : m[nt][1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float p0 = exp2_approx(s[h][nt][0] - m0), p1 = exp2_approx(s[h][nt][1] - m1);
+        const float p2 = exp2_approx(s[h][nt][2] - m0), p3 = exp2_approx(s[h][nt][3] - m1);
+        l[nt][0] += p0 + p2;
+        l[nt][1] += p1 + p3;
+        pf[h][nt][0] = transpose8x8(pack(p0, p1));
+        pf[h][nt][1] = transpose8x8(pack(p2, p3));
+      }
+    }
+    // ---- O^T += V^T P^T
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int ra = 16 * h + g, rb = ra + 8;
+      uint32_t wa[NW], wb[NW];
+      words(codes + L::kCodes + ra * (D / 2) + t * (D / 8), wa);
+      words(codes + L::kCodes + rb * (D / 2) + t * (D / 8), wb);
+      // slots that no token fills may hold anything; an infinity there would meet p = 0
+      const bool ua = whole || (j0 + ra < sq.kv && ((here >> h) & 1u)), ub = whole || (j0 + rb < sq.kv && ((here >> h) & 1u));
+      const BlockScale sa = block_scale(ua ? record(meta + L::kMeta + meta_at(ra)) : 0u, book_at, ua);
+      const BlockScale sb = block_scale(ub ? record(meta + L::kMeta + meta_at(rb)) : 0u, book_at, ub);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        uint32_t va[4], vb[4];
+        decode_word(wa[w], sa, va);
+        decode_word(wb[w], sb, vb);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          va[k] = transpose8x8(va[k]);
+          vb[k] = transpose8x8(vb[k]);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma_bf16(o[nt][2 * w], va[0], va[1], vb[0], vb[1], pf[h][nt][0], pf[h][nt][1]);
+          mma_bf16(o[nt][2 * w + 1], va[2], va[3], vb[2], vb[3], pf[h][nt][0], pf[h][nt][1]);
+        }
+      }
+    }
+    __syncwarp();          // the stage may be filled again
+  }
+  if (lost >= 0) {         // a copy never came: say so, and let the copies still in flight end before the ring is used again
+    if (lane == 0) atomicOr(a.status, 1u);
+    const int32_t asked = lost + ST < n_mine ? lost + ST : n_mine;
+    for (int32_t n = lost + 1; n < asked; ++n) {
+      uint32_t tries = 0;
+      while (!mbar_try_wait(bar + 8 * (n % ST), (uint32_t)(n / ST) & 1u) && ++tries < kSpinLimit) {}
+    }
+  }
+  if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, 2u);
+
+  // ---- join the warps
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) l[nt][k] += __shfl_xor_sync(0xffffffffu, l[nt][k], off);
+      if (g == 0) stat[warp][8 * nt + 2 * t + k] = make_float2(m[nt][k], l[nt][k]);
+    }
+  __syncthreads();         // every warp is done with its ring
+  float* join = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = 8 * nt + 2 * t + k;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWarpsFew; ++w) top = fmaxf(top, stat[w][r].x);
+      const float f = m[nt][k] == -INFINITY ? 0.0f : exp2_approx(m[nt][k] - top);
+      // accumulator (2 w + j, half, column k): nibble {0,1,4,5}[2 j + half] + 2 (g mod 2) of word w of quarter g / 2
+#pragma unroll
+      for (int w = 0; w < NW; ++w)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int c = (g >> 1) * (D / 4) + 8 * w + 4 * j + half + 2 * (g & 1);
+            join[(warp * 8 * NT + r) * D + c] = o[nt][2 * w + j][2 * half + k] * f;
+          }
+    }
+  __syncthreads();
+  for (int x = threadIdx.x; x < n_rows * (D / 4); x += kWarpsFew * 32) {
+    const int r = x / (D / 4), c = x % (D / 4) * 4;
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWarpsFew; ++w) top = fmaxf(top, stat[w][r].x);
+#pragma unroll
+    for (int w = 0; w < kWarpsFew; ++w) sum += stat[w][r].x == -INFINITY ? 0.0f : stat[w][r].y * exp2_approx(stat[w][r].x - top);
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kWarpsFew; ++w) {
+      const float4 u = *reinterpret_cast<const float4*>(join + (w * 8 * NT + r) * D + c);
+      v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    const int32_t i = (row0 + r) / a.group, h = head * a.group + (row0 + r) % a.group;
+    if (a.splits > 1) {
+      const int64_t pr = partial_row(a, b, i, h);
+      if (sum > 0.0f) *reinterpret_cast<float4*>(partial_sums(a, pr, split, D) + c) = v;
+      if (c == 0) *partial_stat(a, pr, split, D) = make_float2(top, sum);
+    } else {
+      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+      store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + c, v, inv);
+      if (c == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    }
+  }
+}
+
+// Joins the splits: one warp per query row and head, lane l holds channels 4 l (D / 128 of them at a time: D = 64 uses half the
+// lanes twice as fast).  Splits that saw nothing have sum 0 and their D sums are not read.
+template <int D>
+__global__ void __launch_bounds__(128) fb4_attend_join_kernel(const __grid_constant__ Fb4Attend a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= partial_rows(a)) return;
+  const int32_t h = (int32_t)(row % a.q_heads);
+  const int64_t bi = row / a.q_heads;
+  const int32_t b = (int32_t)(bi / a.max_q), i = (int32_t)(bi % a.max_q);
+  const Sequence sq = sequence(a, b, false);
+  if (i >= sq.n_q) return;
+  float top = -INFINITY;
+  for (int s = lane; s < a.splits; s += 32) {
+    const float2 st = *partial_stat(a, row, s, D);
+    if (st.y > 0.0f) top = fmaxf(top, st.x);
+  }
+#pragma unroll
+  for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+  float sum = 0.0f;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s0 = 0; s0 < a.splits; s0 += 32) {
+    float w = 0.0f;
+    if (s0 + lane < a.splits) {
+      const float2 st = *partial_stat(a, row, s0 + lane, D);
+      if (st.y > 0.0f) {
+        w = exp2_approx(st.x - top);
+        sum += w * st.y;
+      }
+    }
+    const int n = a.splits - s0 < 32 ? a.splits - s0 : 32;
+#pragma unroll 4
+    for (int s = 0; s < n; ++s) {
+      const float f = __shfl_sync(0xffffffffu, w, s);
+      if (f > 0.0f && lane * 4 < D) {
+        const float4 u = *reinterpret_cast<const float4*>(partial_sums(a, row, s0 + s, D) + lane * 4);
+        v.x = fmaf(u.x, f, v.x); v.y = fmaf(u.y, f, v.y); v.z = fmaf(u.z, f, v.z); v.w = fmaf(u.w, f, v.w);
+      }
+    }
+  }
+#pragma unroll
+  for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  if (lane * 4 < D) store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + lane * 4, v, inv);
+  if (lane == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+}
+
+template <int D, int NT>
+cudaError_t launch(const Fb4Attend& a, cudaStream_t stream) {
+  const int64_t row_tiles = ((int64_t)a.max_q * a.group + 8 * NT - 1) / (8 * NT);
+  const int64_t grid = row_tiles * a.splits * a.cache.n_heads * a.n_seqs;
+  fb4_attend_few_kernel<D, NT><<<(unsigned)grid, kWarpsFew * 32, Few<D>::kBytes, stream>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t fb4_attend_prepare_device() {
+  const cudaFuncAttribute attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(fb4_attend_few_kernel<128, 1>, attr, Few<128>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<128, 2>, attr, Few<128>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<64, 1>, attr, Few<64>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<64, 2>, attr, Few<64>::kBytes);
+  return e;
+}
+
+Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
+                              int32_t max_q, int32_t max_kv) {
+  Fb4AttendPlan p{0, 1, 0x7fffffff / 64, 0};
+  if ((head_dim != 64 && head_dim != 128) || ctx->force_generic || !ctx->attend_ok || n_seqs == 0 || max_q == 0) return p;
+  p.kernel = 1;
+  const int64_t rows = (int64_t)max_q * (q_heads / n_heads), nt = rows <= 8 ? 1 : 2;
+  const int64_t units = (rows + 8 * nt - 1) / (8 * nt) * n_heads * n_seqs;
+  // CTAs that are resident at a time; a split has at least 2 tiles for each of its warps
+  const int64_t slots = (int64_t)ctx->sm_count * (nt == 1 ? 4 : 3);
+  const int64_t tiles = ((int64_t)max_kv + kTile - 1) / kTile + 1;
+  const int64_t most = (tiles + 2 * kWarpsFew - 1) / (2 * kWarpsFew);
+  int64_t s = slots / units;                                        // one wave
+  const int64_t fine = tiles / 32 < 8 ? tiles / 32 : 8;             // sequences of unlike lengths: pieces of 1024 tokens even them out
+  if (s < fine) s = fine;
+  if (s > most) s = most;
+  if (s < 1) s = 1;
+  p.split_tiles = (int32_t)((tiles + s - 1) / s);
+  p.splits = (int32_t)((tiles + p.split_tiles - 1) / p.split_tiles);
+  if (p.splits > 1) p.workspace = (int64_t)n_seqs * max_q * q_heads * p.splits * (head_dim + 2) * 4;
+  return p;
+}
+
+cudaError_t fb4_launch_attend_few(const fb4_ctx*, const Fb4Attend& a, cudaStream_t stream, int* launches) {
+  const bool wide = (int64_t)a.max_q * a.group > 8;
+  cudaError_t e;
+  if (a.cache.head_dim == 128) e = wide ? launch<128, 2>(a, stream) : launch<128, 1>(a, stream);
+  else e = wide ? launch<64, 2>(a, stream) : launch<64, 1>(a, stream);
+  if (e != cudaSuccess || a.splits == 1) return e;
+  const unsigned grid = (unsigned)((partial_rows(a) + 3) / 4);
+  if (a.cache.head_dim == 128) fb4_attend_join_kernel<128><<<grid, 128, 0, stream>>>(a);
+  else fb4_attend_join_kernel<64><<<grid, 128, 0, stream>>>(a);
+  *launches += 1;
+  return cudaGetLastError();
+}

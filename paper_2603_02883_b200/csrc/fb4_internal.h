@@ -51,6 +51,7 @@ struct fb4_ctx {
   size_t fast_table_bytes;
   int force_generic;             // fb4_set_kernel_variant(ctx, 1): always take the generic kernel
   int fast_ok;                   // formatbook/stage-1 table fit the fast kernel's packed layout
+  int attend_ok;                 // the tensor-core attention kernels can be launched on this device
   int sm_count;
   void* d_topk_scratch;          // histograms and counters of the multi-CTA top-k selection (fb4_topk.cu)
   uint32_t* d_status;            // device status word (bit 0: a TMA wait ran out of tries; bit 1: an index argument out of range)
@@ -148,5 +149,16 @@ struct Fb4Attend {
   uint32_t* status;
   float* partial;                // [split][row] records of the split kernels, NULL with one split
   int32_t splits;
+  int32_t split_tiles;           // 32-token tiles per split
 };
+// Launch shape of one call: which kernel, how many splits of the cached tokens.
+struct Fb4AttendPlan {
+  int kernel;                    // 0 = plain, 1 = few query rows per cache head, 2 = many
+  int32_t splits, split_tiles;
+  int64_t workspace;
+};
+Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
+                              int32_t max_q, int32_t max_kv);
+cudaError_t fb4_attend_prepare_device();
+cudaError_t fb4_launch_attend_few(const fb4_ctx* ctx, const Fb4Attend& a, cudaStream_t stream, int* launches);
 cudaError_t fb4_launch_attend_generic(const fb4_ctx* ctx, const Fb4Attend& a, cudaStream_t stream);
