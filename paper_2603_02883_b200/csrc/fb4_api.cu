@@ -726,7 +726,11 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
   int launches = 1;
   cudaError_t e;
   if (plan.kernel == 0) e = fb4_launch_attend_generic(ctx, a, static_cast<cudaStream_t>(stream));
-  else e = fb4_launch_attend_few(ctx, a, static_cast<cudaStream_t>(stream), &launches);
+  else e = plan.kernel == 1 ? fb4_launch_attend_few(a, static_cast<cudaStream_t>(stream)) : fb4_launch_attend_many(a, static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess && plan.splits > 1) {
+    e = fb4_launch_attend_join(a, static_cast<cudaStream_t>(stream));
+    launches = 2;
+  }
   ctx->last_variant = plan.kernel ? "fast" : "generic";
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
   ctx->launches += launches;

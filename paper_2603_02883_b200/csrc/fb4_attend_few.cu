@@ -456,6 +456,7 @@ cudaError_t fb4_attend_prepare_device() {
   if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<128, 2>, attr, Few<128>::kBytes);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<64, 1>, attr, Few<64>::kBytes);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<64, 2>, attr, Few<64>::kBytes);
+  if (e == cudaSuccess) e = fb4_attend_many_prepare_device();
   return e;
 }
 
@@ -463,33 +464,53 @@ Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_hea
                               int32_t max_q, int32_t max_kv) {
   Fb4AttendPlan p{0, 1, 0x7fffffff / 64, 0};
   if ((head_dim != 64 && head_dim != 128) || ctx->force_generic || !ctx->attend_ok || n_seqs == 0 || max_q == 0) return p;
-  p.kernel = 1;
-  const int64_t rows = (int64_t)max_q * (q_heads / n_heads), nt = rows <= 8 ? 1 : 2;
-  const int64_t units = (rows + 8 * nt - 1) / (8 * nt) * n_heads * n_seqs;
-  // CTAs that are resident at a time; a split has at least 2 tiles for each of its warps
-  const int64_t slots = (int64_t)ctx->sm_count * (nt == 1 ? 4 : 3);
-  const int64_t tiles = ((int64_t)max_kv + kTile - 1) / kTile + 1;
-  const int64_t most = (tiles + 2 * kWarpsFew - 1) / (2 * kWarpsFew);
-  int64_t s = slots / units;                                        // one wave
-  const int64_t fine = tiles / 32 < 8 ? tiles / 32 : 8;             // sequences of unlike lengths: pieces of 1024 tokens even them out
-  if (s < fine) s = fine;
-  if (s > most) s = most;
-  if (s < 1) s = 1;
-  p.split_tiles = (int32_t)((tiles + s - 1) / s);
-  p.splits = (int32_t)((tiles + p.split_tiles - 1) / p.split_tiles);
+  const int64_t rows = (int64_t)max_q * (q_heads / n_heads);
+  if (rows <= 16) {
+    p.kernel = 1;
+    const int64_t nt = rows <= 8 ? 1 : 2;
+    const int64_t units = (int64_t)n_heads * n_seqs;
+    // CTAs that are resident at a time; a split has at least 2 tiles for each of its warps
+    const int64_t slots = (int64_t)ctx->sm_count * (nt == 1 ? 4 : 3);
+    const int64_t tiles = ((int64_t)max_kv + kTile - 1) / kTile + 1;
+    const int64_t most = (tiles + 2 * kWarpsFew - 1) / (2 * kWarpsFew);
+    int64_t s = slots / units;                                      // one wave
+    const int64_t fine = tiles / 32 < 8 ? tiles / 32 : 8;           // sequences of unlike lengths: pieces of 1024 tokens even them out
+    if (s < fine) s = fine;
+    if (s > most) s = most;
+    if (s < 1) s = 1;
+    p.split_tiles = (int32_t)((tiles + s - 1) / s);
+    p.splits = (int32_t)((tiles + p.split_tiles - 1) / p.split_tiles);
+  } else {
+    p.kernel = 2;
+    // one CTA per SM: the number of splits that leaves the least of the last wave idle; a split costs about a tile's time
+    // for its start and its partial result, and has at least 4 tiles
+    const int64_t units = (rows + 255) / 256 * n_heads * n_seqs;
+    const int64_t tiles = ((int64_t)max_kv + 127) / 128 + 1;
+    double best = 1e300;
+    p.split_tiles = (int32_t)tiles;
+    for (int64_t s = 1; s <= 32 && (s == 1 || tiles / s >= 4); ++s) {
+      const int64_t per = (tiles + s - 1) / s, waves = (units * s + ctx->sm_count - 1) / ctx->sm_count;
+      const double cost = (double)waves * (double)(per + (s > 1 ? 3 : 1));
+      if (cost < best * 0.97) {
+        best = cost;
+        p.split_tiles = (int32_t)per;
+      }
+    }
+    p.splits = (int32_t)((tiles + p.split_tiles - 1) / p.split_tiles);
+  }
   if (p.splits > 1) p.workspace = (int64_t)n_seqs * max_q * q_heads * p.splits * (head_dim + 2) * 4;
   return p;
 }
 
-cudaError_t fb4_launch_attend_few(const fb4_ctx*, const Fb4Attend& a, cudaStream_t stream, int* launches) {
+cudaError_t fb4_launch_attend_few(const Fb4Attend& a, cudaStream_t stream) {
   const bool wide = (int64_t)a.max_q * a.group > 8;
-  cudaError_t e;
-  if (a.cache.head_dim == 128) e = wide ? launch<128, 2>(a, stream) : launch<128, 1>(a, stream);
-  else e = wide ? launch<64, 2>(a, stream) : launch<64, 1>(a, stream);
-  if (e != cudaSuccess || a.splits == 1) return e;
+  if (a.cache.head_dim == 128) return wide ? launch<128, 2>(a, stream) : launch<128, 1>(a, stream);
+  return wide ? launch<64, 2>(a, stream) : launch<64, 1>(a, stream);
+}
+
+cudaError_t fb4_launch_attend_join(const Fb4Attend& a, cudaStream_t stream) {
   const unsigned grid = (unsigned)((partial_rows(a) + 3) / 4);
   if (a.cache.head_dim == 128) fb4_attend_join_kernel<128><<<grid, 128, 0, stream>>>(a);
   else fb4_attend_join_kernel<64><<<grid, 128, 0, stream>>>(a);
-  *launches += 1;
   return cudaGetLastError();
 }

@@ -1,0 +1,481 @@
+// Attention of many query rows per cache head (prompts in chunks, frames, large groups) over the paged FB4 cache, on the
+// fifth-generation tensor cores.
+//
+// Work: a CTA takes one sequence, one cache head, up to 256 query rows (two tiles of 128; row r = query r / group, head
+// r mod group) and one run of the cached tokens, which it walks in tiles of 128.  Its warps have fixed roles:
+//   load     copies codes and metadata of K and V tiles into a ring (bulk copies, page by page)
+//   decode   8 warps turn them into bf16 tiles in shared memory, 128-byte swizzled, [token][channel] for both K and V
+//   mma      one thread issues S_w = Q_w K^T (both operands in shared memory, accumulator in TMEM) and O_w += P_w V
+//            (P_w from TMEM, V read with the contracted side as the strided one)
+//   softmax  4 warps per query tile, one row per thread: scores from TMEM, running maximum and sum in registers, P back
+//            to TMEM over the scores it came from
+// The two query tiles alternate: while one is in the softmax, the tensor core works for the other, and one decoded tile
+// serves both.  The accumulators stay in TMEM; they are rescaled only when a row's maximum grows by more than 2^8.
+//
+// The decoder leaves channels in the order 0 2 1 3 4 6 5 7 of every eight; Q is staged in the same order (the order of the
+// contracted side is free) and the result is put back in order when it is stored.
+//
+// Bound: per 128 tokens and 256 rows the tensor cores need 2048 cycles, the exponentials 2048 (16 per cycle and SM), and
+// decode + softmax together issue about 6800 of the 8192 instructions that fit in that time.
+#include "fb4_attend.cuh"
+#include "fb4_staging.cuh"
+
+namespace {
+
+using namespace fb4att;
+using fb4blk::smem_u32;
+using fb4stage::bulk_load;
+using fb4stage::kSpinLimit;
+using fb4stage::mbar_expect_tx;
+using fb4stage::mbar_init;
+using fb4stage::mbar_try_wait;
+
+constexpr int kKeys = 128;             // tokens of a tile
+constexpr int kSoftmaxWarps = 8, kDecodeWarps = 8;
+constexpr int kThreads = (kSoftmaxWarps + kDecodeWarps + 2) * 32;
+constexpr int kRing = 3;               // ring stages: a K or a V tile's codes and metadata each
+constexpr int kHave = 8;               // tiles whose page flags are kept
+
+template <int D>
+struct Many {
+  static constexpr int kTileBytes = kKeys * D * 2;                  // one decoded tile, or one query tile
+  static constexpr int kCodes = kKeys * D / 2, kMeta = kKeys * (D / 32) * 2, kStage = kCodes + kMeta;
+  static constexpr int kBytes = 1024 + 2 * kTileBytes + 4 * kTileBytes + kRing * kStage;
+};
+
+struct Bars {
+  uint64_t ring_full[kRing], ring_empty[kRing];
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t s_full[2], p_full[2], o_full[2], drained;
+};
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// Waits for a phase with a limit; a wait that runs out, here or anywhere in the CTA, ends every other one.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
+  uint32_t tries = 0;
+  while (!mbar_try_wait(bar, parity)) {
+    if (++tries >= kSpinLimit || *dead) {
+      *dead = 1u;
+      return false;
+    }
+  }
+  return true;
+}
+
+// ---- tcgen05
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
+  // 128-byte swizzle, descriptor version of sm_100; offsets in units of 16 bytes
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(stride >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// bf16 x bf16 -> f32, M = 128; n_major: B is stored with its N side contiguous
+__host__ __device__ constexpr uint32_t instr_desc(int n, bool n_major) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (n_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
+        "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
+        "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const float (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
+      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]),
+      "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]),
+      "f"(v[30]), "f"(v[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
+// Byte offset of 16-byte run `run` (8 channels) of row `row` in a [128 rows][D] tile of 64-channel columns, 128-byte swizzle
+__device__ __forceinline__ uint32_t swizzled(int row, int run) {
+  return (uint32_t)((run >> 3) * (kKeys * 128) + row * 128 + (((run ^ row) & 7) << 4));
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __grid_constant__ Fb4Attend a) {
+  using L = Many<D>;
+  constexpr int NB = D / 32;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ Bars bars;
+  __shared__ uint32_t book[64];
+  __shared__ uint32_t have[kHave];       // per tile: bit i = its tokens 16 i .. 16 i + 15 lie in a page that exists
+  __shared__ uint32_t tmem_at, dead_flag;
+  const uint32_t base_smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_at = base_smem, k_at = q_at + 2 * L::kTileBytes, v_at = k_at + 2 * L::kTileBytes, ring_at = v_at + 2 * L::kTileBytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile uint32_t* dead = &dead_flag;
+
+  // ---- which work
+  const int32_t row_tiles = (a.max_q * a.group + 255) / 256;
+  int64_t id = blockIdx.x;
+  const int32_t split = (int32_t)(id % a.splits);
+  id /= a.splits;
+  const int32_t rt = row_tiles - 1 - (int32_t)(id % row_tiles);       // under a causal mask the last rows have the most to do
+  id /= row_tiles;
+  const int32_t head = (int32_t)(id % a.cache.n_heads), b = (int32_t)(id / a.cache.n_heads);
+  const Sequence sq = sequence(a, b, threadIdx.x == 0 && split == 0 && head == 0 && rt == 0);
+  const int32_t rows = sq.n_q * a.group, row0 = rt * 256;
+  if (row0 >= rows) return;
+  const int32_t n_rows = rows - row0 < 256 ? rows - row0 : 256;
+  const Range first = visible(a, sq, row0 / a.group), last = visible(a, sq, (row0 + n_rows - 1) / a.group);
+  const int32_t base = first.lo & ~(kKeys - 1);
+  const int32_t all = last.hi > first.lo ? (last.hi - base + kKeys - 1) / kKeys : 0;
+  const int32_t per = a.split_tiles;
+  const int32_t t0 = split * per < all ? split * per : all, t1 = all - t0 < per ? all : t0 + per, n_tiles = t1 - t0;
+  const int n_w = n_rows > 128 ? 2 : 1;                               // query tiles in use
+
+  // ---- set-up
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kRing; ++i) { mbar_init(smem_u32(&bars.ring_full[i]), 1); mbar_init(smem_u32(&bars.ring_empty[i]), kDecodeWarps); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bars.k_full[i]), kDecodeWarps);
+      mbar_init(smem_u32(&bars.k_empty[i]), 1);
+      mbar_init(smem_u32(&bars.v_full[i]), kDecodeWarps);
+      mbar_init(smem_u32(&bars.v_empty[i]), 1);
+      mbar_init(smem_u32(&bars.s_full[i]), 1);
+      mbar_init(smem_u32(&bars.p_full[i]), 4);
+      mbar_init(smem_u32(&bars.o_full[i]), 1);
+    }
+    mbar_init(smem_u32(&bars.drained), 1);
+    dead_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_at)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  if (threadIdx.x >= 64 && threadIdx.x < 128) fill_book(book, a.tables, threadIdx.x - 64);
+  {
+    // Q, in the decoder's channel order; a negative scale is taken into Q's signs (the softmax wants a positive one)
+    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+    for (int x = threadIdx.x; x < n_w * 128 * (D / 8); x += kThreads) {
+      const int row = x / (D / 8), run = x % (D / 8);
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (row < n_rows) {
+        const int32_t r = row0 + row;
+        u = __ldg(reinterpret_cast<const uint4*>(a.q + (int64_t)(sq.q0 + r / a.group) * a.q_ld + (int64_t)(head * a.group + r % a.group) * D + run * 8));
+      }
+      const uint32_t at = q_at + (row >> 7) * L::kTileBytes + swizzled(row & 127, run);
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(prmt(u.x, u.y, 0x5410u) ^ flip), "r"(prmt(u.x, u.y, 0x7632u) ^ flip),
+                   "r"(prmt(u.z, u.w, 0x5410u) ^ flip), "r"(prmt(u.z, u.w, 0x7632u) ^ flip) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = tmem_at;
+  const uint32_t s_col = tmem, o_col = tmem + 256;                    // S_w at columns 128 w (P_w over its first 64), O_w at 256 + D w
+
+  if (warp < kSoftmaxWarps) {
+    // =========================================================== softmax
+    const int w = warp >> 2;
+    if (w < n_w) {
+      const uint32_t lanes = (uint32_t)(warp & 3) << 21;              // this warp's TMEM lanes: 32 (warp mod 4) << 16
+      const uint32_t s_at = s_col + 128 * w + lanes, o_at = o_col + D * w + lanes;
+      const int32_t row = row0 + 128 * w + (warp & 3) * 32 + lane;
+      const bool on = row < rows;
+      const int32_t rc = on ? row : rows - 1;                         // rows behind the last are computed like it and not stored
+      const Range v = visible(a, sq, rc / a.group);
+      const int32_t lo_max = __reduce_max_sync(0xffffffffu, v.lo), hi_min = __reduce_min_sync(0xffffffffu, v.hi);
+      // scale 0 would make 0 * -infinity of a masked score
+      const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);
+      float m = -INFINITY, l = 0.0f;
+      bool ok = true;
+      for (int32_t t = 0; t < n_tiles; ++t) {
+        ok = wait(smem_u32(&bars.s_full[w]), t & 1, dead);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        fence_after();
+        const int32_t j0 = base + (t0 + t) * kKeys;
+        const uint32_t here = *(volatile uint32_t*)&have[t % kHave];
+        const bool whole = j0 >= lo_max && j0 + kKeys <= hi_min && here == 0xffu;
+        float x[32];
+        auto scores = [&](int c) {
+          tmem_ld32(s_at + 32 * c, x);
+          tmem_wait_ld();
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const int32_t j = j0 + 32 * c + i;
+              if (j < v.lo || j >= v.hi || !((here >> (2 * c + (i >> 4))) & 1u)) x[i] = -INFINITY;
+            }
+          }
+        };
+        float top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          scores(c);
+          float u0 = x[0], u1 = x[1], u2 = x[2], u3 = x[3];
+#pragma unroll
+          for (int i = 4; i < 32; i += 4) { u0 = fmaxf(u0, x[i]); u1 = fmaxf(u1, x[i + 1]); u2 = fmaxf(u2, x[i + 2]); u3 = fmaxf(u3, x[i + 3]); }
+          top = fmaxf(top, fmaxf(fmaxf(u0, u1), fmaxf(u2, u3)));
+        }
+        top *= scale;
+        if (__any_sync(0xffffffffu, top > m + 8.0f)) {
+          const float next = fmaxf(m, top);
+          const float f = next == -INFINITY ? 1.0f : exp2_approx(m - next);
+          m = next;
+          l *= f;
+          if (t > 0) {                                                // the product of tile t - 1 was complete before these scores
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              tmem_ld32(o_at + 32 * c, x);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] *= f;
+              tmem_st32(o_at + 32 * c, x);
+            }
+            tmem_wait_st();
+          }
+        }
+        const float mm = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          scores(c);
+          uint32_t p[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float p0 = exp2_approx(fmaf(x[i], scale, -mm)), p1 = exp2_approx(fmaf(x[i + 1], scale, -mm));
+            l += p0 + p1;
+            p[i >> 1] = pack(p0, p1);
+          }
+          tmem_st16(s_at + 16 * c, p);
+        }
+        tmem_wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.p_full[w]));
+      }
+      // ---- result
+      if (ok && n_tiles > 0) {
+        ok = wait(smem_u32(&bars.o_full[w]), 0, dead);
+        ok = __all_sync(0xffffffffu, ok);
+        fence_after();
+      }
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      const int32_t i = rc / a.group, h = head * a.group + rc % a.group;
+      const int64_t pr = partial_row(a, b, i, h);
+      const int64_t out_row = (int64_t)(sq.q0 + i);
+      if (ok) {
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          float x[32];
+          if (n_tiles > 0) {
+            tmem_ld32(o_at + 32 * c, x);
+            tmem_wait_ld();
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) x[k] = 0.0f;
+          }
+          if (on) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {                         // channel order 0 2 1 3 4 6 5 7
+              const float4 u = make_float4(x[k], x[k + 2], x[k + 1], x[k + 3]), z = make_float4(x[k + 4], x[k + 6], x[k + 5], x[k + 7]);
+              if (a.splits > 1) {
+                float4* dst = reinterpret_cast<float4*>(partial_sums(a, pr, split, D) + 32 * c + k);
+                if (l > 0.0f) { dst[0] = u; dst[1] = z; }
+              } else {
+                store_out8(a, out_row * a.out_ld + (int64_t)h * D + 32 * c + k, u, z, inv);
+              }
+            }
+          }
+        }
+        if (on) {
+          if (a.splits > 1) *partial_stat(a, pr, split, D) = make_float2(m, l);
+          else if (a.lse) a.lse[out_row * a.q_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+        }
+      }
+    }
+  } else if (warp < kSoftmaxWarps + kDecodeWarps) {
+    // =========================================================== decode
+    const int dw = warp - kSoftmaxWarps;
+    const uint32_t book_at = smem_u32(book);
+    bool ok = true;
+    for (int32_t part = 0; part < 2 * n_tiles && ok; ++part) {
+      const int32_t t = part >> 1;
+      const bool is_v = part & 1;
+      const int st = part % kRing, buf = t & 1;
+      ok = wait(smem_u32(&bars.ring_full[st]), (part / kRing) & 1, dead);
+      if (ok && t >= 2) ok = wait(smem_u32(is_v ? &bars.v_empty[buf] : &bars.k_empty[buf]), ((t >> 1) - 1) & 1, dead);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const uint32_t codes = ring_at + st * L::kStage, meta = codes + L::kCodes;
+      const uint32_t dst = (is_v ? v_at : k_at) + buf * L::kTileBytes;
+      const uint32_t here = *(volatile uint32_t*)&have[t % kHave];
+      const int32_t j0 = base + (t0 + t) * kKeys;
+#pragma unroll
+      for (int k = 0; k < 4 * NB / kDecodeWarps; ++k) {
+        // 32 rows and one block of each per step; the block varies with the row so that neither side has bank conflicts
+        const int task = dw + k * kDecodeWarps, row = (task & 3) * 32 + lane;
+        const int blk = NB == 4 ? ((task >> 2) + (lane >> 1)) & 3 : task >> 2;
+        uint32_t cw[4];
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cw[0]), "=r"(cw[1]), "=r"(cw[2]), "=r"(cw[3]) : "r"(codes + row * (D / 2) + blk * 16));
+        uint16_t mt;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(mt) : "r"(meta + (row * NB + blk) * 2));
+        // values behind the last token or in a page that is not there must be finite: they meet p = 0
+        const bool use = !is_v || (j0 + row < sq.kv && ((here >> (row >> 4)) & 1u));
+        const BlockScale sc = block_scale(use ? mt : 0u, book_at, use);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t o[4];
+          decode_word(cw[q], sc, o);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + swizzled(row, 4 * blk + q)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(smem_u32(is_v ? &bars.v_full[buf] : &bars.k_full[buf]));
+        mbar_arrive(smem_u32(&bars.ring_empty[st]));
+      }
+    }
+  } else if (warp == kSoftmaxWarps + kDecodeWarps) {
+    // =========================================================== mma
+    if (lane == 0 && n_tiles > 0) {
+      constexpr uint32_t id_s = instr_desc(kKeys, false), id_o = instr_desc(D, true);
+      auto scores = [&](int w, int32_t t) {
+        const uint32_t kb = k_at + (t & 1) * L::kTileBytes, qb = q_at + w * L::kTileBytes;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = (k >> 2) * (kKeys * 128) + (k & 3) * 32;
+          mma_ss(s_col + 128 * w, smem_desc(qb + off, 16, 1024), smem_desc(kb + off, 16, 1024), id_s, k > 0);
+        }
+        commit(smem_u32(&bars.s_full[w]));
+      };
+      auto product = [&](int w, int32_t t) {
+        const uint32_t vb = v_at + (t & 1) * L::kTileBytes;
+#pragma unroll
+        for (int k = 0; k < kKeys / 16; ++k)
+          mma_ts(o_col + D * w, s_col + 128 * w + 8 * k, smem_desc(vb + k * 2048, kKeys * 128, 1024), id_o, t > 0 || k > 0);
+      };
+      bool ok = wait(smem_u32(&bars.k_full[0]), 0, dead);
+      if (ok) {
+        fence_after();
+        for (int w = 0; w < n_w; ++w) scores(w, 0);
+        commit(smem_u32(&bars.k_empty[0]));
+      }
+      for (int32_t t = 0; t < n_tiles && ok; ++t) {
+        ok = wait(smem_u32(&bars.v_full[t & 1]), (t >> 1) & 1, dead);
+        for (int w = 0; w < n_w && ok; ++w) {
+          ok = wait(smem_u32(&bars.p_full[w]), t & 1, dead);
+          if (!ok) break;
+          fence_after();
+          product(w, t);
+          if (t + 1 == n_tiles) commit(smem_u32(&bars.o_full[w]));
+          if (w == n_w - 1) commit(smem_u32(&bars.v_empty[t & 1]));
+          if (t + 1 < n_tiles) {
+            if (w == 0) ok = wait(smem_u32(&bars.k_full[(t + 1) & 1]), ((t + 1) >> 1) & 1, dead);
+            if (!ok) break;
+            fence_after();
+            scores(w, t + 1);
+            if (w == n_w - 1) commit(smem_u32(&bars.k_empty[(t + 1) & 1]));
+          }
+        }
+      }
+      // nothing of this CTA may be on the tensor core when its TMEM is given back
+      commit(smem_u32(&bars.drained));
+      uint32_t tries = 0;
+      while (!mbar_try_wait(smem_u32(&bars.drained), 0) && ++tries < kSpinLimit) {}
+    }
+    __syncwarp();
+  } else {
+    // =========================================================== load
+    const int pieces = a.page_shift >= 7 ? 1 : 128 >> a.page_shift;   // pages that a tile touches (its start is a multiple of 128)
+    const int piece_tokens = kKeys / pieces;
+    bool bad = false, ok = true;
+    int32_t part = 0;
+    for (int32_t t = 0; t < n_tiles && ok; ++t) {
+      const int32_t j0 = base + (t0 + t) * kKeys, j = j0 + lane * piece_tokens;
+      int32_t page = -1;
+      if (lane < pieces && j < sq.kv) {
+        page = __ldg(a.page_table + (int64_t)b * a.max_pages + (j >> a.page_shift));
+        if ((uint32_t)page >= (uint64_t)a.cache.n_pages) { bad = true; page = -1; }
+      }
+      const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
+      uint32_t flags = 0;
+      for (int i = 0; i < 8; ++i) flags |= ((there >> (i * 16 / piece_tokens)) & 1u) << i;
+      const int64_t row = (((int64_t)page * a.cache.n_heads + head) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+      for (int kv = 0; kv < 2; ++kv, ++part) {
+        const int st = part % kRing;
+        if (part >= kRing) ok = wait(smem_u32(&bars.ring_empty[st]), (part / kRing - 1) & 1, dead);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t full = smem_u32(&bars.ring_full[st]), dst = ring_at + st * L::kStage;
+        if (lane == 0) {
+          if (kv == 0) *(volatile uint32_t*)&have[t % kHave] = flags;
+          mbar_expect_tx(full, (uint32_t)__popc(there) * piece_tokens * (D / 2 + D / 16));
+        }
+        __syncwarp();
+        if (page >= 0) {
+          bulk_load(dst + lane * piece_tokens * (D / 2), (kv ? a.cache.v_codes : a.cache.k_codes) + row * (D / 2), piece_tokens * (D / 2), full);
+          bulk_load(dst + L::kCodes + lane * piece_tokens * (D / 16), (kv ? a.cache.v_meta : a.cache.k_meta) + row * NB, piece_tokens * (D / 16), full);
+        }
+      }
+    }
+    if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, 2u);
+    // every copy has to have landed before the CTA ends
+    for (int32_t p = part > kRing ? part - kRing : 0; p < part; ++p) {
+      uint32_t tries = 0;
+      while (!mbar_try_wait(smem_u32(&bars.ring_full[p % kRing]), (p / kRing) & 1) && ++tries < kSpinLimit) {}
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *dead) atomicOr(a.status, 1u);
+  if (warp == 0) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  }
+}
+
+}  // namespace
+
+cudaError_t fb4_attend_many_prepare_device() {
+  const cudaFuncAttribute attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(fb4_attend_many_kernel<128>, attr, Many<128>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_many_kernel<64>, attr, Many<64>::kBytes);
+  return e;
+}
+
+cudaError_t fb4_launch_attend_many(const Fb4Attend& a, cudaStream_t stream) {
+  const int64_t row_tiles = ((int64_t)a.max_q * a.group + 255) / 256;
+  const int64_t grid = row_tiles * a.splits * a.cache.n_heads * a.n_seqs;
+  if (a.cache.head_dim == 128) fb4_attend_many_kernel<128><<<(unsigned)grid, kThreads, Many<128>::kBytes, stream>>>(a);
+  else fb4_attend_many_kernel<64><<<(unsigned)grid, kThreads, Many<64>::kBytes, stream>>>(a);
+  return cudaGetLastError();
+}

@@ -149,7 +149,7 @@ struct Fb4Attend {
   uint32_t* status;
   float* partial;                // [split][row] records of the split kernels, NULL with one split
   int32_t splits;
-  int32_t split_tiles;           // 32-token tiles per split
+  int32_t split_tiles;           // tiles per split: of 32 tokens in the few-row kernel, of 128 in the many-row kernel
 };
 // Launch shape of one call: which kernel, how many splits of the cached tokens.
 struct Fb4AttendPlan {
@@ -160,5 +160,8 @@ struct Fb4AttendPlan {
 Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
                               int32_t max_q, int32_t max_kv);
 cudaError_t fb4_attend_prepare_device();
-cudaError_t fb4_launch_attend_few(const fb4_ctx* ctx, const Fb4Attend& a, cudaStream_t stream, int* launches);
+cudaError_t fb4_attend_many_prepare_device();
+cudaError_t fb4_launch_attend_many(const Fb4Attend& a, cudaStream_t stream);
+cudaError_t fb4_launch_attend_join(const Fb4Attend& a, cudaStream_t stream);
+cudaError_t fb4_launch_attend_few(const Fb4Attend& a, cudaStream_t stream);
 cudaError_t fb4_launch_attend_generic(const fb4_ctx* ctx, const Fb4Attend& a, cudaStream_t stream);
