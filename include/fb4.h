@@ -509,7 +509,7 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q_bf16, int64_t q_ld, int32_t 
 
 /* Size in bytes of the workspace of fb4_cache_attention (0 = none needed; -1 for invalid arguments).  Host only. */
 int64_t fb4_cache_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
-                                      int32_t max_q, int32_t max_kv);
+                                      int32_t max_q, int32_t max_kv, int32_t window);
 
 /*
  * Host-buffer form of fb4_quantize for callers whose tensors live in host memory:

@@ -662,12 +662,12 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
 }
 
 int64_t fb4_cache_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
-                                      int32_t max_q, int32_t max_kv) {
-  if (!ctx || n_heads < 1 || n_heads > 1024 || q_heads < n_heads || q_heads > 1024 || q_heads % n_heads != 0 || head_dim < 32 ||
+                                      int32_t max_q, int32_t max_kv, int32_t window) {
+  if (!ctx || window < 0 || n_heads < 1 || n_heads > 1024 || q_heads < n_heads || q_heads > 1024 || q_heads % n_heads != 0 || head_dim < 32 ||
       head_dim > 256 || head_dim % 32 != 0 || n_seqs < 0 || max_q < 0 || max_kv < 0 || max_kv > (1 << 30) ||
       (int64_t)max_q * q_heads > (1 << 30) || (int64_t)max_q * q_heads * n_seqs > 0x7fffffffLL)
     return -1;
-  return fb4_attend_plan(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv).workspace;
+  return fb4_attend_plan(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window).workspace;
 }
 
 int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_heads, int64_t total_q, const fb4_cache* cache,
@@ -693,7 +693,7 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
   if (((reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(page_table) |
         reinterpret_cast<uintptr_t>(lse)) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return FB4_ERR_ALIGN;
-  const int64_t need = fb4_cache_attention_workspace(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv);
+  const int64_t need = fb4_cache_attention_workspace(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv, window);
   if (need < 0 || workspace_bytes < need || (need > 0 && !workspace)) return FB4_ERR_INVALID_ARG;
   Fb4Attend a{};
   a.q = static_cast<const uint16_t*>(q);
@@ -719,7 +719,7 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
   a.lse = lse;
   a.tables = ctx->d_tables;
   a.status = ctx->d_status;
-  const Fb4AttendPlan plan = fb4_attend_plan(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv);
+  const Fb4AttendPlan plan = fb4_attend_plan(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv, window);
   a.splits = plan.splits;
   a.split_tiles = plan.split_tiles;
   a.partial = plan.splits > 1 ? static_cast<float*>(workspace) : nullptr;

@@ -461,17 +461,19 @@ cudaError_t fb4_attend_prepare_device() {
 }
 
 Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
-                              int32_t max_q, int32_t max_kv) {
+                              int32_t max_q, int32_t max_kv, int32_t window) {
   Fb4AttendPlan p{0, 1, 0x7fffffff / 64, 0};
   if ((head_dim != 64 && head_dim != 128) || ctx->force_generic || !ctx->attend_ok || n_seqs == 0 || max_q == 0) return p;
   const int64_t rows = (int64_t)max_q * (q_heads / n_heads);
+  // the longest run of tokens that a CTA's rows can see together
+  const int64_t span = window > 0 && (int64_t)window + max_q < max_kv ? (int64_t)window + max_q : max_kv;
   if (rows <= 16) {
     p.kernel = 1;
     const int64_t nt = rows <= 8 ? 1 : 2;
     const int64_t units = (int64_t)n_heads * n_seqs;
     // CTAs that are resident at a time; a split has at least 2 tiles for each of its warps
     const int64_t slots = (int64_t)ctx->sm_count * (nt == 1 ? 4 : 3);
-    const int64_t tiles = ((int64_t)max_kv + kTile - 1) / kTile + 1;
+    const int64_t tiles = (span + kTile - 1) / kTile + 1;
     const int64_t most = (tiles + 2 * kWarpsFew - 1) / (2 * kWarpsFew);
     int64_t s = slots / units;                                      // one wave
     const int64_t fine = tiles / 32 < 8 ? tiles / 32 : 8;           // sequences of unlike lengths: pieces of 1024 tokens even them out
@@ -485,7 +487,7 @@ Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_hea
     // one CTA per SM: the number of splits that leaves the least of the last wave idle; a split costs about a tile's time
     // for its start and its partial result, and has at least 4 tiles
     const int64_t units = (rows + 255) / 256 * n_heads * n_seqs;
-    const int64_t tiles = ((int64_t)max_kv + 127) / 128 + 1;
+    const int64_t tiles = (span + 127) / 128 + 1;
     double best = 1e300;
     p.split_tiles = (int32_t)tiles;
     for (int64_t s = 1; s <= 32 && (s == 1 || tiles / s >= 4); ++s) {

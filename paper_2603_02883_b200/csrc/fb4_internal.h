@@ -158,7 +158,7 @@ struct Fb4AttendPlan {
   int64_t workspace;
 };
 Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
-                              int32_t max_q, int32_t max_kv);
+                              int32_t max_q, int32_t max_kv, int32_t window);
 cudaError_t fb4_attend_prepare_device();
 cudaError_t fb4_attend_many_prepare_device();
 cudaError_t fb4_launch_attend_many(const Fb4Attend& a, cudaStream_t stream);

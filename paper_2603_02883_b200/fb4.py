@@ -7,6 +7,7 @@ missing and cannot be built, importing this module raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -111,7 +112,7 @@ def lib() -> ctypes.CDLL:
     L.fb4_cache_attention.argtypes = [vp, vp, i64, i32, i64, cp, vp, i32, vp, vp, i32, i32, i32, cf, ci, i32, vp, i64, ci, vp,
                                       vp, i64, vp]
     L.fb4_cache_attention.restype = ci
-    L.fb4_cache_attention_workspace.argtypes = [vp, i32, i32, i32, i32, i32, i32]
+    L.fb4_cache_attention_workspace.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32]
     L.fb4_cache_attention_workspace.restype = i64
     L.fb4_quantize_mxfp8.argtypes = [vp, vp, i64, i64, i64, vp, vp, i32, vp, vp, ci, vp]
     L.fb4_quantize_mxfp8.restype = ci
@@ -144,15 +145,17 @@ def lib() -> ctypes.CDLL:
 def _ptr(t):
     if t is None:
         return None
-    if isinstance(t, torch.Tensor):
-        return ctypes.c_void_p(t.data_ptr())
-    return ctypes.c_void_p(int(t))
+    return t.data_ptr() if isinstance(t, torch.Tensor) else int(t)
+
+
+# the handle of a device's current stream without building a torch.cuda.Stream around it (3 us of a 10 us call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _stream(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+        return _raw_stream(torch.cuda.current_device())
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _check(rc: int, where: str):
@@ -334,8 +337,8 @@ def fb4_cache_attention(ctx, q, q_ld, q_heads, total_q, cache, page_table, max_p
            "fb4_cache_attention")
 
 
-def fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv) -> int:
-    return int(lib().fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv))
+def fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window) -> int:
+    return int(lib().fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window))
 
 
 def fb4_quantize_host(ctx, x_host, T, C, d_x, d_codes, d_meta, codes_host, meta_host) -> None:
@@ -389,6 +392,11 @@ class Cache:
     k_meta: torch.Tensor                     # uint16 bits in an int16 tensor [n_pages][n_heads][page_tokens][D/32]
     v_codes: torch.Tensor
     v_meta: torch.Tensor
+
+
+_INT4 = ctypes.c_int32 * 4
+_NO_GUARD = contextlib.nullcontext()
+_OUT_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class Fb4:
@@ -567,52 +575,65 @@ class Fb4:
 
     # ---- attention side: norm + rotation of q and k, paged cache, attention over it
 
+    def _guard(self):
+        """the context's device made current, where it is not already"""
+        return _NO_GUARD if torch.cuda.current_device() == self.device else torch.cuda.device(self.device)
+
     def _on(self, *tensors):
         for t in tensors:
-            if t is not None and (not t.is_cuda or t.device.index != self.device):
+            if t is not None and t.get_device() != self.device:
                 raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
 
-    @staticmethod
-    def _heads(x):
+    def _heads(self, x):
         """(T, heads, D, token stride) of a [T][heads][D] bf16 tensor whose heads lie next to one another"""
-        if x.dtype != torch.bfloat16 or x.dim() != 3:
+        shape = x.shape
+        if x.dtype is not torch.bfloat16 or len(shape) != 3:
             raise ValueError("expected a bfloat16 tensor [tokens][heads][D]")
-        T, H, D = x.shape
-        if (D > 1 and x.stride(2) != 1) or (H > 1 and x.stride(1) != D):
+        if x.get_device() != self.device:
+            raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
+        T, H, D = shape
+        ld, hd, one = x.stride()
+        if (one != 1 and D > 1) or (hd != D and H > 1):
             raise ValueError("the heads of a token must lie next to one another, channels contiguous")
-        return T, H, D, (x.stride(0) if T > 1 else H * D)
+        return T, H, D, (ld if T > 1 else H * D)
 
     def _rope(self, rope: Rope | None, T: int, D: int):
         if rope is None:
             return None
-        self._on(rope.table, rope.pos)
-        pairs = [int(n) for n in rope.axis_pairs]
-        if not 1 <= len(pairs) <= 4:
+        table, pos, pairs = rope.table, rope.pos, rope.axis_pairs
+        n = len(pairs)
+        if not 1 <= n <= 4:
             raise ValueError("a rotation has 1 to 4 axes")
-        if rope.table.dtype != torch.float32 or not rope.table.is_contiguous() or tuple(rope.table.shape[1:]) != (D // 2, 2):
+        if table.dtype is not torch.float32 or table.dim() != 3 or table.shape[1] * 2 != D or table.shape[2] != 2 or \
+                not table.is_contiguous():
             raise ValueError("rope.table must be a contiguous float32 tensor [n_pos][D/2][2]")
-        if rope.pos.dtype != torch.int32 or not rope.pos.is_contiguous() or rope.pos.numel() != T * len(pairs) or \
-                (T and rope.pos.shape[0] != T):
+        if pos.dtype is not torch.int32 or pos.numel() != T * n or (T and pos.shape[0] != T) or not pos.is_contiguous():
             raise ValueError("rope.pos must be a contiguous int32 tensor [T][n_axes]")
-        return Fb4Rope(rope.table.data_ptr(), rope.table.shape[0], rope.pos.data_ptr(), len(pairs),
-                       (ctypes.c_int32 * 4)(*pairs), int(bool(rope.interleaved)))
+        self._on(table, pos)
+        return Fb4Rope(table.data_ptr(), table.shape[0], pos.data_ptr(), n, _INT4(*pairs), 1 if rope.interleaved else 0)
 
-    @staticmethod
-    def _gain(gain, D):
-        if gain is not None and (gain.dtype != torch.bfloat16 or gain.numel() != D or not gain.is_contiguous()):
+    def _gain(self, gain, D):
+        """address of a gain, or None"""
+        if gain is None:
+            return None
+        if gain.dtype is not torch.bfloat16 or gain.numel() != D or not gain.is_contiguous():
             raise ValueError("a gain must be a contiguous bfloat16 tensor [D]")
+        self._on(gain)
+        return gain.data_ptr()
 
     def _cache(self, c: Cache) -> Fb4Cache:
-        self._on(c.k_codes, c.k_meta, c.v_codes, c.v_meta)
-        if c.k_codes.dim() != 4:
+        kc, km, vc, vm = c.k_codes, c.k_meta, c.v_codes, c.v_meta
+        if kc.dim() != 4:
             raise ValueError("cache codes must be [n_pages][n_heads][page_tokens][D/2]")
-        n, h, p, half = c.k_codes.shape
-        for codes, meta in ((c.k_codes, c.k_meta), (c.v_codes, c.v_meta)):
-            if codes.dtype != torch.uint8 or tuple(codes.shape) != (n, h, p, half) or not codes.is_contiguous():
-                raise ValueError("cache codes must be contiguous uint8 [n_pages][n_heads][page_tokens][D/2]")
-            if meta.element_size() != 2 or tuple(meta.shape) != (n, h, p, half // 16) or not meta.is_contiguous():
-                raise ValueError("cache meta must be contiguous 16-bit [n_pages][n_heads][page_tokens][D/32]")
-        return Fb4Cache(c.k_codes.data_ptr(), c.k_meta.data_ptr(), c.v_codes.data_ptr(), c.v_meta.data_ptr(), n, p, h, half * 2)
+        n, h, p, half = shape = kc.shape
+        meta = (n, h, p, half // 16)
+        if kc.dtype is not torch.uint8 or vc.dtype is not torch.uint8 or vc.shape != shape or not kc.is_contiguous() or not vc.is_contiguous():
+            raise ValueError("cache codes must be contiguous uint8 [n_pages][n_heads][page_tokens][D/2]")
+        if km.element_size() != 2 or vm.element_size() != 2 or km.shape != meta or vm.shape != meta or not km.is_contiguous() or \
+                not vm.is_contiguous():
+            raise ValueError("cache meta must be contiguous 16-bit [n_pages][n_heads][page_tokens][D/32]")
+        self._on(kc, km, vc, vm)
+        return Fb4Cache(kc.data_ptr(), km.data_ptr(), vc.data_ptr(), vm.data_ptr(), n, p, h, half * 2)
 
     def new_cache(self, n_pages: int, page_tokens: int, n_heads: int, head_dim: int) -> Cache:
         """an empty cache: all zero, so every slot reads as zeros"""
@@ -626,20 +647,19 @@ class Fb4:
         to write to, which may be q and k themselves"""
         T, Hq, D, q_ld = self._heads(q)
         Tk, Hk, Dk, k_ld = self._heads(k)
-        if (Tk, Dk) != (T, D):
+        if Tk != T or Dk != D:
             raise ValueError("q and k must have the same tokens and head dimension")
-        self._on(q, k, q_gain, k_gain)
-        self._gain(q_gain, D)
-        self._gain(k_gain, D)
-        with torch.cuda.device(self.device):
-            qo, ko = out if out is not None else (torch.empty((T, Hq, D), dtype=q.dtype, device=q.device),
-                                                  torch.empty((T, Hk, D), dtype=k.dtype, device=k.device))
-            self._on(qo, ko)
+        qg, kg, r = self._gain(q_gain, D), self._gain(k_gain, D), self._rope(rope, T, D)
+        if out is None:
+            qo, ko, qo_ld, ko_ld = q.new_empty((T, Hq, D)), k.new_empty((T, Hk, D)), Hq * D, Hk * D
+        else:
+            qo, ko = out
             (Ta, Ha, Da, qo_ld), (Tb, Hb, Db, ko_ld) = self._heads(qo), self._heads(ko)
             if (Ta, Ha, Da) != (T, Hq, D) or (Tb, Hb, Db) != (T, Hk, D):
                 raise ValueError("out must have the shapes of q and k")
-            fb4_qk_norm_rope(self.ctx, q, Hq, q_ld, k, Hk, k_ld, T, D, q_gain, k_gain, eps, self._rope(rope, T, D), qo, qo_ld,
-                             ko, ko_ld)
+        with self._guard():
+            _check(lib().fb4_qk_norm_rope(self.ctx, q.data_ptr(), Hq, q_ld, k.data_ptr(), Hk, k_ld, T, D, qg, kg, eps, r, qo.data_ptr(),
+                                          qo_ld, ko.data_ptr(), ko_ld, _raw_stream(self.device)), "fb4_qk_norm_rope")
         return qo, ko
 
     def cache_append(self, cache: Cache, slot, k, v, k_gain=None, eps: float = 1e-6, rope: Rope | None = None, q=None,
@@ -649,23 +669,24 @@ class Fb4:
         T, H, D, k_ld = self._heads(k)
         Tv, Hv, Dv, v_ld = self._heads(v)
         c = self._cache(cache)
-        if (Tv, Hv, Dv) != (T, H, D) or H != c.n_heads or D != c.head_dim:
+        if Tv != T or Hv != H or Dv != D or H != c.n_heads or D != c.head_dim:
             raise ValueError("k and v must have the heads and the head dimension of the cache")
-        if slot.dtype != torch.int64 or slot.numel() != T or not slot.is_contiguous():
+        if slot.dtype is not torch.int64 or slot.numel() != T or not slot.is_contiguous():
             raise ValueError("slot must be a contiguous int64 tensor [T]")
-        self._on(slot, k, v, q, k_gain, q_gain)
-        self._gain(k_gain, D)
-        with torch.cuda.device(self.device):
-            Hq = q_ld = 0
-            qo = None
-            if q is not None:
-                Tq, Hq, Dq, q_ld = self._heads(q)
-                if (Tq, Dq) != (T, D):
-                    raise ValueError("q must have the tokens and the head dimension of k")
-                self._gain(q_gain, D)
-                qo = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
-            fb4_cache_append(self.ctx, c, slot, k, k_ld, v, v_ld, T, k_gain, eps, self._rope(rope, T, D), q, Hq, q_ld, q_gain,
-                             qo, Hq * D)
+        self._on(slot)
+        kg, r = self._gain(k_gain, D), self._rope(rope, T, D)
+        Hq = q_ld = 0
+        qo = qp = qg = qop = None
+        if q is not None:
+            Tq, Hq, Dq, q_ld = self._heads(q)
+            if Tq != T or Dq != D:
+                raise ValueError("q must have the tokens and the head dimension of k")
+            qg = self._gain(q_gain, D)
+            qo = q.new_empty((T, Hq, D))
+            qp, qop = q.data_ptr(), qo.data_ptr()
+        with self._guard():
+            _check(lib().fb4_cache_append(self.ctx, c, slot.data_ptr(), k.data_ptr(), k_ld, v.data_ptr(), v_ld, T, kg, eps, r, qp, Hq,
+                                          q_ld, qg, qop, Hq * D, _raw_stream(self.device)), "fb4_cache_append")
         return qo
 
     def cache_attention(self, q, cache: Cache, page_table, kv_len, q_start, max_q: int, max_kv: int, scale: float | None = None,
@@ -676,32 +697,38 @@ class Fb4:
         c = self._cache(cache)
         if D != c.head_dim:
             raise ValueError("q must have the head dimension of the cache")
-        self._on(q, page_table, kv_len, q_start)
         n = kv_len.numel()
-        for t, shape in ((page_table, (n, page_table.shape[-1])), (kv_len, (n,)), (q_start, (n + 1,))):
-            if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
-                raise ValueError("page_table [n_seqs][max_pages], kv_len [n_seqs] and q_start [n_seqs + 1] must be contiguous int32")
-        with torch.cuda.device(self.device):
-            out = torch.empty((total, Hq, D), dtype=dtype, device=q.device)
-            lse = torch.empty((total, Hq), dtype=torch.float32, device=q.device)
-            need = max(fb4_cache_attention_workspace(self.ctx, Hq, c.n_heads, D, n, max_q, max_kv), 0)
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-            fb4_cache_attention(self.ctx, q, q_ld, Hq, total, c, page_table, page_table.shape[1], kv_len, q_start, n, max_q, max_kv,
-                                D ** -0.5 if scale is None else scale, causal, window, out, Hq * D,
-                                {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[dtype], lse, ws, need)
+        if page_table.dim() != 2 or page_table.shape[0] != n or kv_len.dim() != 1 or q_start.dim() != 1 or q_start.numel() != n + 1:
+            raise ValueError("expected page_table [n_seqs][max_pages], kv_len [n_seqs] and q_start [n_seqs + 1]")
+        for t in (page_table, kv_len, q_start):
+            if t.dtype is not torch.int32 or not t.is_contiguous():
+                raise ValueError("page_table, kv_len and q_start must be contiguous int32")
+        self._on(page_table, kv_len, q_start)
+        L = lib()
+        out = q.new_empty((total, Hq, D)) if dtype is torch.bfloat16 else q.new_empty((total, Hq, D), dtype=dtype)
+        lse = q.new_empty((total, Hq), dtype=torch.float32)
+        need = L.fb4_cache_attention_workspace(self.ctx, Hq, c.n_heads, D, n, max_q, max_kv, window)
+        ws = q.new_empty(need // 2) if need > 0 else None
+        with self._guard():
+            _check(L.fb4_cache_attention(self.ctx, q.data_ptr(), q_ld, Hq, total, c, page_table.data_ptr(), page_table.shape[1],
+                                         kv_len.data_ptr(), q_start.data_ptr(), n, max_q, max_kv, D ** -0.5 if scale is None else scale,
+                                         1 if causal else 0, window, out.data_ptr(), Hq * D, _OUT_DTYPE[dtype], lse.data_ptr(),
+                                         None if ws is None else ws.data_ptr(), need, _raw_stream(self.device)), "fb4_cache_attention")
         return out, lse
 
     def cache_values(self, cache: Cache, dtype=torch.float32):
         """(k, v) [n_pages][n_heads][page_tokens][D]: all that a cache holds, decoded"""
         c = self._cache(cache)
-        out = []
-        with torch.cuda.device(self.device):
-            for codes, meta in ((cache.k_codes, cache.k_meta), (cache.v_codes, cache.v_meta)):
-                x = torch.empty((*codes.shape[:3], c.head_dim), dtype=dtype, device=codes.device)
-                fb4_dequantize(self.ctx, codes, meta, c.n_pages * c.n_heads * c.page_tokens, c.head_dim, None, 0, None, None, x,
-                               {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[dtype])
-                out.append(x)
-        return tuple(out)
+        shape = (c.n_pages, c.n_heads, c.page_tokens, c.head_dim)
+        rows = c.n_pages * c.n_heads * c.page_tokens
+        k, v = cache.k_codes.new_empty(shape, dtype=dtype), cache.k_codes.new_empty(shape, dtype=dtype)
+        L = lib()
+        with self._guard():
+            st = _raw_stream(self.device)
+            for codes, meta, x in ((c.k_codes, c.k_meta, k), (c.v_codes, c.v_meta, v)):
+                _check(L.fb4_dequantize(self.ctx, codes, meta, rows, c.head_dim, None, 0, None, None, x.data_ptr(), _OUT_DTYPE[dtype], st),
+                       "fb4_dequantize")
+        return k, v
 
     def set_kernel_variant(self, variant: int) -> None:
         fb4_set_kernel_variant(self.ctx, variant)

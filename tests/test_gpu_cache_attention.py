@@ -147,7 +147,7 @@ def test_strided_queries_and_rows_of_no_sequence(q32):
     big[:63, 2:6] = q
     out = torch.full((70, 6 * 128), 5.0, dtype=torch.bfloat16, device="cuda")
     lse = torch.full((70, 4), 5.0, device="cuda")
-    need = fb4.fb4_cache_attention_workspace(q32.ctx, 4, 2, 128, 2, mq, mkv)
+    need = fb4.fb4_cache_attention_workspace(q32.ctx, 4, 2, 128, 2, mq, mkv, 0)
     ws = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
     fb4.fb4_cache_attention(q32.ctx, big[:, 2:], 1280, 4, 70, q32._cache(cache), table, table.shape[1], kv, qs, 2, mq, mkv, 128 ** -0.5,
                             True, 0, out[:, 128:], 768, 1, lse, ws if need else None, need)
@@ -226,7 +226,7 @@ def test_refusals(q32):
     q, cache, table, kv, qs, mq, mkv = setup(q32, [2, 3], [100, 60], 4, 2, 64, 16, seed=2)
     c = q32._cache(cache)
     out = torch.empty(5, 4, 64, dtype=torch.bfloat16, device="cuda")
-    need = fb4.fb4_cache_attention_workspace(q32.ctx, 4, 2, 64, 2, mq, mkv)
+    need = fb4.fb4_cache_attention_workspace(q32.ctx, 4, 2, 64, 2, mq, mkv, 0)
     ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
     ok = dict(q=q, q_ld=256, q_heads=4, total_q=5, cache=c, page_table=table, max_pages=table.shape[1], kv_len=kv, q_start=qs, n_seqs=2,
               max_q=mq, max_kv=mkv, scale=0.1, causal=True, window=0, out=out, out_ld=256, out_dtype=1, lse=None, workspace=ws,
@@ -248,7 +248,7 @@ def test_refusals(q32):
     assert code(workspace=ws.data_ptr() + 16) == fb4.ERR_ALIGN and code(kv_len=kv.data_ptr() + 2) == fb4.ERR_ALIGN
     if need:
         assert code(workspace=None) == fb4.ERR_INVALID_ARG and code(workspace_bytes=need - 1) == fb4.ERR_INVALID_ARG
-    assert fb4.fb4_cache_attention_workspace(q32.ctx, 3, 2, 64, 1, 1, 1) == -1
+    assert fb4.fb4_cache_attention_workspace(q32.ctx, 3, 2, 64, 1, 1, 1, 0) == -1
     z = fb4.Fb4(block_size=16)
     assert code(ctx=z.ctx) == fb4.ERR_INVALID_ARG
     z.close()
