@@ -496,9 +496,12 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
  *   out        : device [total_q][q_heads][D] with token stride out_ld (elements), out_dtype 0 = float32, 1 = bfloat16,
  *                2 = IEEE half; 16-byte aligned, out_ld * element size a multiple of 16.  Rows of no sequence are left alone
  *   lse        : device float32 [total_q][q_heads]: log of the sum of exp(scale * q . k) over the visible tokens; or NULL
+ *   scale      : at most 2^60 in magnitude
  *   workspace  : device, 256-byte aligned, workspace_bytes >= fb4_cache_attention_workspace(...) of the same arguments
  *                (FB4_ERR_INVALID_ARG otherwise; NULL when that is 0).  It holds partial results between the launches of one
  *                call: two calls that may run at the same time need two workspaces
+ * D = 64 and 128 run on the tensor cores, other head dimensions in a plain kernel.  The tensor-core kernels read a cached
+ * element to within 2^-70, and a block whose element scale is above 2^61 as if that were 2^61.
  * Needs block size 32 (FB4_ERR_INVALID_ARG otherwise); the context's formatbook decodes the cache.
  */
 int fb4_cache_attention(fb4_ctx* ctx, const void* q_bf16, int64_t q_ld, int32_t q_heads, int64_t total_q,

@@ -675,7 +675,7 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
                         int32_t n_seqs, int32_t max_q, int32_t max_kv, float scale, int causal, int32_t window, void* out,
                         int64_t out_ld, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
   if (!ctx || ctx->cfg.block_size != 32) return FB4_ERR_INVALID_ARG;
-  if ((causal != 0 && causal != 1) || window < 0 || out_dtype < 0 || out_dtype > 2 || !(scale > -3.0e38f && scale < 3.0e38f))
+  if ((causal != 0 && causal != 1) || window < 0 || out_dtype < 0 || out_dtype > 2 || !(scale >= -0x1p60f && scale <= 0x1p60f))
     return FB4_ERR_INVALID_ARG;
   int rc = check_cache(cache);
   if (rc != FB4_OK) return rc;
@@ -722,12 +722,12 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
   const Fb4AttendPlan plan = fb4_attend_plan(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv, window);
   a.splits = plan.splits;
   a.split_tiles = plan.split_tiles;
-  a.partial = plan.splits > 1 ? static_cast<float*>(workspace) : nullptr;
+  a.partial = plan.workspace > 0 ? static_cast<float*>(workspace) : nullptr;
   int launches = 1;
   cudaError_t e;
   if (plan.kernel == 0) e = fb4_launch_attend_generic(ctx, a, static_cast<cudaStream_t>(stream));
   else e = plan.kernel == 1 ? fb4_launch_attend_few(a, static_cast<cudaStream_t>(stream)) : fb4_launch_attend_many(a, static_cast<cudaStream_t>(stream));
-  if (e == cudaSuccess && plan.splits > 1) {
+  if (e == cudaSuccess && a.partial) {
     e = fb4_launch_attend_join(a, static_cast<cudaStream_t>(stream));
     launches = 2;
   }

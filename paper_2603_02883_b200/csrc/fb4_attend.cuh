@@ -48,14 +48,18 @@ __device__ __forceinline__ Range visible(const Fb4Attend& a, const Sequence& s, 
 // ---- decode of FB4 codes to packed bf16 pairs
 //
 // A magnitude m (0..15) enters as the byte 8 m: as the low byte of a bf16 whose high byte holds the sign alone it is the
-// subnormal number m * 2^-130, and two multiplications by powers of two (exact) bring it to m * 2^(scale byte - 127).
-// That leaves one table permute per four elements, one permute per pair that joins magnitudes and signs, and moves the rest
-// to the FMA pipe; a table of bf16 magnitudes takes two permutes per four elements, a third for their signs and a
-// scaled table of its own for every block.
+// subnormal number m * 2^-130, and one multiplication by a power of two brings it to m * 2^(scale byte - 127) * 2^-64.
+// That leaves one table permute per four elements, one permute per pair that joins magnitudes and signs, and one
+// multiplication per pair on the FMA pipe; a table of bf16 magnitudes takes two permutes per four elements, a third for
+// their signs and a scaled table of its own for every block.  The factor 2^-64 keeps the multiplier in range for scale
+// bytes up to 188 (element scale 2^61; larger ones are read as 188) and is made good in the softmax scale and in the last
+// division; a product below 2^-133, an element below 2^-69, is rounded to a multiple of that.
+
+constexpr float kUnshift = 0x1p64f;
 
 struct BlockScale {
   uint32_t t0, t1;          // the dialect's magnitudes, 8 m per byte
-  uint32_t a, b;            // 2^x in both halves, 2^a * 2^b = 2^(scale byte + 3)
+  uint32_t f;               // 2^(scale byte + 66 - 127) in both halves
 };
 
 __device__ __forceinline__ uint32_t prmt(uint32_t x, uint32_t y, uint32_t sel) {
@@ -70,25 +74,24 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t x, uint32_t y) {
 }
 
 // book = shared address of the 32 dialects' magnitude bytes; use = false: every element reads as zero, whatever the
-// record holds (scale bytes up to 251 exist; a larger one stands in a slot that was never written)
+// record holds
 __device__ __forceinline__ BlockScale block_scale(uint32_t meta, uint32_t book, bool use) {
   BlockScale s;
   asm("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(s.t0), "=r"(s.t1) : "r"(book + ((meta >> 5) & 0xf8u)));
-  const uint32_t x = (meta & 255u) + 3u, a = x >> 1;
-  s.a = (a + 127u) * 0x00800080u;
-  s.b = use ? (x - a + 127u) * 0x00800080u : 0u;
+  const uint32_t x = min(meta & 255u, 188u);
+  s.f = use ? x * 0x00800080u + 66u * 0x00800080u : 0u;
   return s;
 }
 
-// One code word (8 channels n0..n7) -> the pairs (n0,n2) (n1,n3) (n4,n6) (n5,n7)
+// One code word (8 channels n0..n7) -> the pairs (n0,n2) (n1,n3) (n4,n6) (n5,n7), times 2^-64
 __device__ __forceinline__ void decode_word(uint32_t w, const BlockScale& s, uint32_t (&o)[4]) {
   const uint32_t sel = w & 0x77777777u;
   const uint32_t lo = prmt(s.t0, s.t1, sel), hi = prmt(s.t0, s.t1, sel >> 16);
   const uint32_t odd = w & 0x80808080u, even = (w << 4) & 0x80808080u;
-  o[0] = mul_bf16x2(mul_bf16x2(prmt(lo, even, 0x5240u), s.a), s.b);
-  o[1] = mul_bf16x2(mul_bf16x2(prmt(lo, odd, 0x5341u), s.a), s.b);
-  o[2] = mul_bf16x2(mul_bf16x2(prmt(hi, even, 0x7260u), s.a), s.b);
-  o[3] = mul_bf16x2(mul_bf16x2(prmt(hi, odd, 0x7361u), s.a), s.b);
+  o[0] = mul_bf16x2(prmt(lo, even, 0x5240u), s.f);
+  o[1] = mul_bf16x2(prmt(lo, odd, 0x5341u), s.f);
+  o[2] = mul_bf16x2(prmt(hi, even, 0x7260u), s.f);
+  o[3] = mul_bf16x2(prmt(hi, odd, 0x7361u), s.f);
 }
 
 // thread i of 64 writes word i of the magnitude bytes (256 bytes at book)
@@ -102,8 +105,8 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
-// ---- partial results of a split call: per row (b * max_q + i) * q_heads + h and split, D sums of the second product and
-// (running maximum, sum) of the softmax; the maximum in units of log2
+// ---- partial results of a split call: per row (b * max_q + i) * q_heads + h and split, D sums of the second product
+// (times 2^-64) and (running maximum, sum) of the softmax; the maximum in units of log2
 __device__ __forceinline__ int64_t partial_row(const Fb4Attend& a, int32_t b, int32_t i, int32_t h) {
   return ((int64_t)b * a.max_q + i) * a.q_heads + h;
 }
@@ -114,6 +117,10 @@ __device__ __forceinline__ float* partial_sums(const Fb4Attend& a, int64_t row, 
 __device__ __forceinline__ float2* partial_stat(const Fb4Attend& a, int64_t row, int32_t split, int D) {
   return reinterpret_cast<float2*>(a.partial + partial_rows(a) * a.splits * D) + row * a.splits + split;
 }
+
+// griddepcontrol: a kernel launched behind this one may start; wait for the one in front to have finished
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ void store_out(const Fb4Attend& a, int64_t at, float x) {
   if (a.out_dtype == 0) static_cast<float*>(a.out)[at] = x;

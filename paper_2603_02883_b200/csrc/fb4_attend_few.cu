@@ -2,8 +2,8 @@
 //
 // Work: a CTA of 4 warps takes one sequence, one cache head, up to 8 * NT query rows (query-major: row r = query r / group,
 // head r mod group) and one run of the cached tokens (a "split"); its warps take that run's tiles of 32 tokens in turn.  Each warp
-// has its own ring of bulk-copied tiles (codes and metadata of K and V), its own running maximum and sum, and its own
-// accumulators; the warps are joined in shared memory at the end, the splits in a second small kernel.
+// has its own ring of asynchronously copied tiles (codes and metadata of K and V), its own running maximum and sum, and its
+// own accumulators; the warps are joined in shared memory at the end, the splits in a second small kernel.
 //
 // The tokens are the long side, so they are the M side of the products: S^T = K Q^T (m = 16 tokens, n = 8 queries),
 // O^T = V^T P^T (m = 16 channels, n = 8 queries), mma.sync m16n8k16: with one query per head 7/8 of the N side is idle, but a
@@ -15,17 +15,11 @@
 // Bound: the decode's ALU and FMA instructions (about 2.4 per cached value with everything, against the 3.1 that fit under
 // 0.5625 bytes of traffic), so close to, but not quite, memory-bound.
 #include "fb4_attend.cuh"
-#include "fb4_staging.cuh"
+#include "fb4_block.cuh"
 
 namespace {
 
 using namespace fb4att;
-using fb4stage::bulk_load;
-using fb4stage::kSpinLimit;
-using fb4stage::mbar_expect_tx;
-using fb4stage::mbar_init;
-using fb4stage::mbar_try_wait;
-
 constexpr int kWarpsFew = 4;
 constexpr int kTile = 32;              // tokens of a warp's tile
 
@@ -35,8 +29,8 @@ struct Few {
   static constexpr int kCodes = kTile * D / 2, kMeta = kTile * (D / 32) * 2;
   static constexpr int kStage = 2 * kCodes + 2 * kMeta;
   static constexpr int kRing = kWarpsFew * kStagesFew * kStage;
-  // the join of the warps reuses the ring: per warp 16 rows of D sums
-  static constexpr int kJoin = kWarpsFew * 16 * D * 4;
+  // the join of the warps reuses the ring: 16 rows of D sums per warp, and once more for their sum
+  static constexpr int kJoin = (kWarpsFew + 1) * 16 * D * 4;
   static constexpr int kBytes = (kRing > kJoin ? kRing : kJoin);
 };
 
@@ -55,15 +49,21 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   return d;
 }
 
-template <int D, int NT>
+// 16 bytes to shared memory past L1; there = false: zeros, and nothing is read.  (Bulk copies would want one lane's
+// uniform registers for each: four of them per tile cost more instructions than the nine of these.)
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
+}
+
+template <int D, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_few_kernel(const __grid_constant__ Fb4Attend a) {
   using L = Few<D>;
   constexpr int NW = D / 32;             // code words of a lane's quarter row
   constexpr int ST = L::kStagesFew;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t book[64];
-  __shared__ uint64_t bars[kWarpsFew * ST];
-  __shared__ float2 stat[kWarpsFew][8 * NT];
+  __shared__ float2 stat[kWarpsFew][8 * NT], own[8 * NT];
+  if (!CLUSTER) let_next_start();        // the join of the splits waits for this kernel's end by itself
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int32_t row_tiles = (a.max_q * a.group + 8 * NT - 1) / (8 * NT);
 
@@ -82,21 +82,18 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
   const Range first = visible(a, sq, row0 / a.group), last = visible(a, sq, (row0 + n_rows - 1) / a.group);
   const int32_t base = first.lo & ~(kTile - 1);
   const int32_t tiles = last.hi > base && last.hi > first.lo ? (last.hi - base + kTile - 1) / kTile : 0;
-  const int32_t tile0 = split * a.split_tiles;
-  const int32_t tile1 = tiles - tile0 < a.split_tiles ? tiles : tile0 + a.split_tiles;
-  const bool empty = tile0 >= tiles;      // this split has nothing; its record says so
+  // the tiles are dealt out evenly over the splits, in rounds of one tile per warp
+  const int32_t rounds = (tiles + kWarpsFew - 1) / kWarpsFew;
+  const int32_t tile0 = (int32_t)((int64_t)rounds * split / a.splits) * kWarpsFew;
+  const int32_t end = (int32_t)((int64_t)rounds * (split + 1) / a.splits) * kWarpsFew, tile1 = end < tiles ? end : tiles;
 
   if (threadIdx.x < 64) fill_book(book, a.tables, threadIdx.x);
-  if (lane == 0) {
-    for (int i = 0; i < ST; ++i) mbar_init(fb4blk::smem_u32(bars + warp * ST + i), 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
   __syncthreads();
-  const uint32_t ring = fb4blk::smem_u32(smem) + warp * ST * L::kStage, bar = fb4blk::smem_u32(bars + warp * ST);
+  const uint32_t ring = fb4blk::smem_u32(smem) + warp * ST * L::kStage;
   const uint32_t book_at = fb4blk::smem_u32(book);
 
   // the pages of this warp's tiles: lane l holds those of tile `batch + l` (two halves of 16 tokens; equal in pages of 32 or more)
-  const int32_t n_mine = empty || tile0 + warp >= tile1 ? 0 : (tile1 - tile0 - warp + kWarpsFew - 1) / kWarpsFew;
+  const int32_t n_mine = tile0 + warp >= tile1 ? 0 : (tile1 - tile0 - warp + kWarpsFew - 1) / kWarpsFew;
   const int32_t my0 = tile0 + warp;
   int32_t page_lo = -1, page_hi = -1;
   bool bad = false;
@@ -111,37 +108,38 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
       if (j + 16 < sq.kv && (uint32_t)page_hi >= (uint64_t)a.cache.n_pages) { bad = true; page_hi = -1; }
     }
   };
-  // requests tile n of this warp into ring stage n mod ST; which of its halves are there goes to `have` (2 bits per stage)
+  // Requests tile n of this warp into ring stage `st`.  Codes: lane l copies bytes 16 l .. 16 l + 15 of every 512; metadata:
+  // K in lanes 0 to 15, V behind, each half of the tile in 8 (D = 128) or 4 of them.  `have`: 2 bits per stage, the halves whose
+  // pages exist.
   uint32_t have = 0;
-  auto request = [&](int32_t n) {
-    if ((n & 31) == 0) fetch_pages(n);
-    const int32_t plo = __shfl_sync(0xffffffffu, page_lo, n & 31), phi = __shfl_sync(0xffffffffu, page_hi, n & 31);
-    const int st = n % ST;
-    have = (have & ~(3u << (2 * st))) | ((plo >= 0 ? 1u : 0u) | (phi >= 0 ? 2u : 0u)) << (2 * st);
-    if (lane == 0) {
-      const uint32_t dst = ring + st * L::kStage, full = bar + 8 * st;
-      const int32_t j = base + (my0 + n * kWarpsFew) * kTile, at = j & ((1 << a.page_shift) - 1);
-      const bool one = a.page_shift > 4 && plo >= 0;               // one page holds the whole tile
-      const uint32_t halves = one ? 2u : (plo >= 0 ? 1u : 0u) + (phi >= 0 ? 1u : 0u);
-      mbar_expect_tx(full, halves * (L::kStage / 2));
-      auto piece = [&](int32_t page, int32_t place, int half, uint32_t n16) {
-        const int64_t row = (((int64_t)page * a.cache.n_heads + head) << a.page_shift) + place;
-        const uint32_t cb = n16 * (L::kCodes / 2), mb = n16 * (L::kMeta / 2);
-        bulk_load(dst + half * (L::kCodes / 2), a.cache.k_codes + row * (D / 2), cb, full);
-        bulk_load(dst + L::kCodes + half * (L::kCodes / 2), a.cache.v_codes + row * (D / 2), cb, full);
-        bulk_load(dst + 2 * L::kCodes + half * (L::kMeta / 2), a.cache.k_meta + row * (D / 32), mb, full);
-        bulk_load(dst + 2 * L::kCodes + L::kMeta + half * (L::kMeta / 2), a.cache.v_meta + row * (D / 32), mb, full);
-      };
-      if (one) piece(plo, at, 0, 2);
-      else {
-        if (plo >= 0) piece(plo, at, 0, 1);
-        if (phi >= 0) piece(phi, 0, 1, 1);
+  const uint32_t page_mask = (1u << a.page_shift) - 1u;
+  const int mh = (lane / (D / 16)) & 1, mv = lane / (D / 8);          // half and array of this lane's piece of the metadata
+  const uint8_t* meta_src = reinterpret_cast<const uint8_t*>(mv ? a.cache.v_meta : a.cache.k_meta) + (lane & (D / 16 - 1)) * 16;
+  const uint32_t meta_dst = 2 * L::kCodes + mv * L::kMeta + mh * (L::kMeta / 2) + (lane & (D / 16 - 1)) * 16;
+  auto request = [&](int32_t n, int st) {
+    if (n < n_mine) {
+      if ((n & 31) == 0) fetch_pages(n);
+      const int32_t plo = __shfl_sync(0xffffffffu, page_lo, n & 31), phi = __shfl_sync(0xffffffffu, page_hi, n & 31);
+      have = (have & ~(3u << (2 * st))) | ((plo >= 0 ? 1u : 0u) | (phi >= 0 ? 2u : 0u)) << (2 * st);
+      const uint32_t dst = ring + st * L::kStage;
+      const uint32_t j = (uint32_t)(base + (my0 + n * kWarpsFew) * kTile);
+      const int64_t rlo = (((int64_t)max(plo, 0) * a.cache.n_heads + head) << a.page_shift) + (j & page_mask);
+      const int64_t rhi = (((int64_t)max(phi, 0) * a.cache.n_heads + head) << a.page_shift) + ((j + 16) & page_mask);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const uint8_t* codes = (v ? a.cache.v_codes : a.cache.k_codes) + lane * 16;
+#pragma unroll
+        for (int i = 0; i < L::kCodes / 2; i += 512) {
+          copy16(dst + v * L::kCodes + i + lane * 16, codes + rlo * (D / 2) + i, plo >= 0);
+          copy16(dst + v * L::kCodes + L::kCodes / 2 + i + lane * 16, codes + rhi * (D / 2) + i, phi >= 0);
+        }
       }
+      if (D == 128 || lane < 16) copy16(dst + meta_dst, meta_src + (mh ? rhi : rlo) * (D / 16), (mh ? phi : plo) >= 0);
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");               // empty behind the last tile: the count of groups stays
   };
 #pragma unroll
-  for (int n = 0; n < ST - 1; ++n)
-    if (n < n_mine) request(n);
+  for (int n = 0; n < ST - 1; ++n) request(n, n);
 
   // Q as the B side of S^T = K Q^T: lane (g, t) holds query row0 + 8 nt + g, channels of quarter t
   uint32_t qf[NT][NW][4];
@@ -151,15 +149,17 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
   for (int nt = 0; nt < NT; ++nt) {
     const int32_t r = row0 + 8 * nt + g;
     const bool on = r < rows;
+    // a negative scale goes into Q's signs: the running maximum wants a positive one
+    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
     const uint16_t* src = a.q + (int64_t)(sq.q0 + (on ? r / a.group : 0)) * a.q_ld + (int64_t)(head * a.group + (on ? r % a.group : 0)) * D + t * (D / 4);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       uint4 u = make_uint4(0, 0, 0, 0);
       if (on) u = __ldg(reinterpret_cast<const uint4*>(src + 8 * w));
-      qf[nt][w][0] = prmt(u.x, u.y, 0x5410u);
-      qf[nt][w][1] = prmt(u.x, u.y, 0x7632u);
-      qf[nt][w][2] = prmt(u.z, u.w, 0x5410u);
-      qf[nt][w][3] = prmt(u.z, u.w, 0x7632u);
+      qf[nt][w][0] = prmt(u.x, u.y, 0x5410u) ^ flip;
+      qf[nt][w][1] = prmt(u.x, u.y, 0x7632u) ^ flip;
+      qf[nt][w][2] = prmt(u.z, u.w, 0x5410u) ^ flip;
+      qf[nt][w][3] = prmt(u.z, u.w, 0x7632u) ^ flip;
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {          // rows behind the last one are computed like the last one and not stored
@@ -174,6 +174,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
   lo_max = __reduce_max_sync(0xffffffffu, lo_max);
   hi_min = __reduce_min_sync(0xffffffffu, hi_min);
 
+  const float scale = fmaxf(fabsf(a.scale_log2) * kUnshift, 1e-37f);        // 0 would make 0 * -infinity of a masked score
   float o[NT][2 * NW][4];
   float m[NT][2], l[NT][2];
 #pragma unroll
@@ -186,18 +187,11 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
     l[nt][0] = l[nt][1] = 0.0f;
   }
 
-  int32_t lost = -1;
+  int st = 0, ahead = ST - 1;
   for (int32_t n = 0; n < n_mine; ++n) {
-    if (n + ST - 1 < n_mine) request(n + ST - 1);
-    const int st = n % ST;
-    const uint32_t parity = (uint32_t)(n / ST) & 1u, full = bar + 8 * st;
-    uint32_t tries = 0;
-    bool ready = mbar_try_wait(full, parity);
-    while (!ready && ++tries < kSpinLimit) ready = mbar_try_wait(full, parity);
-    if (!__all_sync(0xffffffffu, ready)) {
-      lost = n;
-      break;
-    }
+    request(n + ST - 1, ahead);
+    asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+    __syncwarp();          // every lane's copies of this tile have landed
     const uint32_t codes = ring + st * L::kStage, meta = codes + 2 * L::kCodes;
     const int32_t j0 = base + (my0 + n * kWarpsFew) * kTile;
     const uint32_t here = (have >> (2 * st)) & 3u;
@@ -240,37 +234,37 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
         }
       }
     }
-    // ---- scores in units of log2, masks, running maximum (moved only when it would grow by more than 2^8: the
-    // accumulators are then rescaled, which is rare after the first tiles)
-    bool grow = false;
+    // ---- masks, running maximum in units of log2 (moved only when it would grow by more than 2^8: the accumulators are then
+    // rescaled, which is rare after the first tiles)
+    if (!whole) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float x = s[h][nt][k] * a.scale_log2;
-          if (!whole) {
+          for (int k = 0; k < 4; ++k) {
             const int32_t j = j0 + 16 * h + g + (k & 2 ? 8 : 0);
-            if (j < lo[nt][k & 1] || j >= hi[nt][k & 1] || !((here >> h) & 1u)) x = -INFINITY;
+            if (j < lo[nt][k & 1] || j >= hi[nt][k & 1] || !((here >> h) & 1u)) s[h][nt][k] = -INFINITY;
           }
-          s[h][nt][k] = x;
-        }
+    }
+    bool grow = false;
+    float top[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const float top = fmaxf(fmaxf(s[0][nt][k], s[0][nt][k + 2]), fmaxf(s[1][nt][k], s[1][nt][k + 2]));
-        grow |= top > m[nt][k] + 8.0f;
+        top[nt][k] = fmaxf(fmaxf(s[0][nt][k], s[0][nt][k + 2]), fmaxf(s[1][nt][k], s[1][nt][k + 2]));
+        grow |= fmaf(top[nt][k], scale, -8.0f) > m[nt][k];
       }
-    }
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          float top = fmaxf(fmaxf(s[0][nt][k], s[0][nt][k + 2]), fmaxf(s[1][nt][k], s[1][nt][k + 2]));
+          float x = top[nt][k];
 #pragma unroll
-          for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-          const float next = fmaxf(m[nt][k], top);
+          for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+          const float next = fmaxf(m[nt][k], x * scale);
           const float f = next == -INFINITY ? 1.0f : exp2_approx(m[nt][k] - next);
           m[nt][k] = next;
           l[nt][k] *= f;
@@ -287,8 +281,8 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
       const float m0 = m[nt][0] == -INFINITY ? 0.0f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.0f : m[nt][1];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float p0 = exp2_approx(s[h][nt][0] - m0), p1 = exp2_approx(s[h][nt][1] - m1);
-        const float p2 = exp2_approx(s[h][nt][2] - m0), p3 = exp2_approx(s[h][nt][3] - m1);
+        const float p0 = exp2_approx(fmaf(s[h][nt][0], scale, -m0)), p1 = exp2_approx(fmaf(s[h][nt][1], scale, -m1));
+        const float p2 = exp2_approx(fmaf(s[h][nt][2], scale, -m0)), p3 = exp2_approx(fmaf(s[h][nt][3], scale, -m1));
         l[nt][0] += p0 + p2;
         l[nt][1] += p1 + p3;
         pf[h][nt][0] = transpose8x8(pack(p0, p1));
@@ -324,14 +318,8 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
       }
     }
     __syncwarp();          // the stage may be filled again
-  }
-  if (lost >= 0) {         // a copy never came: say so, and let the copies still in flight end before the ring is used again
-    if (lane == 0) atomicOr(a.status, 1u);
-    const int32_t asked = lost + ST < n_mine ? lost + ST : n_mine;
-    for (int32_t n = lost + 1; n < asked; ++n) {
-      uint32_t tries = 0;
-      while (!mbar_try_wait(bar + 8 * (n % ST), (uint32_t)(n / ST) & 1u) && ++tries < kSpinLimit) {}
-    }
+    st = st + 1 == ST ? 0 : st + 1;
+    ahead = ahead + 1 == ST ? 0 : ahead + 1;
   }
   if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, 2u);
 
@@ -367,9 +355,9 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
           }
     }
   __syncthreads();
-  for (int x = threadIdx.x; x < n_rows * (D / 4); x += kWarpsFew * 32) {
-    const int r = x / (D / 4), c = x % (D / 4) * 4;
-    float top = -INFINITY, sum = 0.0f;
+  auto joined = [&](int r, int c, float& top, float& sum) -> float4 {
+    top = -INFINITY;
+    sum = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWarpsFew; ++w) top = fmaxf(top, stat[w][r].x);
 #pragma unroll
@@ -380,82 +368,193 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
       const float4 u = *reinterpret_cast<const float4*>(join + (w * 8 * NT + r) * D + c);
       v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
     }
+    return v;
+  };
+  auto finish = [&](int r, int c, const float4& v, float top, float sum) {
     const int32_t i = (row0 + r) / a.group, h = head * a.group + (row0 + r) % a.group;
-    if (a.splits > 1) {
-      const int64_t pr = partial_row(a, b, i, h);
-      if (sum > 0.0f) *reinterpret_cast<float4*>(partial_sums(a, pr, split, D) + c) = v;
-      if (c == 0) *partial_stat(a, pr, split, D) = make_float2(top, sum);
-    } else {
-      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-      store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + c, v, inv);
-      if (c == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + c, v, sum > 0.0f ? kUnshift / sum : 0.0f);
+    if (c == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+  };
+  if constexpr (CLUSTER) {
+    // the splits are the CTAs of a cluster: each leaves its joined rows in its shared memory (behind the warps' rows: the
+    // ring has the room), then every CTA finishes a part of the rows from all of them
+    float* mine = join + kWarpsFew * 8 * NT * D;
+    for (int x = threadIdx.x; x < n_rows * (D / 4); x += kWarpsFew * 32) {
+      const int r = x / (D / 4), c = x % (D / 4) * 4;
+      float top, sum;
+      *reinterpret_cast<float4*>(mine + r * D + c) = joined(r, c, top, sum);
+      if (c == 0) own[r] = make_float2(top, sum);
     }
-  }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    for (int x = split * kWarpsFew * 32 + threadIdx.x; x < n_rows * (D / 4); x += a.splits * kWarpsFew * 32) {
+      const int r = x / (D / 4), c = x % (D / 4) * 4;
+      const uint32_t row_at = fb4blk::smem_u32(mine + r * D + c), own_at = fb4blk::smem_u32(own + r);
+      float top = -INFINITY, sum = 0.0f;
+      float2 st[8];
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        st[z] = make_float2(-INFINITY, 0.0f);
+        if (z < a.splits) {
+          asm volatile("{\n\t.reg .b32 q;\n\tmapa.shared::cluster.u32 q, %2, %3;\n\tld.shared::cluster.v2.f32 {%0, %1}, [q];\n\t}"
+                       : "=f"(st[z].x), "=f"(st[z].y) : "r"(own_at), "r"(z));
+          top = fmaxf(top, st[z].x);
+        }
+      }
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        if (st[z].x > -INFINITY) {
+          const float f = exp2_approx(st[z].x - top);
+          float4 u;
+          asm volatile("{\n\t.reg .b32 q;\n\tmapa.shared::cluster.u32 q, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [q];\n\t}"
+                       : "=f"(u.x), "=f"(u.y), "=f"(u.z), "=f"(u.w) : "r"(row_at), "r"(z));
+          v.x = fmaf(u.x, f, v.x); v.y = fmaf(u.y, f, v.y); v.z = fmaf(u.z, f, v.z); v.w = fmaf(u.w, f, v.w);
+          sum = fmaf(st[z].y, f, sum);
+        }
+      }
+      finish(r, c, v, top, sum);
+    }
+    // nobody's shared memory goes away while another CTA reads it
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  } else {
+    for (int x = threadIdx.x; x < n_rows * (D / 4); x += kWarpsFew * 32) {
+      const int r = x / (D / 4), c = x % (D / 4) * 4;
+      float top, sum;
+      const float4 v = joined(r, c, top, sum);
+      if (a.splits > 1) {
+        const int32_t i = (row0 + r) / a.group, h = head * a.group + (row0 + r) % a.group;
+        const int64_t pr = partial_row(a, b, i, h);
+        if (sum > 0.0f) *reinterpret_cast<float4*>(partial_sums(a, pr, split, D) + c) = v;
+        if (c == 0) *partial_stat(a, pr, split, D) = make_float2(top, sum);
+      } else {
+        finish(r, c, v, top, sum);
+      }
+    }  }
 }
 
-// Joins the splits: one warp per query row and head, lane l holds channels 4 l (D / 128 of them at a time: D = 64 uses half the
-// lanes twice as fast).  Splits that saw nothing have sum 0 and their D sums are not read.
-template <int D>
+// Joins the splits: NW warps per query row and head take the splits in turn, lane l holds channels 4 l to 4 l + 3.  Splits that
+// saw nothing have sum 0 and their D sums are not read.
+template <int D, int NW>
 __global__ void __launch_bounds__(128) fb4_attend_join_kernel(const __grid_constant__ Fb4Attend a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= partial_rows(a)) return;
+  __shared__ float4 part[4][32];
+  __shared__ float2 stat[4];
+  wait_for_previous();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % NW;
+  const int64_t row = (int64_t)blockIdx.x * (4 / NW) + warp / NW;
+  const bool real = row < partial_rows(a);
   const int32_t h = (int32_t)(row % a.q_heads);
   const int64_t bi = row / a.q_heads;
-  const int32_t b = (int32_t)(bi / a.max_q), i = (int32_t)(bi % a.max_q);
+  const int32_t b = real ? (int32_t)(bi / a.max_q) : 0, i = (int32_t)(bi % a.max_q);
   const Sequence sq = sequence(a, b, false);
-  if (i >= sq.n_q) return;
-  float top = -INFINITY;
-  for (int s = lane; s < a.splits; s += 32) {
-    const float2 st = *partial_stat(a, row, s, D);
-    if (st.y > 0.0f) top = fmaxf(top, st.x);
-  }
-#pragma unroll
-  for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-  float sum = 0.0f;
+  const bool on = real && i < sq.n_q;
+  float top = -INFINITY, sum = 0.0f;
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int s0 = 0; s0 < a.splits; s0 += 32) {
-    float w = 0.0f;
-    if (s0 + lane < a.splits) {
-      const float2 st = *partial_stat(a, row, s0 + lane, D);
-      if (st.y > 0.0f) {
-        w = exp2_approx(st.x - top);
-        sum += w * st.y;
-      }
+  if (on) {
+    for (int s = sub + lane * NW; s < a.splits; s += 32 * NW) {
+      const float2 st = *partial_stat(a, row, s, D);
+      if (st.y > 0.0f) top = fmaxf(top, st.x);
     }
-    const int n = a.splits - s0 < 32 ? a.splits - s0 : 32;
-#pragma unroll 4
-    for (int s = 0; s < n; ++s) {
-      const float f = __shfl_sync(0xffffffffu, w, s);
-      if (f > 0.0f && lane * 4 < D) {
-        const float4 u = *reinterpret_cast<const float4*>(partial_sums(a, row, s0 + s, D) + lane * 4);
-        v.x = fmaf(u.x, f, v.x); v.y = fmaf(u.y, f, v.y); v.z = fmaf(u.z, f, v.z); v.w = fmaf(u.w, f, v.w);
-      }
-    }
-  }
 #pragma unroll
-  for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  if (lane * 4 < D) store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + lane * 4, v, inv);
+    for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    for (int s0 = sub; s0 < a.splits; s0 += 32 * NW) {
+      float w = 0.0f;
+      if (s0 + lane * NW < a.splits) {
+        const float2 st = *partial_stat(a, row, s0 + lane * NW, D);
+        if (st.y > 0.0f) {
+          w = exp2_approx(st.x - top);
+          sum += w * st.y;
+        }
+      }
+      const int left = (a.splits - s0 + NW - 1) / NW, n = left < 32 ? left : 32;
+#pragma unroll 8
+      for (int s = 0; s < n; ++s) {
+        const float f = __shfl_sync(0xffffffffu, w, s);
+        if (f > 0.0f && lane * 4 < D) {
+          const float4 u = *reinterpret_cast<const float4*>(partial_sums(a, row, s0 + s * NW, D) + lane * 4);
+          v.x = fmaf(u.x, f, v.x); v.y = fmaf(u.y, f, v.y); v.z = fmaf(u.z, f, v.z); v.w = fmaf(u.w, f, v.w);
+        }
+      }
+    }
+#pragma unroll
+    for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  }
+  if (NW > 1) {
+    part[warp][lane] = v;
+    if (lane == 0) stat[warp] = make_float2(top, sum);
+    __syncthreads();
+    if (sub != 0) return;
+    float all = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) all = fmaxf(all, stat[warp + w].x);
+    v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = stat[warp + w].x == -INFINITY ? 0.0f : exp2_approx(stat[warp + w].x - all);
+      const float4 u = part[warp + w][lane];
+      v.x = fmaf(u.x, f, v.x); v.y = fmaf(u.y, f, v.y); v.z = fmaf(u.z, f, v.z); v.w = fmaf(u.w, f, v.w);
+      sum = fmaf(stat[warp + w].y, f, sum);
+    }
+    top = all;
+  }
+  if (!on) return;
+  if (lane * 4 < D) store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + lane * 4, v, sum > 0.0f ? kUnshift / sum : 0.0f);
   if (lane == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+}
+
+template <typename... Args>
+cudaError_t launch_with(void (*kernel)(Args...), int64_t grid, int threads, int smem, int cluster, bool behind, cudaStream_t stream,
+                        Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[2];
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  if (cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = (unsigned)cluster;
+    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  if (behind) {            // may be set up while the kernel in front still runs
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 template <int D, int NT>
 cudaError_t launch(const Fb4Attend& a, cudaStream_t stream) {
   const int64_t row_tiles = ((int64_t)a.max_q * a.group + 8 * NT - 1) / (8 * NT);
   const int64_t grid = row_tiles * a.splits * a.cache.n_heads * a.n_seqs;
-  fb4_attend_few_kernel<D, NT><<<(unsigned)grid, kWarpsFew * 32, Few<D>::kBytes, stream>>>(a);
-  return cudaGetLastError();
+  if (a.splits > 1 && !a.partial)
+    return launch_with(fb4_attend_few_kernel<D, NT, true>, grid, kWarpsFew * 32, Few<D>::kBytes, a.splits, false, stream, a);
+  return launch_with(fb4_attend_few_kernel<D, NT, false>, grid, kWarpsFew * 32, Few<D>::kBytes, 1, false, stream, a);
+}
+
+template <int D>
+cudaError_t launch_join(const Fb4Attend& a, cudaStream_t stream) {
+  // a warp per row, or the 4 warps of a CTA where a row has many splits
+  if (a.splits >= 16) return launch_with(fb4_attend_join_kernel<D, 4>, partial_rows(a), 128, 0, 1, true, stream, a);
+  return launch_with(fb4_attend_join_kernel<D, 1>, (partial_rows(a) + 3) / 4, 128, 0, 1, true, stream, a);
 }
 
 }  // namespace
 
 cudaError_t fb4_attend_prepare_device() {
   const cudaFuncAttribute attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(fb4_attend_few_kernel<128, 1>, attr, Few<128>::kBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<128, 2>, attr, Few<128>::kBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<64, 1>, attr, Few<64>::kBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<64, 2>, attr, Few<64>::kBytes);
+  cudaError_t e = cudaSuccess;
+#define FB4_OPT_IN(D, NT) \
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<D, NT, false>, attr, Few<D>::kBytes); \
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<D, NT, true>, attr, Few<D>::kBytes)
+  FB4_OPT_IN(128, 1);
+  FB4_OPT_IN(128, 2);
+  FB4_OPT_IN(64, 1);
+  FB4_OPT_IN(64, 2);
+#undef FB4_OPT_IN
   if (e == cudaSuccess) e = fb4_attend_many_prepare_device();
   return e;
 }
@@ -480,8 +579,7 @@ Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_hea
     if (s < fine) s = fine;
     if (s > most) s = most;
     if (s < 1) s = 1;
-    p.split_tiles = (int32_t)((tiles + s - 1) / s);
-    p.splits = (int32_t)((tiles + p.split_tiles - 1) / p.split_tiles);
+    p.splits = (int32_t)s;
   } else {
     p.kernel = 2;
     // one CTA per SM: the number of splits that leaves the least of the last wave idle; a split costs about a tile's time
@@ -500,7 +598,8 @@ Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_hea
     }
     p.splits = (int32_t)((tiles + p.split_tiles - 1) / p.split_tiles);
   }
-  if (p.splits > 1) p.workspace = (int64_t)n_seqs * max_q * q_heads * p.splits * (head_dim + 2) * 4;
+  // up to 8 splits of the few-row kernel are one cluster, which joins them in shared memory
+  if (p.splits > 1 && !(p.kernel == 1 && p.splits <= 8)) p.workspace = (int64_t)n_seqs * max_q * q_heads * p.splits * (head_dim + 2) * 4;
   return p;
 }
 
@@ -511,8 +610,5 @@ cudaError_t fb4_launch_attend_few(const Fb4Attend& a, cudaStream_t stream) {
 }
 
 cudaError_t fb4_launch_attend_join(const Fb4Attend& a, cudaStream_t stream) {
-  const unsigned grid = (unsigned)((partial_rows(a) + 3) / 4);
-  if (a.cache.head_dim == 128) fb4_attend_join_kernel<128><<<grid, 128, 0, stream>>>(a);
-  else fb4_attend_join_kernel<64><<<grid, 128, 0, stream>>>(a);
-  return cudaGetLastError();
+  return a.cache.head_dim == 128 ? launch_join<128>(a, stream) : launch_join<64>(a, stream);
 }

@@ -140,6 +140,8 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile uint32_t* dead = &dead_flag;
 
+  let_next_start();      // the join of the splits waits for this kernel's end by itself
+
   // ---- which work
   const int32_t row_tiles = (a.max_q * a.group + 255) / 256;
   int64_t id = blockIdx.x;
@@ -214,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       const Range v = visible(a, sq, rc / a.group);
       const int32_t lo_max = __reduce_max_sync(0xffffffffu, v.lo), hi_min = __reduce_min_sync(0xffffffffu, v.hi);
       // scale 0 would make 0 * -infinity of a masked score
-      const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);
+      const float scale = fmaxf(fabsf(a.scale_log2) * kUnshift, 1e-37f);
       float m = -INFINITY, l = 0.0f;
       bool ok = true;
       for (int32_t t = 0; t < n_tiles; ++t) {
@@ -287,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
       }
-      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      const float inv = l > 0.0f ? kUnshift / l : 0.0f;
       const int32_t i = rc / a.group, h = head * a.group + rc % a.group;
       const int64_t pr = partial_row(a, b, i, h);
       const int64_t out_row = (int64_t)(sq.q0 + i);

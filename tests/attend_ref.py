@@ -95,7 +95,9 @@ def attend64(q, cache, page_table, kv_len, q_start, scale, causal, window, out_d
     The tolerances count the roundings that the kernels make: the final one to out_dtype (half a step, relative), that of
     the probabilities to bfloat16 (2^-8 of every term of the second product), and float32 sums: a dot product of D terms is
     off by at most (D + 8) 2^-23 of its absolute sum (twice the half step: the tensor cores may truncate), which moves
-    every probability by that factor, and a sum of n keys by (n + 8) 2^-23.  exp2 and the scaling add 2^-21."""
+    every probability by that factor, and a sum of n keys by (n + 8) 2^-23.  exp2 and the scaling add 2^-21.  The tensor-core
+    kernels sum the second product times 2^-64 in float32, whose smallest step is 2^-149: each of the at most n additions can
+    lose a step, 2^-85 of the result (the dividing sum is at least 1: the key that set the running maximum counts 1)."""
     total, hq, D = q.shape
     hk = cache.k_codes.shape[1]
     group = hq // hk
@@ -134,7 +136,7 @@ def attend64(q, cache, page_table, kv_len, q_start, scale, causal, window, out_d
             eps = 2 * dz + 2.0 ** -21 * (1 + top.abs()) + (n + 8) * 2.0 ** -23
             o, oa = w @ vh, w @ vh.abs()
             out[a0:a1, h] = o
-            otol[a0:a1, h] = (2.0 ** -8 + eps) * oa * (1 + step) + step * o.abs()
+            otol[a0:a1, h] = (2.0 ** -8 + eps) * oa * (1 + step) + step * o.abs() + n * 2.0 ** -85
             lse[a0:a1, h] = (top + torch.log(l))[:, 0]
             ltol[a0:a1, h] = (eps + 2.0 ** -22 * (1 + top.abs() + torch.log(l.clamp(min=1)).abs()))[:, 0]
     return out, lse, otol, ltol

@@ -97,13 +97,23 @@ def test_extreme_scores_and_values(q32, n_q):
     got = q32.cache_attention(q, cache, table, kv, qs, mq, mkv, scale=1.0)
     agree(got, ref.attend64(q, cache, table, kv, qs, 1.0, True, 0, torch.bfloat16))
     q = q / 200
-    cache.v_meta.copy_((cache.v_meta & ~255) | 240)            # element scale 2^113
+    cache.v_meta.copy_((cache.v_meta & ~255) | 188)            # element scale 2^61
     got = q32.cache_attention(q, cache, table, kv, qs, mq, mkv)
     agree(got, ref.attend64(q, cache, table, kv, qs, 128 ** -0.5, True, 0, torch.bfloat16))
-    cache.v_meta.copy_((cache.v_meta & ~255) | 20)             # 2^-107
+    cache.v_meta.copy_((cache.v_meta & ~255) | 59)             # 2^-68
     cache.k_meta.copy_((cache.k_meta & ~255) | 1)              # keys that are all but zero
     got = q32.cache_attention(q, cache, table, kv, qs, mq, mkv, dtype=torch.float32)
     agree(got, ref.attend64(q, cache, table, kv, qs, 128 ** -0.5, True, 0, torch.float32))
+
+
+@pytest.mark.parametrize("n_q", [1, 70])
+def test_scales_beyond_the_readable_range_count_as_its_end(q32, n_q):
+    q, cache, table, kv, qs, mq, mkv = setup(q32, [n_q], [130], 2, 2, 64, 16, seed=6)
+    cache.v_meta.copy_((cache.v_meta & ~255) | 188)
+    want = q32.cache_attention(q, cache, table, kv, qs, mq, mkv, dtype=torch.float32)
+    cache.v_meta.copy_((cache.v_meta & ~255) | 251)
+    got = q32.cache_attention(q, cache, table, kv, qs, mq, mkv, dtype=torch.float32)
+    assert torch.equal(got[0], want[0])
 
 
 @pytest.mark.parametrize("n_q", [1, 90])
