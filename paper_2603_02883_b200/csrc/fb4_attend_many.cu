@@ -4,7 +4,7 @@
 // Work: a CTA takes one sequence, one cache head, up to 256 query rows (two tiles of 128; row r = query r / group, head
 // r mod group) and one run of the cached tokens, which it walks in tiles of 128.  Its warps have fixed roles:
 //   load     copies codes and metadata of K and V tiles into a ring (bulk copies, page by page)
-//   decode   8 warps turn them into bf16 tiles in shared memory, 128-byte swizzled, [token][channel] for both K and V
+//   decode   4 warps turn them into bf16 tiles in shared memory, 128-byte swizzled, [token][channel] for both K and V
 //   mma      one thread issues S_w = Q_w K^T (both operands in shared memory, accumulator in TMEM) and O_w += P_w V
 //            (P_w from TMEM, V read with the contracted side as the strided one)
 //   softmax  4 warps per query tile, one row per thread: scores from TMEM, running maximum and sum in registers, P back
@@ -31,8 +31,12 @@ using fb4stage::mbar_init;
 using fb4stage::mbar_try_wait;
 
 constexpr int kKeys = 128;             // tokens of a tile
-constexpr int kSoftmaxWarps = 8, kDecodeWarps = 8;
-constexpr int kThreads = (kSoftmaxWarps + kDecodeWarps + 2) * 32;
+constexpr int kSoftmaxWarps = 8, kDecodeWarps = 4;
+constexpr int kThreads = 512;          // two warpgroups of softmax, one of decode, one whose first two warps are mma and load
+// Registers per thread of the roles.  The block is launched with 128 for each of its 512 threads; what decode, mma and load
+// give back is what the softmax warps, which keep a row's 128 scores in registers, take: 2 * 192 + 88 + 40 = 4 * 128.
+constexpr int kLaunchRegs = 128, kSoftmaxRegs = 192, kDecodeRegs = 88, kOtherRegs = 40;
+static_assert(2 * kSoftmaxRegs + kDecodeRegs + kOtherRegs <= 4 * kLaunchRegs, "register shares of the warpgroups");
 constexpr int kRing = 3;               // ring stages: a K or a V tile's codes and metadata each
 constexpr int kHave = 8;               // tiles whose page flags are kept
 
@@ -88,7 +92,7 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float* v) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
       "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
@@ -114,6 +118,19 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
       "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+// two float32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*reinterpret_cast<uint64_t*>(&d))
+      : "l"(*reinterpret_cast<uint64_t*>(&x)), "l"(*reinterpret_cast<uint64_t*>(&y)), "l"(*reinterpret_cast<uint64_t*>(&z)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<uint64_t*>(&d))
+      : "l"(*reinterpret_cast<uint64_t*>(&x)), "l"(*reinterpret_cast<uint64_t*>(&y)));
+  return d;
 }
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   uint32_t d;
@@ -206,6 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
 
   if (warp < kSoftmaxWarps) {
     // =========================================================== softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int w = warp >> 2;
     if (w < n_w) {
       const uint32_t lanes = (uint32_t)(warp & 3) << 21;              // this warp's TMEM lanes: 32 (warp mod 4) << 16
@@ -217,7 +235,8 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       const int32_t lo_max = __reduce_max_sync(0xffffffffu, v.lo), hi_min = __reduce_min_sync(0xffffffffu, v.hi);
       // scale 0 would make 0 * -infinity of a masked score
       const float scale = fmaxf(fabsf(a.scale_log2) * kUnshift, 1e-37f);
-      float m = -INFINITY, l = 0.0f;
+      float m = -INFINITY;
+      float2 l = make_float2(0.0f, 0.0f);                             // the sum in two halves
       bool ok = true;
       for (int32_t t = 0; t < n_tiles; ++t) {
         ok = wait(smem_u32(&bars.s_full[w]), t & 1, dead);
@@ -226,55 +245,51 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         const int32_t j0 = base + (t0 + t) * kKeys;
         const uint32_t here = *(volatile uint32_t*)&have[t % kHave];
         const bool whole = j0 >= lo_max && j0 + kKeys <= hi_min && here == 0xffu;
-        float x[32];
-        auto scores = [&](int c) {
-          tmem_ld32(s_at + 32 * c, x);
-          tmem_wait_ld();
-          if (!whole) {
+        float x[kKeys];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const int32_t j = j0 + 32 * c + i;
-              if (j < v.lo || j >= v.hi || !((here >> (2 * c + (i >> 4))) & 1u)) x[i] = -INFINITY;
-            }
-          }
-        };
-        float top = -INFINITY;
+        for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, x + 32 * c);
+        tmem_wait_ld();
+        if (!whole) {
+          const int32_t from = v.lo - j0, to = v.hi - j0;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          scores(c);
-          float u0 = x[0], u1 = x[1], u2 = x[2], u3 = x[3];
-#pragma unroll
-          for (int i = 4; i < 32; i += 4) { u0 = fmaxf(u0, x[i]); u1 = fmaxf(u1, x[i + 1]); u2 = fmaxf(u2, x[i + 2]); u3 = fmaxf(u3, x[i + 3]); }
-          top = fmaxf(top, fmaxf(fmaxf(u0, u1), fmaxf(u2, u3)));
+          for (int i = 0; i < kKeys; ++i)
+            if (i < from || i >= to || !((here >> (i >> 4)) & 1u)) x[i] = -INFINITY;
         }
-        top *= scale;
+        float u[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+        for (int i = 4; i < kKeys; i += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) u[k] = i + 4 < kKeys ? fmaxf(fmaxf(u[k], x[i + k]), x[i + 4 + k]) : fmaxf(u[k], x[i + k]);
+        const float top = fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3])) * scale;
         if (__any_sync(0xffffffffu, top > m + 8.0f)) {
           const float next = fmaxf(m, top);
           const float f = next == -INFINITY ? 1.0f : exp2_approx(m - next);
           m = next;
-          l *= f;
+          l.x *= f;
+          l.y *= f;
           if (t > 0) {                                                // the product of tile t - 1 was complete before these scores
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
-              tmem_ld32(o_at + 32 * c, x);
+              float y[32];
+              tmem_ld32(o_at + 32 * c, y);
               tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] *= f;
-              tmem_st32(o_at + 32 * c, x);
+              for (int i = 0; i < 32; ++i) y[i] *= f;
+              tmem_st32(o_at + 32 * c, y);
             }
             tmem_wait_st();
           }
         }
-        const float mm = m == -INFINITY ? 0.0f : m;
+        const float mm = m == -INFINITY ? 0.0f : -m;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          scores(c);
           uint32_t p[16];
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
-            const float p0 = exp2_approx(fmaf(x[i], scale, -mm)), p1 = exp2_approx(fmaf(x[i + 1], scale, -mm));
-            l += p0 + p1;
-            p[i >> 1] = pack(p0, p1);
+            const float2 e = fma2(make_float2(x[32 * c + i], x[32 * c + i + 1]), make_float2(scale, scale), make_float2(mm, mm));
+            const float2 q = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+            l = add2(l, q);
+            p[i >> 1] = pack(q.x, q.y);
           }
           tmem_st16(s_at + 16 * c, p);
         }
@@ -284,12 +299,13 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         if (lane == 0) mbar_arrive(smem_u32(&bars.p_full[w]));
       }
       // ---- result
+      const float sum = l.x + l.y;
       if (ok && n_tiles > 0) {
         ok = wait(smem_u32(&bars.o_full[w]), 0, dead);
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
       }
-      const float inv = l > 0.0f ? kUnshift / l : 0.0f;
+      const float inv = sum > 0.0f ? kUnshift / sum : 0.0f;
       const int32_t i = rc / a.group, h = head * a.group + rc % a.group;
       const int64_t pr = partial_row(a, b, i, h);
       const int64_t out_row = (int64_t)(sq.q0 + i);
@@ -310,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
               const float4 u = make_float4(x[k], x[k + 2], x[k + 1], x[k + 3]), z = make_float4(x[k + 4], x[k + 6], x[k + 5], x[k + 7]);
               if (a.splits > 1) {
                 float4* dst = reinterpret_cast<float4*>(partial_sums(a, pr, split, D) + 32 * c + k);
-                if (l > 0.0f) { dst[0] = u; dst[1] = z; }
+                if (sum > 0.0f) { dst[0] = u; dst[1] = z; }
               } else {
                 store_out8(a, out_row * a.out_ld + (int64_t)h * D + 32 * c + k, u, z, inv);
               }
@@ -318,13 +334,14 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
           }
         }
         if (on) {
-          if (a.splits > 1) *partial_stat(a, pr, split, D) = make_float2(m, l);
-          else if (a.lse) a.lse[out_row * a.q_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+          if (a.splits > 1) *partial_stat(a, pr, split, D) = make_float2(m, sum);
+          else if (a.lse) a.lse[out_row * a.q_heads + h] = sum > 0.0f ? (m + log2f(sum)) * kLn2 : -INFINITY;
         }
       }
     }
   } else if (warp < kSoftmaxWarps + kDecodeWarps) {
     // =========================================================== decode
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
     const int dw = warp - kSoftmaxWarps;
     const uint32_t book_at = smem_u32(book);
     bool ok = true;
@@ -366,7 +383,9 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         mbar_arrive(smem_u32(&bars.ring_empty[st]));
       }
     }
-  } else if (warp == kSoftmaxWarps + kDecodeWarps) {
+  } else {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  if (warp == kSoftmaxWarps + kDecodeWarps) {
     // =========================================================== mma
     if (lane == 0 && n_tiles > 0) {
       constexpr uint32_t id_s = instr_desc(kKeys, false), id_o = instr_desc(D, true);
@@ -415,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       while (!mbar_try_wait(smem_u32(&bars.drained), 0) && ++tries < kSpinLimit) {}
     }
     __syncwarp();
-  } else {
+  } else if (warp == kSoftmaxWarps + kDecodeWarps + 1) {
     // =========================================================== load
     const int pieces = a.page_shift >= 7 ? 1 : 128 >> a.page_shift;   // pages that a tile touches (its start is a multiple of 128)
     const int piece_tokens = kKeys / pieces;
@@ -456,6 +475,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       while (!mbar_try_wait(smem_u32(&bars.ring_full[p % kRing]), (p / kRing) & 1) && ++tries < kSpinLimit) {}
     }
   }
+  }
   fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *dead) atomicOr(a.status, 1u);
@@ -471,6 +491,12 @@ cudaError_t fb4_attend_many_prepare_device() {
   const cudaFuncAttribute attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e = cudaFuncSetAttribute(fb4_attend_many_kernel<128>, attr, Many<128>::kBytes);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_many_kernel<64>, attr, Many<64>::kBytes);
+  // the register shares count on what the block is launched with
+  cudaFuncAttributes fa{};
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, fb4_attend_many_kernel<128>);
+  if (e == cudaSuccess && fa.numRegs < kLaunchRegs) e = cudaErrorInvalidConfiguration;
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, fb4_attend_many_kernel<64>);
+  if (e == cudaSuccess && fa.numRegs < kLaunchRegs) e = cudaErrorInvalidConfiguration;
   return e;
 }
 
