@@ -5,7 +5,7 @@
 // r mod group) and one run of the cached tokens, which it walks in tiles of 128.  Its warps have fixed roles:
 //   load     copies codes and metadata of K and V tiles into a ring (bulk copies, page by page)
 //   decode   4 warps turn them into bf16 tiles in shared memory, 128-byte swizzled, [token][channel] for both K and V
-//   mma      one thread issues S_w = Q_w K^T (both operands in shared memory, accumulator in TMEM) and O_w += P_w V
+//   mma      one warp issues S_w = Q_w K^T (both operands in shared memory, accumulator in TMEM) and O_w += P_w V
 //            (P_w from TMEM, V read with the contracted side as the strided one)
 //   softmax  4 warps per query tile, one row per thread: scores from TMEM, running maximum and sum in registers, P back
 //            to TMEM over the scores it came from
@@ -70,21 +70,30 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uin
 }
 
 // ---- tcgen05
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
-  // 128-byte swizzle, descriptor version of sm_100; offsets in units of 16 bytes
-  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(stride >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
+// Shared-memory descriptors, 128-byte swizzle, descriptor version of sm_100: the low word holds the address and the leading
+// offset, the high word the stride (1024 bytes between groups of 8 rows) and the layout; all in units of 16 bytes.
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lead) { return ((addr & 0x3ffffu) >> 4) | ((lead >> 4) << 16); }
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
 // bf16 x bf16 -> f32, M = 128; n_major: B is stored with its N side contiguous
 __host__ __device__ constexpr uint32_t instr_desc(int n, bool n_major) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (n_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+// The issuing warp runs warp-uniform code and only these instructions are one lane's: a lane that computes descriptors on its
+// own for every instruction takes longer than the tensor core for 128 x 128 x 16.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t idesc, bool add) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.u32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+               ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(add ? 1u : 0u), "n"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_low, uint32_t idesc, bool add) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.u32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b_low), "r"(idesc), "r"(add ? 1u : 0u), "n"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ bool elected() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
 }
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -154,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
   __shared__ uint32_t tmem_at, dead_flag;
   const uint32_t base_smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q_at = base_smem, k_at = q_at + 2 * L::kTileBytes, v_at = k_at + 2 * L::kTileBytes, ring_at = v_at + 2 * L::kTileBytes;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   volatile uint32_t* dead = &dead_flag;
 
   let_next_start();      // the join of the splits waits for this kernel's end by itself
@@ -218,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = tmem_at;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
   const uint32_t s_col = tmem, o_col = tmem + 256;                    // S_w at columns 128 w (P_w over its first 64), O_w at 256 + D w
 
   if (warp < kSoftmaxWarps) {
@@ -387,49 +396,59 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
   if (warp == kSoftmaxWarps + kDecodeWarps) {
     // =========================================================== mma
-    if (lane == 0 && n_tiles > 0) {
+    if (n_tiles > 0) {
       constexpr uint32_t id_s = instr_desc(kKeys, false), id_o = instr_desc(D, true);
+      const uint32_t q_low = desc_low(q_at, 16), k_low = desc_low(k_at, 16), v_low = desc_low(v_at, kKeys * 128);
+      constexpr uint32_t kTile16 = L::kTileBytes >> 4;
+      // every lane waits, one issues
       auto scores = [&](int w, int32_t t) {
-        const uint32_t kb = k_at + (t & 1) * L::kTileBytes, qb = q_at + w * L::kTileBytes;
+        const uint32_t kb = k_low + (t & 1) * kTile16, qb = q_low + w * kTile16;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = (k >> 2) * (kKeys * 128) + (k & 3) * 32;
-          mma_ss(s_col + 128 * w, smem_desc(qb + off, 16, 1024), smem_desc(kb + off, 16, 1024), id_s, k > 0);
+          const uint32_t off = ((k >> 2) * (kKeys * 128) + (k & 3) * 32) >> 4;
+          mma_ss(s_col + 128 * w, qb + off, kb + off, id_s, k > 0);
         }
         commit(smem_u32(&bars.s_full[w]));
       };
       auto product = [&](int w, int32_t t) {
-        const uint32_t vb = v_at + (t & 1) * L::kTileBytes;
+        const uint32_t vb = v_low + (t & 1) * kTile16;
 #pragma unroll
-        for (int k = 0; k < kKeys / 16; ++k)
-          mma_ts(o_col + D * w, s_col + 128 * w + 8 * k, smem_desc(vb + k * 2048, kKeys * 128, 1024), id_o, t > 0 || k > 0);
+        for (int k = 0; k < kKeys / 16; ++k) mma_ts(o_col + D * w, s_col + 128 * w + 8 * k, vb + k * (2048 >> 4), id_o, k > 0 || t > 0);
       };
-      bool ok = wait(smem_u32(&bars.k_full[0]), 0, dead);
+      bool ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.k_full[0]), 0, dead));
       if (ok) {
         fence_after();
-        for (int w = 0; w < n_w; ++w) scores(w, 0);
-        commit(smem_u32(&bars.k_empty[0]));
+        if (elected()) {
+          scores(0, 0);
+          if (n_w > 1) scores(1, 0);
+          commit(smem_u32(&bars.k_empty[0]));
+        }
+        __syncwarp();
       }
       for (int32_t t = 0; t < n_tiles && ok; ++t) {
-        ok = wait(smem_u32(&bars.v_full[t & 1]), (t >> 1) & 1, dead);
-        for (int w = 0; w < n_w && ok; ++w) {
-          ok = wait(smem_u32(&bars.p_full[w]), t & 1, dead);
+        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.v_full[t & 1]), (t >> 1) & 1, dead));
+        const bool more = t + 1 < n_tiles;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          if (w >= n_w || !ok) break;
+          ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.p_full[w]), t & 1, dead));
+          if (w == 0 && more && ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.k_full[(t + 1) & 1]), ((t + 1) >> 1) & 1, dead));
           if (!ok) break;
           fence_after();
-          product(w, t);
-          if (t + 1 == n_tiles) commit(smem_u32(&bars.o_full[w]));
-          if (w == n_w - 1) commit(smem_u32(&bars.v_empty[t & 1]));
-          if (t + 1 < n_tiles) {
-            if (w == 0) ok = wait(smem_u32(&bars.k_full[(t + 1) & 1]), ((t + 1) >> 1) & 1, dead);
-            if (!ok) break;
-            fence_after();
-            scores(w, t + 1);
-            if (w == n_w - 1) commit(smem_u32(&bars.k_empty[(t + 1) & 1]));
+          if (elected()) {
+            product(w, t);
+            if (!more) commit(smem_u32(&bars.o_full[w]));
+            if (w == n_w - 1) commit(smem_u32(&bars.v_empty[t & 1]));
+            if (more) {
+              scores(w, t + 1);
+              if (w == n_w - 1) commit(smem_u32(&bars.k_empty[(t + 1) & 1]));
+            }
           }
+          __syncwarp();
         }
       }
       // nothing of this CTA may be on the tensor core when its TMEM is given back
-      commit(smem_u32(&bars.drained));
+      if (elected()) commit(smem_u32(&bars.drained));
       uint32_t tries = 0;
       while (!mbar_try_wait(smem_u32(&bars.drained), 0) && ++tries < kSpinLimit) {}
     }
