@@ -141,21 +141,4 @@ __device__ __forceinline__ void store_out4(const Fb4Attend& a, int64_t at, const
   }
 }
 
-// eight neighbouring channels, 16-byte aligned
-__device__ __forceinline__ void store_out8(const Fb4Attend& a, int64_t at, const float4& u, const float4& v, float f) {
-  if (a.out_dtype == 0) {
-    float4* o = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at);
-    o[0] = make_float4(u.x * f, u.y * f, u.z * f, u.w * f);
-    o[1] = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-  } else if (a.out_dtype == 1) {
-    __nv_bfloat162 p[4] = {__floats2bfloat162_rn(u.x * f, u.y * f), __floats2bfloat162_rn(u.z * f, u.w * f),
-                           __floats2bfloat162_rn(v.x * f, v.y * f), __floats2bfloat162_rn(v.z * f, v.w * f)};
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + at) = *reinterpret_cast<uint4*>(p);
-  } else {
-    __half2 p[4] = {__floats2half2_rn(u.x * f, u.y * f), __floats2half2_rn(u.z * f, u.w * f), __floats2half2_rn(v.x * f, v.y * f),
-                    __floats2half2_rn(v.z * f, v.w * f)};
-    *reinterpret_cast<uint4*>(static_cast<__half*>(a.out) + at) = *reinterpret_cast<uint4*>(p);
-  }
-}
-
 }  // namespace fb4att

@@ -50,7 +50,7 @@ struct Many {
 struct Bars {
   uint64_t ring_full[kRing], ring_empty[kRing];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t s_full[2], p_full[2], o_full[2], drained;
+  uint64_t q_full, s_full[2], p_half[2], p_full[2], o_full[2], drained;
 };
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
@@ -147,6 +147,12 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   return d;
 }
 
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
 // Byte offset of 16-byte run `run` (8 channels) of row `row` in a [128 rows][D] tile of 64-channel columns, 128-byte swizzle
 __device__ __forceinline__ uint32_t swizzled(int row, int run) {
   return (uint32_t)((run >> 3) * (kKeys * 128) + row * 128 + (((run ^ row) & 7) << 4));
@@ -196,9 +202,11 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       mbar_init(smem_u32(&bars.v_full[i]), kDecodeWarps);
       mbar_init(smem_u32(&bars.v_empty[i]), 1);
       mbar_init(smem_u32(&bars.s_full[i]), 1);
+      mbar_init(smem_u32(&bars.p_half[i]), 4);
       mbar_init(smem_u32(&bars.p_full[i]), 4);
       mbar_init(smem_u32(&bars.o_full[i]), 1);
     }
+    mbar_init(smem_u32(&bars.q_full), 4 * n_w);
     mbar_init(smem_u32(&bars.drained), 1);
     dead_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -208,22 +216,6 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   if (threadIdx.x >= 64 && threadIdx.x < 128) fill_book(book, a.tables, threadIdx.x - 64);
-  {
-    // Q, in the decoder's channel order; a negative scale is taken into Q's signs (the softmax wants a positive one)
-    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
-    for (int x = threadIdx.x; x < n_w * 128 * (D / 8); x += kThreads) {
-      const int row = x / (D / 8), run = x % (D / 8);
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (row < n_rows) {
-        const int32_t r = row0 + row;
-        u = __ldg(reinterpret_cast<const uint4*>(a.q + (int64_t)(sq.q0 + r / a.group) * a.q_ld + (int64_t)(head * a.group + r % a.group) * D + run * 8));
-      }
-      const uint32_t at = q_at + (row >> 7) * L::kTileBytes + swizzled(row & 127, run);
-      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(prmt(u.x, u.y, 0x5410u) ^ flip), "r"(prmt(u.x, u.y, 0x7632u) ^ flip),
-                   "r"(prmt(u.z, u.w, 0x5410u) ^ flip), "r"(prmt(u.z, u.w, 0x7632u) ^ flip) : "memory");
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
   fence_before();
   __syncthreads();
   fence_after();
@@ -237,6 +229,29 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
     if (w < n_w) {
       const uint32_t lanes = (uint32_t)(warp & 3) << 21;              // this warp's TMEM lanes: 32 (warp mod 4) << 16
       const uint32_t s_at = s_col + 128 * w + lanes, o_at = o_col + D * w + lanes;
+      // This warp's 32 rows of Q, in the decoder's channel order, while the first tile is loaded and decoded; a negative scale is
+      // taken into Q's signs (the softmax wants a positive one)
+      {
+        const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+        constexpr int kRuns = D / 8;
+        uint4 u[kRuns];
+#pragma unroll
+        for (int k = 0; k < kRuns; ++k) {
+          const int x = k * 32 + lane, r32 = 32 * (warp & 3) + x / kRuns, r = row0 + 128 * w + r32;
+          u[k] = make_uint4(0, 0, 0, 0);
+          if (r < rows)
+            u[k] = __ldg(reinterpret_cast<const uint4*>(a.q + (int64_t)(sq.q0 + r / a.group) * a.q_ld + (int64_t)(head * a.group + r % a.group) * D + x % kRuns * 8));
+        }
+#pragma unroll
+        for (int k = 0; k < kRuns; ++k) {
+          const int x = k * 32 + lane, r32 = 32 * (warp & 3) + x / kRuns;
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(q_at + w * L::kTileBytes + swizzled(r32, x % kRuns)), "r"(prmt(u[k].x, u[k].y, 0x5410u) ^ flip),
+                       "r"(prmt(u[k].x, u[k].y, 0x7632u) ^ flip), "r"(prmt(u[k].z, u[k].w, 0x5410u) ^ flip), "r"(prmt(u[k].z, u[k].w, 0x7632u) ^ flip) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.q_full));
+      }
       const int32_t row = row0 + 128 * w + (warp & 3) * 32 + lane;
       const bool on = row < rows;
       const int32_t rc = on ? row : rows - 1;                         // rows behind the last are computed like it and not stored
@@ -301,6 +316,12 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
             p[i >> 1] = pack(q.x, q.y);
           }
           tmem_st16(s_at + 16 * c, p);
+          if (c == 1) {                                               // the product may start on the first 64 tokens
+            tmem_wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.p_half[w]));
+          }
         }
         tmem_wait_st();
         fence_before();
@@ -315,36 +336,70 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         fence_after();
       }
       const float inv = sum > 0.0f ? kUnshift / sum : 0.0f;
-      const int32_t i = rc / a.group, h = head * a.group + rc % a.group;
-      const int64_t pr = partial_row(a, b, i, h);
-      const int64_t out_row = (int64_t)(sq.q0 + i);
       if (ok) {
+        if (on) {
+          const int32_t i = rc / a.group, h = head * a.group + rc % a.group;
+          if (a.splits > 1) *partial_stat(a, partial_row(a, b, i, h), split, D) = make_float2(m, sum);
+          else if (a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (m + log2f(sum)) * kLn2 : -INFINITY;
+        }
+        // The rows go through this warp's part of Q's shared memory, which nobody reads any more, so that a store covers whole rows:
+        // 2 D bytes of each row at a time (all of it in 16 bits, half of it in float32).
+        constexpr int kPieces = D / 8;                                // of 16 bytes
+        const uint32_t stage = q_at + w * L::kTileBytes + (warp & 3) * (32 * 2 * D);
+        const bool wide = a.splits > 1 || a.out_dtype == 0;
+        const float f = a.splits > 1 ? 1.0f : inv;
+        for (int part = 0; part < (wide ? 2 : 1); ++part) {
+          const int c0 = part * (D / 2), c1 = wide ? c0 + D / 2 : D;
+          for (int c = c0; c < c1; c += 32) {
+            float x[32];
+            if (n_tiles > 0) {
+              tmem_ld32(o_at + c, x);
+              tmem_wait_ld();
+            } else {
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          float x[32];
-          if (n_tiles > 0) {
-            tmem_ld32(o_at + 32 * c, x);
-            tmem_wait_ld();
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) x[k] = 0.0f;
-          }
-          if (on) {
+              for (int k = 0; k < 32; ++k) x[k] = 0.0f;
+            }
 #pragma unroll
             for (int k = 0; k < 32; k += 8) {                         // channel order 0 2 1 3 4 6 5 7
-              const float4 u = make_float4(x[k], x[k + 2], x[k + 1], x[k + 3]), z = make_float4(x[k + 4], x[k + 6], x[k + 5], x[k + 7]);
-              if (a.splits > 1) {
-                float4* dst = reinterpret_cast<float4*>(partial_sums(a, pr, split, D) + 32 * c + k);
-                if (sum > 0.0f) { dst[0] = u; dst[1] = z; }
+              const float v[8] = {x[k] * f, x[k + 2] * f, x[k + 1] * f, x[k + 3] * f, x[k + 4] * f, x[k + 6] * f, x[k + 5] * f, x[k + 7] * f};
+              uint32_t o[8];
+              int n16 = 1;
+              if (wide) {
+                n16 = 2;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) o[q] = __float_as_uint(v[q]);
               } else {
-                store_out8(a, out_row * a.out_ld + (int64_t)h * D + 32 * c + k, u, z, inv);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) o[q] = a.out_dtype == 1 ? pack(v[2 * q], v[2 * q + 1]) : pack_half(v[2 * q], v[2 * q + 1]);
+                o[4] = o[5] = o[6] = o[7] = 0u;
+              }
+#pragma unroll
+              for (int q = 0; q < 2; ++q)
+                if (q < n16) {
+                  const int piece = ((c - c0 + k) / 8) * n16 + q;
+                  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * (2 * D) + ((piece ^ (lane & 7)) << 4)), "r"(o[4 * q]), "r"(o[4 * q + 1]), "r"(o[4 * q + 2]), "r"(o[4 * q + 3]) : "memory");
+                }
+            }
+          }
+          __syncwarp();
+#pragma unroll 4
+          for (int it = 0; it < kPieces; ++it) {
+            const int x = it * 32 + lane, r32 = x / kPieces, piece = x % kPieces;
+            const int32_t r = row0 + 128 * w + 32 * (warp & 3) + r32;
+            const float rsum = __shfl_sync(0xffffffffu, sum, r32);
+            const uint4 v = fb4blk::lds_v4(stage + r32 * (2 * D) + ((piece ^ (r32 & 7)) << 4));
+            if (r < rows) {
+              const int32_t i = r / a.group, h = head * a.group + r % a.group;
+              if (a.splits > 1) {
+                if (rsum > 0.0f) *reinterpret_cast<uint4*>(partial_sums(a, partial_row(a, b, i, h), split, D) + c0 + piece * 4) = v;
+              } else {
+                const int64_t at = (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D;
+                if (wide) *reinterpret_cast<uint4*>(static_cast<float*>(a.out) + at + c0 + piece * 4) = v;
+                else *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at + piece * 8) = v;
               }
             }
           }
-        }
-        if (on) {
-          if (a.splits > 1) *partial_stat(a, pr, split, D) = make_float2(m, sum);
-          else if (a.lse) a.lse[out_row * a.q_heads + h] = sum > 0.0f ? (m + log2f(sum)) * kLn2 : -INFINITY;
+          __syncwarp();
         }
       }
     }
@@ -410,12 +465,12 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         }
         commit(smem_u32(&bars.s_full[w]));
       };
-      auto product = [&](int w, int32_t t) {
+      auto product = [&](int w, int32_t t, int part) {                 // one half of the tile's tokens
         const uint32_t vb = v_low + (t & 1) * kTile16;
 #pragma unroll
-        for (int k = 0; k < kKeys / 16; ++k) mma_ts(o_col + D * w, s_col + 128 * w + 8 * k, vb + k * (2048 >> 4), id_o, k > 0 || t > 0);
+        for (int k = part * (kKeys / 32); k < (part + 1) * (kKeys / 32); ++k) mma_ts(o_col + D * w, s_col + 128 * w + 8 * k, vb + k * (2048 >> 4), id_o, k > 0 || t > 0);
       };
-      bool ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.k_full[0]), 0, dead));
+      bool ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.q_full), 0, dead) && wait(smem_u32(&bars.k_full[0]), 0, dead));
       if (ok) {
         fence_after();
         if (elected()) {
@@ -431,12 +486,17 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           if (w >= n_w || !ok) break;
+          ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.p_half[w]), t & 1, dead));
+          if (!ok) break;
+          fence_after();
+          if (elected()) product(w, t, 0);
+          __syncwarp();
           ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.p_full[w]), t & 1, dead));
           if (w == 0 && more && ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.k_full[(t + 1) & 1]), ((t + 1) >> 1) & 1, dead));
           if (!ok) break;
           fence_after();
           if (elected()) {
-            product(w, t);
+            product(w, t, 1);
             if (!more) commit(smem_u32(&bars.o_full[w]));
             if (w == n_w - 1) commit(smem_u32(&bars.v_empty[t & 1]));
             if (more) {
