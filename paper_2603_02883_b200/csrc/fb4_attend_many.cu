@@ -158,6 +158,16 @@ __device__ __forceinline__ uint32_t swizzled(int row, int run) {
   return (uint32_t)((run >> 3) * (kKeys * 128) + row * 128 + (((run ^ row) & 7) << 4));
 }
 
+// Query and head (inside its cache head's group) of a row, moved forward without divisions.
+struct RowAt {
+  int32_t i, h;
+  __device__ __forceinline__ RowAt(int32_t row, int32_t group) : i(row / group), h(row - row / group * group) {}
+  __device__ __forceinline__ void advance(int32_t rows, int32_t group) {
+    h += rows;
+    while (h >= group) { h -= group; ++i; }
+  }
+};
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __grid_constant__ Fb4Attend a) {
   using L = Many<D>;
@@ -235,12 +245,14 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
         constexpr int kRuns = D / 8;
         uint4 u[kRuns];
+        const int32_t r0 = row0 + 128 * w + 32 * (warp & 3) + lane / kRuns;
+        RowAt at(r0 < rows ? r0 : 0, a.group);
 #pragma unroll
         for (int k = 0; k < kRuns; ++k) {
-          const int x = k * 32 + lane, r32 = 32 * (warp & 3) + x / kRuns, r = row0 + 128 * w + r32;
           u[k] = make_uint4(0, 0, 0, 0);
-          if (r < rows)
-            u[k] = __ldg(reinterpret_cast<const uint4*>(a.q + (int64_t)(sq.q0 + r / a.group) * a.q_ld + (int64_t)(head * a.group + r % a.group) * D + x % kRuns * 8));
+          if (r0 + k * (32 / kRuns) < rows)
+            u[k] = __ldg(reinterpret_cast<const uint4*>(a.q + (int64_t)(sq.q0 + at.i) * a.q_ld + (int64_t)(head * a.group + at.h) * D + lane % kRuns * 8));
+          at.advance(32 / kRuns, a.group);
         }
 #pragma unroll
         for (int k = 0; k < kRuns; ++k) {
@@ -382,14 +394,16 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
             }
           }
           __syncwarp();
+          const int piece = lane % kPieces;
+          int32_t r = row0 + 128 * w + 32 * (warp & 3) + lane / kPieces;
+          RowAt at_row(r < rows ? r : 0, a.group);
 #pragma unroll 4
-          for (int it = 0; it < kPieces; ++it) {
-            const int x = it * 32 + lane, r32 = x / kPieces, piece = x % kPieces;
-            const int32_t r = row0 + 128 * w + 32 * (warp & 3) + r32;
+          for (int it = 0; it < kPieces; ++it, r += 32 / kPieces, at_row.advance(32 / kPieces, a.group)) {
+            const int r32 = it * (32 / kPieces) + lane / kPieces;
             const float rsum = __shfl_sync(0xffffffffu, sum, r32);
             const uint4 v = fb4blk::lds_v4(stage + r32 * (2 * D) + ((piece ^ (r32 & 7)) << 4));
             if (r < rows) {
-              const int32_t i = r / a.group, h = head * a.group + r % a.group;
+              const int32_t i = at_row.i, h = head * a.group + at_row.h;
               if (a.splits > 1) {
                 if (rsum > 0.0f) *reinterpret_cast<uint4*>(partial_sums(a, partial_row(a, b, i, h), split, D) + c0 + piece * 4) = v;
               } else {
