@@ -25,7 +25,7 @@ constexpr int kTile = 32;              // tokens of a warp's tile
 
 template <int D>
 struct Few {
-  static constexpr int kStagesFew = D == 128 ? 3 : 6;
+  static constexpr int kStagesFew = D == 128 ? 2 : 4;
   static constexpr int kCodes = kTile * D / 2, kMeta = kTile * (D / 32) * 2;
   static constexpr int kStage = 2 * kCodes + 2 * kMeta;
   static constexpr int kRing = kWarpsFew * kStagesFew * kStage;
@@ -578,6 +578,7 @@ Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_hea
     const int64_t fine = tiles / 32 < 8 ? tiles / 32 : 8;           // sequences of unlike lengths: pieces of 1024 tokens even them out
     if (s < fine) s = fine;
     if (s > most) s = most;
+    if (s > 0x7fffffffLL / units) s = 0x7fffffffLL / units;         // a grid has at most 2^31 - 1 CTAs
     if (s < 1) s = 1;
     p.splits = (int32_t)s;
   } else {

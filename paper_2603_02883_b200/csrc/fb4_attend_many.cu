@@ -34,8 +34,8 @@ constexpr int kKeys = 128;             // tokens of a tile
 constexpr int kSoftmaxWarps = 8, kDecodeWarps = 4;
 constexpr int kThreads = 512;          // two warpgroups of softmax, one of decode, one whose first two warps are mma and load
 // Registers per thread of the roles.  The block is launched with 128 for each of its 512 threads; what decode, mma and load
-// give back is what the softmax warps, which keep a row's 128 scores in registers, take: 2 * 192 + 88 + 40 = 4 * 128.
-constexpr int kLaunchRegs = 128, kSoftmaxRegs = 192, kDecodeRegs = 88, kOtherRegs = 40;
+// give back is what the softmax warps, which keep a row's 128 scores in registers, take: 2 * 200 + 72 + 40 = 4 * 128.
+constexpr int kLaunchRegs = 128, kSoftmaxRegs = 200, kDecodeRegs = 72, kOtherRegs = 40;
 static_assert(2 * kSoftmaxRegs + kDecodeRegs + kOtherRegs <= 4 * kLaunchRegs, "register shares of the warpgroups");
 constexpr int kRing = 3;               // ring stages: a K or a V tile's codes and metadata each
 constexpr int kHave = 8;               // tiles whose page flags are kept
@@ -57,16 +57,18 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Waits for a phase with a limit; a wait that runs out, here or anywhere in the CTA, ends every other one.
+// Waits for a phase with a limit; a wait that runs out, here or anywhere in the CTA, ends every other one.  Eight bare tries
+// for each look at the limit: the roles that wait take issue slots from those that work (a fifth of all instructions went into
+// waiting with a look at every try).
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
-  uint32_t tries = 0;
-  while (!mbar_try_wait(bar, parity)) {
-    if (++tries >= kSpinLimit || *dead) {
-      *dead = 1u;
-      return false;
-    }
+  for (uint32_t tries = 0; tries < kSpinLimit / 8; ++tries) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (*dead) break;
   }
-  return true;
+  *dead = 1u;
+  return false;
 }
 
 // ---- tcgen05

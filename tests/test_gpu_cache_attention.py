@@ -209,8 +209,11 @@ def test_a_layer_step_by_step_equals_the_whole_prompt(q32):
         agree((out, lse), whole)
 
 
-def test_captured_and_replayed(q32):
-    q, cache, table, kv, qs, mq, mkv = setup(q32, [1, 1], [3000, 200], 8, 2, 128, 16, seed=14)
+@pytest.mark.parametrize("q_len,kv_len,heads", [([1, 1], [1500, 200], (8, 2)), ([1, 1], [30000, 20000], (2, 1)), ([150, 40], [6000, 500], (2, 1))],
+                         ids=["cluster", "few rows, workspace", "many rows, workspace"])
+def test_captured_and_replayed(q32, q_len, kv_len, heads):
+    q, cache, table, kv, qs, mq, mkv = setup(q32, q_len, kv_len, *heads, 128, 16, seed=14)
+    assert (fb4.fb4_cache_attention_workspace(q32.ctx, *heads, 128, 2, mq, mkv, 0) > 0) == (mkv > 3000)
     want = q32.cache_attention(q, cache, table, kv, qs, mq, mkv)
     st = torch.cuda.Stream()
     st.wait_stream(torch.cuda.current_stream())
@@ -223,13 +226,56 @@ def test_captured_and_replayed(q32):
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     q2 = torch.randn_like(q)
-    kv2 = i32([1500, 150])
+    kv2 = kv // 2 + 75
     want = q32.cache_attention(q2, cache, table, kv2, qs, mq, mkv)
     q.copy_(q2)
     kv.copy_(kv2)
     gr.replay()
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0])
+
+
+def test_two_calls_at_once_on_two_streams(q32):
+    """every call has a workspace of its own; contexts are only serialised on the host"""
+    args = [setup(q32, [1, 2], [20000, 9000], 4, 1, 128, 16, seed=20), setup(q32, [100, 60], [4000, 9000], 2, 2, 64, 32, seed=21)]
+    want = [q32.cache_attention(*a) for a in args]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(8):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(q32.cache_attention(*args[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert torch.equal(g[0], want[i][0]) and torch.equal(g[1], want[i][1])
+
+
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_a_cache_whose_offsets_pass_32_bits(q32, n_q):
+    """4.6 GB of codes for K and for V; the sequence lives in the last pages and in the first"""
+    heads, page, D = 8, 64, 128
+    n_pages = (1 << 32) // (heads * page * D // 2) + 16000
+    codes = [torch.empty(n_pages, heads, page, D // 2, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    meta = [torch.empty(n_pages, heads, page, D // 32, dtype=torch.int16, device="cuda") for _ in range(2)]
+    big = fb4.Cache(codes[0], meta[0], codes[1], meta[1])
+    ids = [n_pages - 1, 0, n_pages - 7, 131072, 3]
+    n = 5 * page - 9
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    kv = torch.randn(2, n, heads, D, generator=g, device="cuda").to(torch.bfloat16)
+    q = torch.randn(n_q, heads, D, generator=g, device="cuda").to(torch.bfloat16)
+    at = torch.arange(n, device="cuda")
+    slot = torch.tensor(ids, device="cuda")[at // page] * page + at % page
+    assert int(slot.max()) * heads * D // 2 > 1 << 32
+    small = q32.new_cache(5, page, heads, D)
+    q32.cache_append(big, slot, kv[0], kv[1])
+    q32.cache_append(small, at, kv[0], kv[1])
+    a = q32.cache_attention(q, big, i32([ids]), i32([n]), i32([0, n_q]), n_q, n)
+    b = q32.cache_attention(q, small, i32([[0, 1, 2, 3, 4]]), i32([n]), i32([0, n_q]), n_q, n)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert torch.equal(big.k_codes[ids[0]], small.k_codes[0]) and torch.equal(big.v_meta[ids[3]], small.v_meta[3])
 
 
 def test_refusals(q32):
