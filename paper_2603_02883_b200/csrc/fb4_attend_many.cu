@@ -160,6 +160,18 @@ __device__ __forceinline__ uint32_t swizzled(int row, int run) {
   return (uint32_t)((run >> 3) * (kKeys * 128) + row * 128 + (((run ^ row) & 7) << 4));
 }
 
+// The sequence that comes at place `place` when up to 32 of them are put in order of their caches' lengths, longest first.
+__device__ __forceinline__ int32_t by_length(const Fb4Attend& a, int32_t place) {
+  const int lane = threadIdx.x & 31;
+  const int32_t len = lane < a.n_seqs ? __ldg(a.kv_len + lane) : 0;
+  int32_t before = 0;
+  for (int i = 0; i < a.n_seqs; ++i) {
+    const int32_t other = __shfl_sync(0xffffffffu, len, i);
+    before += other > len || (other == len && i < lane) ? 1 : 0;
+  }
+  return __ffs((int)__ballot_sync(0xffffffffu, lane < a.n_seqs && before == place)) - 1;
+}
+
 // Query and head (inside its cache head's group) of a row, moved forward without divisions.
 struct RowAt {
   int32_t i, h;
@@ -193,7 +205,10 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
   id /= a.splits;
   const int32_t rt = row_tiles - 1 - (int32_t)(id % row_tiles);       // under a causal mask the last rows have the most to do
   id /= row_tiles;
-  const int32_t head = (int32_t)(id % a.cache.n_heads), b = (int32_t)(id / a.cache.n_heads);
+  const int32_t head = (int32_t)(id % a.cache.n_heads);
+  int32_t b = (int32_t)(id / a.cache.n_heads);
+  // CTAs start in this order, so the sequences with the longest caches come first (a few of them; many even out by themselves)
+  if (a.n_seqs > 1 && a.n_seqs <= 32) b = by_length(a, b);
   const Sequence sq = sequence(a, b, threadIdx.x == 0 && split == 0 && head == 0 && rt == 0);
   const int32_t rows = sq.n_q * a.group, row0 = rt * 256;
   if (row0 >= rows) return;
