@@ -7,7 +7,6 @@ missing and cannot be built, importing this module raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -375,27 +374,65 @@ class Quantized:
     res_meta: torch.Tensor | None = None
 
 
-@dataclass
+def _device_of(*tensors) -> int:
+    """the CUDA device all of them are on"""
+    d = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != d or d < 0:
+            raise ValueError("the tensors must be on one CUDA device")
+    return d
+
+
+_INT4 = ctypes.c_int32 * 4
+
+
+@dataclass(frozen=True)
 class Rope:
     """Position rotation (see fb4_rope in include/fb4.h): pair i of a head belongs to the axis whose run of `axis_pairs` it
-    lies in and is rotated by the angle that `table` holds for that axis' position"""
+    lies in and is rotated by the angle that `table` holds for that axis' position.  Checked once, here: made for a step, it
+    serves all layers."""
     table: torch.Tensor                      # float32 [n_pos][D/2][2]: cos, sin
     pos: torch.Tensor                        # int32 [T][n_axes] (or [T] with one axis)
     axis_pairs: list
     interleaved: bool = False
 
+    def __post_init__(self):
+        table, pos, pairs = self.table, self.pos, self.axis_pairs
+        n = len(pairs)
+        if not 1 <= n <= 4:
+            raise ValueError("a rotation has 1 to 4 axes")
+        if table.dtype is not torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+            raise ValueError("rope.table must be a contiguous float32 tensor [n_pos][D/2][2]")
+        T = pos.shape[0] if pos.dim() else -1
+        if pos.dtype is not torch.int32 or pos.numel() != T * n or not pos.is_contiguous():
+            raise ValueError("rope.pos must be a contiguous int32 tensor [T][n_axes]")
+        c = Fb4Rope(table.data_ptr(), table.shape[0], pos.data_ptr(), n, _INT4(*pairs), 1 if self.interleaved else 0)
+        object.__setattr__(self, "_c", (c, T, table.shape[1] * 2, _device_of(table, pos)))
 
-@dataclass
+
+@dataclass(frozen=True)
 class Cache:
-    """Paged FB4 cache (see fb4_cache in include/fb4.h)"""
+    """Paged FB4 cache (see fb4_cache in include/fb4.h).  Checked once, here: the object is a handle that a program keeps."""
     k_codes: torch.Tensor                    # uint8 [n_pages][n_heads][page_tokens][D/2]
     k_meta: torch.Tensor                     # uint16 bits in an int16 tensor [n_pages][n_heads][page_tokens][D/32]
     v_codes: torch.Tensor
     v_meta: torch.Tensor
 
+    def __post_init__(self):
+        kc, km, vc, vm = self.k_codes, self.k_meta, self.v_codes, self.v_meta
+        if kc.dim() != 4:
+            raise ValueError("cache codes must be [n_pages][n_heads][page_tokens][D/2]")
+        n, h, p, half = shape = kc.shape
+        meta = (n, h, p, half // 16)
+        if kc.dtype is not torch.uint8 or vc.dtype is not torch.uint8 or vc.shape != shape or not kc.is_contiguous() or not vc.is_contiguous():
+            raise ValueError("cache codes must be contiguous uint8 [n_pages][n_heads][page_tokens][D/2]")
+        if km.element_size() != 2 or vm.element_size() != 2 or km.shape != meta or vm.shape != meta or not km.is_contiguous() or \
+                not vm.is_contiguous():
+            raise ValueError("cache meta must be contiguous 16-bit [n_pages][n_heads][page_tokens][D/32]")
+        c = Fb4Cache(kc.data_ptr(), km.data_ptr(), vc.data_ptr(), vm.data_ptr(), n, p, h, half * 2)
+        object.__setattr__(self, "_c", (c, _device_of(kc, km, vc, vm)))
 
-_INT4 = ctypes.c_int32 * 4
-_NO_GUARD = contextlib.nullcontext()
+
 _OUT_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -575,9 +612,16 @@ class Fb4:
 
     # ---- attention side: norm + rotation of q and k, paged cache, attention over it
 
-    def _guard(self):
-        """the context's device made current, where it is not already"""
-        return _NO_GUARD if torch.cuda.current_device() == self.device else torch.cuda.device(self.device)
+    def _call(self, where, *args):
+        """the C entry point `where` on the context's device and its current stream"""
+        f = getattr(lib(), where)
+        if torch.cuda.current_device() == self.device:
+            rc = f(self.ctx, *args, _raw_stream(self.device))
+        else:
+            with torch.cuda.device(self.device):
+                rc = f(self.ctx, *args, _raw_stream(self.device))
+        if rc != OK:
+            raise Fb4Error(rc, where)
 
     def _on(self, *tensors):
         for t in tensors:
@@ -600,17 +644,12 @@ class Fb4:
     def _rope(self, rope: Rope | None, T: int, D: int):
         if rope is None:
             return None
-        table, pos, pairs = rope.table, rope.pos, rope.axis_pairs
-        n = len(pairs)
-        if not 1 <= n <= 4:
-            raise ValueError("a rotation has 1 to 4 axes")
-        if table.dtype is not torch.float32 or table.dim() != 3 or table.shape[1] * 2 != D or table.shape[2] != 2 or \
-                not table.is_contiguous():
-            raise ValueError("rope.table must be a contiguous float32 tensor [n_pos][D/2][2]")
-        if pos.dtype is not torch.int32 or pos.numel() != T * n or (T and pos.shape[0] != T) or not pos.is_contiguous():
-            raise ValueError("rope.pos must be a contiguous int32 tensor [T][n_axes]")
-        self._on(table, pos)
-        return Fb4Rope(table.data_ptr(), table.shape[0], pos.data_ptr(), n, _INT4(*pairs), 1 if rope.interleaved else 0)
+        c, t, d, device = rope._c
+        if t != T or d != D:
+            raise ValueError("the rotation must have the tokens and the head dimension of the rows it turns")
+        if device != self.device:
+            raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
+        return c
 
     def _gain(self, gain, D):
         """address of a gain, or None"""
@@ -621,19 +660,11 @@ class Fb4:
         self._on(gain)
         return gain.data_ptr()
 
-    def _cache(self, c: Cache) -> Fb4Cache:
-        kc, km, vc, vm = c.k_codes, c.k_meta, c.v_codes, c.v_meta
-        if kc.dim() != 4:
-            raise ValueError("cache codes must be [n_pages][n_heads][page_tokens][D/2]")
-        n, h, p, half = shape = kc.shape
-        meta = (n, h, p, half // 16)
-        if kc.dtype is not torch.uint8 or vc.dtype is not torch.uint8 or vc.shape != shape or not kc.is_contiguous() or not vc.is_contiguous():
-            raise ValueError("cache codes must be contiguous uint8 [n_pages][n_heads][page_tokens][D/2]")
-        if km.element_size() != 2 or vm.element_size() != 2 or km.shape != meta or vm.shape != meta or not km.is_contiguous() or \
-                not vm.is_contiguous():
-            raise ValueError("cache meta must be contiguous 16-bit [n_pages][n_heads][page_tokens][D/32]")
-        self._on(kc, km, vc, vm)
-        return Fb4Cache(kc.data_ptr(), km.data_ptr(), vc.data_ptr(), vm.data_ptr(), n, p, h, half * 2)
+    def _cache(self, cache: Cache) -> Fb4Cache:
+        c, device = cache._c
+        if device != self.device:
+            raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
+        return c
 
     def new_cache(self, n_pages: int, page_tokens: int, n_heads: int, head_dim: int) -> Cache:
         """an empty cache: all zero, so every slot reads as zeros"""
@@ -651,15 +682,14 @@ class Fb4:
             raise ValueError("q and k must have the same tokens and head dimension")
         qg, kg, r = self._gain(q_gain, D), self._gain(k_gain, D), self._rope(rope, T, D)
         if out is None:
-            qo, ko, qo_ld, ko_ld = q.new_empty((T, Hq, D)), k.new_empty((T, Hk, D)), Hq * D, Hk * D
+            qo, ko, qo_ld, ko_ld = q.new_empty(T, Hq, D), k.new_empty(T, Hk, D), Hq * D, Hk * D
         else:
             qo, ko = out
             (Ta, Ha, Da, qo_ld), (Tb, Hb, Db, ko_ld) = self._heads(qo), self._heads(ko)
             if (Ta, Ha, Da) != (T, Hq, D) or (Tb, Hb, Db) != (T, Hk, D):
                 raise ValueError("out must have the shapes of q and k")
-        with self._guard():
-            _check(lib().fb4_qk_norm_rope(self.ctx, q.data_ptr(), Hq, q_ld, k.data_ptr(), Hk, k_ld, T, D, qg, kg, eps, r, qo.data_ptr(),
-                                          qo_ld, ko.data_ptr(), ko_ld, _raw_stream(self.device)), "fb4_qk_norm_rope")
+        self._call("fb4_qk_norm_rope", q.data_ptr(), Hq, q_ld, k.data_ptr(), Hk, k_ld, T, D, qg, kg, eps, r, qo.data_ptr(), qo_ld,
+                   ko.data_ptr(), ko_ld)
         return qo, ko
 
     def cache_append(self, cache: Cache, slot, k, v, k_gain=None, eps: float = 1e-6, rope: Rope | None = None, q=None,
@@ -682,11 +712,10 @@ class Fb4:
             if Tq != T or Dq != D:
                 raise ValueError("q must have the tokens and the head dimension of k")
             qg = self._gain(q_gain, D)
-            qo = q.new_empty((T, Hq, D))
+            qo = q.new_empty(T, Hq, D)
             qp, qop = q.data_ptr(), qo.data_ptr()
-        with self._guard():
-            _check(lib().fb4_cache_append(self.ctx, c, slot.data_ptr(), k.data_ptr(), k_ld, v.data_ptr(), v_ld, T, kg, eps, r, qp, Hq,
-                                          q_ld, qg, qop, Hq * D, _raw_stream(self.device)), "fb4_cache_append")
+        self._call("fb4_cache_append", c, slot.data_ptr(), k.data_ptr(), k_ld, v.data_ptr(), v_ld, T, kg, eps, r, qp, Hq, q_ld, qg, qop,
+                   Hq * D)
         return qo
 
     def cache_attention(self, q, cache: Cache, page_table, kv_len, q_start, max_q: int, max_kv: int, scale: float | None = None,
@@ -704,16 +733,13 @@ class Fb4:
             if t.dtype is not torch.int32 or not t.is_contiguous():
                 raise ValueError("page_table, kv_len and q_start must be contiguous int32")
         self._on(page_table, kv_len, q_start)
-        L = lib()
-        out = q.new_empty((total, Hq, D)) if dtype is torch.bfloat16 else q.new_empty((total, Hq, D), dtype=dtype)
-        lse = q.new_empty((total, Hq), dtype=torch.float32)
-        need = L.fb4_cache_attention_workspace(self.ctx, Hq, c.n_heads, D, n, max_q, max_kv, window)
+        out = q.new_empty(total, Hq, D) if dtype is torch.bfloat16 else q.new_empty(total, Hq, D, dtype=dtype)
+        lse = q.new_empty(total, Hq, dtype=torch.float32)
+        need = lib().fb4_cache_attention_workspace(self.ctx, Hq, c.n_heads, D, n, max_q, max_kv, window)
         ws = q.new_empty(need // 2) if need > 0 else None
-        with self._guard():
-            _check(L.fb4_cache_attention(self.ctx, q.data_ptr(), q_ld, Hq, total, c, page_table.data_ptr(), page_table.shape[1],
-                                         kv_len.data_ptr(), q_start.data_ptr(), n, max_q, max_kv, D ** -0.5 if scale is None else scale,
-                                         1 if causal else 0, window, out.data_ptr(), Hq * D, _OUT_DTYPE[dtype], lse.data_ptr(),
-                                         None if ws is None else ws.data_ptr(), need, _raw_stream(self.device)), "fb4_cache_attention")
+        self._call("fb4_cache_attention", q.data_ptr(), q_ld, Hq, total, c, page_table.data_ptr(), page_table.shape[1], kv_len.data_ptr(),
+                   q_start.data_ptr(), n, max_q, max_kv, D ** -0.5 if scale is None else scale, 1 if causal else 0, window,
+                   out.data_ptr(), Hq * D, _OUT_DTYPE[dtype], lse.data_ptr(), None if ws is None else ws.data_ptr(), need)
         return out, lse
 
     def cache_values(self, cache: Cache, dtype=torch.float32):
@@ -721,13 +747,9 @@ class Fb4:
         c = self._cache(cache)
         shape = (c.n_pages, c.n_heads, c.page_tokens, c.head_dim)
         rows = c.n_pages * c.n_heads * c.page_tokens
-        k, v = cache.k_codes.new_empty(shape, dtype=dtype), cache.k_codes.new_empty(shape, dtype=dtype)
-        L = lib()
-        with self._guard():
-            st = _raw_stream(self.device)
-            for codes, meta, x in ((c.k_codes, c.k_meta, k), (c.v_codes, c.v_meta, v)):
-                _check(L.fb4_dequantize(self.ctx, codes, meta, rows, c.head_dim, None, 0, None, None, x.data_ptr(), _OUT_DTYPE[dtype], st),
-                       "fb4_dequantize")
+        k, v = cache.k_codes.new_empty(*shape, dtype=dtype), cache.k_codes.new_empty(*shape, dtype=dtype)
+        for codes, meta, x in ((c.k_codes, c.k_meta, k), (c.v_codes, c.v_meta, v)):
+            self._call("fb4_dequantize", codes, meta, rows, c.head_dim, None, 0, None, None, x.data_ptr(), _OUT_DTYPE[dtype])
         return k, v
 
     def set_kernel_variant(self, variant: int) -> None:
