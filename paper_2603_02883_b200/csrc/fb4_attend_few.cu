@@ -7,13 +7,14 @@
 //
 // The tokens are the long side, so they are the M side of the products: S^T = K Q^T (m = 16 tokens, n = 8 queries),
 // O^T = V^T P^T (m = 16 channels, n = 8 queries), mma.sync m16n8k16: with one query per head 7/8 of the N side is idle, but a
-// step reads every cached value once and costs 16 mma per 16 tokens; tcgen05 would want the decoded tile in shared
-// memory, which costs more than these products.  A lane decodes a quarter of a token's channels from one 16-byte word of
+// step reads every cached value once and costs 16 mma per 16 tokens.  A lane decodes a quarter of a token's channels from one 16-byte word of
 // codes with one metadata record, straight into the A fragment of the first product (which channel sits at which k is
 // free, as long as Q agrees); V goes through movmatrix once, because there the tokens are the contracted side.
 //
-// Bound: the decode's ALU and FMA instructions (about 2.4 per cached value with everything, against the 3.1 that fit under
-// 0.5625 bytes of traffic), so close to, but not quite, memory-bound.
+// Bound: instructions.  A warp issues 459 of them for 16 tokens of 128 channels (K and V; 311 are the decode and the products), 60 % of
+// the ALU pipe's slots while it runs; 75600 tokens of 12 heads take 51 us, 2.55 TB/s of the cache's 4.5 bits per value, 39 % of the
+// copy bandwidth.  More warps at fewer registers (20 or 24 instead of 16 per SM) came out slower, and so did the same work on
+// tcgen05 (K decoded into tensor memory, V into a swizzled tile, roles by warp: 61 us).
 #include "fb4_attend.cuh"
 #include "fb4_block.cuh"
 
