@@ -460,7 +460,7 @@ Heads heads_of(const void* x, int64_t ld, int32_t n, const void* gain, void* out
   h.out = static_cast<uint16_t*>(out);
   h.ld = ld;
   h.out_ld = out_ld;
-  h.gain = static_cast<const uint16_t*>(gain);
+  h.gain = n > 0 ? static_cast<const uint16_t*>(gain) : nullptr;      // ignored without heads, and then not to be read
   h.n = n;
   return h;
 }

@@ -156,3 +156,13 @@ def test_refusals(q32):
         q32.cache_append(cache, slot, x[:, 2:5], x[:, 4:])
     with pytest.raises(ValueError):
         q32.cache_append(fb4.Cache(cache.k_codes, cache.k_meta[:, :1], cache.v_codes, cache.v_meta), slot, x[:, 2:4], x[:, 4:])
+
+
+def test_without_q_heads_its_pointers_are_ignored(q32):
+    x, g, rope, plain, _ = make(20, 0, 2, 64, (32,), False, seed=13)
+    a, b = q32.new_cache(2, 16, 2, 64), q32.new_cache(2, 16, 2, 64)
+    slot, odd = torch.arange(20, device="cuda"), g.data_ptr() + 2
+    q32.cache_append(a, slot, x[:, :2], x[:, 2:], g[1], 1e-6, rope)
+    fb4.fb4_cache_append(q32.ctx, q32._cache(b), slot, x, 256, x[:, 2:], 256, 20, g[1], 1e-6, q32._rope(rope, 20, 64), odd, 0, -1, odd, odd, -1)
+    for f in ("k_codes", "k_meta", "v_codes", "v_meta"):
+        assert torch.equal(getattr(a, f), getattr(b, f))

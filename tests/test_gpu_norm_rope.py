@@ -154,3 +154,18 @@ def test_refusals(q32):
         q32.qk_norm_rope(q, k, rope=fb4.Rope(rope.table, rope.pos[:5], [32]))
     with pytest.raises(ValueError):
         q32.qk_norm_rope(q.cpu(), k)
+
+
+def test_pointers_of_a_side_without_heads_are_ignored(q32):
+    """not read and not checked: here a gain that is not even aligned"""
+    x, g, rope, plain, _ = make(20, 2, 2, 64, (32,), False, seed=12)
+    q, k = x[:, :2], x[:, 2:4]
+    want = q32.qk_norm_rope(q, k, g[0], g[1], 1e-6, rope)
+    r, odd = q32._rope(rope, 20, 64), g.data_ptr() + 2
+    for side in (0, 1):
+        out = torch.zeros(20, 2, 64, dtype=torch.bfloat16, device="cuda")
+        real = lambda src, gain: [(src, 2, 384), gain, (out, 128)]  # noqa: E731
+        none = [(odd, 0, -1), odd, (odd, -1)]
+        a, b = (real(q, g[0]), none) if side == 0 else (none, real(k, g[1]))
+        fb4.fb4_qk_norm_rope(q32.ctx, *a[0], *b[0], 20, 64, a[1], b[1], 1e-6, r, *a[2], *b[2])
+        assert torch.equal(out, want[side])
