@@ -9,7 +9,7 @@
 // every grid; the square of a bf16 is exact in float32, which lets the first level of sums be fused multiply-adds.
 //
 // Both kernels stream, and the instructions are what has to be kept under the bytes: a row of norm and rotation costs its
-// lanes 282 instructions (32760 tokens of 24 heads of 128: 85 us, 4.75 TB/s, 73 % of the copy bandwidth; a plain copy of the same
+// lanes 282 instructions (32760 tokens of 24 heads of 128: 82 us, 4.9 TB/s, 75 % of the copy bandwidth; a plain copy of the same
 // rows by the same loop takes 70 us), the quantizer adds about 9 per element.  Appending 32760 tokens of 12 + 2 * 12 heads takes
 // 150 us, 3 TB/s.
 #include <cuda_bf16.h>
@@ -155,12 +155,12 @@ __device__ __forceinline__ void load_cs(const RopeTable& r, const LanePairs& lp,
 }
 
 // Norm and rotation of one row; all lanes of the warp call it (the row sum goes over the LG lanes of the row).
-// gain = shared address of this lane's gains, four pieces of 16 bytes LG * 16 apart; 0 = no norm
+// norm: this side has one; gain = shared address of this lane's gains, four pieces of 16 bytes LG * 16 apart
 template <int LG, bool INTER>
-__device__ __forceinline__ void norm_rotate(const uint4& ua, const uint4& ub, uint32_t gain, const NormRopeParams& p, const CosSin& t,
-                                            Share& x) {
+__device__ __forceinline__ void norm_rotate(const uint4& ua, const uint4& ub, bool norm, uint32_t gain, const NormRopeParams& p,
+                                            const CosSin& t, Share& x) {
   unpack<INTER>(ua, ub, x);
-  if (__any_sync(0xffffffffu, gain != 0u)) {
+  if (norm) {
     float v;
     if (INTER)
       v = __fadd_rn(fold8(x.a[0], x.b[0], x.a[1], x.b[1], x.a[2], x.b[2], x.a[3], x.b[3]), fold8(x.a[4], x.b[4], x.a[5], x.b[5], x.a[6], x.b[6], x.a[7], x.b[7]));
@@ -169,15 +169,13 @@ __device__ __forceinline__ void norm_rotate(const uint4& ua, const uint4& ub, ui
 #pragma unroll
     for (int off = LG / 2; off; off >>= 1) v = __fadd_rn(v, __shfl_xor_sync(0xffffffffu, v, off));
     const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(v, p.inv_d), p.eps)));
-    if (gain) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 g = lds_v4(gain + i * (LG * 16));
-        x.a[2 * i] = __fmul_rn(__fmul_rn(x.a[2 * i], r), __uint_as_float(g.x));
-        x.a[2 * i + 1] = __fmul_rn(__fmul_rn(x.a[2 * i + 1], r), __uint_as_float(g.y));
-        x.b[2 * i] = __fmul_rn(__fmul_rn(x.b[2 * i], r), __uint_as_float(g.z));
-        x.b[2 * i + 1] = __fmul_rn(__fmul_rn(x.b[2 * i + 1], r), __uint_as_float(g.w));
-      }
+    for (int i = 0; i < 4; ++i) {
+      const uint4 g = lds_v4(gain + i * (LG * 16));
+      x.a[2 * i] = __fmul_rn(__fmul_rn(x.a[2 * i], r), __uint_as_float(g.x));
+      x.a[2 * i + 1] = __fmul_rn(__fmul_rn(x.a[2 * i + 1], r), __uint_as_float(g.y));
+      x.b[2 * i] = __fmul_rn(__fmul_rn(x.b[2 * i], r), __uint_as_float(g.z));
+      x.b[2 * i + 1] = __fmul_rn(__fmul_rn(x.b[2 * i + 1], r), __uint_as_float(g.w));
     }
   }
   if (p.rope.table) {
@@ -251,7 +249,7 @@ __device__ __forceinline__ void rows_of_warp(const NormRopeParams& p, uint32_t s
       const int32_t first = seg ? p.units[0] : 0, from = max(u0, first) - first, to = min(u1, first + p.units[seg]) - first;
       if (from >= to) continue;
       if (seg == 0 || !CACHE) {
-        const uint32_t gain = hd.gain ? gains + (seg * 4 * LG + j) * 16 : 0u;
+        const uint32_t gain = gains + (seg * 4 * LG + j) * 16;
         int32_t h = from * 2 * per + hs;
         const uint16_t* x = hd.x + token * hd.ld + h * p.D + 8 * j;
         uint16_t* o = hd.out + token * hd.out_ld + h * p.D + 8 * j;
@@ -271,7 +269,7 @@ __device__ __forceinline__ void rows_of_warp(const NormRopeParams& p, uint32_t s
           for (int k = 0; k < 2; ++k) {
             if ((2 * u + k) * per >= hd.n) break;      // the second pass may have no rows at all
             Share y;
-            norm_rotate<LG, INTER>(r.a[k], r.b[k], gain, p, cs, y);
+            norm_rotate<LG, INTER>(r.a[k], r.b[k], hd.gain != nullptr, gain, p, cs, y);
             pack<INTER>(y, pack_bf16, r.a[k], r.b[k]);
             if (v[k]) {
               *reinterpret_cast<uint4*>(o + k * per * p.D) = r.a[k];
@@ -280,7 +278,7 @@ __device__ __forceinline__ void rows_of_warp(const NormRopeParams& p, uint32_t s
           }
         }
       } else {
-        const uint32_t gain = p.k.gain ? gains + (4 * LG + j) * 16 : 0u;
+        const uint32_t gain = gains + (4 * LG + j) * 16;
         // run r of row R goes to 16-byte column (r & ~3) | ((r ^ r >> 2 ^ R) & 3) of it: no bank conflicts on either side
         auto at_run = [&](int row, int run) -> uint32_t {
           return stage + (uint32_t)row * (LG * 32) + (uint32_t)(((run & ~3) | ((run ^ (run >> 2) ^ row) & 3)) * 16);
@@ -312,7 +310,7 @@ __device__ __forceinline__ void rows_of_warp(const NormRopeParams& p, uint32_t s
           for (int k = 0; k < 2; ++k) {
             if (__any_sync(0xffffffffu, key[k])) {      // a pass of v rows alone needs neither norm nor rotation
               Share y;
-              norm_rotate<LG, INTER>(key[k] ? r.a[k] : zero, key[k] ? r.b[k] : zero, gain, p, cs, y);
+              norm_rotate<LG, INTER>(key[k] ? r.a[k] : zero, key[k] ? r.b[k] : zero, p.k.gain != nullptr, gain, p, cs, y);
               if (key[k]) pack<INTER>(y, upper_halves, r.a[k], r.b[k]);
             }
             if (on) {
