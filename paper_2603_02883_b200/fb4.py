@@ -726,6 +726,8 @@ class Fb4:
         c = self._cache(cache)
         if D != c.head_dim:
             raise ValueError("q must have the head dimension of the cache")
+        if max_q >> 31 or max_kv >> 31 or window >> 31:            # they are passed as 32 bits
+            raise ValueError("max_q, max_kv and window must be in [0, 2^31)")
         n = kv_len.numel()
         if page_table.dim() != 2 or page_table.shape[0] != n or kv_len.dim() != 1 or q_start.dim() != 1 or q_start.numel() != n + 1:
             raise ValueError("expected page_table [n_seqs][max_pages], kv_len [n_seqs] and q_start [n_seqs + 1]")

@@ -312,3 +312,13 @@ def test_refusals(q32):
         q32.cache_attention(q, cache, table, kv.long(), qs, mq, mkv)
     with pytest.raises(ValueError):
         q32.cache_attention(q[..., :32], cache, table, kv, qs, mq, mkv)
+
+
+def test_sizes_that_do_not_fit_32_bits_are_refused(q32):
+    q, cache, table, kv, qs, mq, mkv = setup(q32, [2], [100], 4, 2, 64, 16, seed=2)
+    for bad in ((2 ** 32 + mq, mkv, 0), (mq, 2 ** 32 + mkv, 0), (mq, mkv, 2 ** 32 + 1), (mq, mkv, 2 ** 63 - 1), (mq, mkv, -1)):
+        with pytest.raises(ValueError):
+            q32.cache_attention(q, cache, table, kv, qs, *bad[:2], window=bad[2])
+    want = q32.cache_attention(q, cache, table, kv, qs, mq, mkv)
+    got = q32.cache_attention(q, cache, table, kv, qs, mq, mkv, window=2 ** 31 - 1)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and q32.last_variant == "fast"
