@@ -460,8 +460,8 @@ typedef struct {
  * Appends T tokens to the cache: k goes through the norm and the rotation of fb4_qk_norm_rope and, like v, is quantized
  * from float32 registers as fb4_quantize_f32 quantizes a float32 tensor (no rounding to bfloat16 in between);
  * token t's blocks are written at slot[t].  q, if given, goes through the norm and the rotation in the same pass and
- * leaves as bfloat16.  Default configuration only (block 32, 8 groups, two-stage selection, full exponent range):
- * FB4_ERR_INVALID_ARG otherwise.
+ * leaves as bfloat16.  Default configuration only (block 32, 8 groups, two-stage selection, full exponent range), with stage-1
+ * groups of at most 8 dialects: FB4_ERR_INVALID_ARG otherwise.
  *   slot   : device int64 [T].  -1 = nothing is cached for this token (a row that pads a batch; its q row is still
  *            written).  Any other value outside [0, n_pages * page_tokens) is treated as -1 and raises bit 1 of the status
  *            word.  The slots of one call must differ from one another (precondition: with a slot given twice, the
@@ -494,7 +494,8 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
  *   max_q, max_kv : host bounds of the lengths; they fix the launch shape (and only that).  max_kv <= 2^30,
  *                n_seqs * max_q * q_heads < 2^31 (FB4_ERR_SHAPE)
  *   out        : device [total_q][q_heads][D] with token stride out_ld (elements), out_dtype 0 = float32, 1 = bfloat16,
- *                2 = IEEE half; 16-byte aligned, out_ld * element size a multiple of 16.  Rows of no sequence are left alone
+ *                2 = IEEE half; 16-byte aligned, out_ld * element size a multiple of 16; must not overlap q.  Rows of no
+ *                sequence are left alone
  *   lse        : device float32 [total_q][q_heads]: log of the sum of exp(scale * q . k) over the visible tokens; or NULL
  *   scale      : at most 2^60 in magnitude
  *   workspace  : device, 256-byte aligned, workspace_bytes >= fb4_cache_attention_workspace(...) of the same arguments

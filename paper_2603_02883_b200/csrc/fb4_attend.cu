@@ -5,9 +5,9 @@ namespace {
 
 using namespace fb4att;
 
-// One warp per query row and head; lane l holds channel 32 b + l of every block b.  Two passes over nothing: the running
-// maximum and sum of the softmax are updated key by key.  Latency-bound and only meant for head dimensions that the tensor-core
-// kernels do not have (and to check them against).
+// One warp per query row and head; lane l holds channel 32 b + l of every block b.  The running maximum and sum of the softmax
+// are updated key by key.  Latency-bound and only meant for head dimensions that the tensor-core kernels do not have (and to
+// check them against).
 template <int NB>
 __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_constant__ Fb4Attend a) {
   __shared__ uint8_t book[32][8];
@@ -69,7 +69,6 @@ __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_co
 
 cudaError_t fb4_launch_attend_generic(const fb4_ctx*, const Fb4Attend& a, cudaStream_t stream) {
   const int64_t grid = ((int64_t)a.max_q * a.q_heads + 3) / 4 * a.n_seqs;
-  if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   switch (a.cache.head_dim / 32) {
     case 1: fb4_attend_generic_kernel<1><<<(unsigned)grid, 128, 0, stream>>>(a); break;
     case 2: fb4_attend_generic_kernel<2><<<(unsigned)grid, 128, 0, stream>>>(a); break;

@@ -15,10 +15,12 @@
 // The decoder leaves channels in the order 0 2 1 3 4 6 5 7 of every eight; Q is staged in the same order (the order of the
 // contracted side is free) and the result is put back in order when it is stored.
 //
-// Bound: issue slots.  Per 128 tokens and 256 rows the tensor cores need 2048 cycles and the exponentials 1900 (16 per cycle and
-// SM); decode, softmax and waiting together issue 10700 instructions, two thirds of the slots of the 4000 cycles (2.2 us) that
-// it takes.  1560 queries of 12 heads over 32760 tokens take 376 us, 835 TFLOP/s, half of the measured bf16 product rate.
-// Without the decode the same loop takes 3200 cycles.
+// Bound: the chain scores -> softmax -> product of a query tile, which the other tile's fills only in part.  Per 128 tokens and
+// 256 rows (2.06 us, 4000 cycles) the tensor cores need 2048 cycles and the exponentials 1900 (16 per cycle and SM), each 45 % of
+// the time; all roles together issue 8200 instructions, 48 % of the slots.  1560 queries of 12 heads over 32760 tokens take
+// 376 us, 835 TFLOP/s, half of the measured bf16 product rate; without the decode the same loop takes 3200 cycles.
+// Two threads to a row (16 softmax warps, half a row's exponentials each) took 4.0 us for the same work, a polynomial in place of
+// the special function for a part of the columns 2.2 us (4 of 32) to 2.9 us (16 of 32).
 #include "fb4_attend.cuh"
 #include "fb4_staging.cuh"
 

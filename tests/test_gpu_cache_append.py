@@ -166,3 +166,40 @@ def test_without_q_heads_its_pointers_are_ignored(q32):
     fb4.fb4_cache_append(q32.ctx, q32._cache(b), slot, x, 256, x[:, 2:], 256, 20, g[1], 1e-6, q32._rope(rope, 20, 64), odd, 0, -1, odd, odd, -1)
     for f in ("k_codes", "k_meta", "v_codes", "v_meta"):
         assert torch.equal(getattr(a, f), getattr(b, f))
+
+
+def test_another_formatbook(q32):
+    """a formatbook that the packed tables hold is used; one with more than 8 candidates to a stage-1 group is refused"""
+    base = np.array([[0, 1, 2, 3, 5, 7, 9, 8 + d % 8] for d in range(32)], np.uint8)
+    base[:, 6] = np.minimum(base[:, 6], base[:, 7] - 1)
+    base[:, 5] = np.minimum(base[:, 5], base[:, 6] - 1)
+    mask = np.array([0xff << (8 * (k % 4)) for k in range(32)], np.uint32)
+    assert (np.diff(base.astype(int), axis=1) > 0).all()
+    f = fb4.Fb4(formatbook=base, stage1_mask=mask)
+    x, *_ = make(50, 0, 2, 128, (64,), False, seed=14)
+    cache = f.new_cache(4, 16, 2, 128)
+    f.cache_append(cache, torch.arange(50, device="cuda"), x[:, :2], x[:, 2:])
+    rows = as_f32(x[:, 2:].contiguous()).reshape(100, 128)
+    z = orc.quantize_f32(np.ascontiguousarray(rows), base, stage1=mask)
+    got = cache.v_codes.transpose(1, 2).reshape(64, 2, 64)[:50].reshape(100, 64).cpu().numpy()
+    assert np.array_equal(got, z.codes)
+    q = torch.randn(3, 4, 128, device="cuda").to(torch.bfloat16)
+    table = torch.arange(4, dtype=torch.int32, device="cuda")[None]
+    lens = torch.tensor([50], dtype=torch.int32, device="cuda"), torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    out, _ = f.cache_attention(q, cache, table, *lens, 3, 50, dtype=torch.float32)
+    kv = [t.double().transpose(1, 2).reshape(64, 2, 128)[:50].repeat_interleave(2, 1) for t in f.cache_values(cache)]
+    p = torch.einsum("ihd,jhd->hij", q.double(), kv[0]) * 128 ** -0.5
+    p = p.masked_fill(torch.arange(50, device="cuda") > 47 + torch.arange(3, device="cuda")[:, None], float("-inf")).softmax(-1)
+    want, size = torch.einsum("hij,jhd->ihd", p, kv[1]), torch.einsum("hij,jhd->ihd", p, kv[1].abs())
+    # probabilities rounded to bfloat16, 2^-8 of each term; float32 sums of 128 and of 50 terms move them by less than 2^-10 more
+    # what underflows: the second product is summed times 2^-64 in float32, whose smallest step is 2^-149, so each of its 50
+    # additions can lose 2^-85 of the result; a probability below 2^-126 is 0, and 50 of those times a value below 2^41 are less
+    # than 50 * 2^-85 again
+    assert kv[1].abs().max() < 2.0 ** 41
+    assert ((out.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -10) * size + 2 * 50 * 2.0 ** -85).all()
+    f.close()
+    wide = fb4.Fb4(stage1_mask=np.full(32, 0x1ff, np.uint32))
+    with pytest.raises(fb4.Fb4Error) as e:
+        wide.cache_append(wide.new_cache(4, 16, 2, 128), torch.arange(50, device="cuda"), x[:, :2], x[:, 2:])
+    assert e.value.code == fb4.ERR_INVALID_ARG
+    wide.close()
