@@ -5,22 +5,28 @@
 // r mod group) and one run of the cached tokens, which it walks in tiles of 128.  Its warps have fixed roles:
 //   load     copies codes and metadata of K and V tiles into a ring (bulk copies, page by page)
 //   decode   4 warps turn them into bf16 tiles in shared memory, 128-byte swizzled, [token][channel] for both K and V
-//   mma      one warp issues S_w = Q_w K^T (both operands in shared memory, accumulator in TMEM) and O_w += P_w V
-//            (P_w from TMEM, V read with the contracted side as the strided one)
-//   softmax  4 warps per query tile, one row per thread: scores from TMEM, running maximum and sum in registers, P back
-//            to TMEM over the scores it came from
-// The two query tiles alternate: while one is in the softmax, the tensor core works for the other, and one decoded tile
-// serves both.  The accumulators stay in TMEM; they are rescaled only when a row's maximum grows by more than 2^8.
+//   scores   one warp issues S_w = Q_w K^T (both operands in shared memory, accumulator in TMEM)
+//   product  one warp issues O_w += P_w V (P_w from TMEM, V read with the contracted side as the strided one)
+//   softmax  4 warps per query tile, one row per thread: a row's 128 scores go from TMEM into registers at once, which
+//            frees their columns; running maximum and sum in registers, P back to columns of its own
+// The two query tiles take turns with one buffer of scores: while one is in its exponentials, the other's scores are
+// computed, and one decoded tile serves both.  TMEM: S at column 0, P_w at 128 + 64 w, O_w at 256 + D w.  Scores and products wait
+// for different things, so they are issued by different warps: one warp for both, in the best order, waited with the tensor core
+// idle (359 against 342 us for the frame below; P over the scores it came from, so that a tile's next scores wait for its
+// product: 376 us).  The accumulators are rescaled only when a row's maximum grows by more than 2^8.
 //
 // The decoder leaves channels in the order 0 2 1 3 4 6 5 7 of every eight; Q is staged in the same order (the order of the
 // contracted side is free) and the result is put back in order when it is stored.
 //
-// Bound: the chain scores -> softmax -> product of a query tile, which the other tile's fills only in part.  Per 128 tokens and
-// 256 rows (2.06 us, 4000 cycles) the tensor cores need 2048 cycles and the exponentials 1900 (16 per cycle and SM), each 45 % of
-// the time; all roles together issue 8200 instructions, 48 % of the slots.  1560 queries of 12 heads over 32760 tokens take
-// 376 us, 835 TFLOP/s, half of the measured bf16 product rate; without the decode the same loop takes 3200 cycles.
-// Two threads to a row (16 softmax warps, half a row's exponentials each) took 4.0 us for the same work, a polynomial in place of
-// the special function for a part of the columns 2.2 us (4 of 32) to 2.9 us (16 of 32).
+// Bound: the shared memory that decode and tensor core have in common.  Per 128 tokens and 256 rows (2.0 us, 3800 cycles) the
+// tensor core reads 192 KB of operands from it (1536 cycles; 2048 of arithmetic), decode writes 64 KB and reads 18, P goes to
+// TMEM past it: three quarters of its cycles.  The exponentials take 2048 (16 per cycle and SM), all roles issue half of the
+// slots.  Leaving out the decode's arithmetic (and 3/4 of its stores) gives 1.45 us, leaving out the softmax's 1.9, both 1.5.
+// 1560 queries of 12 heads over 32760 tokens take 342 us, 917 TFLOP/s, 55 % of the measured bf16 product rate.
+// Without gain: 8 decode warps (four for K, four for V: 339 to 349 / 136 us for the frame and four causal prompts of 1024,
+// against 342 / 133), decode with the next tile's codes already in registers (375 / 141), a copy of the dialects for every lane of a
+// half-warp (no bank conflicts: 349 / 133), two threads to a row (16 softmax warps: 507 / 171), a polynomial in place of the
+// special function for a part of the columns (2.2 to 2.9 us per tile).
 #include "fb4_attend.cuh"
 #include "fb4_staging.cuh"
 
@@ -36,9 +42,9 @@ using fb4stage::mbar_try_wait;
 
 constexpr int kKeys = 128;             // tokens of a tile
 constexpr int kSoftmaxWarps = 8, kDecodeWarps = 4;
-constexpr int kThreads = 512;          // two warpgroups of softmax, one of decode, one whose first two warps are mma and load
-// Registers per thread of the roles.  The block is launched with 128 for each of its 512 threads; what decode, mma and load
-// give back is what the softmax warps, which keep a row's 128 scores in registers, take: 2 * 200 + 72 + 40 = 4 * 128.
+constexpr int kThreads = 512;          // two warpgroups of softmax, one of decode, one whose first three warps are scores, load and product
+// Registers per thread of the roles.  The block is launched with 128 for each of its 512 threads; what decode and the last
+// warpgroup give back is what the softmax warps, which keep a row's 128 scores in registers, take: 2 * 200 + 72 + 40 = 4 * 128.
 constexpr int kLaunchRegs = 128, kSoftmaxRegs = 200, kDecodeRegs = 72, kOtherRegs = 40;
 static_assert(2 * kSoftmaxRegs + kDecodeRegs + kOtherRegs <= 4 * kLaunchRegs, "register shares of the warpgroups");
 constexpr int kRing = 3;               // ring stages: a K or a V tile's codes and metadata each
@@ -54,7 +60,7 @@ struct Many {
 struct Bars {
   uint64_t ring_full[kRing], ring_empty[kRing];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t q_full, s_full[2], p_half[2], p_full[2], o_full[2], drained;
+  uint64_t q_full, s_full[2], s_free, p_half[2], p_full[2], o_done[2], drained;
 };
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
@@ -117,17 +123,15 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float* v) {
         "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
       : "r"(addr));
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(addr));
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const float (&v)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
-      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]),
-      "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]),
-      "f"(v[30]), "f"(v[31]) : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -235,10 +239,11 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       mbar_init(smem_u32(&bars.s_full[i]), 1);
       mbar_init(smem_u32(&bars.p_half[i]), 4);
       mbar_init(smem_u32(&bars.p_full[i]), 4);
-      mbar_init(smem_u32(&bars.o_full[i]), 1);
+      mbar_init(smem_u32(&bars.o_done[i]), 1);
     }
     mbar_init(smem_u32(&bars.q_full), 4 * n_w);
-    mbar_init(smem_u32(&bars.drained), 1);
+    mbar_init(smem_u32(&bars.s_free), 4);
+    mbar_init(smem_u32(&bars.drained), 2);
     dead_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -251,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
   __syncthreads();
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
-  const uint32_t s_col = tmem, o_col = tmem + 256;                    // S_w at columns 128 w (P_w over its first 64), O_w at 256 + D w
+  const uint32_t s_col = tmem, p_col = tmem + 128, o_col = tmem + 256;      // S at column 0, P_w at 128 + 64 w, O_w at 256 + D w
 
   if (warp < kSoftmaxWarps) {
     // =========================================================== softmax
@@ -259,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
     const int w = warp >> 2;
     if (w < n_w) {
       const uint32_t lanes = (uint32_t)(warp & 3) << 21;              // this warp's TMEM lanes: 32 (warp mod 4) << 16
-      const uint32_t s_at = s_col + 128 * w + lanes, o_at = o_col + D * w + lanes;
+      const uint32_t s_at = s_col + lanes, p_at = p_col + 64 * w + lanes, o_at = o_col + D * w + lanes;
       // This warp's 32 rows of Q, in the decoder's channel order, while the first tile is loaded and decoded; a negative scale is
       // taken into Q's signs (the softmax wants a positive one)
       {
@@ -306,6 +311,9 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, x + 32 * c);
         tmem_wait_ld();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.s_free));            // the other tile's scores may come
         if (!whole) {
           const int32_t from = v.lo - j0, to = v.hi - j0;
 #pragma unroll
@@ -318,21 +326,26 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
 #pragma unroll
           for (int k = 0; k < 4; ++k) u[k] = i + 4 < kKeys ? fmaxf(fmaxf(u[k], x[i + k]), x[i + 4 + k]) : fmaxf(u[k], x[i + k]);
         const float top = fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3])) * scale;
+        if (t > 0) {                                                  // the product of tile t - 1 has read its P and left its sums
+          ok = wait(smem_u32(&bars.o_done[w]), (t - 1) & 1, dead);
+          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+          fence_after();
+        }
         if (__any_sync(0xffffffffu, top > m + 8.0f)) {
           const float next = fmaxf(m, top);
           const float f = next == -INFINITY ? 1.0f : exp2_approx(m - next);
           m = next;
           l.x *= f;
           l.y *= f;
-          if (t > 0) {                                                // the product of tile t - 1 was complete before these scores
+          if (t > 0) {
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-              float y[32];
-              tmem_ld32(o_at + 32 * c, y);
+            for (int c = 0; c < D / 16; ++c) {                        // 16 at a time: all of the row's scores are held meanwhile
+              uint32_t y[16];
+              tmem_ld16(o_at + 16 * c, y);
               tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) y[i] *= f;
-              tmem_st32(o_at + 32 * c, y);
+              for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
+              tmem_st16(o_at + 16 * c, y);
             }
             tmem_wait_st();
           }
@@ -348,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
             l = add2(l, q);
             p[i >> 1] = pack(q.x, q.y);
           }
-          tmem_st16(s_at + 16 * c, p);
+          tmem_st16(p_at + 16 * c, p);
           if (c == 1) {                                               // the product may start on the first 64 tokens
             tmem_wait_st();
             fence_before();
@@ -364,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       // ---- result
       const float sum = l.x + l.y;
       if (ok && n_tiles > 0) {
-        ok = wait(smem_u32(&bars.o_full[w]), 0, dead);
+        ok = wait(smem_u32(&bars.o_done[w]), (n_tiles - 1) & 1, dead);
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
       }
@@ -448,98 +461,101 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       const int32_t t = part >> 1;
       const bool is_v = part & 1;
       const int st = part % kRing, buf = t & 1;
-      ok = wait(smem_u32(&bars.ring_full[st]), (part / kRing) & 1, dead);
-      if (ok && t >= 2) ok = wait(smem_u32(is_v ? &bars.v_empty[buf] : &bars.k_empty[buf]), ((t >> 1) - 1) & 1, dead);
-      ok = __all_sync(0xffffffffu, ok);
+      ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.ring_full[st]), (part / kRing) & 1, dead));
       if (!ok) break;
       const uint32_t codes = ring_at + st * L::kStage, meta = codes + L::kCodes;
       const uint32_t dst = (is_v ? v_at : k_at) + buf * L::kTileBytes;
       const uint32_t here = *(volatile uint32_t*)&have[t % kHave];
       const int32_t j0 = base + (t0 + t) * kKeys;
+      // 32 rows and one block of each per task; the block varies with the row so that neither side has bank conflicts.  All loads
+      // come first: the ring's stage is free early, and the tasks' latencies overlap.
+      constexpr int kTasks = 4 * NB / kDecodeWarps;
+      uint32_t cw[kTasks][4];
+      uint16_t mt[kTasks];
+      auto row_of = [&](int k) -> int { return ((dw + k * kDecodeWarps) & 3) * 32 + lane; };
+      auto block_of = [&](int k) -> int { return NB == 4 ? (((dw + k * kDecodeWarps) >> 2) + (lane >> 1)) & 3 : (dw + k * kDecodeWarps) >> 2; };
 #pragma unroll
-      for (int k = 0; k < 4 * NB / kDecodeWarps; ++k) {
-        // 32 rows and one block of each per step; the block varies with the row so that neither side has bank conflicts
-        const int task = dw + k * kDecodeWarps, row = (task & 3) * 32 + lane;
-        const int blk = NB == 4 ? ((task >> 2) + (lane >> 1)) & 3 : task >> 2;
-        uint32_t cw[4];
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cw[0]), "=r"(cw[1]), "=r"(cw[2]), "=r"(cw[3]) : "r"(codes + row * (D / 2) + blk * 16));
-        uint16_t mt;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(mt) : "r"(meta + (row * NB + blk) * 2));
+      for (int k = 0; k < kTasks; ++k) {
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cw[k][0]), "=r"(cw[k][1]), "=r"(cw[k][2]), "=r"(cw[k][3]) : "r"(codes + row_of(k) * (D / 2) + block_of(k) * 16));
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(mt[k]) : "r"(meta + (row_of(k) * NB + block_of(k)) * 2));
+      }
+      BlockScale sc[kTasks];
+#pragma unroll
+      for (int k = 0; k < kTasks; ++k) {
         // values behind the last token or in a page that is not there must be finite: they meet p = 0
-        const bool use = !is_v || (j0 + row < sq.kv && ((here >> (row >> 4)) & 1u));
-        const BlockScale sc = block_scale(use ? mt : 0u, book_at, use);
+        const bool use = !is_v || (j0 + row_of(k) < sq.kv && ((here >> (row_of(k) >> 4)) & 1u));
+        sc[k] = block_scale(use ? mt[k] : 0u, book_at, use);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.ring_empty[st]));
+      if (t >= 2) ok = __all_sync(0xffffffffu, wait(smem_u32(is_v ? &bars.v_empty[buf] : &bars.k_empty[buf]), ((t >> 1) - 1) & 1, dead));
+      if (!ok) break;
+#pragma unroll
+      for (int k = 0; k < kTasks; ++k)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           uint32_t o[4];
-          decode_word(cw[q], sc, o);
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + swizzled(row, 4 * blk + q)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+          decode_word(cw[k][q], sc[k], o);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + swizzled(row_of(k), 4 * block_of(k) + q)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
         }
-      }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(smem_u32(is_v ? &bars.v_full[buf] : &bars.k_full[buf]));
-        mbar_arrive(smem_u32(&bars.ring_empty[st]));
-      }
+      if (lane == 0) mbar_arrive(smem_u32(is_v ? &bars.v_full[buf] : &bars.k_full[buf]));
     }
   } else {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-  if (warp == kSoftmaxWarps + kDecodeWarps) {
-    // =========================================================== mma
+  if (warp == kSoftmaxWarps + kDecodeWarps || warp == kSoftmaxWarps + kDecodeWarps + 2) {
+    // =========================================================== scores, product: every lane waits, one issues
     if (n_tiles > 0) {
-      constexpr uint32_t id_s = instr_desc(kKeys, false), id_o = instr_desc(D, true);
-      const uint32_t q_low = desc_low(q_at, 16), k_low = desc_low(k_at, 16), v_low = desc_low(v_at, kKeys * 128);
       constexpr uint32_t kTile16 = L::kTileBytes >> 4;
-      // every lane waits, one issues
-      auto scores = [&](int w, int32_t t) {
-        const uint32_t kb = k_low + (t & 1) * kTile16, qb = q_low + w * kTile16;
+      bool ok = true;
+      if (warp == kSoftmaxWarps + kDecodeWarps) {
+        constexpr uint32_t id_s = instr_desc(kKeys, false);
+        const uint32_t q_low = desc_low(q_at, 16), k_low = desc_low(k_at, 16);
+        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.q_full), 0, dead));
+        int32_t used = 0;                                              // score tiles so far: they share a buffer
+        for (int32_t t = 0; t < n_tiles && ok; ++t) {
+          ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.k_full[t & 1]), (t >> 1) & 1, dead));
+          for (int w = 0; w < n_w; ++w, ++used) {
+            if (used > 0 && ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.s_free), (used - 1) & 1, dead));
+            if (!ok) break;
+            fence_after();
+            if (elected()) {
+              const uint32_t kb = k_low + (t & 1) * kTile16, qb = q_low + w * kTile16;
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = ((k >> 2) * (kKeys * 128) + (k & 3) * 32) >> 4;
-          mma_ss(s_col + 128 * w, qb + off, kb + off, id_s, k > 0);
-        }
-        commit(smem_u32(&bars.s_full[w]));
-      };
-      auto product = [&](int w, int32_t t, int part) {                 // one half of the tile's tokens
-        const uint32_t vb = v_low + (t & 1) * kTile16;
-#pragma unroll
-        for (int k = part * (kKeys / 32); k < (part + 1) * (kKeys / 32); ++k) mma_ts(o_col + D * w, s_col + 128 * w + 8 * k, vb + k * (2048 >> 4), id_o, k > 0 || t > 0);
-      };
-      bool ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.q_full), 0, dead) && wait(smem_u32(&bars.k_full[0]), 0, dead));
-      if (ok) {
-        fence_after();
-        if (elected()) {
-          scores(0, 0);
-          if (n_w > 1) scores(1, 0);
-          commit(smem_u32(&bars.k_empty[0]));
-        }
-        __syncwarp();
-      }
-      for (int32_t t = 0; t < n_tiles && ok; ++t) {
-        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.v_full[t & 1]), (t >> 1) & 1, dead));
-        const bool more = t + 1 < n_tiles;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          if (w >= n_w || !ok) break;
-          ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.p_half[w]), t & 1, dead));
-          if (!ok) break;
-          fence_after();
-          if (elected()) product(w, t, 0);
-          __syncwarp();
-          ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.p_full[w]), t & 1, dead));
-          if (w == 0 && more && ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.k_full[(t + 1) & 1]), ((t + 1) >> 1) & 1, dead));
-          if (!ok) break;
-          fence_after();
-          if (elected()) {
-            product(w, t, 1);
-            if (!more) commit(smem_u32(&bars.o_full[w]));
-            if (w == n_w - 1) commit(smem_u32(&bars.v_empty[t & 1]));
-            if (more) {
-              scores(w, t + 1);
-              if (w == n_w - 1) commit(smem_u32(&bars.k_empty[(t + 1) & 1]));
+              for (int k = 0; k < D / 16; ++k) {
+                const uint32_t off = ((k >> 2) * (kKeys * 128) + (k & 3) * 32) >> 4;
+                mma_ss(s_col, qb + off, kb + off, id_s, k > 0);
+              }
+              commit(smem_u32(&bars.s_full[w]));
+              if (w == n_w - 1) commit(smem_u32(&bars.k_empty[t & 1]));
             }
+            __syncwarp();
           }
-          __syncwarp();
+        }
+      } else {
+        constexpr uint32_t id_o = instr_desc(D, true);
+        const uint32_t v_low = desc_low(v_at, kKeys * 128);
+        for (int32_t t = 0; t < n_tiles && ok; ++t) {
+          ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.v_full[t & 1]), (t >> 1) & 1, dead));
+          const uint32_t vb = v_low + (t & 1) * kTile16;
+          for (int w = 0; w < n_w && ok; ++w)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {                     // one half of the tile's tokens each
+              ok = __all_sync(0xffffffffu, wait(smem_u32(part ? &bars.p_full[w] : &bars.p_half[w]), t & 1, dead));
+              if (!ok) break;
+              fence_after();
+              if (elected()) {
+#pragma unroll
+                for (int k = part * (kKeys / 32); k < (part + 1) * (kKeys / 32); ++k)
+                  mma_ts(o_col + D * w, p_col + 64 * w + 8 * k, vb + k * (2048 >> 4), id_o, k > 0 || t > 0);
+                if (part) {
+                  commit(smem_u32(&bars.o_done[w]));
+                  if (w == n_w - 1) commit(smem_u32(&bars.v_empty[t & 1]));
+                }
+              }
+              __syncwarp();
+            }
         }
       }
       // nothing of this CTA may be on the tensor core when its TMEM is given back
