@@ -3,7 +3,8 @@
 // Work: a CTA of 4 warps takes one sequence, one cache head, up to 8 * NT query rows (query-major: row r = query r / group,
 // head r mod group) and one run of the cached tokens (a "split"); its warps take that run's tiles of 32 tokens in turn.  Each warp
 // has its own ring of asynchronously copied tiles (codes and metadata of K and V), its own running maximum and sum, and its
-// own accumulators; the warps are joined in shared memory at the end, the splits in a second small kernel.
+// own accumulators; the warps are joined in shared memory at the end, up to 8 splits in that of their cluster, more in a second
+// small kernel.
 //
 // The tokens are the long side, so they are the M side of the products: S^T = K Q^T (m = 16 tokens, n = 8 queries),
 // O^T = V^T P^T (m = 16 channels, n = 8 queries), mma.sync m16n8k16: with one query per head 7/8 of the N side is idle, but a
