@@ -267,8 +267,9 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       const uint32_t lanes = (uint32_t)(warp & 3) << 21;              // this warp's TMEM lanes: 32 (warp mod 4) << 16
       const uint32_t s_at = s_col + lanes, p_at = p_col + 64 * w + lanes, o_at = o_col + D * w + lanes;
       // This warp's 32 rows of Q, in the decoder's channel order, while the first tile is loaded and decoded; a negative scale is
-      // taken into Q's signs (the softmax wants a positive one)
-      {
+      // taken into Q's signs (the softmax wants a positive one).  Without tiles nothing would order these writes and the other
+      // warps' use of the same memory for their results.
+      if (n_tiles > 0) {
         const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
         constexpr int kRuns = D / 8;
         uint4 u[kRuns];

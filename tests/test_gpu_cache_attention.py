@@ -322,3 +322,17 @@ def test_sizes_that_do_not_fit_32_bits_are_refused(q32):
     want = q32.cache_attention(q, cache, table, kv, qs, mq, mkv)
     got = q32.cache_attention(q, cache, table, kv, qs, mq, mkv, window=2 ** 31 - 1)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and q32.last_variant == "fast"
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 128])
+def test_row_tiles_that_see_nothing(q32, D, dtype):
+    """whole tiles of query rows stand before the cache begins: they have no tile of tokens to wait for, and still get zeros"""
+    q, cache, table, kv, qs, mq, mkv = setup(q32, [18, 33, 7] * 20, [2, 1, 60] * 20, 128, 8, D, 128, seed=30)
+    want = ref.attend64(q[:58], cache, table[:3], kv[:3], qs[:4], D ** -0.5, True, 0, dtype)
+    for _ in range(5):
+        out, lse = q32.cache_attention(q, cache, table, kv, qs, mq, mkv, dtype=dtype)
+        agree((out[:58], lse[:58]), want, dtype)
+        o, l = out.view(20, 58, 128, D), lse.view(20, 58, 128)
+        empty = torch.cat([torch.arange(16), 18 + torch.arange(32)]).cuda()
+        assert not o[:, empty].any() and torch.isinf(l[:, empty]).all()
