@@ -104,10 +104,12 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
     if (from + lane < n_mine) {
       const int32_t j = base + (my0 + (from + lane) * kWarpsFew) * kTile;
       const int32_t* pt = a.page_table + (int64_t)b * a.max_pages;
-      if (j < sq.kv) page_lo = __ldg(pt + (j >> a.page_shift));
-      if (j + 16 < sq.kv) page_hi = a.page_shift > 4 ? page_lo : __ldg(pt + ((j + 16) >> a.page_shift));
-      if (j < sq.kv && (uint32_t)page_lo >= (uint64_t)a.cache.n_pages) { bad = true; page_lo = -1; }
-      if (j + 16 < sq.kv && (uint32_t)page_hi >= (uint64_t)a.cache.n_pages) { bad = true; page_hi = -1; }
+      // only halves that some row sees are read: pages in front of a window may be gone
+      const bool lo_seen = j < last.hi && j + 16 > first.lo, hi_seen = j + 16 < last.hi && j + 32 > first.lo;
+      if (lo_seen) page_lo = __ldg(pt + (j >> a.page_shift));
+      if (hi_seen) page_hi = __ldg(pt + ((j + 16) >> a.page_shift));
+      if (lo_seen && (uint32_t)page_lo >= (uint64_t)a.cache.n_pages) { bad = true; page_lo = -1; }
+      if (hi_seen && (uint32_t)page_hi >= (uint64_t)a.cache.n_pages) { bad = true; page_hi = -1; }
     }
   };
   // Requests tile n of this warp into ring stage `st`.  Codes: lane l copies bytes 16 l .. 16 l + 15 of every 512; metadata:

@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
     for (int32_t t = 0; t < n_tiles && ok; ++t) {
       const int32_t j0 = base + (t0 + t) * kKeys, j = j0 + lane * piece_tokens;
       int32_t page = -1;
-      if (lane < pieces && j < sq.kv) {
+      if (lane < pieces && j < last.hi && j + piece_tokens > first.lo) {      // pages in front of a window may be gone
         page = __ldg(a.page_table + (int64_t)b * a.max_pages + (j >> a.page_shift));
         if ((uint32_t)page >= (uint64_t)a.cache.n_pages) { bad = true; page = -1; }
       }

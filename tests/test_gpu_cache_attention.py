@@ -336,3 +336,18 @@ def test_row_tiles_that_see_nothing(q32, D, dtype):
         o, l = out.view(20, 58, 128, D), lse.view(20, 58, 128)
         empty = torch.cat([torch.arange(16), 18 + torch.arange(32)]).cuda()
         assert not o[:, empty].any() and torch.isinf(l[:, empty]).all()
+
+
+@pytest.mark.parametrize("case", [([1, 3], 4, 16), ([70, 5], 4, 32), ([300, 150], 2, 64)], ids=["few", "many", "several tiles"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_pages_in_front_of_the_window_may_be_gone(case, D):
+    """a page that no query sees is neither read nor reported, also where tiles of tokens begin in front of the window"""
+    n_q, group, page = case
+    f = fb4.Fb4()
+    q, cache, table, kv, qs, mq, mkv = setup(f, n_q, [1000, 777], 2 * group, 2, D, page, seed=31)
+    want = f.cache_attention(q, cache, table, kv, qs, mq, mkv, window=100)
+    for b, (n, k) in enumerate(zip([1000, 777], n_q)):
+        table[b, :(n - k - 100 + 1) // page] = -1
+    got = f.cache_attention(q, cache, table, kv, qs, mq, mkv, window=100)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and f.device_status == 0
+    f.close()
