@@ -441,7 +441,8 @@ int fb4_qk_norm_rope(fb4_ctx* ctx, const void* q_bf16, int32_t q_heads, int64_t 
  * page_tokens tokens of every head:
  *     codes : uint8  [n_pages][n_heads][page_tokens][D/2],   meta : uint16 [n_pages][n_heads][page_tokens][D/32]
  * so the rows of a cache read in order are a quantized tensor of n_pages * n_heads * page_tokens tokens and D channels,
- * which fb4_dequantize and fb4_to_mxfp8 take as it is.  Slot s = page * page_tokens + place in the page.
+ * which fb4_dequantize and fb4_to_mxfp8 take as it is, in a context of block size 32 (another one would look for metadata of its
+ * own block size, past the end of these arrays).  Slot s = page * page_tokens + place in the page.
  *   n_pages     : >= 1;  page_tokens: a power of two, 16 to 4096;  n_heads: 1 to 1024;
  *   head_dim    : D, a multiple of 32, at most 256.  All four arrays 16-byte aligned.
  */

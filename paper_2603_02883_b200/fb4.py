@@ -745,7 +745,9 @@ class Fb4:
         return out, lse
 
     def cache_values(self, cache: Cache, dtype=torch.float32):
-        """(k, v) [n_pages][n_heads][page_tokens][D]: all that a cache holds, decoded"""
+        """(k, v) [n_pages][n_heads][page_tokens][D]: all that a cache holds, decoded.  Needs block size 32, like the cache"""
+        if self.block_size != 32:                # the decoder would look for metadata of its own block size, past the cache's
+            raise Fb4Error(ERR_INVALID_ARG, "cache_values")
         c = self._cache(cache)
         shape = (c.n_pages, c.n_heads, c.page_tokens, c.head_dim)
         rows = c.n_pages * c.n_heads * c.page_tokens
