@@ -436,6 +436,13 @@ class Cache:
 _OUT_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
+def _out_dtype(dtype) -> int:
+    code = _OUT_DTYPE.get(dtype)
+    if code is None:
+        raise ValueError("the output type must be torch.float32, torch.bfloat16 or torch.float16")
+    return code
+
+
 class Fb4:
     """Owns one context; allocates outputs with torch and calls the entry points above."""
 
@@ -728,6 +735,7 @@ class Fb4:
             raise ValueError("q must have the head dimension of the cache")
         if max_q >> 31 or max_kv >> 31 or window >> 31:            # they are passed as 32 bits
             raise ValueError("max_q, max_kv and window must be in [0, 2^31)")
+        code = _out_dtype(dtype)
         n = kv_len.numel()
         if page_table.dim() != 2 or page_table.shape[0] != n or kv_len.dim() != 1 or q_start.dim() != 1 or q_start.numel() != n + 1:
             raise ValueError("expected page_table [n_seqs][max_pages], kv_len [n_seqs] and q_start [n_seqs + 1]")
@@ -741,19 +749,20 @@ class Fb4:
         ws = q.new_empty(need // 2) if need > 0 else None
         self._call("fb4_cache_attention", q.data_ptr(), q_ld, Hq, total, c, page_table.data_ptr(), page_table.shape[1], kv_len.data_ptr(),
                    q_start.data_ptr(), n, max_q, max_kv, D ** -0.5 if scale is None else scale, 1 if causal else 0, window,
-                   out.data_ptr(), Hq * D, _OUT_DTYPE[dtype], lse.data_ptr(), None if ws is None else ws.data_ptr(), need)
+                   out.data_ptr(), Hq * D, code, lse.data_ptr(), None if ws is None else ws.data_ptr(), need)
         return out, lse
 
     def cache_values(self, cache: Cache, dtype=torch.float32):
         """(k, v) [n_pages][n_heads][page_tokens][D]: all that a cache holds, decoded.  Needs block size 32, like the cache"""
         if self.block_size != 32:                # the decoder would look for metadata of its own block size, past the cache's
             raise Fb4Error(ERR_INVALID_ARG, "cache_values")
+        code = _out_dtype(dtype)
         c = self._cache(cache)
         shape = (c.n_pages, c.n_heads, c.page_tokens, c.head_dim)
         rows = c.n_pages * c.n_heads * c.page_tokens
         k, v = cache.k_codes.new_empty(*shape, dtype=dtype), cache.k_codes.new_empty(*shape, dtype=dtype)
         for codes, meta, x in ((c.k_codes, c.k_meta, k), (c.v_codes, c.v_meta, v)):
-            self._call("fb4_dequantize", codes, meta, rows, c.head_dim, None, 0, None, None, x.data_ptr(), _OUT_DTYPE[dtype])
+            self._call("fb4_dequantize", codes, meta, rows, c.head_dim, None, 0, None, None, x.data_ptr(), code)
         return k, v
 
     def set_kernel_variant(self, variant: int) -> None:

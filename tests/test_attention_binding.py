@@ -31,3 +31,16 @@ def test_cache_values_needs_block_size_32(monkeypatch):
     g = context(monkeypatch)
     k, v = g.cache_values(cpu_cache(), torch.bfloat16)
     assert k.shape == v.shape == (3, 2, 16, 64) and [c[0] for c in g.calls] == ["fb4_dequantize"] * 2
+
+
+def test_an_output_type_that_is_none_of_the_three_is_refused_first(monkeypatch):
+    f = context(monkeypatch)
+    made = []
+    monkeypatch.setattr(torch.Tensor, "new_empty", lambda self, *a, **k: made.append(a))
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32)  # noqa: E731
+    for bad in (torch.float64, torch.int8, torch.float8_e4m3fn, None, "bf16"):
+        with pytest.raises(ValueError):
+            f.cache_values(cpu_cache(), bad)
+        with pytest.raises(ValueError):
+            f.cache_attention(torch.zeros(1, 4, 64, dtype=torch.bfloat16), cpu_cache(), i32(0)[None], i32(1), i32(0, 1), 1, 1, dtype=bad)
+    assert not f.calls and not made
