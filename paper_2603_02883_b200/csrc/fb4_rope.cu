@@ -5,11 +5,10 @@
 // pairing ((i, i + D/2): the two runs; (2i, 2i + 1): inside a run), and the cosines and sines of a lane's 8 pairs stay in
 // 16 registers while it walks over the heads of a token: the table is read once per token and lane instead of once per head.
 //
-// Every operation is rounded once and stands in a fixed order (include/fb4.h states it), so the result is the same for
-// every grid; the square of a bf16 is exact in float32, which lets the first level of sums be fused multiply-adds.
+// Every operation is rounded once and stands in a fixed order (include/fb4.h states it), so the result is the same for every grid.
 //
 // Both kernels stream, and the instructions are what has to be kept under the bytes: a row of norm and rotation costs its
-// lanes 282 instructions (32760 tokens of 24 heads of 128: 82 us, 4.9 TB/s, 75 % of the copy bandwidth; a plain copy of the same
+// lanes 290 instructions (32760 tokens of 24 heads of 128: 84 us, 4.8 TB/s, 74 % of the copy bandwidth; a plain copy of the same
 // rows by the same loop takes 70 us), the quantizer adds about 9 per element.  Appending 32760 tokens of 12 + 2 * 12 heads takes
 // 150 us, 3 TB/s.
 #include <cuda_bf16.h>
@@ -96,10 +95,11 @@ __device__ __forceinline__ void pack(const Share& x, Join join, uint4& ua, uint4
   }
 }
 
-// (v0 + v4) + (v2 + v6) + ((v1 + v5) + (v3 + v7)) of the squares: those of a bf16 are exact, so a sum of two is one fused operation
+// (v0 + v4) + (v2 + v6) + ((v1 + v5) + (v3 + v7)) of the squares.  Not fused: the square of a bf16 has 16 bits and is exact, but only
+// down to 2^-149; below that the stated order rounds it before it is added.
 __device__ __forceinline__ float fold8(float v0, float v1, float v2, float v3, float v4, float v5, float v6, float v7) {
-  const float a = __fmaf_rn(v4, v4, __fmul_rn(v0, v0)), b = __fmaf_rn(v5, v5, __fmul_rn(v1, v1));
-  const float c = __fmaf_rn(v6, v6, __fmul_rn(v2, v2)), d = __fmaf_rn(v7, v7, __fmul_rn(v3, v3));
+  const float a = __fadd_rn(__fmul_rn(v0, v0), __fmul_rn(v4, v4)), b = __fadd_rn(__fmul_rn(v1, v1), __fmul_rn(v5, v5));
+  const float c = __fadd_rn(__fmul_rn(v2, v2), __fmul_rn(v6, v6)), d = __fadd_rn(__fmul_rn(v3, v3), __fmul_rn(v7, v7));
   return __fadd_rn(__fadd_rn(a, c), __fadd_rn(b, d));
 }
 
