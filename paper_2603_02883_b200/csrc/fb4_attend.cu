@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_co
     for (int k = 0; k < NB; ++k) s = fmaf(q[k], value(a.cache.k_codes, a.cache.k_meta, at, k), s);
 #pragma unroll
     for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    s *= a.scale_log2;
+    s = __fmul_rn(s, a.scale_log2);            // rounded as the maximum is, not fused with the subtraction below
     const float mn = fmaxf(m, s), f = exp2f(m - mn), e = exp2f(s - mn);
     l = l * f + e;
 #pragma unroll

@@ -105,6 +105,12 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// The running maximum is a rounded product, score * scale; a probability takes the exact one, in one operation with the
+// subtraction of the maximum.  The two differ by half a step of the maximum, which cancels between numerator and denominator as long
+// as it is small: up to 2^24 it is a factor of two at most.  Beyond, the scores are multiplied first, so that the largest is the
+// maximum itself (with the exact product a maximum of 2^31 gives 2^128 or 2^-128 for the very key that set it).
+__device__ __forceinline__ bool beyond_fused(float m) { return fabsf(m) > 0x1p24f && m > -INFINITY; }
+
 // ---- partial results of a split call: per row (b * max_q + i) * q_heads + h and split, D sums of the second product
 // (times 2^-64) and (running maximum, sum) of the softmax; the maximum in units of log2
 __device__ __forceinline__ int64_t partial_row(const Fb4Attend& a, int32_t b, int32_t i, int32_t h) {

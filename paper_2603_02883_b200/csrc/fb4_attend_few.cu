@@ -191,6 +191,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
     l[nt][0] = l[nt][1] = 0.0f;
   }
 
+  bool huge = false;       // some row's maximum is beyond_fused
   int st = 0, ahead = ST - 1;
   for (int32_t n = 0; n < n_mine; ++n) {
     request(n + ST - 1, ahead);
@@ -258,9 +259,10 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         top[nt][k] = fmaxf(fmaxf(s[0][nt][k], s[0][nt][k + 2]), fmaxf(s[1][nt][k], s[1][nt][k + 2]));
-        grow |= fmaf(top[nt][k], scale, -8.0f) > m[nt][k];
+        grow |= top[nt][k] * scale > m[nt][k] + 8.0f;
       }
     if (__any_sync(0xffffffffu, grow)) {
+      bool far = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -271,6 +273,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
           const float next = fmaxf(m[nt][k], x * scale);
           const float f = next == -INFINITY ? 1.0f : exp2_approx(m[nt][k] - next);
           m[nt][k] = next;
+          far |= beyond_fused(next);
           l[nt][k] *= f;
 #pragma unroll
           for (int i = 0; i < 2 * NW; ++i) {
@@ -278,15 +281,25 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
             o[nt][i][k + 2] *= f;
           }
         }
+      huge = __any_sync(0xffffffffu, far);
     }
+    if (huge) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s[h][nt][k] = __fmul_rn(s[h][nt][k], scale);
+    }
+    const float factor = huge ? 1.0f : scale;
     uint32_t pf[2][NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float m0 = m[nt][0] == -INFINITY ? 0.0f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.0f : m[nt][1];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float p0 = exp2_approx(fmaf(s[h][nt][0], scale, -m0)), p1 = exp2_approx(fmaf(s[h][nt][1], scale, -m1));
-        const float p2 = exp2_approx(fmaf(s[h][nt][2], scale, -m0)), p3 = exp2_approx(fmaf(s[h][nt][3], scale, -m1));
+        const float p0 = exp2_approx(fmaf(s[h][nt][0], factor, -m0)), p1 = exp2_approx(fmaf(s[h][nt][1], factor, -m1));
+        const float p2 = exp2_approx(fmaf(s[h][nt][2], factor, -m0)), p3 = exp2_approx(fmaf(s[h][nt][3], factor, -m1));
         l[nt][0] += p0 + p2;
         l[nt][1] += p1 + p3;
         pf[h][nt][0] = transpose8x8(pack(p0, p1));

@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       const float scale = fmaxf(fabsf(a.scale_log2) * kUnshift, 1e-37f);
       float m = -INFINITY;
       float2 l = make_float2(0.0f, 0.0f);                             // the sum in two halves
-      bool ok = true;
+      bool ok = true, huge = false;                                   // huge: some row's maximum is beyond_fused
       for (int32_t t = 0; t < n_tiles; ++t) {
         ok = wait(smem_u32(&bars.s_full[w]), t & 1, dead);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
@@ -337,6 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
           const float next = fmaxf(m, top);
           const float f = next == -INFINITY ? 1.0f : exp2_approx(m - next);
           m = next;
+          huge = __any_sync(0xffffffffu, beyond_fused(m));
           l.x *= f;
           l.y *= f;
           if (t > 0) {
@@ -352,13 +353,18 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
             tmem_wait_st();
           }
         }
+        if (huge) {
+#pragma unroll
+          for (int i = 0; i < kKeys; ++i) x[i] = __fmul_rn(x[i], scale);
+        }
+        const float factor = huge ? 1.0f : scale;
         const float mm = m == -INFINITY ? 0.0f : -m;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t p[16];
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
-            const float2 e = fma2(make_float2(x[32 * c + i], x[32 * c + i + 1]), make_float2(scale, scale), make_float2(mm, mm));
+            const float2 e = fma2(make_float2(x[32 * c + i], x[32 * c + i + 1]), make_float2(factor, factor), make_float2(mm, mm));
             const float2 q = make_float2(exp2_approx(e.x), exp2_approx(e.y));
             l = add2(l, q);
             p[i >> 1] = pack(q.x, q.y);
