@@ -482,7 +482,10 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
  * at place j mod page_tokens of page page_table[b][j / page_tokens].  The new tokens are in the cache already (append
  * first): query i stands at position kv_len - n_q + i.  It sees the tokens j < kv_len with
  *     j <= position (causal 1),   j > position - window (window > 0).
- * A query that sees nothing gets out = 0 and lse = -infinity.  Query head h reads cache head h / (q_heads / n_heads).
+ * A query that sees nothing gets out = 0 and lse = -infinity.  A query that sees a token and holds an infinity or NaN gets NaN in out
+ * and lse; other rows are unaffected.  Scores (scale * q . k, times log2 e) have to be within float32: one that overflows
+ * upwards makes its row NaN, one that overflows downwards gets no weight (a row of such scores alone counts as one that sees
+ * nothing).  Query head h reads cache head h / (q_heads / n_heads).
  * Products are summed in float32, the statistics of the softmax are float32, probabilities enter the second product as
  * bfloat16 (relative to the row's running maximum; the sum that divides is that of the unrounded ones).
  *   q          : device bfloat16 [total_q][q_heads][D] with token stride q_ld; 16-byte aligned, q_ld a multiple of 8

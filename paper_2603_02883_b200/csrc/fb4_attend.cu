@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_co
   float q[NB], acc[NB];
 #pragma unroll
   for (int k = 0; k < NB; ++k) {
-    q[k] = __uint_as_float((uint32_t)a.q[row * a.q_ld + (int64_t)h * D + 32 * k + lane] << 16);
+    q[k] = __uint_as_float(query_pair((uint32_t)a.q[row * a.q_ld + (int64_t)h * D + 32 * k + lane] << 16));
     acc[k] = 0.0f;
   }
   const Range v = visible(a, sq, i);
@@ -50,17 +50,18 @@ __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_co
 #pragma unroll
     for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
     s = __fmul_rn(s, a.scale_log2);            // rounded as the maximum is, not fused with the subtraction below
+    if (s == -INFINITY && m == -INFINITY) continue;      // overflowed downwards: no weight, and no maximum to stand against yet
     const float mn = fmaxf(m, s), f = exp2f(m - mn), e = exp2f(s - mn);
     l = l * f + e;
 #pragma unroll
     for (int k = 0; k < NB; ++k) acc[k] = fmaf(e, value(a.cache.v_codes, a.cache.v_meta, at, k), acc[k] * f);
     m = mn;
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = inverse_of(l, 1.0f);
 #pragma unroll
   for (int k = 0; k < NB; ++k) store_out(a, row * a.out_ld + (int64_t)h * D + 32 * k + lane, acc[k] * inv);
   if (lane == 0) {
-    if (a.lse) a.lse[row * a.q_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    if (a.lse) a.lse[row * a.q_heads + h] = lse_of(m, l);
     if (bad) atomicOr(a.status, 2u);
   }
 }

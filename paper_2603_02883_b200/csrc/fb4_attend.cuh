@@ -111,6 +111,20 @@ __device__ __forceinline__ float exp2_approx(float x) {
 // maximum itself (with the exact product a maximum of 2^31 gives 2^128 or 2^-128 for the very key that set it).
 __device__ __forceinline__ bool beyond_fused(float m) { return fabsf(m) > 0x1p24f && m > -INFINITY; }
 
+// Two bf16 of a query, an infinity in them turned into a NaN: every score of a query that is not finite is then NaN, and so is
+// its sum (an infinity times a zero element is NaN and times others is not, and a score of -infinity would pass for a hidden one).
+__device__ __forceinline__ uint32_t query_pair(uint32_t x) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %1;" : "=r"(d) : "r"(x), "r"(0u));        // x * 0 + x: x itself, or NaN
+  return d;
+}
+
+// What the sum of a row's weights divides by: a row that sees nothing has sum 0 and gets zeros, one that is not finite has sum NaN.
+__device__ __forceinline__ float inverse_of(float sum, float one) { return sum == 0.0f ? 0.0f : one / sum; }
+__device__ __forceinline__ float lse_of(float top, float sum) { return sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2; }
+// A running maximum of +infinity (a score beyond float32) has no weights: the row's sum is NaN.
+__device__ __forceinline__ float finished(float sum, float m) { return m == INFINITY ? NAN : sum; }
+
 // ---- partial results of a split call: per row (b * max_q + i) * q_heads + h and split, D sums of the second product
 // (times 2^-64) and (running maximum, sum) of the softmax; the maximum in units of log2
 __device__ __forceinline__ int64_t partial_row(const Fb4Attend& a, int32_t b, int32_t i, int32_t h) {

@@ -160,6 +160,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
     for (int w = 0; w < NW; ++w) {
       uint4 u = make_uint4(0, 0, 0, 0);
       if (on) u = __ldg(reinterpret_cast<const uint4*>(src + 8 * w));
+      u = make_uint4(query_pair(u.x), query_pair(u.y), query_pair(u.z), query_pair(u.w));
       qf[nt][w][0] = prmt(u.x, u.y, 0x5410u) ^ flip;
       qf[nt][w][1] = prmt(u.x, u.y, 0x7632u) ^ flip;
       qf[nt][w][2] = prmt(u.z, u.w, 0x5410u) ^ flip;
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
       for (int off = 4; off < 32; off <<= 1) l[nt][k] += __shfl_xor_sync(0xffffffffu, l[nt][k], off);
-      if (g == 0) stat[warp][8 * nt + 2 * t + k] = make_float2(m[nt][k], l[nt][k]);
+      if (g == 0) stat[warp][8 * nt + 2 * t + k] = make_float2(m[nt][k], finished(l[nt][k], m[nt][k]));
     }
   __syncthreads();         // every warp is done with its ring
   float* join = reinterpret_cast<float*>(smem);
@@ -378,7 +379,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
 #pragma unroll
     for (int w = 0; w < kWarpsFew; ++w) top = fmaxf(top, stat[w][r].x);
 #pragma unroll
-    for (int w = 0; w < kWarpsFew; ++w) sum += stat[w][r].x == -INFINITY ? 0.0f : stat[w][r].y * exp2_approx(stat[w][r].x - top);
+    for (int w = 0; w < kWarpsFew; ++w) sum += stat[w][r].y == 0.0f ? 0.0f : stat[w][r].y * exp2_approx(stat[w][r].x - top);
     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
     for (int w = 0; w < kWarpsFew; ++w) {
@@ -389,8 +390,8 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
   };
   auto finish = [&](int r, int c, const float4& v, float top, float sum) {
     const int32_t i = (row0 + r) / a.group, h = head * a.group + (row0 + r) % a.group;
-    store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + c, v, sum > 0.0f ? kUnshift / sum : 0.0f);
-    if (c == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + c, v, inverse_of(sum, kUnshift));
+    if (c == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = lse_of(top, sum);
   };
   if constexpr (CLUSTER) {
     // the splits are the CTAs of a cluster: each leaves its joined rows in its shared memory (behind the warps' rows: the
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
       float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int z = 0; z < 8; ++z) {
-        if (st[z].x > -INFINITY) {
+        if (st[z].y != 0.0f) {
           const float f = exp2_approx(st[z].x - top);
           float4 u;
           asm volatile("{\n\t.reg .b32 q;\n\tmapa.shared::cluster.u32 q, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [q];\n\t}"
@@ -441,7 +442,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
       if (a.splits > 1) {
         const int32_t i = (row0 + r) / a.group, h = head * a.group + (row0 + r) % a.group;
         const int64_t pr = partial_row(a, b, i, h);
-        if (sum > 0.0f) *reinterpret_cast<float4*>(partial_sums(a, pr, split, D) + c) = v;
+        if (sum != 0.0f) *reinterpret_cast<float4*>(partial_sums(a, pr, split, D) + c) = v;
         if (c == 0) *partial_stat(a, pr, split, D) = make_float2(top, sum);
       } else {
         finish(r, c, v, top, sum);
@@ -477,7 +478,7 @@ __global__ void __launch_bounds__(128) fb4_attend_join_kernel(const __grid_const
       float w = 0.0f;
       if (s0 + lane * NW < a.splits) {
         const float2 st = *partial_stat(a, row, s0 + lane * NW, D);
-        if (st.y > 0.0f) {
+        if (st.y != 0.0f) {
           w = exp2_approx(st.x - top);
           sum += w * st.y;
         }
@@ -507,7 +508,7 @@ __global__ void __launch_bounds__(128) fb4_attend_join_kernel(const __grid_const
     sum = 0.0f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float f = stat[warp + w].x == -INFINITY ? 0.0f : exp2_approx(stat[warp + w].x - all);
+      const float f = stat[warp + w].y == 0.0f ? 0.0f : exp2_approx(stat[warp + w].x - all);
       const float4 u = part[warp + w][lane];
       v.x = fmaf(u.x, f, v.x); v.y = fmaf(u.y, f, v.y); v.z = fmaf(u.z, f, v.z); v.w = fmaf(u.w, f, v.w);
       sum = fmaf(stat[warp + w].y, f, sum);
@@ -515,8 +516,8 @@ __global__ void __launch_bounds__(128) fb4_attend_join_kernel(const __grid_const
     top = all;
   }
   if (!on) return;
-  if (lane * 4 < D) store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + lane * 4, v, sum > 0.0f ? kUnshift / sum : 0.0f);
-  if (lane == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+  if (lane * 4 < D) store_out4(a, (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D + lane * 4, v, inverse_of(sum, kUnshift));
+  if (lane == 0 && a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = lse_of(top, sum);
 }
 
 template <typename... Args>

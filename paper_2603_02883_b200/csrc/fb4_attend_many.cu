@@ -284,6 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         }
 #pragma unroll
         for (int k = 0; k < kRuns; ++k) {
+          u[k] = make_uint4(query_pair(u[k].x), query_pair(u[k].y), query_pair(u[k].z), query_pair(u[k].w));
           const int x = k * 32 + lane, r32 = 32 * (warp & 3) + x / kRuns;
           asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(q_at + w * L::kTileBytes + swizzled(r32, x % kRuns)), "r"(prmt(u[k].x, u[k].y, 0x5410u) ^ flip),
                        "r"(prmt(u[k].x, u[k].y, 0x7632u) ^ flip), "r"(prmt(u[k].z, u[k].w, 0x5410u) ^ flip), "r"(prmt(u[k].z, u[k].w, 0x7632u) ^ flip) : "memory");
@@ -383,18 +384,18 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         if (lane == 0) mbar_arrive(smem_u32(&bars.p_full[w]));
       }
       // ---- result
-      const float sum = l.x + l.y;
+      const float sum = finished(l.x + l.y, m);
       if (ok && n_tiles > 0) {
         ok = wait(smem_u32(&bars.o_done[w]), (n_tiles - 1) & 1, dead);
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
       }
-      const float inv = sum > 0.0f ? kUnshift / sum : 0.0f;
+      const float inv = inverse_of(sum, kUnshift);
       if (ok) {
         if (on) {
           const int32_t i = rc / a.group, h = head * a.group + rc % a.group;
           if (a.splits > 1) *partial_stat(a, partial_row(a, b, i, h), split, D) = make_float2(m, sum);
-          else if (a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = sum > 0.0f ? (m + log2f(sum)) * kLn2 : -INFINITY;
+          else if (a.lse) a.lse[(int64_t)(sq.q0 + i) * a.q_heads + h] = lse_of(m, sum);
         }
         // The rows go through this warp's part of Q's shared memory, which nobody reads any more, so that a store covers whole rows:
         // 2 D bytes of each row at a time (all of it in 16 bits, half of it in float32).
@@ -447,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
             if (r < rows) {
               const int32_t i = at_row.i, h = head * a.group + at_row.h;
               if (a.splits > 1) {
-                if (rsum > 0.0f) *reinterpret_cast<uint4*>(partial_sums(a, partial_row(a, b, i, h), split, D) + c0 + piece * 4) = v;
+                if (rsum != 0.0f) *reinterpret_cast<uint4*>(partial_sums(a, partial_row(a, b, i, h), split, D) + c0 + piece * 4) = v;
               } else {
                 const int64_t at = (int64_t)(sq.q0 + i) * a.out_ld + (int64_t)h * D;
                 if (wide) *reinterpret_cast<uint4*>(static_cast<float*>(a.out) + at + c0 + piece * 4) = v;
