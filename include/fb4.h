@@ -505,7 +505,8 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
  *   workspace  : device, 256-byte aligned, workspace_bytes >= fb4_cache_attention_workspace(...) of the same arguments
  *                (FB4_ERR_INVALID_ARG otherwise; NULL when that is 0).  It holds partial results between the launches of one
  *                call: two calls that may run at the same time need two workspaces
- * D = 64 and 128 run on the tensor cores, other head dimensions in a plain kernel.  The tensor-core kernels read a cached
+ * D = 64 and 128 run on the tensor cores (FB4_ERR_CUDA if fb4_init could not set those kernels up), other head dimensions in a
+ * plain kernel.  The tensor-core kernels read a cached
  * element to within 2^-70, and a block whose element scale is above 2^61 as if that were 2^61.
  * Needs block size 32 (FB4_ERR_INVALID_ARG otherwise); the context's formatbook decodes the cache.
  */

@@ -213,9 +213,10 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
   }
   size_t fast_bytes = 0;
   if (fb4_fast_build_tables(ctx->host_tables, c.select_mode, &ctx->d_fast_tables, &fast_bytes) &&
-      fb4_fast_prepare_device() == cudaSuccess && fb4_rope_prepare_device() == cudaSuccess)
+      fb4_fast_prepare_device() == cudaSuccess)
     ctx->fast_ok = 1;
-  ctx->attend_ok = fb4_attend_prepare_device() == cudaSuccess;
+  ctx->append_error = fb4_rope_prepare_device();
+  ctx->attend_error = fb4_attend_prepare_device();
   ctx->fast_table_bytes = fast_bytes;
   cudaGetLastError();
   *out = ctx;
@@ -654,6 +655,7 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
   if (rc != FB4_OK) return rc;
   if (q_heads > 0 && q == q_out && q_ld != q_out_ld) return FB4_ERR_INVALID_ARG;
   if (!aligned16(k_gain) || (q_heads > 0 && !aligned16(q_gain))) return FB4_ERR_ALIGN;
+  if (ctx->append_error != cudaSuccess) return fb4_set_cuda_error(ctx->append_error);
   const cudaError_t e = fb4_launch_cache_append(ctx, q, q_heads, q_ld, k, k_ld, v, v_ld, T, q_gain, k_gain, eps, rope, slot,
                                                 cache, q_out, q_out_ld, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
@@ -693,6 +695,8 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
   if (((reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(page_table) |
         reinterpret_cast<uintptr_t>(lse)) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return FB4_ERR_ALIGN;
+  // not the plain kernel instead: many times slower, and only fb4_last_variant would tell
+  if (ctx->attend_error != cudaSuccess && (D == 64 || D == 128) && !ctx->force_generic) return fb4_set_cuda_error(ctx->attend_error);
   const int64_t need = fb4_cache_attention_workspace(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv, window);
   if (need < 0 || workspace_bytes < need || (need > 0 && !workspace)) return FB4_ERR_INVALID_ARG;
   Fb4Attend a{};

@@ -51,7 +51,8 @@ struct fb4_ctx {
   size_t fast_table_bytes;
   int force_generic;             // fb4_set_kernel_variant(ctx, 1): always take the generic kernel
   int fast_ok;                   // formatbook/stage-1 table fit the fast kernel's packed layout
-  int attend_ok;                 // the tensor-core attention kernels can be launched on this device
+  cudaError_t append_error;      // why the append kernels cannot be launched on this device; their calls return it
+  cudaError_t attend_error;      // the same for the tensor-core attention kernels
   int sm_count;
   void* d_topk_scratch;          // histograms and counters of the multi-CTA top-k selection (fb4_topk.cu)
   uint32_t* d_status;            // device status word (bit 0: a TMA wait ran out of tries; bit 1: an index argument out of range)
