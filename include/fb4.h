@@ -33,9 +33,11 @@
  *     same time; one-time library set-up (driver entry points, the address of the built-in
  *     scratch of the *_static call) is guarded inside the library.  fb4_init / fb4_destroy of
  *     different contexts may run concurrently.
- *   - Device code has no unbounded wait loops: the only waits (for asynchronous loads into
- *     shared memory) give up after a fixed number of tries and raise a status bit
- *     (fb4_device_status); a call cannot hang.
+ *   - Device code has no unbounded wait loops: waits for asynchronous loads into shared memory and between the
+ *     warps of a CTA give up after a fixed number of tries and raise a status bit (fb4_device_status).
+ *     fb4_cache_attention also waits in hardware, where no limit can be set: for the other CTAs of a cluster
+ *     (scheduled together), for tensor memory (until kernels on the same SM that hold it have ended) and, in
+ *     its second launch, for the end of its first.
  *
  * Output layout
  *   codes : uint8 [T][C/2].  Byte j of a row holds element 2j in its low nibble
@@ -496,7 +498,7 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
  *   q_start    : device int32 [n_seqs + 1], ascending, from >= 0 to <= total_q, steps of at most max_q.  kv_len and q_start
  *                are clamped to these ranges on the device; a value that was outside raises bit 1 of the status word
  *   max_q, max_kv : host bounds of the lengths; they fix the launch shape (and only that).  max_kv <= 2^30,
- *                n_seqs * max_q * q_heads < 2^31 (FB4_ERR_SHAPE)
+ *                max_q * q_heads <= 2^30 and n_seqs * max_q * q_heads < 2^31 (FB4_ERR_SHAPE)
  *   out        : device [total_q][q_heads][D] with token stride out_ld (elements), out_dtype 0 = float32, 1 = bfloat16,
  *                2 = IEEE half; 16-byte aligned, out_ld * element size a multiple of 16; must not overlap q.  Rows of no
  *                sequence are left alone
@@ -506,8 +508,8 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
  *                (FB4_ERR_INVALID_ARG otherwise; NULL when that is 0).  It holds partial results between the launches of one
  *                call: two calls that may run at the same time need two workspaces
  * D = 64 and 128 run on the tensor cores (FB4_ERR_CUDA if fb4_init could not set those kernels up), other head dimensions in a
- * plain kernel.  The tensor-core kernels read a cached
- * element to within 2^-70, and a block whose element scale is above 2^61 as if that were 2^61.
+ * plain kernel.  The tensor-core kernels read a cached element to within 2^-70, and a block whose element scale is above
+ * 2^61 as if that were 2^61.
  * Needs block size 32 (FB4_ERR_INVALID_ARG otherwise); the context's formatbook decodes the cache.
  */
 int fb4_cache_attention(fb4_ctx* ctx, const void* q_bf16, int64_t q_ld, int32_t q_heads, int64_t total_q,
@@ -549,8 +551,8 @@ int fb4_device_status(fb4_ctx* ctx, uint32_t* status);
 /* Number of kernel launches this context has enqueued so far (diagnostic counter). */
 int64_t fb4_launch_count(const fb4_ctx* ctx);
 
-/* Name of the kernel variant the last quantize call on this context used
- * ("fast" = TMA-staged sm_100a path, "generic" = fallback for other shapes). */
+/* Name of the kernel variant the last quantize or fb4_cache_attention call on this context used ("fast" =
+ * TMA-staged sm_100a path, for attention the tensor-core kernels; "generic" = fallback for other shapes). */
 const char* fb4_last_variant(const fb4_ctx* ctx);
 
 /* cudaError_t of the last failing CUDA call made through this library (0 if none). */
