@@ -105,6 +105,13 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// ---- softmax
+//
+// Probabilities enter the second product as bf16, in both tensor-core kernels.  V needs bf16's exponent range (its block scales), and the
+// two operands of a product have one type; in two bf16 pieces p would keep 16 bits, at twice the second product's instructions and twice P's
+// room.  Each weight is off by at most 2^-8 of itself, as much as the rounding of a bf16 result, and the errors of a row's weights
+// mostly cancel; the sum that divides is that of the unrounded ones, so lse does not see it.
+//
 // The running maximum is a rounded product, score * scale; a probability takes the exact one, in one operation with the
 // subtraction of the maximum.  The two differ by half a step of the maximum, which cancels between numerator and denominator as long
 // as it is small: up to 2^24 it is a factor of two at most.  Beyond, the scores are multiplied first, so that the largest is the
