@@ -12,10 +12,11 @@
 // codes with one metadata record, straight into the A fragment of the first product (which channel sits at which k is
 // free, as long as Q agrees); V goes through movmatrix once, because there the tokens are the contracted side.
 //
-// Bound: instructions.  A warp issues 459 of them for 16 tokens of 128 channels (K and V; 311 are the decode and the products), 60 % of
-// the ALU pipe's slots while it runs; 75600 tokens of 12 heads take 51 us, 2.55 TB/s of the cache's 4.5 bits per value, 39 % of the
-// copy bandwidth.  More warps at fewer registers (20 or 24 instead of 16 per SM) came out slower, and so did the same work on
-// tcgen05 (K decoded into tensor memory, V into a swizzled tile, roles by warp: 61 us).
+// Bound: the chain of a tile and the instructions in it, neither at its limit.  Scores, maximum, exponentials and product of a tile
+// follow one another in each of the 16 warps of an SM; a warp issues 464 instructions for 16 tokens of 128 channels (K and V; 311 are the
+// decode and the products), 60 % of the issue slots and of the ALU pipe's.  75600 tokens of 12 heads take 51 us, 2.55 TB/s of the cache's
+// 4.5 bits per value, 39 % of the copy bandwidth.  More warps at fewer registers (20 or 24 instead of 16 per SM) came out slower, and so
+// did the same work on tcgen05 (K decoded into tensor memory, V into a swizzled tile, roles by warp: 61 us).
 #include "fb4_attend.cuh"
 #include "fb4_block.cuh"
 

@@ -20,9 +20,11 @@
 //
 // Bound: the shared memory that decode and tensor core have in common.  Per 128 tokens and 256 rows (2.0 us, 3800 cycles) the
 // tensor core reads 192 KB of operands from it (1536 cycles; 2048 of arithmetic), decode writes 64 KB and reads 18, P goes to
-// TMEM past it: 69 % of its cycles by the counters.  The exponentials take 2048 (16 per cycle and SM), all roles issue 55 % of the
+// TMEM past it: 69 % of its cycles by the counters.  The exponentials take 2048 (16 per cycle and SM), all roles issue 56 % of the
 // slots.  Leaving out the decode's arithmetic (and 3/4 of its stores) gives 1.45 us, leaving out the softmax's 1.9, both 1.5.
-// 1560 queries of 12 heads over 32760 tokens take 335 us, 938 TFLOP/s, 56 % of the measured bf16 product rate.
+// 1560 queries of 12 heads over 32760 tokens take 352 us a call, 890 TFLOP/s, 53 % of the measured bf16 product rate (336 to 345 us
+// where a graph repeats it and the pages stay in L2).  The other pairs of figures here were each taken on one box, with the kernel as it
+// stood then.
 // Without gain (us for that frame and for four causal prompts of 1024 tokens, against 342 / 133): 8 decode warps, four for K and four
 // for V (339 to 349 / 136); decode with the next tile's codes already in registers (375 / 141); a copy of the dialects for
 // every lane of a half-warp, which ends the bank conflicts (349 / 133); the first tile's Q in TMEM and P in half the columns

@@ -7,10 +7,11 @@
 //
 // Every operation is rounded once and stands in a fixed order (include/fb4.h states it), so the result is the same for every grid.
 //
-// Both kernels stream, and the instructions are what has to be kept under the bytes: a row of norm and rotation costs its
-// lanes 290 instructions (32760 tokens of 24 heads of 128: 84 us, 4.8 TB/s, 74 % of the copy bandwidth; a plain copy of the same
-// rows by the same loop takes 70 us), the quantizer adds about 9 per element.  Appending 32760 tokens of 12 + 2 * 12 heads takes
-// 150 us, 3 TB/s.
+// Both kernels stream.  Norm and rotation: 288 instructions a row and lane, 66 % of the issue slots, the rest waits for loads: 32760
+// tokens of 24 heads of 128 in 83 us, 4.9 TB/s, 74 % of the copy bandwidth (a plain copy of the same rows by the same loop takes 70).
+// Append, where the quantizer adds about 9 instructions per element: 32760 tokens of 12 + 2 * 12 heads in 147 us, 3.1 TB/s.  Nothing
+// is saturated (60 % of the issue slots, 36 % of DRAM): 128 registers leave 16 warps per SM, which wait for the rows of a unit before they
+// work on it.
 #include <cuda_bf16.h>
 
 #include "fb4_block.cuh"
