@@ -523,6 +523,39 @@ int64_t fb4_cache_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32
                                       int32_t max_q, int32_t max_kv, int32_t window);
 
 /*
+ * Plan of a serving step: the pages that every sequence holds afterwards, and sequence, position and slot of the step's rows, all on the
+ * device (a step recorded into a CUDA graph plans itself from the lengths it finds).  Sequence b holds kv_len[b] tokens, in its pages
+ * page_table[b][0 .. ceil(kv_len[b] / page_tokens) - 1].  It keeps the first keep[b] of them (fewer than all: drafted tokens
+ * that were rejected; 0: the sequence has ended, a new one may take its place) and asks for new_len[b] more.  In this order:
+ *   1. The pages behind the kept tokens go back to the free list free_pages[0 .. n_free - 1], its end being the top: page f of
+ *      all that go back (sequences in order, a sequence's pages in order) becomes entry top - 1 - f, top = n_free + their number.
+ *   2. Sequences are served in order while both the free pages and the T rows last; from the first that finds too few of either
+ *      on, none that asks for tokens is served.  One that asks for more than max_pages pages hold is not served and does
+ *      not count.  Page f of all that are taken is entry top - 1 - f.
+ *   3. kv_len[b] = keep[b] + the tokens that b was given; q_start[b] = the rows given to the sequences in front of b, q_start[n_seqs] =
+ *      all of them.  Row q_start[b] + i is token keep[b] + i of sequence b: pos = that number, slot = its place in the cache
+ *      (fb4_cache_append).  Rows behind the last one get pos 0 and slot -1.
+ * The same step planned again (same keep and new_len, keep not above what was held) gives the same plan: every page goes back to where it came from.
+ * page_table, kv_len, keep, q_start, slot and pos are what fb4_cache_append, fb4_cache8_append, fb4_rope and the attention calls read.
+ *   page_table : device int32 [n_seqs][max_pages], in and out; entries behind a sequence's pages are left as they are
+ *   page_tokens: a power of two, 16 to 4096;  max_pages * page_tokens <= 2^30, n_seqs * max_pages < 2^31
+ *   kv_len     : device int32 [n_seqs], in and out
+ *   keep       : device int32 [n_seqs]; NULL = all tokens.  More than kv_len counts as kv_len
+ *   new_len    : device int32 [n_seqs]
+ *   n_seqs     : at most FB4_PLAN_MAX_SEQS
+ *   free_pages : device int32 [free_cap], in and out; n_free: device int32 [1], in and out.  Pages that go back to a full list are lost
+ *   T          : rows of the step, at most 2^31 - 1
+ *   q_start    : device int32 [n_seqs + 1] (out);  slot: device int64 [T] (out) or NULL;  pos: device int32 [T] (out) or NULL
+ * A kv_len outside [0, max_pages * page_tokens] or an n_free outside [0, free_cap] is clamped, a negative keep or new_len counts as 0, and each
+ * of them, and a lost page, raises bit 1 of the status word.  Page numbers are passed on as they are, and never used as addresses.
+ * Works with every context configuration.
+ */
+#define FB4_PLAN_MAX_SEQS 32768
+int fb4_cache_plan(fb4_ctx* ctx, int32_t* page_table, int32_t max_pages, int32_t page_tokens, int32_t* kv_len, const int32_t* keep,
+                   const int32_t* new_len, int32_t n_seqs, int32_t* free_pages, int32_t free_cap, int32_t* n_free, int64_t T,
+                   int32_t* q_start, int64_t* slot, int32_t* pos, void* stream);
+
+/*
  * Host-buffer form of fb4_quantize for callers whose tensors live in host memory:
  * copies x from the host, quantizes, and copies codes and meta back, in row
  * chunks pipelined over the context's own streams, then waits for completion.

@@ -217,6 +217,7 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
     ctx->fast_ok = 1;
   ctx->append_error = fb4_rope_prepare_device();
   ctx->attend_error = fb4_attend_prepare_device();
+  ctx->plan_error = fb4_plan_prepare_device();
   ctx->fast_table_bytes = fast_bytes;
   cudaGetLastError();
   *out = ctx;
@@ -738,6 +739,29 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
   ctx->last_variant = plan.kernel ? "fast" : "generic";
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
   ctx->launches += launches;
+  return FB4_OK;
+}
+
+int fb4_cache_plan(fb4_ctx* ctx, int32_t* page_table, int32_t max_pages, int32_t page_tokens, int32_t* kv_len, const int32_t* keep,
+                   const int32_t* new_len, int32_t n_seqs, int32_t* free_pages, int32_t free_cap, int32_t* n_free, int64_t T,
+                   int32_t* q_start, int64_t* slot, int32_t* pos, void* stream) {
+  if (!ctx) return FB4_ERR_INVALID_ARG;
+  if (page_tokens < 16 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0 || max_pages < 0 || n_seqs < 0 ||
+      n_seqs > FB4_PLAN_MAX_SEQS || free_cap < 0 || T < 0 || T > 0x7fffffffLL || (int64_t)max_pages * page_tokens > (1 << 30) ||
+      (int64_t)max_pages * n_seqs > 0x7fffffffLL)
+    return FB4_ERR_SHAPE;
+  if (!q_start || !n_free || (n_seqs > 0 && (!kv_len || !new_len)) || ((int64_t)max_pages * n_seqs > 0 && !page_table) ||
+      (free_cap > 0 && !free_pages))
+    return FB4_ERR_INVALID_ARG;
+  const uintptr_t words = reinterpret_cast<uintptr_t>(page_table) | reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(keep) |
+                          reinterpret_cast<uintptr_t>(new_len) | reinterpret_cast<uintptr_t>(free_pages) | reinterpret_cast<uintptr_t>(n_free) |
+                          reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(pos);
+  if ((words & 3u) || (reinterpret_cast<uintptr_t>(slot) & 7u)) return FB4_ERR_ALIGN;
+  if (ctx->plan_error != cudaSuccess) return fb4_set_cuda_error(ctx->plan_error);
+  const cudaError_t e = fb4_launch_cache_plan(ctx, page_table, max_pages, page_tokens, kv_len, keep, new_len, n_seqs, free_pages, free_cap,
+                                              n_free, T, q_start, slot, pos, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fb4_set_cuda_error(e);
+  ctx->launches += 1;
   return FB4_OK;
 }
 

@@ -53,6 +53,7 @@ struct fb4_ctx {
   int fast_ok;                   // formatbook/stage-1 table fit the fast kernel's packed layout
   cudaError_t append_error;      // why the append kernels cannot be launched on this device; their calls return it
   cudaError_t attend_error;      // the same for the tensor-core attention kernels
+  cudaError_t plan_error;        // the same for the plan of a step
   int sm_count;
   void* d_topk_scratch;          // histograms and counters of the multi-CTA top-k selection (fb4_topk.cu)
   uint32_t* d_status;            // device status word (bit 0: a TMA wait ran out of tries; bit 1: an index argument out of range)
@@ -166,3 +167,9 @@ cudaError_t fb4_launch_attend_many(const Fb4Attend& a, cudaStream_t stream);
 cudaError_t fb4_launch_attend_join(const Fb4Attend& a, cudaStream_t stream);
 cudaError_t fb4_launch_attend_few(const Fb4Attend& a, cudaStream_t stream);
 cudaError_t fb4_launch_attend_generic(const fb4_ctx* ctx, const Fb4Attend& a, cudaStream_t stream);
+
+// plan of a serving step (fb4_plan.cu)
+cudaError_t fb4_plan_prepare_device();
+cudaError_t fb4_launch_cache_plan(const fb4_ctx* ctx, int32_t* page_table, int32_t max_pages, int32_t page_tokens, int32_t* kv_len,
+                                  const int32_t* keep, const int32_t* new_len, int32_t n_seqs, int32_t* free_pages, int32_t free_cap,
+                                  int32_t* n_free, int64_t T, int32_t* q_start, int64_t* slot, int32_t* pos, cudaStream_t stream);

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -23,7 +24,7 @@ STATIC_MAX_CLUSTERS = 1024
 EXPORTS = [
     "fb4_default_config", "fb4_init", "fb4_destroy", "fb4_get_tables", "fb4_block_tables", "fb4_quantize", "fb4_quantize_f32", "fb4_quantize_affine", "fb4_quantize_affine_mxfp8", "fb4_quantize_layernorm", "fb4_quantize_seda",
     "fb4_build_subformatbook", "fb4_build_subformatbook_static", "fb4_select_salient", "fb4_select_salient_topk", "fb4_quantize_decomposed", "fb4_quantize_decomposed_idx", "fb4_dequantize",
-    "fb4_quantize_weights", "fb4_qk_norm_rope", "fb4_cache_append", "fb4_cache_attention", "fb4_cache_attention_workspace", "fb4_quantize_mxfp8", "fb4_quantize_mxfp8_decomposed", "fb4_to_mxfp8", "fb4_mxfp8_scale_bytes", "fb4_quantize_host", "fb4_set_kernel_variant", "fb4_device_status", "fb4_launch_count", "fb4_last_variant", "fb4_last_cuda_error", "fb4_strerror",
+    "fb4_quantize_weights", "fb4_qk_norm_rope", "fb4_cache_append", "fb4_cache_attention", "fb4_cache_attention_workspace", "fb4_cache_plan", "fb4_quantize_mxfp8", "fb4_quantize_mxfp8_decomposed", "fb4_to_mxfp8", "fb4_mxfp8_scale_bytes", "fb4_quantize_host", "fb4_set_kernel_variant", "fb4_device_status", "fb4_launch_count", "fb4_last_variant", "fb4_last_cuda_error", "fb4_strerror",
 ]
 
 
@@ -113,6 +114,8 @@ def lib() -> ctypes.CDLL:
     L.fb4_cache_attention.restype = ci
     L.fb4_cache_attention_workspace.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32]
     L.fb4_cache_attention_workspace.restype = i64
+    L.fb4_cache_plan.argtypes = [vp, vp, i32, i32, vp, vp, vp, i32, vp, i32, vp, i64, vp, vp, vp, vp]
+    L.fb4_cache_plan.restype = ci
     L.fb4_quantize_mxfp8.argtypes = [vp, vp, i64, i64, i64, vp, vp, i32, vp, vp, ci, vp]
     L.fb4_quantize_mxfp8.restype = ci
     L.fb4_quantize_mxfp8_decomposed.argtypes = [vp, vp, i64, i64, i64, vp, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp,
@@ -340,6 +343,13 @@ def fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q
     return int(lib().fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window))
 
 
+def fb4_cache_plan(ctx, page_table, max_pages, page_tokens, kv_len, keep, new_len, n_seqs, free_pages, free_cap, n_free, T, q_start,
+                   slot, pos, stream=None) -> None:
+    _check(lib().fb4_cache_plan(ctx, _ptr(page_table), max_pages, page_tokens, _ptr(kv_len), _ptr(keep), _ptr(new_len), n_seqs,
+                                _ptr(free_pages), free_cap, _ptr(n_free), T, _ptr(q_start), _ptr(slot), _ptr(pos), _stream(stream)),
+           "fb4_cache_plan")
+
+
 def fb4_quantize_host(ctx, x_host, T, C, d_x, d_codes, d_meta, codes_host, meta_host) -> None:
     _check(lib().fb4_quantize_host(ctx, _ptr(x_host), T, C, _ptr(d_x), _ptr(d_codes), _ptr(d_meta),
                                    _ptr(codes_host), _ptr(meta_host)), "fb4_quantize_host")
@@ -431,6 +441,34 @@ class Cache:
             raise ValueError("cache meta must be contiguous 16-bit [n_pages][n_heads][page_tokens][D/32]")
         c = Fb4Cache(kc.data_ptr(), km.data_ptr(), vc.data_ptr(), vm.data_ptr(), n, p, h, half * 2)
         object.__setattr__(self, "_c", (c, _device_of(kc, km, vc, vm)))
+
+
+@dataclass(frozen=True)
+class PageTables:
+    """Pages and lengths of the sequences of a server, and the free list (see fb4_cache_plan in include/fb4.h), all int32.  Checked
+    once, here: the object is a handle that a program keeps, and planning a step changes what the tensors hold."""
+    page_table: torch.Tensor                 # [n_seqs][max_pages]
+    kv_len: torch.Tensor                     # [n_seqs]
+    free_pages: torch.Tensor                 # [as many as the cache has], the first n_free of them free
+    n_free: torch.Tensor                     # [1]
+    page_tokens: int
+
+    def __post_init__(self):
+        pt, kv, fp, nf = self.page_table, self.kv_len, self.free_pages, self.n_free
+        if pt.dim() != 2 or kv.dim() != 1 or kv.shape[0] != pt.shape[0] or fp.dim() != 1 or nf.numel() != 1:
+            raise ValueError("expected page_table [n_seqs][max_pages], kv_len [n_seqs], free_pages [n] and n_free [1]")
+        for t in (pt, kv, fp, nf):
+            if t.dtype is not torch.int32 or not t.is_contiguous():
+                raise ValueError("page_table, kv_len, free_pages and n_free must be contiguous int32")
+        c = (pt.data_ptr(), pt.shape[1], self.page_tokens, kv.data_ptr()), (fp.data_ptr(), fp.shape[0], nf.data_ptr()), pt.shape[0]
+        object.__setattr__(self, "_c", (c, _device_of(pt, kv, fp, nf)))
+
+
+class Plan(NamedTuple):
+    """The rows of a step: q_start int32 [n_seqs + 1], slot int64 [T] (-1: no token's), pos int32 [T]"""
+    q_start: torch.Tensor
+    slot: torch.Tensor
+    pos: torch.Tensor
 
 
 _OUT_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -751,6 +789,30 @@ class Fb4:
                    q_start.data_ptr(), n, max_q, max_kv, D ** -0.5 if scale is None else scale, 1 if causal else 0, window,
                    out.data_ptr(), Hq * D, code, lse.data_ptr(), None if ws is None else ws.data_ptr(), need)
         return out, lse
+
+    def new_page_tables(self, n_seqs: int, max_pages: int, n_pages: int, page_tokens: int) -> PageTables:
+        """tables of n_seqs empty sequences; all of a cache's n_pages pages are free"""
+        new = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=torch.device("cuda", self.device))  # noqa: E731
+        free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=torch.device("cuda", self.device))      # page 0 on top
+        return PageTables(new(n_seqs, max_pages), new(n_seqs), free, torch.full((1,), n_pages, dtype=torch.int32, device=free.device), page_tokens)
+
+    def cache_plan(self, pages: PageTables, new_len, rows: int, keep=None) -> Plan:
+        """plans a step of `rows` rows: every sequence keeps its first keep[b] tokens (None: all) and gets new_len[b] more, as far as pages
+        and rows last (int32 [n_seqs] each).  Changes what `pages` holds, and returns the rows' q_start, slot and pos"""
+        ((table, max_pages, page_tokens, kv_len), (free, cap, n_free), n), device = pages._c
+        if device != self.device:
+            raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
+        for t in (new_len,) if keep is None else (new_len, keep):
+            if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+                raise ValueError("new_len and keep must be contiguous int32 tensors [n_seqs]")
+            if t.get_device() != device:
+                raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
+        if not 0 <= rows < 1 << 31:
+            raise ValueError("rows must be in [0, 2^31)")
+        q_start, slot, pos = new_len.new_empty(n + 1), new_len.new_empty(rows, dtype=torch.int64), new_len.new_empty(rows)
+        self._call("fb4_cache_plan", table, max_pages, page_tokens, kv_len, None if keep is None else keep.data_ptr(), new_len.data_ptr(), n,
+                   free, cap, n_free, rows, q_start.data_ptr(), slot.data_ptr(), pos.data_ptr())
+        return Plan(q_start, slot, pos)
 
     def cache_values(self, cache: Cache, dtype=torch.float32):
         """(k, v) [n_pages][n_heads][page_tokens][D]: all that a cache holds, decoded.  Needs block size 32, like the cache"""
