@@ -523,6 +523,69 @@ int64_t fb4_cache_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32
                                       int32_t max_q, int32_t max_kv, int32_t window);
 
 /*
+ * A paged cache of keys and values in 8 bits, for layers that lose too much in 4: the 16 tokens of a block (places 16 i .. 16 i + 15 of a
+ * page) share one power of two for each head, separately for keys and values.  Page p holds page_tokens tokens of every head:
+ *     codes : uint8 [n_pages][n_heads][page_tokens][D],   scales : uint8 [n_pages][n_heads][page_tokens / 16]
+ *     value = (code - 128) * 2^(scale - 127),   a scale below 58 or above 185 being read as 58 or 185
+ * Slots, page tables, lengths and their bounds are those of fb4_cache.
+ *   n_pages     : >= 1, n_pages * page_tokens * n_heads <= 2^40;  page_tokens: a power of two, 16 to 4096;  n_heads: 1 to 1024
+ *   head_dim    : D, a multiple of 32, at most 256.  k and v 16-byte aligned
+ */
+typedef struct {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int64_t n_pages;
+  int32_t page_tokens;
+  int32_t n_heads;
+  int32_t head_dim;
+} fb4_cache8;
+
+/*
+ * Appends the new tokens of several sequences to the 8-bit cache: rows q_start[b] .. q_start[b+1]-1 of k and v (n_q of them) are
+ * the tokens at positions kv_len[b] - n_q .. kv_len[b] - 1 of sequence b, at place j mod page_tokens of page
+ * page_table[b][j / page_tokens] (what fb4_cache_plan leaves).  k goes through the norm and the rotation of fb4_qk_norm_rope and, like v,
+ * is rounded from float32 to codes (no rounding to bfloat16 in between); q, if given, goes through the norm and the rotation in the
+ * same pass and leaves as bfloat16.  For each block and head that gets tokens:
+ *     e    = the smallest integer in [-69, 58] with max |x| < 127.5 * 2^e over its new tokens
+ *     s    = e, or the larger of e and the block's exponent if it holds tokens in front of the new ones (places below the first new one)
+ *     code = 128 + x / 2^s rounded to the nearest integer, ties to even (beyond 127 * 2^58: saturated)
+ * Tokens in front are rounded in the same way to the new exponent; a block that is filled token by token is off by one step of its last
+ * exponent at most, half a step otherwise.  Codes behind the new tokens are left alone.
+ *   page_table, max_pages, kv_len, q_start, n_seqs, max_q : as in fb4_cache_attention (clamped and reported alike; a page outside
+ *            [0, n_pages) gets no tokens and raises bit 1 of the status word); n_seqs <= 2^28.  The pages that are written to belong to one
+ *            sequence each (precondition).  Positions below 0 (n_q above kv_len) are left out
+ *   T      : rows of q, k and v; rows of no sequence are left out, and so are their rows of q_out
+ *   q_heads: 0 = no q (q, q_gain and q_out are ignored)
+ *   other arguments as in fb4_qk_norm_rope; k and v have cache->n_heads heads.  Works with every context configuration
+ */
+int fb4_cache8_append(fb4_ctx* ctx, const fb4_cache8* cache, const int32_t* page_table, int32_t max_pages, const int32_t* kv_len,
+                      const int32_t* q_start, int32_t n_seqs, int32_t max_q, const void* k_bf16, int64_t k_ld, const void* v_bf16,
+                      int64_t v_ld, int64_t T, const void* k_gain, float eps, const fb4_rope* rope, const void* q_bf16, int32_t q_heads,
+                      int64_t q_ld, const void* q_gain, void* q_out, int64_t q_out_ld, void* stream);
+
+/*
+ * fb4_cache_attention over the 8-bit cache: the same formulas, masks, arguments, refusals and clamped values.  D = 64 and 128 run on the
+ * tensor cores, which read every value exactly; no context configuration is refused.
+ */
+int fb4_cache8_attention(fb4_ctx* ctx, const void* q_bf16, int64_t q_ld, int32_t q_heads, int64_t total_q,
+                         const fb4_cache8* cache, const int32_t* page_table, int32_t max_pages, const int32_t* kv_len,
+                         const int32_t* q_start, int32_t n_seqs, int32_t max_q, int32_t max_kv, float scale, int causal,
+                         int32_t window, void* out, int64_t out_ld, int out_dtype, float* lse, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
+/* Size in bytes of the workspace of fb4_cache8_attention (0 = none needed; -1 for invalid arguments).  Host only. */
+int64_t fb4_cache8_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
+                                       int32_t max_q, int32_t max_kv, int32_t window);
+
+/*
+ * All that an 8-bit cache holds, decoded: k_out and v_out [n_pages][n_heads][page_tokens][D], out_dtype 0 = float32, 1 = bfloat16
+ * (both exact), 2 = IEEE half (rounded to nearest even); 16-byte aligned.
+ */
+int fb4_cache8_values(fb4_ctx* ctx, const fb4_cache8* cache, void* k_out, void* v_out, int out_dtype, void* stream);
+
+/*
  * Plan of a serving step: the pages that every sequence holds afterwards, and sequence, position and slot of the step's rows, all on the
  * device (a step recorded into a CUDA graph plans itself from the lengths it finds).  Sequence b holds kv_len[b] tokens, in its pages
  * page_table[b][0 .. ceil(kv_len[b] / page_tokens) - 1].  It keeps the first keep[b] of them (fewer than all: drafted tokens

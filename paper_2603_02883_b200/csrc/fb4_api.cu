@@ -123,6 +123,94 @@ int check_cache(const fb4_cache* c) {
   return FB4_OK;
 }
 
+int check_cache8(const fb4_cache8* c) {
+  if (!c) return FB4_ERR_INVALID_ARG;
+  if (c->n_pages < 1 || c->page_tokens < 16 || c->page_tokens > 4096 || (c->page_tokens & (c->page_tokens - 1)) != 0 ||
+      c->n_heads < 1 || c->n_heads > 1024 || c->head_dim < 32 || c->head_dim > 256 || c->head_dim % 32 != 0 ||
+      c->n_pages > (1LL << 40) / ((int64_t)c->page_tokens * c->n_heads))
+    return FB4_ERR_SHAPE;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale) return FB4_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v)) return FB4_ERR_ALIGN;
+  return FB4_OK;
+}
+
+int64_t attention_workspace(const fb4_ctx* ctx, int int8, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs, int32_t max_q,
+                            int32_t max_kv, int32_t window) {
+  if (!ctx || window < 0 || n_heads < 1 || n_heads > 1024 || q_heads < n_heads || q_heads > 1024 || q_heads % n_heads != 0 || head_dim < 32 ||
+      head_dim > 256 || head_dim % 32 != 0 || n_seqs < 0 || max_q < 0 || max_kv < 0 || max_kv > (1 << 30) ||
+      (int64_t)max_q * q_heads > (1 << 30) || (int64_t)max_q * q_heads * n_seqs > 0x7fffffffLL)
+    return -1;
+  return fb4_attend_plan(ctx, int8, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window).workspace;
+}
+
+bool attention_options(float scale, int causal, int32_t window, int out_dtype) {
+  return (causal == 0 || causal == 1) && window >= 0 && out_dtype >= 0 && out_dtype <= 2 && scale >= -0x1p60f && scale <= 0x1p60f;
+}
+
+// What both attention calls do once the cache, which `a` holds, and the options are checked.
+int run_attention(fb4_ctx* ctx, Fb4Attend& a, const void* q, int64_t q_ld, int32_t q_heads, int64_t total_q, const int32_t* page_table,
+                  int32_t max_pages, const int32_t* kv_len, const int32_t* q_start, int32_t n_seqs, int32_t max_q, int32_t max_kv, float scale,
+                  int causal, int32_t window, void* out, int64_t out_ld, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes,
+                  void* stream) {
+  const fb4_cache* cache = &a.cache;
+  if (q_heads < 1 || q_heads > 1024 || q_heads % cache->n_heads != 0 || total_q < 0 || total_q > 0x7fffffffLL || n_seqs < 0 ||
+      max_q < 0 || max_kv < 0 || max_pages < 0 || max_kv > (1 << 30) || (int64_t)max_q * q_heads > (1 << 30) ||
+      (int64_t)max_q * q_heads * n_seqs > 0x7fffffffLL)
+    return FB4_ERR_SHAPE;
+  if (total_q == 0 || n_seqs == 0 || max_q == 0) return FB4_OK;
+  const int32_t D = cache->head_dim;
+  const int rc = check_heads(q, q_heads, D, q_ld);
+  if (rc != FB4_OK) return rc;
+  if (!out || !kv_len || !q_start || (!page_table && max_pages > 0)) return FB4_ERR_INVALID_ARG;
+  if (out_ld < (int64_t)q_heads * D) return FB4_ERR_SHAPE;
+  if (!aligned16(out) || (out_ld * (out_dtype == 0 ? 4 : 2)) % 16 != 0) return FB4_ERR_ALIGN;
+  if (((reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(page_table) |
+        reinterpret_cast<uintptr_t>(lse)) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return FB4_ERR_ALIGN;
+  // not the plain kernel instead: many times slower, and only fb4_last_variant would tell
+  if (ctx->attend_error != cudaSuccess && (D == 64 || D == 128) && !ctx->force_generic) return fb4_set_cuda_error(ctx->attend_error);
+  const int64_t need = attention_workspace(ctx, a.int8, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv, window);
+  if (need < 0 || workspace_bytes < need || (need > 0 && !workspace)) return FB4_ERR_INVALID_ARG;
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_ld = q_ld;
+  a.total_q = total_q;
+  a.q_heads = q_heads;
+  a.group = q_heads / cache->n_heads;
+  while ((1 << a.page_shift) < cache->page_tokens) ++a.page_shift;
+  a.page_table = page_table;
+  a.max_pages = max_pages;
+  a.kv_len = kv_len;
+  a.q_start = q_start;
+  a.n_seqs = n_seqs;
+  a.max_q = max_q;
+  a.max_kv = max_kv;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.causal = causal;
+  a.window = window;
+  a.out = out;
+  a.out_ld = out_ld;
+  a.out_dtype = out_dtype;
+  a.lse = lse;
+  a.tables = ctx->d_tables;
+  a.status = ctx->d_status;
+  const Fb4AttendPlan plan = fb4_attend_plan(ctx, a.int8, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv, window);
+  a.splits = plan.splits;
+  a.split_tiles = plan.split_tiles;
+  a.partial = plan.workspace > 0 ? static_cast<float*>(workspace) : nullptr;
+  int launches = 1;
+  cudaError_t e;
+  if (plan.kernel == 0) e = fb4_launch_attend_generic(ctx, a, static_cast<cudaStream_t>(stream));
+  else e = plan.kernel == 1 ? fb4_launch_attend_few(a, static_cast<cudaStream_t>(stream)) : fb4_launch_attend_many(a, static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess && a.partial) {
+    e = fb4_launch_attend_join(a, static_cast<cudaStream_t>(stream));
+    launches = 2;
+  }
+  ctx->last_variant = plan.kernel ? "fast" : "generic";
+  if (e != cudaSuccess) return fb4_set_cuda_error(e);
+  ctx->launches += launches;
+  return FB4_OK;
+}
+
 int run_quantize(fb4_ctx* ctx, const void* x, int64_t T, int64_t C, int64_t ld, const Fb4RowExtras& ex,
                  uint8_t* codes, uint16_t* meta, cudaStream_t stream) {
   if (T == 0) return FB4_OK;
@@ -666,11 +754,12 @@ int fb4_cache_append(fb4_ctx* ctx, const fb4_cache* cache, const int64_t* slot, 
 
 int64_t fb4_cache_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
                                       int32_t max_q, int32_t max_kv, int32_t window) {
-  if (!ctx || window < 0 || n_heads < 1 || n_heads > 1024 || q_heads < n_heads || q_heads > 1024 || q_heads % n_heads != 0 || head_dim < 32 ||
-      head_dim > 256 || head_dim % 32 != 0 || n_seqs < 0 || max_q < 0 || max_kv < 0 || max_kv > (1 << 30) ||
-      (int64_t)max_q * q_heads > (1 << 30) || (int64_t)max_q * q_heads * n_seqs > 0x7fffffffLL)
-    return -1;
-  return fb4_attend_plan(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window).workspace;
+  return attention_workspace(ctx, 0, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window);
+}
+
+int64_t fb4_cache8_attention_workspace(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
+                                       int32_t max_q, int32_t max_kv, int32_t window) {
+  return attention_workspace(ctx, 1, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window);
 }
 
 int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_heads, int64_t total_q, const fb4_cache* cache,
@@ -678,67 +767,69 @@ int fb4_cache_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_hea
                         int32_t n_seqs, int32_t max_q, int32_t max_kv, float scale, int causal, int32_t window, void* out,
                         int64_t out_ld, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
   if (!ctx || ctx->cfg.block_size != 32) return FB4_ERR_INVALID_ARG;
-  if ((causal != 0 && causal != 1) || window < 0 || out_dtype < 0 || out_dtype > 2 || !(scale >= -0x1p60f && scale <= 0x1p60f))
-    return FB4_ERR_INVALID_ARG;
-  int rc = check_cache(cache);
+  if (!attention_options(scale, causal, window, out_dtype)) return FB4_ERR_INVALID_ARG;
+  const int rc = check_cache(cache);
   if (rc != FB4_OK) return rc;
-  if (q_heads < 1 || q_heads > 1024 || q_heads % cache->n_heads != 0 || total_q < 0 || total_q > 0x7fffffffLL || n_seqs < 0 ||
-      max_q < 0 || max_kv < 0 || max_pages < 0 || max_kv > (1 << 30) || (int64_t)max_q * q_heads > (1 << 30) ||
-      (int64_t)max_q * q_heads * n_seqs > 0x7fffffffLL)
-    return FB4_ERR_SHAPE;
-  if (total_q == 0 || n_seqs == 0 || max_q == 0) return FB4_OK;
-  const int32_t D = cache->head_dim;
-  rc = check_heads(q, q_heads, D, q_ld);
-  if (rc != FB4_OK) return rc;
-  if (!out || !kv_len || !q_start || (!page_table && max_pages > 0)) return FB4_ERR_INVALID_ARG;
-  if (out_ld < (int64_t)q_heads * D) return FB4_ERR_SHAPE;
-  if (!aligned16(out) || (out_ld * (out_dtype == 0 ? 4 : 2)) % 16 != 0) return FB4_ERR_ALIGN;
-  if (((reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(page_table) |
-        reinterpret_cast<uintptr_t>(lse)) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
-    return FB4_ERR_ALIGN;
-  // not the plain kernel instead: many times slower, and only fb4_last_variant would tell
-  if (ctx->attend_error != cudaSuccess && (D == 64 || D == 128) && !ctx->force_generic) return fb4_set_cuda_error(ctx->attend_error);
-  const int64_t need = fb4_cache_attention_workspace(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv, window);
-  if (need < 0 || workspace_bytes < need || (need > 0 && !workspace)) return FB4_ERR_INVALID_ARG;
   Fb4Attend a{};
-  a.q = static_cast<const uint16_t*>(q);
-  a.q_ld = q_ld;
-  a.total_q = total_q;
-  a.q_heads = q_heads;
-  a.group = q_heads / cache->n_heads;
   a.cache = *cache;
-  while ((1 << a.page_shift) < cache->page_tokens) ++a.page_shift;
-  a.page_table = page_table;
-  a.max_pages = max_pages;
-  a.kv_len = kv_len;
-  a.q_start = q_start;
-  a.n_seqs = n_seqs;
-  a.max_q = max_q;
-  a.max_kv = max_kv;
-  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-  a.causal = causal;
-  a.window = window;
-  a.out = out;
-  a.out_ld = out_ld;
-  a.out_dtype = out_dtype;
-  a.lse = lse;
-  a.tables = ctx->d_tables;
-  a.status = ctx->d_status;
-  const Fb4AttendPlan plan = fb4_attend_plan(ctx, q_heads, cache->n_heads, D, n_seqs, max_q, max_kv, window);
-  a.splits = plan.splits;
-  a.split_tiles = plan.split_tiles;
-  a.partial = plan.workspace > 0 ? static_cast<float*>(workspace) : nullptr;
-  int launches = 1;
-  cudaError_t e;
-  if (plan.kernel == 0) e = fb4_launch_attend_generic(ctx, a, static_cast<cudaStream_t>(stream));
-  else e = plan.kernel == 1 ? fb4_launch_attend_few(a, static_cast<cudaStream_t>(stream)) : fb4_launch_attend_many(a, static_cast<cudaStream_t>(stream));
-  if (e == cudaSuccess && a.partial) {
-    e = fb4_launch_attend_join(a, static_cast<cudaStream_t>(stream));
-    launches = 2;
-  }
-  ctx->last_variant = plan.kernel ? "fast" : "generic";
+  return run_attention(ctx, a, q, q_ld, q_heads, total_q, page_table, max_pages, kv_len, q_start, n_seqs, max_q, max_kv, scale, causal, window,
+                       out, out_ld, out_dtype, lse, workspace, workspace_bytes, stream);
+}
+
+int fb4_cache8_attention(fb4_ctx* ctx, const void* q, int64_t q_ld, int32_t q_heads, int64_t total_q, const fb4_cache8* cache,
+                         const int32_t* page_table, int32_t max_pages, const int32_t* kv_len, const int32_t* q_start,
+                         int32_t n_seqs, int32_t max_q, int32_t max_kv, float scale, int causal, int32_t window, void* out,
+                         int64_t out_ld, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!ctx || !attention_options(scale, causal, window, out_dtype)) return FB4_ERR_INVALID_ARG;
+  const int rc = check_cache8(cache);
+  if (rc != FB4_OK) return rc;
+  Fb4Attend a{};
+  a.cache = fb4_cache{cache->k, nullptr, cache->v, nullptr, cache->n_pages, cache->page_tokens, cache->n_heads, cache->head_dim};
+  a.int8 = 1;
+  a.k_scale = cache->k_scale;
+  a.v_scale = cache->v_scale;
+  return run_attention(ctx, a, q, q_ld, q_heads, total_q, page_table, max_pages, kv_len, q_start, n_seqs, max_q, max_kv, scale, causal, window,
+                       out, out_ld, out_dtype, lse, workspace, workspace_bytes, stream);
+}
+
+int fb4_cache8_append(fb4_ctx* ctx, const fb4_cache8* cache, const int32_t* page_table, int32_t max_pages, const int32_t* kv_len,
+                      const int32_t* q_start, int32_t n_seqs, int32_t max_q, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                      int64_t T, const void* k_gain, float eps, const fb4_rope* rope, const void* q, int32_t q_heads, int64_t q_ld,
+                      const void* q_gain, void* q_out, int64_t q_out_ld, void* stream) {
+  if (!ctx) return FB4_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f) || eps > 3.0e38f || q_heads < 0) return FB4_ERR_INVALID_ARG;
+  int rc = check_cache8(cache);
+  if (rc != FB4_OK) return rc;
+  const int32_t D = cache->head_dim;
+  if (T < 0 || T > 0x7fffffffLL || q_heads > 1024 || n_seqs < 0 || n_seqs > (1 << 28) || max_q < 0 || max_pages < 0) return FB4_ERR_SHAPE;
+  rc = check_rope(rope, T, D);
+  if (rc != FB4_OK) return rc;
+  if (T == 0 || n_seqs == 0 || max_q == 0 || max_pages == 0) return FB4_OK;
+  if (!page_table || !kv_len || !q_start) return FB4_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(page_table) | reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(q_start)) & 3u) return FB4_ERR_ALIGN;
+  rc = check_heads(k, cache->n_heads, D, k_ld);
+  if (rc == FB4_OK) rc = check_heads(v, cache->n_heads, D, v_ld);
+  if (rc == FB4_OK && q_heads > 0) rc = check_heads(q, q_heads, D, q_ld);
+  if (rc == FB4_OK && q_heads > 0) rc = check_heads(q_out, q_heads, D, q_out_ld);
+  if (rc != FB4_OK) return rc;
+  if (q_heads > 0 && q == q_out && q_ld != q_out_ld) return FB4_ERR_INVALID_ARG;
+  if (!aligned16(k_gain) || (q_heads > 0 && !aligned16(q_gain))) return FB4_ERR_ALIGN;
+  const cudaError_t e = fb4_launch_cache8_append(ctx, cache, page_table, max_pages, kv_len, q_start, n_seqs, max_q, k, k_ld, v, v_ld, T, k_gain,
+                                                 eps, rope, q, q_heads, q_ld, q_gain, q_out, q_out_ld, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
-  ctx->launches += launches;
+  ctx->launches += 1;
+  return FB4_OK;
+}
+
+int fb4_cache8_values(fb4_ctx* ctx, const fb4_cache8* cache, void* k_out, void* v_out, int out_dtype, void* stream) {
+  if (!ctx || out_dtype < 0 || out_dtype > 2) return FB4_ERR_INVALID_ARG;
+  const int rc = check_cache8(cache);
+  if (rc != FB4_OK) return rc;
+  if (!k_out || !v_out) return FB4_ERR_INVALID_ARG;
+  if (!aligned16(k_out) || !aligned16(v_out)) return FB4_ERR_ALIGN;
+  const cudaError_t e = fb4_launch_cache8_values(cache, k_out, v_out, out_dtype, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fb4_set_cuda_error(e);
+  ctx->launches += 1;
   return FB4_OK;
 }
 

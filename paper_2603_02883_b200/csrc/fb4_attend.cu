@@ -1,4 +1,4 @@
-// Attention over the paged FB4 cache: the plain kernel (any head dimension).
+// Attention over the paged caches: the plain kernel (any head dimension).
 #include "fb4_attend.cuh"
 
 namespace {
@@ -8,7 +8,7 @@ using namespace fb4att;
 // One warp per query row and head; lane l holds channel 32 b + l of every block b.  The running maximum and sum of the softmax
 // are updated key by key.  Latency-bound and only meant for head dimensions that the tensor-core kernels do not have (and to
 // check them against).
-template <int NB>
+template <int NB, bool INT8>
 __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_constant__ Fb4Attend a) {
   __shared__ uint8_t book[32][8];
   if (threadIdx.x < 64) reinterpret_cast<uint32_t*>(book)[threadIdx.x] = reinterpret_cast<const uint32_t*>(a.tables->formatbook)[threadIdx.x];
@@ -31,7 +31,8 @@ __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_co
   const Range v = visible(a, sq, i);
   float m = -INFINITY, l = 0.0f;
   bool bad = false;
-  auto value = [&](const uint8_t* codes, const uint16_t* meta, int64_t at, int k) -> float {
+  auto value = [&](const uint8_t* codes, const uint16_t* meta, const uint8_t* scale, int64_t at, int k) -> float {
+    if (INT8) return ldexpf((float)codes[at * D + 32 * k + lane] - 128.0f, min(max((int)scale[at >> 4], 58), 185) - 127);
     const uint32_t c = codes[at * (D / 2) + 16 * k + (lane >> 1)], mt = meta[at * NB + k];
     const uint32_t code = (lane & 1) ? c >> 4 : c & 15u;
     const float x = ldexpf((float)book[(mt >> 8) & 31u][code & 7u], (int)(mt & 255u) - 127);
@@ -46,7 +47,7 @@ __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_co
     const int64_t at = ((page * a.cache.n_heads + head) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
     float s = 0.0f;
 #pragma unroll
-    for (int k = 0; k < NB; ++k) s = fmaf(q[k], value(a.cache.k_codes, a.cache.k_meta, at, k), s);
+    for (int k = 0; k < NB; ++k) s = fmaf(q[k], value(a.cache.k_codes, a.cache.k_meta, a.k_scale, at, k), s);
 #pragma unroll
     for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
     s = __fmul_rn(s, a.scale_log2);            // rounded as the maximum is, not fused with the subtraction below
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_co
     const float mn = fmaxf(m, s), f = exp2f(m - mn), e = exp2f(s - mn);
     l = l * f + e;
 #pragma unroll
-    for (int k = 0; k < NB; ++k) acc[k] = fmaf(e, value(a.cache.v_codes, a.cache.v_meta, at, k), acc[k] * f);
+    for (int k = 0; k < NB; ++k) acc[k] = fmaf(e, value(a.cache.v_codes, a.cache.v_meta, a.v_scale, at, k), acc[k] * f);
     m = mn;
   }
   const float inv = inverse_of(l, 1.0f);
@@ -70,15 +71,18 @@ __global__ void __launch_bounds__(128) fb4_attend_generic_kernel(const __grid_co
 
 cudaError_t fb4_launch_attend_generic(const fb4_ctx*, const Fb4Attend& a, cudaStream_t stream) {
   const int64_t grid = ((int64_t)a.max_q * a.q_heads + 3) / 4 * a.n_seqs;
+#define FB4_PLAIN(NB) \
+  a.int8 ? fb4_attend_generic_kernel<NB, true><<<(unsigned)grid, 128, 0, stream>>>(a) : fb4_attend_generic_kernel<NB, false><<<(unsigned)grid, 128, 0, stream>>>(a)
   switch (a.cache.head_dim / 32) {
-    case 1: fb4_attend_generic_kernel<1><<<(unsigned)grid, 128, 0, stream>>>(a); break;
-    case 2: fb4_attend_generic_kernel<2><<<(unsigned)grid, 128, 0, stream>>>(a); break;
-    case 3: fb4_attend_generic_kernel<3><<<(unsigned)grid, 128, 0, stream>>>(a); break;
-    case 4: fb4_attend_generic_kernel<4><<<(unsigned)grid, 128, 0, stream>>>(a); break;
-    case 5: fb4_attend_generic_kernel<5><<<(unsigned)grid, 128, 0, stream>>>(a); break;
-    case 6: fb4_attend_generic_kernel<6><<<(unsigned)grid, 128, 0, stream>>>(a); break;
-    case 7: fb4_attend_generic_kernel<7><<<(unsigned)grid, 128, 0, stream>>>(a); break;
-    default: fb4_attend_generic_kernel<8><<<(unsigned)grid, 128, 0, stream>>>(a); break;
+    case 1: FB4_PLAIN(1); break;
+    case 2: FB4_PLAIN(2); break;
+    case 3: FB4_PLAIN(3); break;
+    case 4: FB4_PLAIN(4); break;
+    case 5: FB4_PLAIN(5); break;
+    case 6: FB4_PLAIN(6); break;
+    case 7: FB4_PLAIN(7); break;
+    default: FB4_PLAIN(8); break;
   }
+#undef FB4_PLAIN
   return cudaGetLastError();
 }

@@ -1,4 +1,4 @@
-// What the attention kernels over the paged FB4 cache share: the sequence and mask arithmetic and the output store.
+// What the attention kernels over the paged caches share: the sequence and mask arithmetic and the output store.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -18,7 +18,8 @@ struct Sequence {
 };
 
 // The lengths of sequence b, clamped to what the call allows; `tell`: report a value that was outside.
-__device__ __forceinline__ Sequence sequence(const Fb4Attend& a, int32_t b, bool tell) {
+template <typename Call>
+__device__ __forceinline__ Sequence sequence(const Call& a, int32_t b, bool tell) {
   const int64_t s0 = __ldg(a.q_start + b), s1 = __ldg(a.q_start + b + 1), len = __ldg(a.kv_len + b);
   const int64_t q0 = s0 < 0 ? 0 : s0 < a.total_q ? s0 : a.total_q;
   int64_t q1 = s1 < q0 ? q0 : s1 < a.total_q ? s1 : a.total_q;
@@ -97,6 +98,35 @@ __device__ __forceinline__ void decode_word(uint32_t w, const BlockScale& s, uin
 // thread i of 64 writes word i of the magnitude bytes (256 bytes at book)
 __device__ __forceinline__ void fill_book(uint32_t* book, const Fb4DeviceTables* t, int i) {
   book[i] = reinterpret_cast<const uint32_t*>(t->formatbook)[i] << 3;      // magnitudes are at most 15: no carry between bytes
+}
+
+// ---- decode of the 8-bit cache to packed bf16 pairs
+//
+// A code (0..255) as the low byte of a bf16 is the number code * 2^-133, subnormals and the first normal binade being one scale; one
+// fused multiply-add takes it to (code - 128) * 2^(scale byte - 127) * 2^-64, exactly: 8 instructions per 8 elements.  Scale bytes are read as
+// 58 to 185, for which every value and both constants are bf16 numbers.
+struct Int8Scale {
+  uint32_t f, c;            // 2^(scale byte + 69 - 127) and -128 * 2^(scale byte - 127 - 64), in both halves
+};
+
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t x, uint32_t y, uint32_t z) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(y), "r"(z));
+  return d;
+}
+
+// use = false: every element reads as zero
+__device__ __forceinline__ Int8Scale int8_scale(uint32_t byte, bool use) {
+  const uint32_t x = min(max(byte, 58u), 185u);
+  return Int8Scale{use ? (x + 69u) * 0x00800080u : 0u, use ? (x - 57u) * 0x00800080u | 0x80008000u : 0u};
+}
+
+// 8 codes n0..n7 -> the pairs (n0,n2) (n1,n3) (n4,n6) (n5,n7), times 2^-64: the order of decode_word
+__device__ __forceinline__ void decode_bytes(uint32_t w0, uint32_t w1, const Int8Scale& s, uint32_t (&o)[4]) {
+  o[0] = fma_bf16x2(w0 & 0x00ff00ffu, s.f, s.c);
+  o[1] = fma_bf16x2(prmt(w0, 0u, 0x4341u), s.f, s.c);
+  o[2] = fma_bf16x2(w1 & 0x00ff00ffu, s.f, s.c);
+  o[3] = fma_bf16x2(prmt(w1, 0u, 0x4341u), s.f, s.c);
 }
 
 __device__ __forceinline__ float exp2_approx(float x) {

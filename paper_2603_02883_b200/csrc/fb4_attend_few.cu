@@ -578,9 +578,10 @@ cudaError_t fb4_attend_prepare_device() {
   return e;
 }
 
-Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
+Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int int8, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
                               int32_t max_q, int32_t max_kv, int32_t window) {
   Fb4AttendPlan p{0, 1, 0x7fffffff / 64, 0};
+  if (int8) return p;
   if ((head_dim != 64 && head_dim != 128) || ctx->force_generic || n_seqs == 0 || max_q == 0) return p;
   const int64_t rows = (int64_t)max_q * (q_heads / n_heads);
   // the longest run of tokens that a CTA's rows can see together

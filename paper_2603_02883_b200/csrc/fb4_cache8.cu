@@ -1,0 +1,391 @@
+// Append of keys and values to the paged 8-bit cache, and its decode.
+//
+// The 16 tokens of a block (16 neighbouring places of a page) share one power of two 2^e for each head, separately for K and V; a
+// value is (code - 128) * 2^e.  e is the smallest with max |x| < 127.5 * 2^e, so that rounding to the nearest code never leaves
+// [-127, 127].  A power of two and not the maximum over 127: a block that is filled token by token grows its scale a few times, and codes that
+// are halved are off by at most one step of the last scale in all, while factors just above one would add half a step each time.
+//
+// Work: a CTA takes the new tokens of one block of one sequence, over all heads of K, V and Q (or one of `parts` shares of them).  The
+// tokens' cosines and sines go to shared memory once.  A warp takes a head of K or V at a time: the block's rows, norm and rotation, the
+// maximum over all of it, the codes.  Nobody else writes to a block, so there are no atomics, and the result is the same for every grid.
+#include "fb4_attend.cuh"
+#include "fb4_rope.cuh"
+
+namespace {
+
+using namespace fb4rope;
+
+constexpr int kWarps = 8;
+constexpr int kPlaces = 16;                // tokens of a block
+constexpr int kMinByte = 58, kMaxByte = 185;
+
+struct Append8 {
+  Heads q, k, v;
+  RopeTable rope;
+  fb4_cache8 cache;
+  int32_t D;
+  float eps, inv_d;
+  // which rows belong where, as in the attention
+  const int32_t* page_table;
+  int32_t max_pages, page_shift;
+  const int32_t* kv_len;
+  const int32_t* q_start;
+  int32_t n_seqs, max_q, max_kv;
+  int64_t total_q;
+  int32_t blocks;           // > 0: CTAs per sequence; 0: the sequence is looked up (see owner)
+  uint32_t* status;
+};
+
+// Sequence b owns the CTAs from (q_start[b] >> 4) + 2 b on: the rows of a sequence touch at most rows / 16 + 2 blocks, so these
+// runs hold them, and together they are not many more than the blocks that there are.
+__device__ __forceinline__ int64_t first_cta(const Append8& p, int32_t b) { return (__ldg(p.q_start + b) >> 4) + 2 * (int64_t)b; }
+
+__device__ __forceinline__ int32_t owner(const Append8& p, int64_t cta) {
+  const int lane = threadIdx.x & 31;
+  int32_t lo = 0, hi = p.n_seqs;           // the last b in [lo, hi) with first_cta(b) <= cta
+  while (hi - lo > 1) {
+    const int32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const uint32_t below = __ballot_sync(0xffffffffu, at < hi && first_cta(p, at) <= cta);
+    const int k = below ? 31 - __clz((int)below) : 0;
+    lo += k * step;
+    if (lo + step < hi) hi = lo + step;
+  }
+  return lo;
+}
+
+// cos / sin of the block's tokens in shared memory: couple c (two pairs) of token i at this 16-byte piece, so that the lanes of a
+// pass meet in different banks
+__device__ __forceinline__ int cs_piece(int couples, int i, int c) { return i * couples + (c ^ ((c >> 3) & 3) ^ ((i & 1) << 1)); }
+
+template <bool INTER>
+__device__ __forceinline__ void read_cs(const float4* cs, int couples, int i, int j, int D, CosSin& t) {
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int c = INTER ? 2 * j + (n & 1) + (n < 2 ? 0 : D / 8) : 4 * j + n;
+    const float4 v = cs[cs_piece(couples, i, c)];
+    t.c[2 * n] = v.x; t.s[2 * n] = v.y; t.c[2 * n + 1] = v.z; t.s[2 * n + 1] = v.w;
+  }
+}
+
+__device__ __forceinline__ float top_of(const Share& x, float top) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(x.a[i]), fabsf(x.b[i])));
+  return top;
+}
+
+// scale byte of a block whose largest magnitude is `top`: e + 127, e the smallest with top < 127.5 * 2^e
+__device__ __forceinline__ int byte_of(float top) {
+  const int field = (int)((__float_as_uint(top) + 0x10000u) >> 23);       // 127.5 = 255 / 128 * 2^6: the carry of the mantissa
+  return min(max(field - 6, kMinByte), kMaxByte);
+}
+
+// x / 2^e as a code: the sum with 1.5 * 2^23 + 128 is rounded to an integer (ties to even), whose low byte is the code
+__device__ __forceinline__ uint32_t code_bits(float x, float inv, bool clamp) {
+  float y = fmaf(x, inv, 0x1.8p23f + 128.0f);
+  if (clamp) y = fminf(fmaxf(y, 0x1.8p23f + 1.0f), 0x1.8p23f + 255.0f);   // beyond the largest scale only
+  return __float_as_uint(y);
+}
+
+__device__ __forceinline__ uint32_t join_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
+// a lane's two runs of 8 channels as codes
+template <bool INTER>
+__device__ __forceinline__ void encode(const Share& x, float inv, bool clamp, uint2& ca, uint2& cb) {
+  uint32_t a[8], b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    a[i] = code_bits(x.a[i], inv, clamp);
+    b[i] = code_bits(x.b[i], inv, clamp);
+  }
+  if (INTER) {
+    ca = make_uint2(join_bytes(a[0], b[0], a[1], b[1]), join_bytes(a[2], b[2], a[3], b[3]));
+    cb = make_uint2(join_bytes(a[4], b[4], a[5], b[5]), join_bytes(a[6], b[6], a[7], b[7]));
+  } else {
+    ca = make_uint2(join_bytes(a[0], a[1], a[2], a[3]), join_bytes(a[4], a[5], a[6], a[7]));
+    cb = make_uint2(join_bytes(b[0], b[1], b[2], b[3]), join_bytes(b[4], b[5], b[6], b[7]));
+  }
+}
+
+// four held codes at a scale that is 2^d times theirs
+__device__ __forceinline__ uint32_t rescaled(uint32_t w, float down) {
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = code_bits((float)(int)((w >> (8 * i)) & 255u) - 128.0f, down, false);
+  return join_bytes(y[0], y[1], y[2], y[3]);
+}
+
+__device__ __forceinline__ float two_to(int byte) { return __uint_as_float((uint32_t)byte << 23); }      // 2^(byte - 127), byte >= 1
+
+template <int LG, bool INTER>
+__global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const __grid_constant__ Append8 p) {
+  constexpr int RP = 32 / LG, NP = kPlaces / RP;      // rows of a pass, passes of a block
+  constexpr bool kHold = NP <= 4;                     // rows stay in registers between maximum and codes; else they are computed twice
+  extern __shared__ __align__(16) float4 cs_smem[];
+  __shared__ __align__(16) uint8_t gain_smem[kGainBytes];
+  const uint32_t gains = fb4blk::smem_u32(gain_smem);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane % LG, g = lane / LG;
+  const bool on = j < p.D / 16;
+  const int half = p.D / 2, couples = p.D / 4;
+
+  // ---- which tokens
+  int32_t b, nth;
+  if (p.blocks > 0) {
+    b = (int32_t)(blockIdx.x / p.blocks);
+    nth = (int32_t)(blockIdx.x - (int64_t)b * p.blocks);
+  } else {
+    b = owner(p, blockIdx.x);
+    const int64_t d = blockIdx.x - first_cta(p, b);
+    nth = d < 0 || d > 0x7ffffff ? 0x7ffffff : (int32_t)d;
+  }
+  const fb4att::Sequence sq = fb4att::sequence(p, b, nth == 0 && blockIdx.y == 0 && threadIdx.x == 0);
+  const int32_t first = sq.kv - sq.n_q, from = first > 0 ? first : 0;
+  const int64_t base = ((int64_t)(from >> 4) + nth) << 4;                 // position of the block's first place
+  const int32_t lo = base > from ? 0 : from & 15;                         // places lo <= i < hi are new
+  if (base >= sq.kv || sq.n_q == 0) return;
+  const int32_t hi = sq.kv - base < kPlaces ? (int32_t)(sq.kv - base) : kPlaces, n_new = hi - lo;
+  const int64_t row0 = sq.q0 + (base - first);                            // row of place 0 (which may be no row of the call)
+  bool bad = false;
+
+  stage_gains<LG, INTER>(p, gains);
+  if (p.rope.table) {
+    for (int x = threadIdx.x; x < n_new * couples; x += kWarps * 32) {
+      const int i = lo + x / couples, c = x % couples;
+      const int32_t* pos = p.rope.pos + (row0 + i) * p.rope.n_axes;
+      int ax[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        ax[k] = 0;
+#pragma unroll
+        for (int a = 0; a < 3; ++a) ax[k] += (a + 1 < p.rope.n_axes && 2 * c + k >= p.rope.end[a]) ? 1 : 0;
+      }
+      uint32_t at = (uint32_t)__ldg(pos + ax[0]);
+      if (at >= (uint32_t)p.rope.n_pos) { bad = true; at = 0u; }
+      float4 v = __ldg(reinterpret_cast<const float4*>(p.rope.table + (int64_t)at * p.rope.P + 2 * c));
+      if (ax[0] != ax[1]) {                                               // the couple straddles two axes
+        at = (uint32_t)__ldg(pos + ax[1]);
+        if (at >= (uint32_t)p.rope.n_pos) { bad = true; at = 0u; }
+        const float2 w = __ldg(p.rope.table + (int64_t)at * p.rope.P + 2 * c + 1);
+        v.z = w.x;
+        v.w = w.y;
+      }
+      cs_smem[cs_piece(couples, i, c)] = v;
+    }
+  }
+  int64_t page = __ldg(p.page_table + (int64_t)b * p.max_pages + (base >> p.page_shift));
+  if (page < 0 || page >= p.cache.n_pages) { bad = true; page = -1; }
+  __syncthreads();
+
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  const int32_t H = p.cache.n_heads, q_units = (n_new * p.q.n + kPlaces - 1) / kPlaces;
+  for (int32_t unit = blockIdx.y * kWarps + warp; unit < 2 * H + q_units; unit += gridDim.y * kWarps) {
+    if (unit < 2 * H) {
+      // ------------------------------------------------ a head of K or V
+      if (page < 0) continue;
+      const bool is_v = unit >= H;
+      const int32_t h = is_v ? unit - H : unit;
+      const Heads& hd = is_v ? p.v : p.k;
+      const int64_t cell = (page * H + h) << p.page_shift;                // the head's tokens in the page
+      const int32_t in_page = (int32_t)(base & ((1 << p.page_shift) - 1));
+      uint8_t* codes = (is_v ? p.cache.v : p.cache.k) + (cell + in_page) * p.D;
+      uint8_t* scale = (is_v ? p.cache.v_scale : p.cache.k_scale) + ((cell + in_page) >> 4);
+      const int held = lo > 0 ? min(max((int)*scale, kMinByte), kMaxByte) : kMinByte;
+      const uint16_t* x = hd.x + row0 * hd.ld + (int64_t)h * p.D + 8 * j;
+      const uint32_t gain = gains + (4 * LG + j) * 16;
+      uint4 ra[NP], rb[NP];
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        const int i = n * RP + g;
+        ra[n] = rb[n] = zero;
+        if (on && i >= lo && i < hi) {
+          ra[n] = __ldg(reinterpret_cast<const uint4*>(x + i * hd.ld));
+          rb[n] = __ldg(reinterpret_cast<const uint4*>(x + i * hd.ld + half));
+        }
+      }
+      auto row = [&](int n, Share& y) {
+        if (is_v) {
+          unpack<INTER>(ra[n], rb[n], y);
+        } else {
+          CosSin t;
+          const int i = n * RP + g;
+          if (p.rope.table) read_cs<INTER>(cs_smem, couples, on && i >= lo && i < hi ? i : lo, on ? j : 0, p.D, t);
+          norm_rotate<LG, INTER>(ra[n], rb[n], p.k.gain != nullptr, gain, p, t, y);
+        }
+      };
+      Share y[kHold ? NP : 1];
+      float top = 0.0f;
+#pragma unroll
+      for (int n = 0; n < NP; ++n)
+        if ((n + 1) * RP > lo && n * RP < hi) {
+          Share& z = y[kHold ? n : 0];
+          row(n, z);
+          const int i = n * RP + g;
+          if (on && i >= lo && i < hi) top = top_of(z, top);
+        }
+#pragma unroll
+      for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      const int byte = max(byte_of(top), held);
+      const float inv = two_to(254 - byte);
+      const bool clamp = byte == kMaxByte;
+#pragma unroll
+      for (int n = 0; n < NP; ++n)
+        if ((n + 1) * RP > lo && n * RP < hi) {
+          Share& z = y[kHold ? n : 0];
+          if (!kHold) row(n, z);
+          const int i = n * RP + g;
+          uint2 ca, cb;
+          encode<INTER>(z, inv, clamp, ca, cb);
+          if (on && i >= lo && i < hi) {
+            *reinterpret_cast<uint2*>(codes + i * p.D + 8 * j) = ca;
+            *reinterpret_cast<uint2*>(codes + i * p.D + 8 * j + half) = cb;
+          }
+        }
+      if (lo > 0 && byte > held) {                                        // the tokens that the block holds take the new scale
+        const float down = two_to(127 + held - byte);
+        for (int x16 = lane; x16 < lo * p.D / 16; x16 += 32) {
+          uint4 w = *reinterpret_cast<const uint4*>(codes + 16 * x16);
+          w = make_uint4(rescaled(w.x, down), rescaled(w.y, down), rescaled(w.z, down), rescaled(w.w, down));
+          *reinterpret_cast<uint4*>(codes + 16 * x16) = w;
+        }
+      }
+      __syncwarp();
+      if (lane == 0) *scale = (uint8_t)byte;
+    } else {
+      // ------------------------------------------------ 16 rows of Q (head-major: row r = head r / n_new, token r mod n_new)
+      const int32_t r0 = (unit - 2 * H) * kPlaces;
+      const uint32_t gain = gains + j * 16;
+#pragma unroll 2
+      for (int n = 0; n < NP; ++n) {
+        const int32_t r = r0 + n * RP + g;
+        if (r0 + n * RP >= n_new * p.q.n) break;
+        const bool real = on && r < n_new * p.q.n;
+        const int32_t h = real ? r / n_new : 0, i = lo + (real ? r - h * n_new : 0);
+        const int64_t at = (int64_t)h * p.D + 8 * j;
+        uint4 qa = zero, qb = zero;
+        if (real) {
+          const uint16_t* x = p.q.x + (row0 + i) * p.q.ld + at;
+          qa = *reinterpret_cast<const uint4*>(x);
+          qb = *reinterpret_cast<const uint4*>(x + half);
+        }
+        CosSin t;
+        if (p.rope.table) read_cs<INTER>(cs_smem, couples, i, on ? j : 0, p.D, t);
+        Share y;
+        norm_rotate<LG, INTER>(qa, qb, p.q.gain != nullptr, gain, p, t, y);
+        pack<INTER>(y, pack_bf16, qa, qb);
+        if (real) {
+          uint16_t* o = p.q.out + (row0 + i) * p.q.out_ld + at;
+          *reinterpret_cast<uint4*>(o) = qa;
+          *reinterpret_cast<uint4*>(o + half) = qb;
+        }
+      }
+    }
+  }
+  if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, 2u);
+}
+
+// ---- decode: 8 codes per thread and step, K then V
+__global__ void __launch_bounds__(256) fb4_cache8_values_kernel(const uint8_t* __restrict__ k, const uint8_t* __restrict__ k_scale, const uint8_t* __restrict__ v,
+                                                                const uint8_t* __restrict__ v_scale, void* __restrict__ k_out, void* __restrict__ v_out,
+                                                                int64_t pieces, int32_t per_block, int out_dtype) {
+  const bool is_v = blockIdx.y != 0;
+  const uint2* src = reinterpret_cast<const uint2*>(is_v ? v : k);
+  const uint8_t* scale = is_v ? v_scale : k_scale;
+  void* out = is_v ? v_out : k_out;
+  constexpr int kStep = 4;                 // pieces of a thread, 256 apart
+  const int64_t p0 = (int64_t)blockIdx.x * (256 * kStep) + threadIdx.x;
+  uint2 c[kStep];
+  int s[kStep];
+#pragma unroll
+  for (int n = 0; n < kStep; ++n) {
+    const int64_t at = p0 + n * 256;
+    if (at < pieces) {
+      c[n] = __ldg(src + at);
+      s[n] = __ldg(scale + at / per_block);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < kStep; ++n) {
+    const int64_t at = p0 + n * 256;
+    if (at >= pieces) continue;
+    const float f = two_to(min(max(s[n], kMinByte), kMaxByte));
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = ((float)((i < 4 ? c[n].x : c[n].y) >> (8 * (i & 3)) & 255u) - 128.0f) * f;
+    if (out_dtype == 0) {
+      float4* o = static_cast<float4*>(out) + 2 * at;
+      o[0] = make_float4(x[0], x[1], x[2], x[3]);
+      o[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (out_dtype == 1) {
+          w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+        } else {
+          const __half2 y = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+          w[i] = *reinterpret_cast<const uint32_t*>(&y);
+        }
+      }
+      static_cast<uint4*>(out)[at] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t fb4_launch_cache8_append(const fb4_ctx* ctx, const fb4_cache8* cache, const int32_t* page_table, int32_t max_pages,
+                                     const int32_t* kv_len, const int32_t* q_start, int32_t n_seqs, int32_t max_q, const void* k,
+                                     int64_t k_ld, const void* v, int64_t v_ld, int64_t T, const void* k_gain, float eps,
+                                     const fb4_rope* rope, const void* q, int32_t q_heads, int64_t q_ld, const void* q_gain,
+                                     void* q_out, int64_t q_out_ld, cudaStream_t stream) {
+  Append8 p{};
+  p.D = cache->head_dim;
+  p.eps = eps;
+  p.inv_d = (float)(1.0 / p.D);
+  p.rope = rope_of(rope, p.D);
+  p.cache = *cache;
+  p.q = heads_of(q, q_ld, q_heads, q_gain, q_out, q_out_ld);
+  p.k = heads_of(k, k_ld, cache->n_heads, k_gain, nullptr, 0);
+  p.v = heads_of(v, v_ld, cache->n_heads, nullptr, nullptr, 0);
+  p.page_table = page_table;
+  p.max_pages = max_pages;
+  while ((1 << p.page_shift) < cache->page_tokens) ++p.page_shift;
+  p.kv_len = kv_len;
+  p.q_start = q_start;
+  p.n_seqs = n_seqs;
+  p.max_q = max_q;
+  p.max_kv = 0x7fffffff;
+  p.total_q = T;
+  p.status = ctx->d_status;
+  // CTAs by sequence where that is not many more of them than by rows (one row each: exactly as many as there are blocks)
+  const int64_t by_seq = ((int64_t)max_q + 30) / 16 * n_seqs, by_rows = (T >> 4) + 2 * (int64_t)n_seqs;
+  const int64_t grid = by_seq <= by_rows ? by_seq : by_rows;
+  p.blocks = by_seq <= by_rows ? (int32_t)(((int64_t)max_q + 30) / 16) : 0;
+  // few blocks: a block's heads are shared out until every warp has one unit
+  const int64_t units = 2 * cache->n_heads + q_heads, slots = (int64_t)ctx->sm_count * 2;
+  int64_t parts = (slots + grid - 1) / grid;
+  const int64_t most = (units + kWarps - 1) / kWarps;
+  if (parts > most) parts = most;
+  const dim3 dims((unsigned)grid, (unsigned)parts);
+  const size_t smem = rope ? (size_t)kPlaces * p.D * 4 : 0;
+  const bool inter = rope && rope->interleaved;
+#define FB4_APPEND8(LG) \
+  inter ? fb4_cache8_append_kernel<LG, true><<<dims, kWarps * 32, smem, stream>>>(p) \
+        : fb4_cache8_append_kernel<LG, false><<<dims, kWarps * 32, smem, stream>>>(p)
+  switch (lanes_of(p.D)) {
+    case 2: FB4_APPEND8(2); break;
+    case 4: FB4_APPEND8(4); break;
+    case 8: FB4_APPEND8(8); break;
+    default: FB4_APPEND8(16); break;
+  }
+#undef FB4_APPEND8
+  return cudaGetLastError();
+}
+
+cudaError_t fb4_launch_cache8_values(const fb4_cache8* cache, void* k_out, void* v_out, int out_dtype, cudaStream_t stream) {
+  const int64_t pieces = cache->n_pages * cache->n_heads * cache->page_tokens * (cache->head_dim / 8);
+  const dim3 grid((unsigned)((pieces + 1023) / 1024), 2);
+  fb4_cache8_values_kernel<<<grid, 256, 0, stream>>>(cache->k, cache->k_scale, cache->v, cache->v_scale, k_out, v_out, pieces, 2 * cache->head_dim, out_dtype);
+  return cudaGetLastError();
+}

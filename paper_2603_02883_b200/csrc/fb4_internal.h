@@ -129,12 +129,23 @@ cudaError_t fb4_launch_cache_append(const fb4_ctx* ctx, const void* q, int32_t q
                                     const void* k_gain, float eps, const fb4_rope* rope, const int64_t* slot,
                                     const fb4_cache* cache, void* q_out, int64_t q_out_ld, cudaStream_t stream);
 
-// One fb4_cache_attention call as its kernels see it.
+// append to the 8-bit cache and its decode (fb4_cache8.cu)
+cudaError_t fb4_launch_cache8_append(const fb4_ctx* ctx, const fb4_cache8* cache, const int32_t* page_table, int32_t max_pages,
+                                     const int32_t* kv_len, const int32_t* q_start, int32_t n_seqs, int32_t max_q, const void* k,
+                                     int64_t k_ld, const void* v, int64_t v_ld, int64_t T, const void* k_gain, float eps,
+                                     const fb4_rope* rope, const void* q, int32_t q_heads, int64_t q_ld, const void* q_gain,
+                                     void* q_out, int64_t q_out_ld, cudaStream_t stream);
+cudaError_t fb4_launch_cache8_values(const fb4_cache8* cache, void* k_out, void* v_out, int out_dtype, cudaStream_t stream);
+
+// One fb4_cache_attention or fb4_cache8_attention call as its kernels see it.
 struct Fb4Attend {
   const uint16_t* q;
   int64_t q_ld, total_q;
   int32_t q_heads, group;        // group = q_heads / cache.n_heads
-  fb4_cache cache;
+  fb4_cache cache;               // 8 bits: k_codes and v_codes hold its bytes, the meta pointers are NULL
+  int32_t int8;                  // the cache is an fb4_cache8
+  const uint8_t* k_scale;        // its scale bytes
+  const uint8_t* v_scale;
   int32_t page_shift;
   const int32_t* page_table;
   int32_t max_pages;
@@ -159,7 +170,7 @@ struct Fb4AttendPlan {
   int32_t splits, split_tiles;
   int64_t workspace;
 };
-Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
+Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int int8, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
                               int32_t max_q, int32_t max_kv, int32_t window);
 cudaError_t fb4_attend_prepare_device();
 cudaError_t fb4_attend_many_prepare_device();

@@ -24,7 +24,7 @@ STATIC_MAX_CLUSTERS = 1024
 EXPORTS = [
     "fb4_default_config", "fb4_init", "fb4_destroy", "fb4_get_tables", "fb4_block_tables", "fb4_quantize", "fb4_quantize_f32", "fb4_quantize_affine", "fb4_quantize_affine_mxfp8", "fb4_quantize_layernorm", "fb4_quantize_seda",
     "fb4_build_subformatbook", "fb4_build_subformatbook_static", "fb4_select_salient", "fb4_select_salient_topk", "fb4_quantize_decomposed", "fb4_quantize_decomposed_idx", "fb4_dequantize",
-    "fb4_quantize_weights", "fb4_qk_norm_rope", "fb4_cache_append", "fb4_cache_attention", "fb4_cache_attention_workspace", "fb4_cache_plan", "fb4_quantize_mxfp8", "fb4_quantize_mxfp8_decomposed", "fb4_to_mxfp8", "fb4_mxfp8_scale_bytes", "fb4_quantize_host", "fb4_set_kernel_variant", "fb4_device_status", "fb4_launch_count", "fb4_last_variant", "fb4_last_cuda_error", "fb4_strerror",
+    "fb4_quantize_weights", "fb4_qk_norm_rope", "fb4_cache_append", "fb4_cache_attention", "fb4_cache_attention_workspace", "fb4_cache_plan", "fb4_cache8_append", "fb4_cache8_attention", "fb4_cache8_attention_workspace", "fb4_cache8_values", "fb4_quantize_mxfp8", "fb4_quantize_mxfp8_decomposed", "fb4_to_mxfp8", "fb4_mxfp8_scale_bytes", "fb4_quantize_host", "fb4_set_kernel_variant", "fb4_device_status", "fb4_launch_count", "fb4_last_variant", "fb4_last_cuda_error", "fb4_strerror",
 ]
 
 
@@ -42,6 +42,11 @@ class Fb4Cache(ctypes.Structure):
     _fields_ = [("k_codes", ctypes.c_void_p), ("k_meta", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
                 ("v_meta", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32),
                 ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class Fb4Cache8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class Fb4Error(RuntimeError):
@@ -116,6 +121,15 @@ def lib() -> ctypes.CDLL:
     L.fb4_cache_attention_workspace.restype = i64
     L.fb4_cache_plan.argtypes = [vp, vp, i32, i32, vp, vp, vp, i32, vp, i32, vp, i64, vp, vp, vp, vp]
     L.fb4_cache_plan.restype = ci
+    cp8 = ctypes.POINTER(Fb4Cache8)
+    L.fb4_cache8_append.argtypes = [vp, cp8, vp, i32, vp, vp, i32, i32, vp, i64, vp, i64, i64, vp, cf, rp, vp, i32, i64, vp, vp, i64, vp]
+    L.fb4_cache8_append.restype = ci
+    L.fb4_cache8_attention.argtypes = [vp, vp, i64, i32, i64, cp8, vp, i32, vp, vp, i32, i32, i32, cf, ci, i32, vp, i64, ci, vp, vp, i64, vp]
+    L.fb4_cache8_attention.restype = ci
+    L.fb4_cache8_attention_workspace.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32]
+    L.fb4_cache8_attention_workspace.restype = i64
+    L.fb4_cache8_values.argtypes = [vp, cp8, vp, vp, ci, vp]
+    L.fb4_cache8_values.restype = ci
     L.fb4_quantize_mxfp8.argtypes = [vp, vp, i64, i64, i64, vp, vp, i32, vp, vp, ci, vp]
     L.fb4_quantize_mxfp8.restype = ci
     L.fb4_quantize_mxfp8_decomposed.argtypes = [vp, vp, i64, i64, i64, vp, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp,
@@ -343,6 +357,28 @@ def fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q
     return int(lib().fb4_cache_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window))
 
 
+def fb4_cache8_append(ctx, cache, page_table, max_pages, kv_len, q_start, n_seqs, max_q, k, k_ld, v, v_ld, T, k_gain, eps, rope, q, q_heads,
+                      q_ld, q_gain, q_out, q_out_ld, stream=None) -> None:
+    _check(lib().fb4_cache8_append(ctx, cache, _ptr(page_table), max_pages, _ptr(kv_len), _ptr(q_start), n_seqs, max_q, _ptr(k), k_ld, _ptr(v),
+                                   v_ld, T, _ptr(k_gain), eps, rope, _ptr(q), q_heads, q_ld, _ptr(q_gain), _ptr(q_out), q_out_ld,
+                                   _stream(stream)), "fb4_cache8_append")
+
+
+def fb4_cache8_attention(ctx, q, q_ld, q_heads, total_q, cache, page_table, max_pages, kv_len, q_start, n_seqs, max_q, max_kv, scale,
+                         causal, window, out, out_ld, out_dtype, lse, workspace, workspace_bytes, stream=None) -> None:
+    _check(lib().fb4_cache8_attention(ctx, _ptr(q), q_ld, q_heads, total_q, cache, _ptr(page_table), max_pages, _ptr(kv_len),
+                                      _ptr(q_start), n_seqs, max_q, max_kv, scale, causal, window, _ptr(out), out_ld, out_dtype, _ptr(lse),
+                                      _ptr(workspace), workspace_bytes, _stream(stream)), "fb4_cache8_attention")
+
+
+def fb4_cache8_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window) -> int:
+    return int(lib().fb4_cache8_attention_workspace(ctx, q_heads, n_heads, head_dim, n_seqs, max_q, max_kv, window))
+
+
+def fb4_cache8_values(ctx, cache, k_out, v_out, out_dtype, stream=None) -> None:
+    _check(lib().fb4_cache8_values(ctx, cache, _ptr(k_out), _ptr(v_out), out_dtype, _stream(stream)), "fb4_cache8_values")
+
+
 def fb4_cache_plan(ctx, page_table, max_pages, page_tokens, kv_len, keep, new_len, n_seqs, free_pages, free_cap, n_free, T, q_start,
                    slot, pos, stream=None) -> None:
     _check(lib().fb4_cache_plan(ctx, _ptr(page_table), max_pages, page_tokens, _ptr(kv_len), _ptr(keep), _ptr(new_len), n_seqs,
@@ -441,6 +477,26 @@ class Cache:
             raise ValueError("cache meta must be contiguous 16-bit [n_pages][n_heads][page_tokens][D/32]")
         c = Fb4Cache(kc.data_ptr(), km.data_ptr(), vc.data_ptr(), vm.data_ptr(), n, p, h, half * 2)
         object.__setattr__(self, "_c", (c, _device_of(kc, km, vc, vm)))
+
+
+@dataclass(frozen=True)
+class Cache8:
+    """Paged 8-bit cache (see fb4_cache8 in include/fb4.h).  Checked once, here: the object is a handle that a program keeps."""
+    k: torch.Tensor                          # uint8 [n_pages][n_heads][page_tokens][D]
+    k_scale: torch.Tensor                    # uint8 [n_pages][n_heads][page_tokens / 16]
+    v: torch.Tensor
+    v_scale: torch.Tensor
+
+    def __post_init__(self):
+        k, ks, v, vs = self.k, self.k_scale, self.v, self.v_scale
+        if k.dim() != 4:
+            raise ValueError("cache codes must be [n_pages][n_heads][page_tokens][D]")
+        n, h, p, d = shape = k.shape
+        for t, want in ((k, shape), (v, shape), (ks, (n, h, p // 16)), (vs, (n, h, p // 16))):
+            if t.dtype is not torch.uint8 or t.shape != want or not t.is_contiguous():
+                raise ValueError("cache codes must be contiguous uint8 [n_pages][n_heads][page_tokens][D], scales [n_pages][n_heads][page_tokens / 16]")
+        c = Fb4Cache8(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), n, p, h, d)
+        object.__setattr__(self, "_c", (c, _device_of(k, ks, v, vs)))
 
 
 @dataclass(frozen=True)
@@ -705,7 +761,19 @@ class Fb4:
         self._on(gain)
         return gain.data_ptr()
 
-    def _cache(self, cache: Cache) -> Fb4Cache:
+    def _sequences(self, page_table, kv_len, q_start) -> int:
+        """number of sequences"""
+        n = kv_len.numel()
+        if page_table.dim() != 2 or page_table.shape[0] != n or kv_len.dim() != 1 or q_start.dim() != 1 or q_start.numel() != n + 1:
+            raise ValueError("expected page_table [n_seqs][max_pages], kv_len [n_seqs] and q_start [n_seqs + 1]")
+        for t in (page_table, kv_len, q_start):
+            if t.dtype is not torch.int32 or not t.is_contiguous():
+                raise ValueError("page_table, kv_len and q_start must be contiguous int32")
+        self._on(page_table, kv_len, q_start)
+        return n
+
+    def _cache(self, cache):
+        """the C struct of a Cache or a Cache8"""
         c, device = cache._c
         if device != self.device:
             raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
@@ -717,6 +785,49 @@ class Fb4:
         codes = lambda: torch.zeros((n_pages, n_heads, page_tokens, head_dim // 2), dtype=torch.uint8, device=dev)  # noqa: E731
         meta = lambda: torch.zeros((n_pages, n_heads, page_tokens, head_dim // 32), dtype=torch.int16, device=dev)  # noqa: E731
         return Cache(codes(), meta(), codes(), meta())
+
+    def new_cache8(self, n_pages: int, page_tokens: int, n_heads: int, head_dim: int) -> Cache8:
+        """an empty 8-bit cache: every slot reads as zeros"""
+        dev = torch.device("cuda", self.device)
+        codes = lambda: torch.full((n_pages, n_heads, page_tokens, head_dim), 128, dtype=torch.uint8, device=dev)  # noqa: E731
+        scale = lambda: torch.full((n_pages, n_heads, page_tokens // 16), 58, dtype=torch.uint8, device=dev)  # noqa: E731
+        return Cache8(codes(), scale(), codes(), scale())
+
+    def cache8_append(self, cache: Cache8, k, v, page_table, kv_len, q_start, max_q: int, k_gain=None, eps: float = 1e-6,
+                      rope: Rope | None = None, q=None, q_gain=None):
+        """writes the sequences' new tokens, keys after norm and rotation, to their pages of an 8-bit cache (rows q_start[b] to q_start[b+1] - 1
+        are the last ones of the kv_len[b] tokens of sequence b); returns q after norm and rotation, if q is given (rows that belong to
+        no sequence are left undefined)"""
+        T, H, D, k_ld = self._heads(k)
+        Tv, Hv, Dv, v_ld = self._heads(v)
+        c = self._cache(cache)
+        if Tv != T or Hv != H or Dv != D or H != c.n_heads or D != c.head_dim:
+            raise ValueError("k and v must have the heads and the head dimension of the cache")
+        if max_q >> 31:                                             # passed as 32 bits
+            raise ValueError("max_q must be in [0, 2^31)")
+        n = self._sequences(page_table, kv_len, q_start)
+        kg, r = self._gain(k_gain, D), self._rope(rope, T, D)
+        Hq = q_ld = 0
+        qo = qp = qg = qop = None
+        if q is not None:
+            Tq, Hq, Dq, q_ld = self._heads(q)
+            if Tq != T or Dq != D:
+                raise ValueError("q must have the tokens and the head dimension of k")
+            qg = self._gain(q_gain, D)
+            qo = q.new_empty(T, Hq, D)
+            qp, qop = q.data_ptr(), qo.data_ptr()
+        self._call("fb4_cache8_append", c, page_table.data_ptr(), page_table.shape[1], kv_len.data_ptr(), q_start.data_ptr(), n, max_q,
+                   k.data_ptr(), k_ld, v.data_ptr(), v_ld, T, kg, eps, r, qp, Hq, q_ld, qg, qop, Hq * D)
+        return qo
+
+    def cache8_values(self, cache: Cache8, dtype=torch.float32):
+        """(k, v) [n_pages][n_heads][page_tokens][D]: all that an 8-bit cache holds, decoded"""
+        code = _out_dtype(dtype)
+        c = self._cache(cache)
+        k = cache.k.new_empty(cache.k.shape, dtype=dtype)
+        v = cache.k.new_empty(cache.k.shape, dtype=dtype)
+        self._call("fb4_cache8_values", c, k.data_ptr(), v.data_ptr(), code)
+        return k, v
 
     def qk_norm_rope(self, q, k, q_gain=None, k_gain=None, eps: float = 1e-6, rope: Rope | None = None, out=None):
         """(q, k) [T][heads][D] after the RMS norm of every head (gain None: no norm) and the rotation; out: (q_out, k_out)
@@ -767,6 +878,14 @@ class Fb4:
                         causal: bool = True, window: int = 0, dtype=torch.bfloat16):
         """(out [total_q][q_heads][D], lse float32 [total_q][q_heads]) of the queries over their sequences' pages; rows that
         belong to no sequence are left undefined.  scale None = D ** -0.5"""
+        return self._attention("fb4_cache_attention", q, cache, page_table, kv_len, q_start, max_q, max_kv, scale, causal, window, dtype)
+
+    def cache8_attention(self, q, cache: Cache8, page_table, kv_len, q_start, max_q: int, max_kv: int, scale: float | None = None,
+                         causal: bool = True, window: int = 0, dtype=torch.bfloat16):
+        """cache_attention over an 8-bit cache"""
+        return self._attention("fb4_cache8_attention", q, cache, page_table, kv_len, q_start, max_q, max_kv, scale, causal, window, dtype)
+
+    def _attention(self, where, q, cache, page_table, kv_len, q_start, max_q, max_kv, scale, causal, window, dtype):
         total, Hq, D, q_ld = self._heads(q)
         c = self._cache(cache)
         if D != c.head_dim:
@@ -774,18 +893,12 @@ class Fb4:
         if max_q >> 31 or max_kv >> 31 or window >> 31:            # they are passed as 32 bits
             raise ValueError("max_q, max_kv and window must be in [0, 2^31)")
         code = _out_dtype(dtype)
-        n = kv_len.numel()
-        if page_table.dim() != 2 or page_table.shape[0] != n or kv_len.dim() != 1 or q_start.dim() != 1 or q_start.numel() != n + 1:
-            raise ValueError("expected page_table [n_seqs][max_pages], kv_len [n_seqs] and q_start [n_seqs + 1]")
-        for t in (page_table, kv_len, q_start):
-            if t.dtype is not torch.int32 or not t.is_contiguous():
-                raise ValueError("page_table, kv_len and q_start must be contiguous int32")
-        self._on(page_table, kv_len, q_start)
+        n = self._sequences(page_table, kv_len, q_start)
         out = q.new_empty(total, Hq, D) if dtype is torch.bfloat16 else q.new_empty(total, Hq, D, dtype=dtype)
         lse = q.new_empty(total, Hq, dtype=torch.float32)
-        need = lib().fb4_cache_attention_workspace(self.ctx, Hq, c.n_heads, D, n, max_q, max_kv, window)
+        need = getattr(lib(), where + "_workspace")(self.ctx, Hq, c.n_heads, D, n, max_q, max_kv, window)
         ws = q.new_empty(need // 2) if need > 0 else None
-        self._call("fb4_cache_attention", q.data_ptr(), q_ld, Hq, total, c, page_table.data_ptr(), page_table.shape[1], kv_len.data_ptr(),
+        self._call(where, q.data_ptr(), q_ld, Hq, total, c, page_table.data_ptr(), page_table.shape[1], kv_len.data_ptr(),
                    q_start.data_ptr(), n, max_q, max_kv, D ** -0.5 if scale is None else scale, 1 if causal else 0, window,
                    out.data_ptr(), Hq * D, code, lse.data_ptr(), None if ws is None else ws.data_ptr(), need)
         return out, lse

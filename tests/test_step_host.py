@@ -73,3 +73,113 @@ def test_cache_plan_in_the_binding(monkeypatch):
     with pytest.raises(ValueError):
         f.cache_plan(pt, i32(3), 7)
     assert len(f.calls) == 1
+
+
+CACHE8 = r"""
+  fb4_cache8 c8;
+  memset(&c8, 0, sizeof c8);
+  c8.k = c8.v = c8.k_scale = c8.v_scale = room;
+  c8.n_pages = 4;
+  c8.page_tokens = 16;
+  c8.n_heads = 2;
+  c8.head_dim = 64;
+  struct Args {
+    fb4_cache8 c;
+    const int32_t *table, *kv, *start;
+    int max_pages, n, max_q;
+    const void *k, *v, *q, *gain;
+    int64_t k_ld, v_ld, q_ld, T, out_ld;
+    float eps;
+    int q_heads;
+    void* out;
+  };
+  const Args ok{c8, lens, lens, lens, 4, 2, 8, room, room, room, room, 128, 128, 64, 10, 64, 1e-6f, 1, room + 4096};
+  auto append = [&](const Args& a) {
+    return fb4_cache8_append(&ctx, &a.c, a.table, a.max_pages, a.kv, a.start, a.n, a.max_q, a.k, a.k_ld, a.v, a.v_ld, a.T, a.gain, a.eps, 0, a.q, a.q_heads,
+                             a.q_ld, a.gain, a.out, a.out_ld, 0);
+  };
+  auto attend = [&](const Args& a, float scale, int causal, int window, int dtype, int max_kv) {
+    return fb4_cache8_attention(&ctx, a.q, 128, 2, a.T, &a.c, a.table, a.max_pages, a.kv, a.start, a.n, a.max_q, max_kv, scale, causal, window, a.out, 128, dtype,
+                                0, 0, 0, 0);
+  };
+  auto both = [&](const Args& a, int code) { return append(a) == code && attend(a, 0.1f, 1, 0, 1, 64) == code && fb4_cache8_values(&ctx, &a.c, room, room, 0, 0) == code; };
+  ctx.attend_error = cudaErrorInvalidConfiguration;
+  if (attend(ok, 0.1f, 1, 0, 1, 64) != FB4_ERR_CUDA || fb4_last_cuda_error() != (int)cudaErrorInvalidConfiguration) return 1;
+  Args a = ok;
+  for (int page : {0, 8, 24, 8192}) { a.c.page_tokens = page; if (!both(a, FB4_ERR_SHAPE)) return 2; }
+  for (int D : {0, 16, 48, 288}) { a = ok; a.c.head_dim = D; if (!both(a, FB4_ERR_SHAPE)) return 3; }
+  for (int h : {0, 1025}) { a = ok; a.c.n_heads = h; if (!both(a, FB4_ERR_SHAPE)) return 4; }
+  for (int64_t n : {0LL, -1LL, 1LL << 37}) { a = ok; a.c.n_pages = n; if (!both(a, FB4_ERR_SHAPE)) return 5; }
+  a = ok; a.c.k = 0; if (!both(a, FB4_ERR_INVALID_ARG)) return 6;
+  a = ok; a.c.v_scale = 0; if (!both(a, FB4_ERR_INVALID_ARG)) return 7;
+  a = ok; a.c.v = room + 8; if (!both(a, FB4_ERR_ALIGN)) return 8;
+  a = ok; a.T = -1; if (append(a) != FB4_ERR_SHAPE) return 9;
+  a = ok; a.n = -1; if (append(a) != FB4_ERR_SHAPE) return 10;
+  a = ok; a.n = (1 << 28) + 1; if (append(a) != FB4_ERR_SHAPE) return 11;
+  a = ok; a.max_q = -1; if (append(a) != FB4_ERR_SHAPE) return 12;
+  a = ok; a.table = 0; if (append(a) != FB4_ERR_INVALID_ARG) return 13;
+  a = ok; a.kv = 0; if (append(a) != FB4_ERR_INVALID_ARG) return 14;
+  a = ok; a.k = 0; if (append(a) != FB4_ERR_INVALID_ARG) return 15;
+  a = ok; a.k_ld = 120; if (append(a) != FB4_ERR_SHAPE) return 16;
+  a = ok; a.v_ld = 132; if (append(a) != FB4_ERR_ALIGN) return 17;
+  a = ok; a.q = 0; if (append(a) != FB4_ERR_INVALID_ARG) return 18;
+  a = ok; a.out = room + 8; if (append(a) != FB4_ERR_ALIGN) return 19;
+  a = ok; a.gain = room + 2; if (append(a) != FB4_ERR_ALIGN) return 20;
+  a = ok; a.eps = -1.0f; if (append(a) != FB4_ERR_INVALID_ARG) return 21;
+  a = ok; a.q_heads = 1025; if (append(a) != FB4_ERR_SHAPE) return 22;
+  a = ok; a.q = a.out; a.q_ld = 72; if (append(a) != FB4_ERR_INVALID_ARG) return 23;                     // in place with another stride
+  a = ok; a.start = reinterpret_cast<const int32_t*>(room + 2); if (append(a) != FB4_ERR_ALIGN) return 24;
+  for (int none = 0; none < 4; ++none) {                                                               // nothing to do
+    a = ok;
+    (none == 0 ? a.n : none == 1 ? a.max_q : a.max_pages) = 0;
+    if (none == 3) a.T = 0;
+    if (append(a) != FB4_OK) return 25;
+  }
+  if (fb4_cache8_values(&ctx, &c8, 0, room, 0, 0) != FB4_ERR_INVALID_ARG || fb4_cache8_values(&ctx, &c8, room, room + 8, 0, 0) != FB4_ERR_ALIGN) return 26;
+  if (fb4_cache8_values(&ctx, &c8, room, room, 3, 0) != FB4_ERR_INVALID_ARG) return 27;
+  if (attend(ok, 0.1f, 2, 0, 1, 64) != FB4_ERR_INVALID_ARG || attend(ok, 0.1f, 1, -1, 1, 64) != FB4_ERR_INVALID_ARG || attend(ok, 0.1f, 1, 0, 3, 64) != FB4_ERR_INVALID_ARG) return 28;
+  if (attend(ok, 0x1p61f, 1, 0, 1, 64) != FB4_ERR_INVALID_ARG || attend(ok, 0.0f / 0.0f, 1, 0, 1, 64) != FB4_ERR_INVALID_ARG) return 29;
+  if (attend(ok, 0.1f, 1, 0, 1, (1 << 30) + 1) != FB4_ERR_SHAPE) return 30;
+  if (fb4_cache8_attention_workspace(&ctx, 3, 2, 64, 1, 1, 1, 0) != -1 || fb4_cache8_attention_workspace(0, 2, 2, 64, 1, 1, 1, 0) != -1) return 31;
+  if (fb4_cache8_append(0, &c8, lens, 4, lens, lens, 2, 8, room, 128, room, 128, 10, 0, 0.0f, 0, 0, 0, 0, 0, 0, 0, 0) != FB4_ERR_INVALID_ARG) return 32;
+  if (ctx.launches != 0) return 33;
+  puts("ok");
+  return 0;
+}
+"""
+
+
+def test_cache8_refusals(tmp_path):
+    run(tmp_path, CACHE8)
+
+
+def cache8(monkeypatch, n=4, heads=2, page=16, D=64):
+    monkeypatch.setattr(fb4, "_device_of", lambda *t: -1)
+    codes, scale = torch.zeros(n, heads, page, D, dtype=torch.uint8), torch.zeros(n, heads, page // 16, dtype=torch.uint8)
+    return fb4.Cache8(codes, scale, codes.clone(), scale.clone())
+
+
+def test_cache8_in_the_binding(monkeypatch):
+    f = context(monkeypatch)
+    c = cache8(monkeypatch)
+    u8 = lambda *s: torch.zeros(s, dtype=torch.uint8)  # noqa: E731
+    for bad in ((u8(4, 2, 16), u8(4, 2, 1)), (u8(4, 2, 16, 64).short(), u8(4, 2, 1)), (u8(4, 2, 16, 64), u8(4, 2, 2)), (u8(4, 2, 64, 16).transpose(2, 3), u8(4, 2, 1))):
+        with pytest.raises(ValueError):
+            fb4.Cache8(*bad, u8(4, 2, 16, 64), u8(4, 2, 1))
+    kv = torch.zeros(5, 2, 64, dtype=torch.bfloat16)
+    ok = (c, kv, kv, i32(3, 4), i32(3), i32(4), 2)
+    assert f.cache8_append(*ok) is None and f.cache8_append(*ok, q=torch.zeros(5, 6, 64, dtype=torch.bfloat16)).shape == (5, 6, 64)
+    n = len(f.calls)
+    swap = lambda at, x: tuple(x if i == at else y for i, y in enumerate(ok))  # noqa: E731
+    for args, more in ((swap(1, kv[:, :1]), {}), (swap(1, kv.float()), {}), (swap(2, kv[:4]), {}), (swap(3, i32(2, 4)), {}), (swap(4, i32(3).long()), {}), (swap(5, i32(3)), {}),
+                       (swap(6, 1 << 31), {}), (swap(6, -1), {}), (ok, dict(q=kv[:4])), (ok, dict(k_gain=kv[0, 0, :32])), (ok, dict(q=kv, q_gain=kv[0, 0].float()))):
+        with pytest.raises(ValueError):
+            f.cache8_append(*args, **more)
+    for bad in (torch.float64, torch.int8, None):
+        with pytest.raises(ValueError):
+            f.cache8_values(c, bad)
+        with pytest.raises(ValueError):
+            f.cache8_attention(kv, c, i32(3, 4), i32(3), i32(4), 2, 16, dtype=bad)
+    with pytest.raises(ValueError):
+        f.cache8_attention(kv[..., :32], c, i32(3, 4), i32(3), i32(4), 2, 16)
+    assert len(f.calls) == n
