@@ -26,10 +26,11 @@ using namespace fb4att;
 constexpr int kWarpsFew = 4;
 constexpr int kTile = 32;              // tokens of a warp's tile
 
-template <int D>
+template <int D, bool INT8>
 struct Few {
-  static constexpr int kStagesFew = D == 128 ? 2 : 4;
-  static constexpr int kCodes = kTile * D / 2, kMeta = kTile * (D / 32) * 2;
+  static constexpr int kStagesFew = D == 128 ? 2 : INT8 ? 3 : 4;
+  static constexpr int kRow = INT8 ? D : D / 2;                            // bytes of a token's codes
+  static constexpr int kCodes = kTile * kRow, kMeta = INT8 ? 0 : kTile * (D / 32) * 2;
   static constexpr int kStage = 2 * kCodes + 2 * kMeta;
   static constexpr int kRing = kWarpsFew * kStagesFew * kStage;
   // the join of the warps reuses the ring: 16 rows of D sums per warp, and once more for their sum
@@ -58,9 +59,12 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
 }
 
-template <int D, int NT, bool CLUSTER>
-__global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_few_kernel(const __grid_constant__ Fb4Attend a) {
-  using L = Few<D>;
+// CTAs per SM: registers, or with the 8-bit cache and D = 128 the ring (64 KB a CTA)
+constexpr int resident(int D, int NT, bool int8) { return NT == 1 && !(int8 && D == 128) ? 4 : 3; }
+
+template <int D, int NT, bool CLUSTER, bool INT8>
+__global__ void __launch_bounds__(kWarpsFew * 32, resident(D, NT, INT8)) fb4_attend_few_kernel(const __grid_constant__ Fb4Attend a) {
+  using L = Few<D, INT8>;
   constexpr int NW = D / 32;             // code words of a lane's quarter row
   constexpr int ST = L::kStagesFew;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -90,8 +94,10 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
   const int32_t tile0 = (int32_t)((int64_t)rounds * split / a.splits) * kWarpsFew;
   const int32_t end = (int32_t)((int64_t)rounds * (split + 1) / a.splits) * kWarpsFew, tile1 = end < tiles ? end : tiles;
 
-  if (threadIdx.x < 64) fill_book(book, a.tables, threadIdx.x);
-  __syncthreads();
+  if (!INT8) {
+    if (threadIdx.x < 64) fill_book(book, a.tables, threadIdx.x);
+    __syncthreads();
+  }
   const uint32_t ring = fb4blk::smem_u32(smem) + warp * ST * L::kStage;
   const uint32_t book_at = fb4blk::smem_u32(book);
 
@@ -99,6 +105,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
   const int32_t n_mine = tile0 + warp >= tile1 ? 0 : (tile1 - tile0 - warp + kWarpsFew - 1) / kWarpsFew;
   const int32_t my0 = tile0 + warp;
   int32_t page_lo = -1, page_hi = -1;
+  uint32_t scales = 0;                     // 8 bits: the scale bytes of K (first half, second half) and V
   bool bad = false;
   auto fetch_pages = [&](int32_t from) {
     page_lo = page_hi = -1;
@@ -111,17 +118,28 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
       if (hi_seen) page_hi = __ldg(pt + ((j + 16) >> a.page_shift));
       if (lo_seen && (uint32_t)page_lo >= (uint64_t)a.cache.n_pages) { bad = true; page_lo = -1; }
       if (hi_seen && (uint32_t)page_hi >= (uint64_t)a.cache.n_pages) { bad = true; page_hi = -1; }
+      if constexpr (INT8) {
+        auto byte_at = [&](int32_t page, int32_t jj) -> int64_t {
+          return (((int64_t)page * a.cache.n_heads + head) << (a.page_shift - 4)) + ((jj & ((1 << a.page_shift) - 1)) >> 4);
+        };
+        scales = 0;
+        if (page_lo >= 0) scales = (uint32_t)__ldg(a.k_scale + byte_at(page_lo, j)) | (uint32_t)__ldg(a.v_scale + byte_at(page_lo, j)) << 16;
+        if (page_hi >= 0) scales |= (uint32_t)__ldg(a.k_scale + byte_at(page_hi, j + 16)) << 8 | (uint32_t)__ldg(a.v_scale + byte_at(page_hi, j + 16)) << 24;
+      }
     }
   };
   // Requests tile n of this warp into ring stage `st`.  Codes: lane l copies bytes 16 l .. 16 l + 15 of every 512; metadata:
   // K in lanes 0 to 15, V behind, each half of the tile in 8 (D = 128) or 4 of them.  `have`: 2 bits per stage, the halves whose
-  // pages exist.
+  // pages exist.  8 bits: returns the tile's scale bytes; the 16-byte pieces of odd rows of 128 are exchanged in pairs, so that the two rows
+  // that eight lanes read together lie in different banks.
   uint32_t have = 0;
   const uint32_t page_mask = (1u << a.page_shift) - 1u;
   const int mh = (lane / (D / 16)) & 1, mv = lane / (D / 8);          // half and array of this lane's piece of the metadata
   const uint8_t* meta_src = reinterpret_cast<const uint8_t*>(mv ? a.cache.v_meta : a.cache.k_meta) + (lane & (D / 16 - 1)) * 16;
   const uint32_t meta_dst = 2 * L::kCodes + mv * L::kMeta + mh * (L::kMeta / 2) + (lane & (D / 16 - 1)) * 16;
-  auto request = [&](int32_t n, int st) {
+  const uint32_t lane_dst = (lane * 16) ^ (INT8 && D == 128 ? (lane & 8) << 1 : 0);
+  auto request = [&](int32_t n, int st) -> uint32_t {
+    uint32_t sc = 0;
     if (n < n_mine) {
       if ((n & 31) == 0) fetch_pages(n);
       const int32_t plo = __shfl_sync(0xffffffffu, page_lo, n & 31), phi = __shfl_sync(0xffffffffu, page_hi, n & 31);
@@ -135,16 +153,19 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
         const uint8_t* codes = (v ? a.cache.v_codes : a.cache.k_codes) + lane * 16;
 #pragma unroll
         for (int i = 0; i < L::kCodes / 2; i += 512) {
-          copy16(dst + v * L::kCodes + i + lane * 16, codes + rlo * (D / 2) + i, plo >= 0);
-          copy16(dst + v * L::kCodes + L::kCodes / 2 + i + lane * 16, codes + rhi * (D / 2) + i, phi >= 0);
+          copy16(dst + v * L::kCodes + i + lane_dst, codes + rlo * L::kRow + i, plo >= 0);
+          copy16(dst + v * L::kCodes + L::kCodes / 2 + i + lane_dst, codes + rhi * L::kRow + i, phi >= 0);
         }
       }
-      if (D == 128 || lane < 16) copy16(dst + meta_dst, meta_src + (mh ? rhi : rlo) * (D / 16), (mh ? phi : plo) >= 0);
+      if (INT8) sc = __shfl_sync(0xffffffffu, scales, n & 31);
+      else if (D == 128 || lane < 16) copy16(dst + meta_dst, meta_src + (mh ? rhi : rlo) * (D / 16), (mh ? phi : plo) >= 0);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");               // empty behind the last tile: the count of groups stays
+    return sc;
   };
+  uint32_t sc[ST];                         // 8 bits: scale bytes of the tiles from the present one on
 #pragma unroll
-  for (int n = 0; n < ST - 1; ++n) request(n, n);
+  for (int n = 0; n < ST - 1; ++n) sc[n] = request(n, n);
 
   // Q as the B side of S^T = K Q^T: lane (g, t) holds query row0 + 8 nt + g, channels of quarter t
   uint32_t qf[NT][NW][4];
@@ -196,7 +217,7 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
   bool huge = false;       // some row's maximum is beyond_fused
   int st = 0, ahead = ST - 1;
   for (int32_t n = 0; n < n_mine; ++n) {
-    request(n + ST - 1, ahead);
+    sc[ST - 1] = request(n + ST - 1, ahead);
     asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
     __syncwarp();          // every lane's copies of this tile have landed
     const uint32_t codes = ring + st * L::kStage, meta = codes + 2 * L::kCodes;
@@ -204,8 +225,14 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
     const uint32_t here = (have >> (2 * st)) & 3u;
     const bool whole = j0 >= lo_max && j0 + kTile <= hi_min && here == 3u;      // nothing of the tile is masked for any row
 
-    auto words = [&](uint32_t at, uint32_t (&w)[NW]) {
-      if (NW == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[NW - 2]), "=r"(w[NW - 1]) : "r"(at));
+    constexpr int WR = INT8 ? 2 * NW : NW; // words of a lane's quarter row
+    auto words = [&](uint32_t array, int row, uint32_t (&w)[WR]) {
+      const uint32_t at = array + row * L::kRow + t * (L::kRow / 4);
+      if constexpr (WR == 8) {
+        const uint32_t odd = (g & 1) * 16;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at + odd));
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(at + (16 - odd)));
+      } else if (WR == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[WR - 2]), "=r"(w[WR - 1]) : "r"(at));
       else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
     };
     auto record = [&](uint32_t at) -> uint32_t {
@@ -224,16 +251,27 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
 #pragma unroll
         for (int k = 0; k < 4; ++k) s[h][nt][k] = 0.0f;
       const int ra = 16 * h + g, rb = ra + 8;
-      uint32_t wa[NW], wb[NW];
-      words(codes + ra * (D / 2) + t * (D / 8), wa);
-      words(codes + rb * (D / 2) + t * (D / 8), wb);
-      const BlockScale sa = block_scale(record(meta + meta_at(ra)), book_at, true);
-      const BlockScale sb = block_scale(record(meta + meta_at(rb)), book_at, true);
+      uint32_t wa[WR], wb[WR];
+      words(codes, ra, wa);
+      words(codes, rb, wb);
+      BlockScale sa, sb;
+      Int8Scale s8;
+      if (INT8) {
+        s8 = int8_scale((sc[0] >> (8 * h)) & 255u, true);
+      } else {
+        sa = block_scale(record(meta + meta_at(ra)), book_at, true);
+        sb = block_scale(record(meta + meta_at(rb)), book_at, true);
+      }
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
         uint32_t ka[4], kb[4];
-        decode_word(wa[w], sa, ka);
-        decode_word(wb[w], sb, kb);
+        if constexpr (INT8) {
+          decode_bytes(wa[2 * w], wa[2 * w + 1], s8, ka);
+          decode_bytes(wb[2 * w], wb[2 * w + 1], s8, kb);
+        } else {
+          decode_word(wa[w], sa, ka);
+          decode_word(wb[w], sb, kb);
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           mma_bf16(s[h][nt], ka[0], kb[0], ka[1], kb[1], qf[nt][w][0], qf[nt][w][1]);
@@ -312,18 +350,29 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int ra = 16 * h + g, rb = ra + 8;
-      uint32_t wa[NW], wb[NW];
-      words(codes + L::kCodes + ra * (D / 2) + t * (D / 8), wa);
-      words(codes + L::kCodes + rb * (D / 2) + t * (D / 8), wb);
-      // slots that no token fills may hold anything; an infinity there would meet p = 0
-      const bool ua = whole || (j0 + ra < sq.kv && ((here >> h) & 1u)), ub = whole || (j0 + rb < sq.kv && ((here >> h) & 1u));
-      const BlockScale sa = block_scale(ua ? record(meta + L::kMeta + meta_at(ra)) : 0u, book_at, ua);
-      const BlockScale sb = block_scale(ub ? record(meta + L::kMeta + meta_at(rb)) : 0u, book_at, ub);
+      uint32_t wa[WR], wb[WR];
+      words(codes + L::kCodes, ra, wa);
+      words(codes + L::kCodes, rb, wb);
+      BlockScale sa, sb;
+      Int8Scale s8;
+      if (INT8) {          // whatever a slot that no token fills holds is finite, and meets p = 0
+        s8 = int8_scale((sc[0] >> (16 + 8 * h)) & 255u, true);
+      } else {
+        // slots that no token fills may hold anything; an infinity there would meet p = 0
+        const bool ua = whole || (j0 + ra < sq.kv && ((here >> h) & 1u)), ub = whole || (j0 + rb < sq.kv && ((here >> h) & 1u));
+        sa = block_scale(ua ? record(meta + L::kMeta + meta_at(ra)) : 0u, book_at, ua);
+        sb = block_scale(ub ? record(meta + L::kMeta + meta_at(rb)) : 0u, book_at, ub);
+      }
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
         uint32_t va[4], vb[4];
-        decode_word(wa[w], sa, va);
-        decode_word(wb[w], sb, vb);
+        if constexpr (INT8) {
+          decode_bytes(wa[2 * w], wa[2 * w + 1], s8, va);
+          decode_bytes(wb[2 * w], wb[2 * w + 1], s8, vb);
+        } else {
+          decode_word(wa[w], sa, va);
+          decode_word(wb[w], sb, vb);
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           va[k] = transpose8x8(va[k]);
@@ -339,6 +388,8 @@ __global__ void __launch_bounds__(kWarpsFew * 32, NT == 1 ? 4 : 3) fb4_attend_fe
     __syncwarp();          // the stage may be filled again
     st = st + 1 == ST ? 0 : st + 1;
     ahead = ahead + 1 == ST ? 0 : ahead + 1;
+#pragma unroll
+    for (int k = 0; k + 1 < ST; ++k) sc[k] = sc[k + 1];
   }
   if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, 2u);
 
@@ -545,13 +596,13 @@ cudaError_t launch_with(void (*kernel)(Args...), int64_t grid, int threads, int 
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <int D, int NT>
+template <int D, int NT, bool INT8>
 cudaError_t launch(const Fb4Attend& a, cudaStream_t stream) {
   const int64_t row_tiles = ((int64_t)a.max_q * a.group + 8 * NT - 1) / (8 * NT);
   const int64_t grid = row_tiles * a.splits * a.cache.n_heads * a.n_seqs;
   if (a.splits > 1 && !a.partial)
-    return launch_with(fb4_attend_few_kernel<D, NT, true>, grid, kWarpsFew * 32, Few<D>::kBytes, a.splits, false, stream, a);
-  return launch_with(fb4_attend_few_kernel<D, NT, false>, grid, kWarpsFew * 32, Few<D>::kBytes, 1, false, stream, a);
+    return launch_with(fb4_attend_few_kernel<D, NT, true, INT8>, grid, kWarpsFew * 32, Few<D, INT8>::kBytes, a.splits, false, stream, a);
+  return launch_with(fb4_attend_few_kernel<D, NT, false, INT8>, grid, kWarpsFew * 32, Few<D, INT8>::kBytes, 1, false, stream, a);
 }
 
 template <int D>
@@ -566,13 +617,17 @@ cudaError_t launch_join(const Fb4Attend& a, cudaStream_t stream) {
 cudaError_t fb4_attend_prepare_device() {
   const cudaFuncAttribute attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e = cudaSuccess;
-#define FB4_OPT_IN(D, NT) \
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<D, NT, false>, attr, Few<D>::kBytes); \
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<D, NT, true>, attr, Few<D>::kBytes)
-  FB4_OPT_IN(128, 1);
-  FB4_OPT_IN(128, 2);
-  FB4_OPT_IN(64, 1);
-  FB4_OPT_IN(64, 2);
+#define FB4_OPT_IN(D, NT, INT8) \
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<D, NT, false, INT8>, attr, Few<D, INT8>::kBytes); \
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_few_kernel<D, NT, true, INT8>, attr, Few<D, INT8>::kBytes)
+  FB4_OPT_IN(128, 1, false);
+  FB4_OPT_IN(128, 2, false);
+  FB4_OPT_IN(64, 1, false);
+  FB4_OPT_IN(64, 2, false);
+  FB4_OPT_IN(128, 1, true);
+  FB4_OPT_IN(128, 2, true);
+  FB4_OPT_IN(64, 1, true);
+  FB4_OPT_IN(64, 2, true);
 #undef FB4_OPT_IN
   if (e == cudaSuccess) e = fb4_attend_many_prepare_device();
   return e;
@@ -581,7 +636,6 @@ cudaError_t fb4_attend_prepare_device() {
 Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int int8, int32_t q_heads, int32_t n_heads, int32_t head_dim, int32_t n_seqs,
                               int32_t max_q, int32_t max_kv, int32_t window) {
   Fb4AttendPlan p{0, 1, 0x7fffffff / 64, 0};
-  if (int8) return p;
   if ((head_dim != 64 && head_dim != 128) || ctx->force_generic || n_seqs == 0 || max_q == 0) return p;
   const int64_t rows = (int64_t)max_q * (q_heads / n_heads);
   // the longest run of tokens that a CTA's rows can see together
@@ -594,7 +648,7 @@ Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int int8, int32_t q_heads, int
     const int64_t nt = rows <= 8 ? 1 : 2;
     const int64_t units = (rows + 8 * nt - 1) / (8 * nt) * n_heads * n_seqs;
     // CTAs that are resident at a time; a split has at least 2 tiles for each of its warps
-    const int64_t slots = (int64_t)ctx->sm_count * (nt == 1 ? 4 : 3);
+    const int64_t slots = (int64_t)ctx->sm_count * resident(head_dim, (int)nt, int8 != 0);
     const int64_t tiles = (span + kTile - 1) / kTile + 1;
     const int64_t most = (tiles + 2 * kWarpsFew - 1) / (2 * kWarpsFew);
     int64_t s = slots / units;                                      // one wave
@@ -630,8 +684,12 @@ Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int int8, int32_t q_heads, int
 
 cudaError_t fb4_launch_attend_few(const Fb4Attend& a, cudaStream_t stream) {
   const bool wide = (int64_t)a.max_q * a.group > 8;
-  if (a.cache.head_dim == 128) return wide ? launch<128, 2>(a, stream) : launch<128, 1>(a, stream);
-  return wide ? launch<64, 2>(a, stream) : launch<64, 1>(a, stream);
+  if (a.int8) {
+    if (a.cache.head_dim == 128) return wide ? launch<128, 2, true>(a, stream) : launch<128, 1, true>(a, stream);
+    return wide ? launch<64, 2, true>(a, stream) : launch<64, 1, true>(a, stream);
+  }
+  if (a.cache.head_dim == 128) return wide ? launch<128, 2, false>(a, stream) : launch<128, 1, false>(a, stream);
+  return wide ? launch<64, 2, false>(a, stream) : launch<64, 1, false>(a, stream);
 }
 
 cudaError_t fb4_launch_attend_join(const Fb4Attend& a, cudaStream_t stream) {

@@ -50,18 +50,20 @@ constexpr int kThreads = 512;          // two warpgroups of softmax, one of deco
 // warpgroup give back is what the softmax warps, which keep a row's 128 scores in registers, take: 2 * 200 + 72 + 40 = 4 * 128.
 constexpr int kLaunchRegs = 128, kSoftmaxRegs = 200, kDecodeRegs = 72, kOtherRegs = 40;
 static_assert(2 * kSoftmaxRegs + kDecodeRegs + kOtherRegs <= 4 * kLaunchRegs, "register shares of the warpgroups");
-constexpr int kRing = 3;               // ring stages: a K or a V tile's codes and metadata each
+constexpr int kMaxRing = 3;
 constexpr int kHave = 8;               // tiles whose page flags are kept
 
-template <int D>
+template <int D, bool INT8>
 struct Many {
+  static constexpr int kRing = INT8 && D == 128 ? 2 : kMaxRing;     // ring stages: a K or a V tile's codes and metadata each
   static constexpr int kTileBytes = kKeys * D * 2;                  // one decoded tile, or one query tile
-  static constexpr int kCodes = kKeys * D / 2, kMeta = kKeys * (D / 32) * 2, kStage = kCodes + kMeta;
+  static constexpr int kRow = INT8 ? D : D / 2, kMetaRow = INT8 ? 0 : D / 16;   // bytes of a token's codes and metadata
+  static constexpr int kCodes = kKeys * kRow, kMeta = kKeys * kMetaRow, kStage = kCodes + kMeta;
   static constexpr int kBytes = 1024 + 2 * kTileBytes + 4 * kTileBytes + kRing * kStage;
 };
 
 struct Bars {
-  uint64_t ring_full[kRing], ring_empty[kRing];
+  uint64_t ring_full[kMaxRing], ring_empty[kMaxRing];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t q_full, s_full[2], s_free, p_half[2], p_full[2], o_done[2], drained;
 };
@@ -193,10 +195,10 @@ struct RowAt {
   }
 };
 
-template <int D>
+template <int D, bool INT8>
 __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __grid_constant__ Fb4Attend a) {
-  using L = Many<D>;
-  constexpr int NB = D / 32;
+  using L = Many<D, INT8>;
+  constexpr int NB = D / 32, kRing = L::kRing;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Bars bars;
   __shared__ uint32_t book[64];
@@ -254,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_at)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
-  if (threadIdx.x >= 64 && threadIdx.x < 128) fill_book(book, a.tables, threadIdx.x - 64);
+  if (!INT8 && threadIdx.x >= 64 && threadIdx.x < 128) fill_book(book, a.tables, threadIdx.x - 64);
   fence_before();
   __syncthreads();
   fence_after();
@@ -468,6 +470,25 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
     const int dw = warp - kSoftmaxWarps;
     const uint32_t book_at = smem_u32(book);
     bool ok = true;
+    // 8 bits: this lane's token of a tile is 32 dw + lane; its scale bytes are loaded a tile ahead, and their page two tiles ahead
+    int32_t page_next = -1;
+    uint32_t k_byte = 0, v_byte = 0, k_next = 0, v_next = 0;
+    auto page_of = [&](int32_t t) -> int32_t {
+      const int32_t j = base + (t0 + t) * kKeys + dw * 32 + (lane & 16);
+      if (t >= n_tiles || j >= last.hi || j + 16 <= first.lo) return -1;      // pages in front of a window may be gone
+      return __ldg(a.page_table + (int64_t)b * a.max_pages + (j >> a.page_shift));
+    };
+    auto scales_of = [&](int32_t t, int32_t page, uint32_t& k8, uint32_t& v8) {
+      if ((uint32_t)page >= (uint64_t)a.cache.n_pages) return;                // nothing of it counts; any scale will do
+      const int32_t j = base + (t0 + t) * kKeys + dw * 32 + (lane & 16);
+      const int64_t at = (((int64_t)page * a.cache.n_heads + head) << (a.page_shift - 4)) + ((j & ((1 << a.page_shift) - 1)) >> 4);
+      k8 = __ldg(a.k_scale + at);
+      v8 = __ldg(a.v_scale + at);
+    };
+    if (INT8) {
+      scales_of(0, page_of(0), k_next, v_next);
+      page_next = page_of(1);
+    }
     for (int32_t part = 0; part < 2 * n_tiles && ok; ++part) {
       const int32_t t = part >> 1;
       const bool is_v = part & 1;
@@ -476,6 +497,36 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
       if (!ok) break;
       const uint32_t codes = ring_at + st * L::kStage, meta = codes + L::kCodes;
       const uint32_t dst = (is_v ? v_at : k_at) + buf * L::kTileBytes;
+      if constexpr (INT8) {
+        if (!is_v) {
+          k_byte = k_next;
+          v_byte = v_next;
+          scales_of(t + 1, page_next, k_next, v_next);
+          page_next = page_of(t + 2);
+        }
+        // 16 channels of a row per task; which, varies with the row so that neither side has bank conflicts (a row is 128 or 64 bytes
+        // of codes, and its runs of 8 channels are swizzled by the row)
+        constexpr int kTasks = D / 16;
+        const int row = dw * 32 + lane;
+        const int mix = D == 128 ? lane & 7 : (lane & 2) | (((lane >> 1) ^ (lane >> 2)) & 1);
+        uint32_t cw[kTasks][4];
+#pragma unroll
+        for (int k = 0; k < kTasks; ++k)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cw[k][0]), "=r"(cw[k][1]), "=r"(cw[k][2]), "=r"(cw[k][3]) : "r"(codes + row * D + (k ^ mix) * 16));
+        const Int8Scale sc = int8_scale(is_v ? v_byte : k_byte, true);          // whatever a slot that no token fills holds is finite
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.ring_empty[st]));
+        if (t >= 2) ok = __all_sync(0xffffffffu, wait(smem_u32(is_v ? &bars.v_empty[buf] : &bars.k_empty[buf]), ((t >> 1) - 1) & 1, dead));
+        if (!ok) break;
+#pragma unroll
+        for (int k = 0; k < kTasks; ++k)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            uint32_t o[4];
+            decode_bytes(cw[k][2 * q], cw[k][2 * q + 1], sc, o);
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + swizzled(row, 2 * (k ^ mix) + q)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+          }
+      } else {
       const uint32_t here = *(volatile uint32_t*)&have[t % kHave];
       const int32_t j0 = base + (t0 + t) * kKeys;
       // 32 rows and one block of each per task; the block varies with the row so that neither side has bank conflicts.  All loads
@@ -509,6 +560,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
           decode_word(cw[k][q], sc[k], o);
           asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + swizzled(row_of(k), 4 * block_of(k) + q)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
         }
+      }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(is_v ? &bars.v_full[buf] : &bars.k_full[buf]));
@@ -600,12 +652,12 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         const uint32_t full = smem_u32(&bars.ring_full[st]), dst = ring_at + st * L::kStage;
         if (lane == 0) {
           if (kv == 0) *(volatile uint32_t*)&have[t % kHave] = flags;
-          mbar_expect_tx(full, (uint32_t)__popc(there) * piece_tokens * (D / 2 + D / 16));
+          mbar_expect_tx(full, (uint32_t)__popc(there) * piece_tokens * (L::kRow + L::kMetaRow));
         }
         __syncwarp();
         if (page >= 0) {
-          bulk_load(dst + lane * piece_tokens * (D / 2), (kv ? a.cache.v_codes : a.cache.k_codes) + row * (D / 2), piece_tokens * (D / 2), full);
-          bulk_load(dst + L::kCodes + lane * piece_tokens * (D / 16), (kv ? a.cache.v_meta : a.cache.k_meta) + row * NB, piece_tokens * (D / 16), full);
+          bulk_load(dst + lane * piece_tokens * L::kRow, (kv ? a.cache.v_codes : a.cache.k_codes) + row * L::kRow, piece_tokens * L::kRow, full);
+          if (!INT8) bulk_load(dst + L::kCodes + lane * piece_tokens * (D / 16), (kv ? a.cache.v_meta : a.cache.k_meta) + row * NB, piece_tokens * (D / 16), full);
         }
       }
     }
@@ -629,22 +681,32 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
 }  // namespace
 
 cudaError_t fb4_attend_many_prepare_device() {
-  const cudaFuncAttribute attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(fb4_attend_many_kernel<128>, attr, Many<128>::kBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_attend_many_kernel<64>, attr, Many<64>::kBytes);
+  cudaError_t e = cudaSuccess;
   // the register shares count on what the block is launched with
-  cudaFuncAttributes fa{};
-  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, fb4_attend_many_kernel<128>);
-  if (e == cudaSuccess && fa.numRegs < kLaunchRegs) e = cudaErrorInvalidConfiguration;
-  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, fb4_attend_many_kernel<64>);
-  if (e == cudaSuccess && fa.numRegs < kLaunchRegs) e = cudaErrorInvalidConfiguration;
+  auto prepare = [&](void (*kernel)(Fb4Attend), int smem) {
+    cudaFuncAttributes fa{};
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, kernel);
+    if (e == cudaSuccess && fa.numRegs < kLaunchRegs) e = cudaErrorInvalidConfiguration;
+  };
+  prepare(fb4_attend_many_kernel<128, false>, Many<128, false>::kBytes);
+  prepare(fb4_attend_many_kernel<64, false>, Many<64, false>::kBytes);
+  prepare(fb4_attend_many_kernel<128, true>, Many<128, true>::kBytes);
+  prepare(fb4_attend_many_kernel<64, true>, Many<64, true>::kBytes);
   return e;
 }
 
 cudaError_t fb4_launch_attend_many(const Fb4Attend& a, cudaStream_t stream) {
   const int64_t row_tiles = ((int64_t)a.max_q * a.group + 255) / 256;
   const int64_t grid = row_tiles * a.splits * a.cache.n_heads * a.n_seqs;
-  if (a.cache.head_dim == 128) fb4_attend_many_kernel<128><<<(unsigned)grid, kThreads, Many<128>::kBytes, stream>>>(a);
-  else fb4_attend_many_kernel<64><<<(unsigned)grid, kThreads, Many<64>::kBytes, stream>>>(a);
+#define FB4_MANY(D, INT8) fb4_attend_many_kernel<D, INT8><<<(unsigned)grid, kThreads, Many<D, INT8>::kBytes, stream>>>(a)
+  if (a.cache.head_dim == 128) {
+    if (a.int8) FB4_MANY(128, true);
+    else FB4_MANY(128, false);
+  } else {
+    if (a.int8) FB4_MANY(64, true);
+    else FB4_MANY(64, false);
+  }
+#undef FB4_MANY
   return cudaGetLastError();
 }
