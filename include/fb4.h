@@ -334,6 +334,22 @@ int fb4_quantize_weights(fb4_ctx* ctx, const void* w_bf16, int64_t N, int64_t K,
                          uint16_t* meta, void* stream);
 
 /*
+ * Products of rows of x with FB4 weights (App. D.2: 4-bit codes are decoded on the fly with the block scale applied):
+ *     out[t][n] = sum_k x[t][k] * w[n][k] + bias[n],   w = value(codes, meta) of fb4_quantize_weights (or fb4_quantize)
+ * without the weights ever being written out: 4.5 bits of memory traffic per weight.  Made for few rows (single and drafted tokens of a decoding
+ * batch); any number is taken, and every 64 rows read the weights again.  Products are exact, sums float32 in an order that depends on
+ * the sizes alone, the result is rounded once to the type of out.  A row of x that holds an infinity or NaN affects its own row of out only.
+ *   x       : device bfloat16 [T][ld_elems], T at most 2^22, 16-byte aligned, ld_elems a multiple of 8 (>= K)
+ *   codes, meta : device [N][K/2], [N][K/32], 16-byte aligned; K a multiple of 32, at least 32.  An element scale above 2^61 is read as
+ *             2^61, a weight to within 2^-70, and the sums are in steps of 2^-85 where they are smaller than float32 steps
+ *   bias    : device bfloat16 [N], or NULL
+ *   out     : device [T][out_ld] (out_ld >= N), out_dtype 0 = float32, 1 = bfloat16, 2 = IEEE half; 16-byte aligned; must not overlap x
+ * Needs block size 32 (FB4_ERR_INVALID_ARG otherwise); the context's formatbook decodes the weights.
+ */
+int fb4_linear(fb4_ctx* ctx, const void* x_bf16, int64_t T, int64_t K, int64_t ld_elems, const uint8_t* codes, const uint16_t* meta,
+               int64_t N, const void* bias_bf16, void* out, int64_t out_ld, int out_dtype, void* stream);
+
+/*
  * MXFP8 view of a quantized tensor (App. D.2: every integer magnitude 0..15 is an e4m3 number and
  * the block scale is a power of two, so an FB4 tensor is an MXFP8 GEMM operand as it stands).
  * Element -> the e4m3 byte of its signed magnitude; block -> the E8M0 byte of its

@@ -306,6 +306,7 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
   ctx->append_error = fb4_rope_prepare_device();
   ctx->attend_error = fb4_attend_prepare_device();
   ctx->plan_error = fb4_plan_prepare_device();
+  ctx->linear_error = fb4_linear_prepare_device();
   ctx->fast_table_bytes = fast_bytes;
   cudaGetLastError();
   *out = ctx;
@@ -685,6 +686,21 @@ int fb4_to_mxfp8(fb4_ctx* ctx, const uint8_t* codes, const uint16_t* meta, int64
   if (!aligned16(codes) || !aligned16(meta) || !aligned16(e4m3)) return FB4_ERR_ALIGN;
   cudaError_t e = fb4_launch_to_mxfp8(ctx, codes, meta, T, C, e4m3, scales, scale_layout,
                                       static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fb4_set_cuda_error(e);
+  ctx->launches += 1;
+  return FB4_OK;
+}
+
+int fb4_linear(fb4_ctx* ctx, const void* x, int64_t T, int64_t K, int64_t ld_elems, const uint8_t* codes, const uint16_t* meta, int64_t N,
+               const void* bias, void* out, int64_t out_ld, int out_dtype, void* stream) {
+  if (!ctx || ctx->cfg.block_size != 32 || out_dtype < 0 || out_dtype > 2) return FB4_ERR_INVALID_ARG;
+  if (T < 0 || T > (1 << 22) || N < 0 || N > 0x7fffffffLL || K < 32 || K > 0x7fffffffLL || K % 32 != 0 || ld_elems < K || out_ld < N) return FB4_ERR_SHAPE;
+  if (T == 0 || N == 0) return FB4_OK;
+  if (!x || !codes || !meta || !out) return FB4_ERR_INVALID_ARG;
+  if (!aligned16(x) || (ld_elems & 7) || !aligned16(codes) || !aligned16(meta) || !aligned16(out) || (reinterpret_cast<uintptr_t>(bias) & 1u))
+    return FB4_ERR_ALIGN;
+  if (ctx->linear_error != cudaSuccess) return fb4_set_cuda_error(ctx->linear_error);
+  const cudaError_t e = fb4_launch_linear(ctx, x, T, ld_elems, codes, meta, N, K, bias, out, out_ld, out_dtype, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
   ctx->launches += 1;
   return FB4_OK;

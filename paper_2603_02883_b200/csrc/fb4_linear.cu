@@ -1,0 +1,257 @@
+// Products of few rows with FB4 weights: y[t][n] = sum_k x[t][k] w[n][k] + bias[n].
+//
+// The weights are the long side, so their rows are the M side of mma.sync m16n8k16 and up to 64 rows of x its N side: a warp reads a
+// weight once for all of them.  A lane decodes a block of 32 channels of two rows at a time from two 16-byte words of codes, straight into
+// the A fragments (which channel sits at which k is free, as long as x agrees).  x lies in shared memory in the order in which the
+// lanes read it, 16 bytes for 8 channels.
+//
+// Work: a CTA of 8 warps takes 128 rows of W (256 in warps of 32 rows, where more than 8 rows of x share the fragments) and one run of the
+// channels, the CTAs of a row tile are a cluster, which joins their sums through distributed shared memory, always in the same order.
+#include "fb4_attend.cuh"
+#include "fb4_block.cuh"
+
+namespace {
+
+using namespace fb4att;
+
+constexpr int kWarps = 8;                       // a step of a warp is 128 channels: 4 blocks, one to each lane of a quad
+__host__ __device__ constexpr int ahead(int MT) { return MT == 1 ? 4 : 2; }      // steps that are loaded ahead: 2 KB or so a warp and step
+constexpr int kMaxSplits = 8;                    // portable cluster size
+constexpr int kXBytes = 64 * 1024;               // most of x that a CTA holds at a time
+
+struct Linear {
+  const uint16_t* x;
+  int64_t ld;
+  const uint8_t* codes;
+  const uint16_t* meta;
+  const uint16_t* bias;
+  void* out;
+  int64_t out_ld;
+  int64_t T, N;
+  int32_t nb;               // blocks of a row
+  int32_t splits;           // CTAs of a cluster
+  int32_t chunk;            // steps whose x a CTA holds at a time
+  int32_t out_dtype;
+  const Fb4DeviceTables* tables;
+};
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// MT: tiles of 16 rows of W to a warp; NT: tiles of 8 rows of x
+template <int MT, int NT>
+__global__ void __launch_bounds__(kWarps * 32, 2) fb4_linear_kernel(const __grid_constant__ Linear p) {
+  constexpr int kRows = kWarps * 16 * MT, kAhead = ahead(MT);      // rows of W to a CTA
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint32_t book[64];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int32_t split = (int32_t)(blockIdx.x % p.splits);
+  const int64_t tile = blockIdx.x / p.splits;
+  const int64_t n0 = tile * kRows + warp * (16 * MT), t0 = (int64_t)blockIdx.y * (8 * NT);
+  const int32_t n_tok = (int32_t)(p.T - t0 < 8 * NT ? p.T - t0 : 8 * NT);
+  const int32_t steps = (p.nb + 3) / 4;
+  const int32_t s_begin = (int32_t)((int64_t)steps * split / p.splits), s_end = (int32_t)((int64_t)steps * (split + 1) / p.splits);
+  const uint32_t x_at = fb4blk::smem_u32(smem), book_at = fb4blk::smem_u32(book);
+  if (threadIdx.x < 64) fill_book(book, p.tables, threadIdx.x);
+
+  // this lane's rows of W; rows behind the last are computed like it and not stored
+  const uint4* codes[MT][2];
+  const uint16_t* meta[MT][2];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int64_t n = n0 + 16 * m + 8 * r + g, row = n < p.N ? n : p.N - 1;
+      codes[m][r] = reinterpret_cast<const uint4*>(p.codes) + row * p.nb + t;
+      meta[m][r] = p.meta + row * p.nb + t;
+    }
+  float acc[MT][NT][4];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[m][n][k] = 0.0f;
+
+  uint4 cw[kAhead][MT][2];
+  uint32_t mt[kAhead][MT];                          // the two rows' metadata
+  auto load = [&](int32_t s, int at) {
+    const bool there = 4 * s + t < p.nb;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      uint32_t lo = 0, hi = 0;
+      cw[at][m][0] = cw[at][m][1] = make_uint4(0, 0, 0, 0);
+      if (there) {
+        cw[at][m][0] = __ldg(codes[m][0] + 4 * s);
+        cw[at][m][1] = __ldg(codes[m][1] + 4 * s);
+        lo = __ldg(meta[m][0] + 4 * s);
+        hi = __ldg(meta[m][1] + 4 * s);
+      }
+      mt[at][m] = lo | hi << 16;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    if (s_begin + i < s_end) load(s_begin + i, i);
+
+  for (int32_t c0 = s_begin; c0 < s_end; c0 += p.chunk) {
+    const int32_t c1 = c0 + p.chunk < s_end ? c0 + p.chunk : s_end;
+    __syncthreads();                                // nobody reads the x of the chunk before any more
+    // piece (s, w, n, g, t): channels 8 w .. 8 w + 7 of block 4 s + t of row 8 n + g, in the order 0 2 1 3 4 6 5 7 of the decoder
+    for (int32_t i = threadIdx.x; i < (c1 - c0) * 16 * (8 * NT); i += kWarps * 32) {
+      const int32_t k16 = i % ((c1 - c0) * 16), tok = i / ((c1 - c0) * 16);      // 16-byte piece of the chunk's row
+      const int32_t s = k16 >> 4, tt = (k16 >> 2) & 3, w = k16 & 3;
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (tok < n_tok && 4 * (c0 + s) + tt < p.nb) u = __ldg(reinterpret_cast<const uint4*>(p.x + (t0 + tok) * p.ld) + (int64_t)c0 * 16 + k16);
+      const uint32_t dst = x_at + ((((s * 4 + w) * NT + (tok >> 3)) * 32 + (tok & 7) * 4 + tt) << 4);
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(prmt(u.x, u.y, 0x5410u)), "r"(prmt(u.x, u.y, 0x7632u)),
+                   "r"(prmt(u.z, u.w, 0x5410u)), "r"(prmt(u.z, u.w, 0x7632u)) : "memory");
+    }
+    __syncthreads();
+    for (int32_t s0 = c0; s0 < c1; s0 += kAhead) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int32_t s = s0 + i;
+        if (s >= c1) break;
+        const bool there = 4 * s + t < p.nb;
+        BlockScale sc[MT][2];
+        uint32_t words[MT][2][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          sc[m][0] = block_scale(mt[i][m] & 0xffffu, book_at, there);
+          sc[m][1] = block_scale(mt[i][m] >> 16, book_at, there);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            words[m][r][0] = cw[i][m][r].x; words[m][r][1] = cw[i][m][r].y; words[m][r][2] = cw[i][m][r].z; words[m][r][3] = cw[i][m][r].w;
+          }
+        }
+        if (s + kAhead < s_end) load(s + kAhead, i);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t a[MT][2][4];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            decode_word(words[m][0][w], sc[m][0], a[m][0]);
+            decode_word(words[m][1][w], sc[m][1], a[m][1]);
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint4 b = fb4blk::lds_v4(x_at + (((((s - c0) * 4 + w) * NT + n) * 32 + lane) << 4));
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              mma_bf16(acc[m][n], a[m][0][0], a[m][1][0], a[m][0][1], a[m][1][1], b.x, b.y);
+              mma_bf16(acc[m][n], a[m][0][2], a[m][1][2], a[m][0][3], a[m][1][3], b.z, b.w);
+            }
+          }
+        }
+      }
+      // the ring's place is s - s_begin mod kAhead: chunks are multiples of it
+    }
+  }
+
+  // ---- the sums, [row of x][row of W], to shared memory; then the cluster's CTAs each finish a part of them
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(smem);
+  constexpr int kLd = kRows + 4;                    // the quads' rows of x fall into different banks
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sums[(8 * n + 2 * t + (k & 1)) * kLd + warp * 16 * MT + 16 * m + g + 8 * (k >> 1)] = acc[m][n][k];
+  if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else __syncthreads();
+  for (int32_t i = split * (kWarps * 32) + threadIdx.x; i < n_tok * kRows; i += p.splits * (kWarps * 32)) {
+    const int32_t tok = i / kRows, r = i % kRows;
+    const int64_t n = tile * kRows + r;
+    if (n >= p.N) continue;
+    float v = 0.0f;
+    if (p.splits > 1) {
+      const uint32_t at = fb4blk::smem_u32(sums + tok * kLd + r);
+#pragma unroll
+      for (int z = 0; z < kMaxSplits; ++z)
+        if (z < p.splits) {
+          float u;
+          asm volatile("{\n\t.reg .b32 q;\n\tmapa.shared::cluster.u32 q, %1, %2;\n\tld.shared::cluster.f32 %0, [q];\n\t}" : "=f"(u) : "r"(at), "r"(z));
+          v += u;
+        }
+    } else {
+      v = sums[tok * kLd + r];
+    }
+    v *= kUnshift;
+    if (p.bias) v += __uint_as_float((uint32_t)__ldg(p.bias + n) << 16);
+    const int64_t at = (t0 + tok) * p.out_ld + n;
+    if (p.out_dtype == 0) static_cast<float*>(p.out)[at] = v;
+    else if (p.out_dtype == 1) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
+    else static_cast<__half*>(p.out)[at] = __float2half_rn(v);
+  }
+  // nobody's shared memory goes away while another CTA reads it
+  if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int MT, int NT>
+constexpr int join_bytes() { return 8 * NT * (kWarps * 16 * MT + 4) * 4; }
+
+template <int MT, int NT>
+cudaError_t launch(const fb4_ctx* ctx, Linear p, cudaStream_t stream) {
+  constexpr int kRows = kWarps * 16 * MT, kAhead = ahead(MT);
+  const int64_t tiles = (p.N + kRows - 1) / kRows, z = (p.T + 8 * NT - 1) / (8 * NT);
+  const int32_t steps = (p.nb + 3) / 4;
+  // splits: the fewest waves of two CTAs per SM, counting a CTA's start and its part of the join as 4 steps
+  double best = 1e300;
+  p.splits = 1;
+  for (int s = 1; s <= kMaxSplits && (s == 1 || steps / s >= 2); ++s) {
+    const int64_t waves = (tiles * z * s + 2 * ctx->sm_count - 1) / (2 * ctx->sm_count);
+    const double cost = (double)waves * ((steps + s - 1) / s + 4);
+    if (cost < best * 0.97) {
+      best = cost;
+      p.splits = s;
+    }
+  }
+  const int32_t mine = (steps + p.splits - 1) / p.splits;
+  const int32_t most = kXBytes / (2048 * NT) / kAhead * kAhead;
+  p.chunk = mine < most ? (mine + kAhead - 1) / kAhead * kAhead : most;
+  int smem = p.chunk * 2048 * NT;
+  if (smem < join_bytes<MT, NT>()) smem = join_bytes<MT, NT>();
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  cfg.gridDim = dim3((unsigned)(tiles * p.splits), (unsigned)z);
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  if (p.splits > 1) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.splits;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+  }
+  return cudaLaunchKernelEx(&cfg, fb4_linear_kernel<MT, NT>, p);
+}
+
+}  // namespace
+
+cudaError_t fb4_linear_prepare_device() {
+  cudaError_t e = cudaSuccess;
+#define FB4_OPT_IN(MT, NT) \
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_linear_kernel<MT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, \
+                                                 kXBytes > join_bytes<MT, NT>() ? kXBytes : join_bytes<MT, NT>())
+  FB4_OPT_IN(1, 1);
+  FB4_OPT_IN(2, 2);
+  FB4_OPT_IN(2, 4);
+  FB4_OPT_IN(2, 8);
+#undef FB4_OPT_IN
+  return e;
+}
+
+cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
+                              int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream) {
+  Linear p{static_cast<const uint16_t*>(x), ld, codes, meta, static_cast<const uint16_t*>(bias), out, out_ld, T, N, (int32_t)(K / 32), 1, 1,
+           out_dtype, ctx->d_tables};
+  if (T <= 8) return launch<1, 1>(ctx, p, stream);
+  if (T <= 16) return launch<2, 2>(ctx, p, stream);
+  if (T <= 32) return launch<2, 4>(ctx, p, stream);
+  return launch<2, 8>(ctx, p, stream);
+}

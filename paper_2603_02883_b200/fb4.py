@@ -24,7 +24,7 @@ STATIC_MAX_CLUSTERS = 1024
 EXPORTS = [
     "fb4_default_config", "fb4_init", "fb4_destroy", "fb4_get_tables", "fb4_block_tables", "fb4_quantize", "fb4_quantize_f32", "fb4_quantize_affine", "fb4_quantize_affine_mxfp8", "fb4_quantize_layernorm", "fb4_quantize_seda",
     "fb4_build_subformatbook", "fb4_build_subformatbook_static", "fb4_select_salient", "fb4_select_salient_topk", "fb4_quantize_decomposed", "fb4_quantize_decomposed_idx", "fb4_dequantize",
-    "fb4_quantize_weights", "fb4_qk_norm_rope", "fb4_cache_append", "fb4_cache_attention", "fb4_cache_attention_workspace", "fb4_cache_plan", "fb4_cache8_append", "fb4_cache8_attention", "fb4_cache8_attention_workspace", "fb4_cache8_values", "fb4_quantize_mxfp8", "fb4_quantize_mxfp8_decomposed", "fb4_to_mxfp8", "fb4_mxfp8_scale_bytes", "fb4_quantize_host", "fb4_set_kernel_variant", "fb4_device_status", "fb4_launch_count", "fb4_last_variant", "fb4_last_cuda_error", "fb4_strerror",
+    "fb4_quantize_weights", "fb4_linear", "fb4_qk_norm_rope", "fb4_cache_append", "fb4_cache_attention", "fb4_cache_attention_workspace", "fb4_cache_plan", "fb4_cache8_append", "fb4_cache8_attention", "fb4_cache8_attention_workspace", "fb4_cache8_values", "fb4_quantize_mxfp8", "fb4_quantize_mxfp8_decomposed", "fb4_to_mxfp8", "fb4_mxfp8_scale_bytes", "fb4_quantize_host", "fb4_set_kernel_variant", "fb4_device_status", "fb4_launch_count", "fb4_last_variant", "fb4_last_cuda_error", "fb4_strerror",
 ]
 
 
@@ -109,6 +109,8 @@ def lib() -> ctypes.CDLL:
     L.fb4_dequantize.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, ci, vp]
     L.fb4_quantize_weights.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp]
     L.fb4_quantize_weights.restype = ci
+    L.fb4_linear.argtypes = [vp, vp, i64, i64, i64, vp, vp, i64, vp, vp, i64, ci, vp]
+    L.fb4_linear.restype = ci
     cf, rp, cp = ctypes.c_float, ctypes.POINTER(Fb4Rope), ctypes.POINTER(Fb4Cache)
     L.fb4_qk_norm_rope.argtypes = [vp, vp, i32, i64, vp, i32, i64, i64, i32, vp, vp, cf, rp, vp, i64, vp, i64, vp]
     L.fb4_qk_norm_rope.restype = ci
@@ -305,6 +307,11 @@ def fb4_dequantize(ctx, codes, meta, T, C, salient_idx, n_salient, res_codes, re
 def fb4_quantize_weights(ctx, w, N, K, ld_elems, codes, meta, stream=None) -> None:
     _check(lib().fb4_quantize_weights(ctx, _ptr(w), N, K, ld_elems, _ptr(codes), _ptr(meta), _stream(stream)),
            "fb4_quantize_weights")
+
+
+def fb4_linear(ctx, x, T, K, ld_elems, codes, meta, N, bias, out, out_ld, out_dtype, stream=None) -> None:
+    _check(lib().fb4_linear(ctx, _ptr(x), T, K, ld_elems, _ptr(codes), _ptr(meta), N, _ptr(bias), _ptr(out), out_ld, out_dtype, _stream(stream)),
+           "fb4_linear")
 
 
 def fb4_quantize_mxfp8(ctx, x, T, C, ld_elems, cluster_id, cluster_mask, n_clusters, e4m3, scales, scale_layout,
@@ -671,6 +678,26 @@ class Fb4:
         codes, meta = self._outs(N, K)
         fb4_quantize_weights(self.ctx, w, N, K, ld, codes, meta)
         return Quantized(codes, meta)
+
+    def linear(self, x, w: Quantized, bias=None, dtype=torch.bfloat16):
+        """x [T][K] (bfloat16) times FB4 weights w [N][K], plus bias [N]: [T][N].  Made for few rows; w as quantize_weights gives it"""
+        codes, meta = w.codes, w.meta
+        code = _out_dtype(dtype)
+        if x.dtype is not torch.bfloat16 or x.dim() != 2 or codes.dim() != 2 or meta.dim() != 2:
+            raise ValueError("expected x bfloat16 [T][K] and weights [N][K]")
+        (T, K), (N, half) = x.shape, codes.shape
+        ld, one = x.stride()
+        if codes.dtype is not torch.uint8 or meta.element_size() != 2 or half * 2 != K or meta.shape != (N, K // 32) or (one != 1 and K > 1):
+            raise ValueError("the weights must have the channels of x, in blocks of 32, and x contiguous channels")
+        if not codes.is_contiguous() or not meta.is_contiguous():
+            raise ValueError("the weights must be contiguous")
+        if bias is not None and (bias.dtype is not torch.bfloat16 or bias.shape != (N,) or not bias.is_contiguous()):
+            raise ValueError("the bias must be a contiguous bfloat16 tensor [N]")
+        self._on(x, codes, meta, bias)
+        out = x.new_empty(T, N, dtype=dtype)
+        self._call("fb4_linear", x.data_ptr(), T, K, ld if T > 1 else K, codes.data_ptr(), meta.data_ptr(), N, None if bias is None else bias.data_ptr(),
+                   out.data_ptr(), N, code)
+        return out
 
     def quantize_mxfp8(self, x, scale_layout: int = 1, cluster_id=None, cluster_mask=None):
         """quantize straight to (e4m3 bytes [T][C], E8M0 scale bytes)"""

@@ -183,3 +183,47 @@ def test_cache8_in_the_binding(monkeypatch):
     with pytest.raises(ValueError):
         f.cache8_attention(kv[..., :32], c, i32(3, 4), i32(3), i32(4), 2, 16)
     assert len(f.calls) == n
+
+
+LINEAR = r"""
+  const uint16_t* meta = reinterpret_cast<const uint16_t*>(room);
+  ctx.linear_error = cudaErrorInvalidConfiguration;
+  auto linear = [&](const void* x, int64_t T, int64_t K, int64_t ld, const uint8_t* codes, const uint16_t* m, int64_t N, const void* bias, void* out, int64_t out_ld, int dtype) {
+    return fb4_linear(&ctx, x, T, K, ld, codes, m, N, bias, out, out_ld, dtype, 0);
+  };
+  if (linear(room, 4, 64, 64, room, meta, 10, room, room, 10, 1) != FB4_ERR_CUDA || fb4_last_cuda_error() != (int)cudaErrorInvalidConfiguration) return 1;
+  for (int64_t K : {0, 16, 33, 48, -32}) if (linear(room, 4, K, 64, room, meta, 10, room, room, 10, 1) != FB4_ERR_SHAPE) return 2;
+  if (linear(room, 4, 64, 56, room, meta, 10, 0, room, 10, 1) != FB4_ERR_SHAPE || linear(room, 4, 64, 64, room, meta, 10, 0, room, 9, 1) != FB4_ERR_SHAPE) return 3;
+  if (linear(room, -1, 64, 64, room, meta, 10, 0, room, 10, 1) != FB4_ERR_SHAPE || linear(room, (1 << 22) + 1, 64, 64, room, meta, 10, 0, room, 10, 1) != FB4_ERR_SHAPE) return 4;
+  if (linear(room, 4, 64, 64, room, meta, -1, 0, room, 10, 1) != FB4_ERR_SHAPE || linear(room, 4, 64, 64, room, meta, 1LL << 31, 0, room, 1LL << 31, 1) != FB4_ERR_SHAPE) return 5;
+  if (linear(0, 4, 64, 64, room, meta, 10, 0, room, 10, 1) != FB4_ERR_INVALID_ARG || linear(room, 4, 64, 64, 0, meta, 10, 0, room, 10, 1) != FB4_ERR_INVALID_ARG) return 6;
+  if (linear(room, 4, 64, 64, room, 0, 10, 0, room, 10, 1) != FB4_ERR_INVALID_ARG || linear(room, 4, 64, 64, room, meta, 10, 0, 0, 10, 1) != FB4_ERR_INVALID_ARG) return 7;
+  if (linear(room, 4, 64, 64, room, meta, 10, 0, room, 10, 3) != FB4_ERR_INVALID_ARG || linear(room, 4, 64, 64, room, meta, 10, 0, room, 10, -1) != FB4_ERR_INVALID_ARG) return 8;
+  if (linear(room + 8, 4, 64, 64, room, meta, 10, 0, room, 10, 1) != FB4_ERR_ALIGN || linear(room, 4, 64, 68, room, meta, 10, 0, room, 10, 1) != FB4_ERR_ALIGN) return 9;
+  if (linear(room, 4, 64, 64, room + 8, meta, 10, 0, room, 10, 1) != FB4_ERR_ALIGN || linear(room, 4, 64, 64, room, meta + 1, 10, 0, room, 10, 1) != FB4_ERR_ALIGN) return 10;
+  if (linear(room, 4, 64, 64, room, meta, 10, room + 1, room, 10, 1) != FB4_ERR_ALIGN || linear(room, 4, 64, 64, room, meta, 10, 0, room + 4, 10, 1) != FB4_ERR_ALIGN) return 11;
+  if (linear(0, 0, 64, 64, 0, 0, 10, 0, 0, 10, 1) != FB4_OK || linear(0, 4, 64, 64, 0, 0, 0, 0, 0, 10, 1) != FB4_OK) return 12;
+  ctx.cfg.block_size = 16;
+  if (linear(room, 4, 64, 64, room, meta, 10, 0, room, 10, 1) != FB4_ERR_INVALID_ARG) return 13;
+  if (fb4_linear(0, room, 4, 64, 64, room, meta, 10, 0, room, 10, 1, 0) != FB4_ERR_INVALID_ARG || ctx.launches != 0) return 14;
+  puts("ok");
+  return 0;
+}
+"""
+
+
+def test_linear_refusals(tmp_path):
+    run(tmp_path, LINEAR)
+
+
+def test_linear_in_the_binding(monkeypatch):
+    f = context(monkeypatch)
+    w = fb4.Quantized(torch.zeros(10, 32, dtype=torch.uint8), torch.zeros(10, 2, dtype=torch.int16))
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    assert f.linear(x, w).shape == (4, 10) and f.linear(x, w, bias=x[0, :10], dtype=torch.float32).dtype == torch.float32 and len(f.calls) == 2
+    swap = lambda **k: fb4.Quantized(**{**dict(codes=w.codes, meta=w.meta), **k})  # noqa: E731
+    for bad in ((x.float(), w), (x[0], w), (x[:, :32], w), (x.t().contiguous().t(), w), (x, swap(codes=w.codes.short())), (x, swap(meta=w.meta[:9])), (x, swap(meta=w.meta.int())),
+                (x, swap(codes=torch.zeros(32, 10, dtype=torch.uint8).t())), (x, w, x[0, :9]), (x, w, x[0, :10].float()), (x, w, x[:, 0]), (x, w, None, torch.float64)):
+        with pytest.raises(ValueError):
+            f.linear(*bad)
+    assert len(f.calls) == 2
