@@ -306,7 +306,7 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
   ctx->append_error = fb4_rope_prepare_device();
   ctx->attend_error = fb4_attend_prepare_device();
   ctx->plan_error = fb4_plan_prepare_device();
-  ctx->linear_error = fb4_linear_prepare_device();
+  ctx->linear_error = fb4_linear_prepare_device(ctx->linear_slots);
   ctx->fast_table_bytes = fast_bytes;
   cudaGetLastError();
   *out = ctx;

@@ -15,7 +15,8 @@ namespace {
 using namespace fb4att;
 
 constexpr int kWarps = 8;                       // a step of a warp is 128 channels: 4 blocks, one to each lane of a quad
-__host__ __device__ constexpr int ahead(int MT) { return MT == 1 ? 4 : 2; }      // steps that are loaded ahead: 2 KB or so a warp and step
+__host__ __device__ constexpr int ahead(int MT) { return 2; }      // steps that are loaded ahead
+__host__ __device__ constexpr int resident(int MT) { return MT == 1 ? 3 : 2; }      // CTAs per SM
 constexpr int kMaxSplits = 8;                    // portable cluster size
 constexpr int kXBytes = 64 * 1024;               // most of x that a CTA holds at a time
 
@@ -31,6 +32,7 @@ struct Linear {
   int32_t nb;               // blocks of a row
   int32_t splits;           // CTAs of a cluster
   int32_t chunk;            // steps whose x a CTA holds at a time
+  int32_t wide;             // rows of x that have room in shared memory, with one tile of them
   int32_t out_dtype;
   const Fb4DeviceTables* tables;
 };
@@ -42,7 +44,7 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 
 // MT: tiles of 16 rows of W to a warp; NT: tiles of 8 rows of x
 template <int MT, int NT>
-__global__ void __launch_bounds__(kWarps * 32, 2) fb4_linear_kernel(const __grid_constant__ Linear p) {
+__global__ void __launch_bounds__(kWarps * 32, resident(MT)) fb4_linear_kernel(const __grid_constant__ Linear p) {
   constexpr int kRows = kWarps * 16 * MT, kAhead = ahead(MT);      // rows of W to a CTA
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t book[64];
@@ -56,16 +58,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_linear_kernel(const __grid
   const uint32_t x_at = fb4blk::smem_u32(smem), book_at = fb4blk::smem_u32(book);
   if (threadIdx.x < 64) fill_book(book, p.tables, threadIdx.x);
 
-  // this lane's rows of W; rows behind the last are computed like it and not stored
-  const uint4* codes[MT][2];
+  // this lane's rows of W, from the run's first block on; rows behind the last are computed like it and not stored
+  const uint8_t* codes[MT][2];
   const uint16_t* meta[MT][2];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int64_t n = n0 + 16 * m + 8 * r + g, row = n < p.N ? n : p.N - 1;
-      codes[m][r] = reinterpret_cast<const uint4*>(p.codes) + row * p.nb + t;
-      meta[m][r] = p.meta + row * p.nb + t;
+      const int64_t n = n0 + 16 * m + 8 * r + g, at = (n < p.N ? n : p.N - 1) * p.nb + 4 * (int64_t)s_begin + t;
+      codes[m][r] = p.codes + at * 16;
+      meta[m][r] = p.meta + at;
     }
   float acc[MT][NT][4];
 #pragma unroll
@@ -76,58 +78,66 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_linear_kernel(const __grid
       for (int k = 0; k < 4; ++k) acc[m][n][k] = 0.0f;
 
   uint4 cw[kAhead][MT][2];
-  uint32_t mt[kAhead][MT];                          // the two rows' metadata
-  auto load = [&](int32_t s, int at) {
-    const bool there = 4 * s + t < p.nb;
+  uint16_t mt[kAhead][MT][2];                       // joined only when used: that would wait for the load
+  const int32_t whole = p.nb / 4;                   // steps whose four blocks all exist; there is at most one more
+  // loads step s, which lies i steps behind the pointers, into ring place `at`
+  auto load = [&](int32_t s, int i, int at) {
+    const bool there = s < whole || 4 * s + t < p.nb;
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      uint32_t lo = 0, hi = 0;
-      cw[at][m][0] = cw[at][m][1] = make_uint4(0, 0, 0, 0);
-      if (there) {
-        cw[at][m][0] = __ldg(codes[m][0] + 4 * s);
-        cw[at][m][1] = __ldg(codes[m][1] + 4 * s);
-        lo = __ldg(meta[m][0] + 4 * s);
-        hi = __ldg(meta[m][1] + 4 * s);
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        cw[at][m][r] = make_uint4(0, 0, 0, 0);
+        mt[at][m][r] = 0;                           // scale byte 0 and codes 0: zeros
+        if (there) {
+          cw[at][m][r] = __ldg(reinterpret_cast<const uint4*>(codes[m][r] + 64 * i));
+          mt[at][m][r] = __ldg(meta[m][r] + 4 * i);
+        }
       }
-      mt[at][m] = lo | hi << 16;
-    }
   };
 #pragma unroll
   for (int i = 0; i < kAhead; ++i)
-    if (s_begin + i < s_end) load(s_begin + i, i);
+    if (s_begin + i < s_end) load(s_begin + i, i, i);
 
+  // x of a chunk, piece (s, w, n, g, t): channels 8 w .. 8 w + 7 of block 4 s + t of row 8 n + g, in the order 0 2 1 3 4 6 5 7 of the
+  // decoder; with one tile of rows only `wide` of them (a power of two) have room, and the lanes behind read zeros
+  const int wide = NT > 1 ? 8 : p.wide;
+  const uint32_t x_lane = NT > 1 ? lane << 4 : (lane & (4 * wide - 1)) << 4;
+  const uint32_t x_piece = NT > 1 ? NT * 512 : wide * 64;
+  const bool x_there = NT > 1 || lane < 4 * wide;
   for (int32_t c0 = s_begin; c0 < s_end; c0 += p.chunk) {
     const int32_t c1 = c0 + p.chunk < s_end ? c0 + p.chunk : s_end;
     __syncthreads();                                // nobody reads the x of the chunk before any more
-    // piece (s, w, n, g, t): channels 8 w .. 8 w + 7 of block 4 s + t of row 8 n + g, in the order 0 2 1 3 4 6 5 7 of the decoder
-    for (int32_t i = threadIdx.x; i < (c1 - c0) * 16 * (8 * NT); i += kWarps * 32) {
-      const int32_t k16 = i % ((c1 - c0) * 16), tok = i / ((c1 - c0) * 16);      // 16-byte piece of the chunk's row
-      const int32_t s = k16 >> 4, tt = (k16 >> 2) & 3, w = k16 & 3;
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (tok < n_tok && 4 * (c0 + s) + tt < p.nb) u = __ldg(reinterpret_cast<const uint4*>(p.x + (t0 + tok) * p.ld) + (int64_t)c0 * 16 + k16);
-      const uint32_t dst = x_at + ((((s * 4 + w) * NT + (tok >> 3)) * 32 + (tok & 7) * 4 + tt) << 4);
-      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(prmt(u.x, u.y, 0x5410u)), "r"(prmt(u.x, u.y, 0x7632u)),
-                   "r"(prmt(u.z, u.w, 0x5410u)), "r"(prmt(u.z, u.w, 0x7632u)) : "memory");
+    for (int32_t tok = warp; tok < (NT > 1 ? 8 * NT : wide); tok += kWarps) {
+      const uint4* src = reinterpret_cast<const uint4*>(p.x + (t0 + tok) * p.ld) + (int64_t)c0 * 16;
+      const uint32_t row_at = x_at + (NT > 1 ? (tok >> 3) * 512 : 0) + (tok & 7) * 64;
+#pragma unroll 4
+      for (int32_t k16 = lane; k16 < (c1 - c0) * 16; k16 += 32) {                       // 16-byte pieces of the chunk's row
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (tok < n_tok && 4 * c0 + (k16 >> 2) < p.nb) u = __ldg(src + k16);
+        const uint32_t dst = row_at + ((k16 >> 4) * 4 + (k16 & 3)) * x_piece + ((k16 >> 2) & 3) * 16;
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(prmt(u.x, u.y, 0x5410u)), "r"(prmt(u.x, u.y, 0x7632u)),
+                     "r"(prmt(u.z, u.w, 0x5410u)), "r"(prmt(u.z, u.w, 0x7632u)) : "memory");
+      }
     }
     __syncthreads();
+    uint32_t x_step = x_at + x_lane;
     for (int32_t s0 = c0; s0 < c1; s0 += kAhead) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int32_t s = s0 + i;
         if (s >= c1) break;
-        const bool there = 4 * s + t < p.nb;
         BlockScale sc[MT][2];
         uint32_t words[MT][2][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          sc[m][0] = block_scale(mt[i][m] & 0xffffu, book_at, there);
-          sc[m][1] = block_scale(mt[i][m] >> 16, book_at, there);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
+            sc[m][r] = block_scale(mt[i][m][r], book_at, true);
             words[m][r][0] = cw[i][m][r].x; words[m][r][1] = cw[i][m][r].y; words[m][r][2] = cw[i][m][r].z; words[m][r][3] = cw[i][m][r].w;
           }
         }
-        if (s + kAhead < s_end) load(s + kAhead, i);
+        if (s + kAhead < s_end) load(s + kAhead, i + kAhead, i);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           uint32_t a[MT][2][4];
@@ -138,7 +148,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_linear_kernel(const __grid
           }
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            const uint4 b = fb4blk::lds_v4(x_at + (((((s - c0) * 4 + w) * NT + n) * 32 + lane) << 4));
+            uint4 b = make_uint4(0, 0, 0, 0);
+            if (x_there) b = fb4blk::lds_v4(x_step + (i * 4 + w) * x_piece + n * 512);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
               mma_bf16(acc[m][n], a[m][0][0], a[m][1][0], a[m][0][1], a[m][1][1], b.x, b.y);
@@ -147,7 +158,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_linear_kernel(const __grid
           }
         }
       }
-      // the ring's place is s - s_begin mod kAhead: chunks are multiples of it
+      x_step += kAhead * 4 * x_piece;
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          codes[m][r] += 64 * kAhead;
+          meta[m][r] += 4 * kAhead;
+        }
     }
   }
 
@@ -195,15 +213,15 @@ template <int MT, int NT>
 constexpr int join_bytes() { return 8 * NT * (kWarps * 16 * MT + 4) * 4; }
 
 template <int MT, int NT>
-cudaError_t launch(const fb4_ctx* ctx, Linear p, cudaStream_t stream) {
+cudaError_t launch(const fb4_ctx* ctx, const int32_t* slots, Linear p, cudaStream_t stream) {
   constexpr int kRows = kWarps * 16 * MT, kAhead = ahead(MT);
   const int64_t tiles = (p.N + kRows - 1) / kRows, z = (p.T + 8 * NT - 1) / (8 * NT);
   const int32_t steps = (p.nb + 3) / 4;
-  // splits: the fewest waves of two CTAs per SM, counting a CTA's start and its part of the join as 4 steps
+  // splits: the least of waves x work of a CTA, its start and its part of the join counted as 4 steps
   double best = 1e300;
   p.splits = 1;
   for (int s = 1; s <= kMaxSplits && (s == 1 || steps / s >= 2); ++s) {
-    const int64_t waves = (tiles * z * s + 2 * ctx->sm_count - 1) / (2 * ctx->sm_count);
+    const int64_t waves = (tiles * z * s + slots[s] - 1) / slots[s];
     const double cost = (double)waves * ((steps + s - 1) / s + 4);
     if (cost < best * 0.97) {
       best = cost;
@@ -211,9 +229,11 @@ cudaError_t launch(const fb4_ctx* ctx, Linear p, cudaStream_t stream) {
     }
   }
   const int32_t mine = (steps + p.splits - 1) / p.splits;
-  const int32_t most = kXBytes / (2048 * NT) / kAhead * kAhead;
+  for (p.wide = 1; p.wide < 8 && p.wide < p.T; p.wide *= 2) {}
+  const int per_step = NT > 1 ? 2048 * NT : 256 * p.wide;
+  const int32_t most = kXBytes / per_step / kAhead * kAhead;
   p.chunk = mine < most ? (mine + kAhead - 1) / kAhead * kAhead : most;
-  int smem = p.chunk * 2048 * NT;
+  int smem = p.chunk * per_step;
   if (smem < join_bytes<MT, NT>()) smem = join_bytes<MT, NT>();
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
@@ -233,25 +253,43 @@ cudaError_t launch(const fb4_ctx* ctx, Linear p, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t fb4_linear_prepare_device() {
+// Opt-in to the dynamic shared memory, and how many CTAs are resident at a time in clusters of 1 to 8 (fewer than without clusters: a
+// cluster lies in one group of SMs).
+cudaError_t fb4_linear_prepare_device(int32_t (*slots)[kMaxSplits + 1]) {
   cudaError_t e = cudaSuccess;
-#define FB4_OPT_IN(MT, NT) \
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_linear_kernel<MT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, \
-                                                 kXBytes > join_bytes<MT, NT>() ? kXBytes : join_bytes<MT, NT>())
-  FB4_OPT_IN(1, 1);
-  FB4_OPT_IN(2, 2);
-  FB4_OPT_IN(2, 4);
-  FB4_OPT_IN(2, 8);
-#undef FB4_OPT_IN
+  auto prepare = [&](void (*kernel)(Linear), int smem, int32_t* of) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    for (int s = 1; s <= kMaxSplits && e == cudaSuccess; ++s) {
+      cudaLaunchConfig_t cfg{};
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = (unsigned)s;
+      attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+      cfg.gridDim = dim3((unsigned)(s * 1024));
+      cfg.blockDim = dim3(kWarps * 32);
+      cfg.dynamicSmemBytes = (size_t)smem;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      int n = 0;
+      e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+      of[s] = n * s > 1 ? n * s : 1;
+    }
+  };
+#define FB4_PREPARE(MT, NT, i) prepare(fb4_linear_kernel<MT, NT>, kXBytes > join_bytes<MT, NT>() ? kXBytes : join_bytes<MT, NT>(), slots[i])
+  FB4_PREPARE(1, 1, 0);
+  FB4_PREPARE(2, 2, 1);
+  FB4_PREPARE(2, 4, 2);
+  FB4_PREPARE(2, 8, 3);
+#undef FB4_PREPARE
   return e;
 }
 
 cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
                               int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream) {
-  Linear p{static_cast<const uint16_t*>(x), ld, codes, meta, static_cast<const uint16_t*>(bias), out, out_ld, T, N, (int32_t)(K / 32), 1, 1,
+  Linear p{static_cast<const uint16_t*>(x), ld, codes, meta, static_cast<const uint16_t*>(bias), out, out_ld, T, N, (int32_t)(K / 32), 1, 1, 8,
            out_dtype, ctx->d_tables};
-  if (T <= 8) return launch<1, 1>(ctx, p, stream);
-  if (T <= 16) return launch<2, 2>(ctx, p, stream);
-  if (T <= 32) return launch<2, 4>(ctx, p, stream);
-  return launch<2, 8>(ctx, p, stream);
+  if (T <= 8) return launch<1, 1>(ctx, ctx->linear_slots[0], p, stream);
+  if (T <= 16) return launch<2, 2>(ctx, ctx->linear_slots[1], p, stream);
+  if (T <= 32) return launch<2, 4>(ctx, ctx->linear_slots[2], p, stream);
+  return launch<2, 8>(ctx, ctx->linear_slots[3], p, stream);
 }
