@@ -623,13 +623,13 @@ int fb4_cache8_values(fb4_ctx* ctx, const fb4_cache8* cache, void* k_out, void* 
  *   new_len    : device int32 [n_seqs]
  *   n_seqs     : at most FB4_PLAN_MAX_SEQS
  *   free_pages : device int32 [free_cap], in and out; n_free: device int32 [1], in and out.  Pages that go back to a full list are lost
- *   T          : rows of the step, at most 2^31 - 1
+ *   T          : rows of the step, at most 2^30
  *   q_start    : device int32 [n_seqs + 1] (out);  slot: device int64 [T] (out) or NULL;  pos: device int32 [T] (out) or NULL
  * A kv_len outside [0, max_pages * page_tokens] or an n_free outside [0, free_cap] is clamped, a negative keep or new_len counts as 0, and each
  * of them, and a lost page, raises bit 1 of the status word.  Page numbers are passed on as they are, and never used as addresses.
  * Works with every context configuration.
  */
-#define FB4_PLAN_MAX_SEQS 32768
+#define FB4_PLAN_MAX_SEQS 8192
 int fb4_cache_plan(fb4_ctx* ctx, int32_t* page_table, int32_t max_pages, int32_t page_tokens, int32_t* kv_len, const int32_t* keep,
                    const int32_t* new_len, int32_t n_seqs, int32_t* free_pages, int32_t free_cap, int32_t* n_free, int64_t T,
                    int32_t* q_start, int64_t* slot, int32_t* pos, void* stream);

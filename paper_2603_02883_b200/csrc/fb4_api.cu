@@ -854,7 +854,7 @@ int fb4_cache_plan(fb4_ctx* ctx, int32_t* page_table, int32_t max_pages, int32_t
                    int32_t* q_start, int64_t* slot, int32_t* pos, void* stream) {
   if (!ctx) return FB4_ERR_INVALID_ARG;
   if (page_tokens < 16 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0 || max_pages < 0 || n_seqs < 0 ||
-      n_seqs > FB4_PLAN_MAX_SEQS || free_cap < 0 || T < 0 || T > 0x7fffffffLL || (int64_t)max_pages * page_tokens > (1 << 30) ||
+      n_seqs > FB4_PLAN_MAX_SEQS || free_cap < 0 || T < 0 || T > (1 << 30) || (int64_t)max_pages * page_tokens > (1 << 30) ||
       (int64_t)max_pages * n_seqs > 0x7fffffffLL)
     return FB4_ERR_SHAPE;
   if (!q_start || !n_free || (n_seqs > 0 && (!kv_len || !new_len)) || ((int64_t)max_pages * n_seqs > 0 && !page_table) ||
@@ -865,10 +865,11 @@ int fb4_cache_plan(fb4_ctx* ctx, int32_t* page_table, int32_t max_pages, int32_t
                           reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(pos);
   if ((words & 3u) || (reinterpret_cast<uintptr_t>(slot) & 7u)) return FB4_ERR_ALIGN;
   if (ctx->plan_error != cudaSuccess) return fb4_set_cuda_error(ctx->plan_error);
+  int launches = 0;
   const cudaError_t e = fb4_launch_cache_plan(ctx, page_table, max_pages, page_tokens, kv_len, keep, new_len, n_seqs, free_pages, free_cap,
-                                              n_free, T, q_start, slot, pos, static_cast<cudaStream_t>(stream));
+                                              n_free, T, q_start, slot, pos, static_cast<cudaStream_t>(stream), &launches);
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
-  ctx->launches += 1;
+  ctx->launches += launches;
   return FB4_OK;
 }
 

@@ -190,4 +190,4 @@ cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int6
 cudaError_t fb4_plan_prepare_device();
 cudaError_t fb4_launch_cache_plan(const fb4_ctx* ctx, int32_t* page_table, int32_t max_pages, int32_t page_tokens, int32_t* kv_len,
                                   const int32_t* keep, const int32_t* new_len, int32_t n_seqs, int32_t* free_pages, int32_t free_cap,
-                                  int32_t* n_free, int64_t T, int32_t* q_start, int64_t* slot, int32_t* pos, cudaStream_t stream);
+                                  int32_t* n_free, int64_t T, int32_t* q_start, int64_t* slot, int32_t* pos, cudaStream_t stream, int* launches);

@@ -5,8 +5,11 @@
 // page f of those that go back is entry top - 1 - f of the free list (top: its length with all of them), and page f of those that are
 // taken is entry top - 1 - f too, so a step that is planned again gives every page back to where it came from.
 //
-// Bound: latency.  A CTA or, for larger steps, a cluster of 8 that computes the sums in every CTA (a few loads and scans; nothing of
-// them has to be passed on) and shares out the pages and the rows, with a barrier where one may read what another wrote.
+// Bound: latency.  One CTA, or for larger steps a cluster of 8, computes the sums (in every CTA: a few loads and one scan; nothing of them
+// has to be passed on) and shares out the pages, with a barrier where one may read what another wrote; many rows are left to a second
+// kernel on all SMs, launched early.  Lists are dealt out in runs: a warp looks up the sequence of its first entry and walks on from it, and
+// only 32 entries that belong to several sequences cost a search each.  64 sequences of one token take 5.1 us on the device, 2048 of them with
+// 270 000 rows and 49 000 pages that move 14.
 #include "fb4_internal.h"
 
 namespace {
@@ -27,17 +30,22 @@ struct Plan {
   int32_t* q_start;
   int64_t* slot;            // NULL = not wanted
   int32_t* pos;             // NULL = not wanted
+  int32_t rows_here;        // the rows are written by the first kernel
   uint32_t* status;
 };
 
 struct Step {
   int32_t keep, n;          // tokens that stay, tokens asked for (0 where the table has no room for them)
-  int32_t kept, back, need; // pages that stay, that go back, that are asked for
+  int32_t back, need;       // pages that go back, that are asked for
 };
 
+__device__ __forceinline__ int32_t pages_of(const Plan& p, int64_t tokens) { return (int32_t)((tokens + (1 << p.page_shift) - 1) >> p.page_shift); }
+
+// plain loads: the kernel writes some of these arrays at its end
 __device__ __forceinline__ Step step_of(const Plan& p, int32_t b, bool& bad) {
   const int64_t room = (int64_t)p.max_pages << p.page_shift;
-  const int64_t len = p.kv_len[b];             // plain loads: the kernel writes some of these arrays at its end
+  const int64_t len = p.kv_len[b];
+  int64_t n = p.new_len[b];
   const int64_t held = len < 0 ? 0 : len < room ? len : room;
   int64_t keep = held;
   if (p.keep) {
@@ -45,17 +53,10 @@ __device__ __forceinline__ Step step_of(const Plan& p, int32_t b, bool& bad) {
     if (k < 0) bad = true;
     keep = k < 0 ? 0 : k < held ? k : held;
   }
-  int64_t n = p.new_len[b];
   if (held != len || n < 0) bad = true;
   if (n < 0 || keep + n > room) n = 0;
-  const int64_t up = (1 << p.page_shift) - 1;
-  Step s;
-  s.keep = (int32_t)keep;
-  s.n = (int32_t)n;
-  s.kept = (int32_t)((keep + up) >> p.page_shift);
-  s.back = (int32_t)((held + up) >> p.page_shift) - s.kept;
-  s.need = (int32_t)((keep + n + up) >> p.page_shift) - s.kept;
-  return s;
+  const int32_t kept = pages_of(p, keep);
+  return Step{(int32_t)keep, (int32_t)n, pages_of(p, held) - kept, pages_of(p, keep + n) - kept};
 }
 
 __device__ __forceinline__ void all_sync(bool cluster) {
@@ -63,32 +64,21 @@ __device__ __forceinline__ void all_sync(bool cluster) {
   else __syncthreads();
 }
 
-// Inclusive sums over the threads of the CTA; the totals come back in `all`.  Two barriers.
 struct Sums {
-  int64_t pages, rows;
+  int32_t back, need;       // below 2^31: a page table has fewer entries
+  uint32_t rows;            // counted up to T + 1 at most, so that sums stay below 2^32
 };
-__device__ __forceinline__ Sums inclusive(Sums v, Sums& all, Sums* part) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+
+__device__ __forceinline__ Sums add(const Sums& x, const Sums& y, uint32_t most) {
+  return Sums{x.back + y.back, x.need + y.need, min(x.rows + y.rows, most)};
+}
+__device__ __forceinline__ Sums scanned(Sums v, uint32_t most) {      // over the lanes of a warp
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const int64_t a = __shfl_up_sync(0xffffffffu, v.pages, off), b = __shfl_up_sync(0xffffffffu, v.rows, off);
-    if (lane >= off) { v.pages += a; v.rows += b; }
+    const Sums u{__shfl_up_sync(0xffffffffu, v.back, off), __shfl_up_sync(0xffffffffu, v.need, off), __shfl_up_sync(0xffffffffu, v.rows, off)};
+    if (lane >= off) v = add(v, u, most);
   }
-  if (lane == 31) part[warp] = v;
-  __syncthreads();
-  Sums w{0, 0};
-  if (lane < warps) w = part[lane];
-#pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const int64_t a = __shfl_up_sync(0xffffffffu, w.pages, off), b = __shfl_up_sync(0xffffffffu, w.rows, off);
-    if (lane >= off) { w.pages += a; w.rows += b; }
-  }
-  all.pages = __shfl_sync(0xffffffffu, w.pages, 31);
-  all.rows = __shfl_sync(0xffffffffu, w.rows, 31);
-  const int before = warp ? warp - 1 : 0;
-  const int64_t a = __shfl_sync(0xffffffffu, w.pages, before), b = __shfl_sync(0xffffffffu, w.rows, before);
-  if (warp) { v.pages += a; v.rows += b; }
-  __syncthreads();
   return v;
 }
 
@@ -102,155 +92,193 @@ __device__ __forceinline__ int32_t find(const int32_t* at, int32_t lo, int32_t h
   return lo;
 }
 
-__global__ void __launch_bounds__(kMaxThreads) fb4_plan_kernel(const __grid_constant__ Plan p) {
-  extern __shared__ int32_t starts[];      // [n_seqs + 1], q_start
-  __shared__ Sums part[32];
-  __shared__ int32_t first[kMaxThreads], kept_of[kMaxThreads];
-  const bool cluster = gridDim.x > 1;
-  const int tid = threadIdx.x;
-  const int32_t all = blockDim.x * gridDim.x, me = blockIdx.x * blockDim.x + tid;
-  bool bad = false;
-
-  // ---- how many pages go back
-  const int32_t f0 = *p.n_free;
-  int64_t free0 = f0 < 0 ? 0 : f0 < p.free_cap ? f0 : p.free_cap;
-  if (free0 != f0) bad = true;
-  int64_t back = 0;
-  for (int32_t b0 = 0; b0 < p.n_seqs; b0 += blockDim.x) {
-    Sums v{0, 0}, sum;
-    if (b0 + tid < p.n_seqs) v.pages = step_of(p, b0 + tid, bad).back;
-    inclusive(v, sum, part);
-    back += sum.pages;
-  }
-  int64_t top = free0 + back;
-  const int64_t over = top > p.free_cap ? top - p.free_cap : 0;      // pages that the list has no room for are lost, and reported
-  if (over) bad = true;
-
-  // ---- they go to the free list
-  if (back) {
-    int64_t before = 0;
-    for (int32_t b0 = 0; b0 < p.n_seqs; b0 += blockDim.x) {
-      Sums v{0, 0}, sum;
-      Step s{};
-      if (b0 + tid < p.n_seqs) s = step_of(p, b0 + tid, bad);
-      v.pages = s.back;
-      const Sums at = inclusive(v, sum, part);
-      first[tid] = (int32_t)(at.pages - s.back);
-      kept_of[tid] = s.kept;
-      __syncthreads();
-      for (int64_t f = me; f < sum.pages; f += all) {
-        const int32_t i = find(first, 0, blockDim.x, f);
-        const int64_t to = top - 1 - before - f;
-        if (to < p.free_cap) p.free_pages[to] = p.page_table[(int64_t)(b0 + i) * p.max_pages + kept_of[i] + (f - first[i])];
+// Calls f(i, owner) for this lane's entries i of `count`, of which the first at[n] belong to owners 0 .. n - 1 (owner b has entries
+// at[b] .. at[b + 1] - 1) and the others to none (-1).  b: owner of the run's first entry.
+template <typename F>
+__device__ __forceinline__ void walk(const int32_t* at, int32_t n, int64_t from, int64_t to, int32_t b, F f) {
+  const int lane = threadIdx.x & 31;
+  const int64_t owned = at[n];
+  for (int64_t i = from + lane; i - lane < to; i += 32) {
+    int32_t mine = -1;
+    if (i - lane < owned) {
+      mine = b;
+      if (i - lane + 31 >= at[b + 1]) {
+        mine = find(at, b, n, i < owned ? i : owned - 1);
+        b = __shfl_sync(0xffffffffu, mine, 31);
       }
-      before += sum.pages;
-      __syncthreads();
+      if (i >= owned) mine = -1;
     }
-    all_sync(cluster);
+    if (i < to) f(i, mine);
   }
-  top -= over;
+}
 
-  // ---- who is served, and with which pages
-  Sums before{0, 0};                                                  // asked for by the sequences in front
-  int64_t rows = 0, taken = 0;                                        // given to them
-  for (int32_t b0 = 0; b0 < p.n_seqs; b0 += blockDim.x) {
-    Sums sum;
-    Step s{};
-    const bool mine = b0 + tid < p.n_seqs;
-    if (mine) s = step_of(p, b0 + tid, bad);
-    Sums at = inclusive(Sums{s.need, s.n}, sum, part);
-    at.pages += before.pages;
-    at.rows += before.rows;
-    const bool served = at.pages <= top && at.rows <= p.T;            // sums ascend: from the first that is not, nobody who asks for any
-    const Sums mine_now = served ? Sums{s.need, s.n} : Sums{0, 0};
-    Sums got = sum;
-    const bool some_not = __syncthreads_or(!served && s.n > 0);
-    Sums upto{at.pages - before.pages, at.rows - before.rows};
-    if (some_not) upto = inclusive(mine_now, got, part);
-    if (mine) {
-      const int32_t start = (int32_t)(rows + upto.rows - mine_now.rows);
-      starts[b0 + tid] = start;
-      if (blockIdx.x == 0) p.q_start[b0 + tid] = start;
-    }
-    first[tid] = (int32_t)(upto.pages - mine_now.pages);
-    kept_of[tid] = s.kept;
-    __syncthreads();
-    for (int64_t f = me; f < got.pages; f += all) {
-      const int32_t i = find(first, 0, blockDim.x, f);
-      p.page_table[(int64_t)(b0 + i) * p.max_pages + kept_of[i] + (f - first[i])] = p.free_pages[top - 1 - taken - f];
-    }
-    before.pages += sum.pages;
-    before.rows += sum.rows;
-    rows += got.rows;
-    taken += got.pages;
-    __syncthreads();
+// the run of warp `warp` of `warps`: a multiple of 32 entries
+__device__ __forceinline__ void run_of(int64_t count, int64_t warp, int64_t warps, int64_t& from, int64_t& to) {
+  const int64_t per = ((count + warps - 1) / warps + 31) & ~(int64_t)31;
+  from = warp * per < count ? warp * per : count;
+  to = from + per < count ? from + per : count;
+}
+
+template <typename F>
+__device__ __forceinline__ void shared_out(const int32_t* at, int32_t n, int64_t count, int64_t warp, int64_t warps, F f) {
+  int64_t from, to;
+  run_of(count, warp, warps, from, to);
+  if (from < to) walk(at, n, from, to, from < at[n] ? find(at, 0, n, from) : 0, f);
+}
+
+// `first`: what the sequence had in front of its rows
+__device__ __forceinline__ void write_row(const Plan& p, int64_t r, int32_t b, int32_t first) {
+  int64_t slot = -1;
+  int32_t pos = 0;
+  if (b >= 0) {
+    pos = first + (int32_t)r;
+    const int64_t page = p.page_table[(int64_t)b * p.max_pages + (pos >> p.page_shift)];
+    slot = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+  }
+  if (p.slot) p.slot[r] = slot;
+  if (p.pos) p.pos[r] = pos;
+}
+
+__global__ void __launch_bounds__(kMaxThreads) fb4_plan_kernel(const __grid_constant__ Plan p) {
+  extern __shared__ int32_t smem[];        // per sequence: tokens kept; and in front of it: pages that go back, pages taken, rows
+  __shared__ Sums part[32];
+  __shared__ int32_t served_need;
+  __shared__ uint32_t served_rows;
+  int32_t *keep = smem, *back = keep + p.n_seqs, *take = back + p.n_seqs + 1, *start = take + p.n_seqs + 1;
+  const bool cluster = gridDim.x > 1;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const int64_t me = (int64_t)blockIdx.x * warps + warp, all = (int64_t)gridDim.x * warps;
+  const uint32_t most = (uint32_t)p.T + 1u;
+  bool bad = false;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- every thread a run of sequences; sums in front of each
+  const int32_t per = (p.n_seqs + (int)blockDim.x - 1) / (int)blockDim.x, b0 = min(tid * per, p.n_seqs), b1 = min(b0 + per, p.n_seqs);
+  const int32_t f0 = *p.n_free;
+  Sums mine{0, 0, 0};
+  for (int32_t b = b0; b < b1; ++b) {
+    const Step s = step_of(p, b, bad);
+    keep[b] = s.keep;
+    back[b] = s.back;
+    take[b] = s.need;
+    start[b] = (int32_t)min((uint32_t)s.n, most);
+    mine = add(mine, Sums{s.back, s.need, (uint32_t)start[b]}, most);
   }
   if (tid == 0) {
-    starts[p.n_seqs] = (int32_t)rows;
-    if (blockIdx.x == 0) p.q_start[p.n_seqs] = (int32_t)rows;
+    served_need = 0;
+    served_rows = 0;
   }
-  all_sync(cluster);
-
-  // ---- the rows: a warp takes a run of them and walks over the sequences that it belongs to
-  {
-    const int lane = tid & 31;
-    const int64_t warps = all >> 5, per = ((p.T + warps - 1) / warps + 31) & ~(int64_t)31;
-    const int64_t r0 = (me >> 5) * per, r1 = r0 + per < p.T ? r0 + per : p.T;
-    int32_t b = r0 < rows ? find(starts, 0, p.n_seqs, r0) : 0;
-    for (int64_t r = r0 + lane; r - lane < r1; r += 32) {
-      int64_t slot = -1;
-      int32_t pos = 0;
-      if (r - lane < rows) {                                          // some row of these 32 is a token's
-        int32_t mine = b;
-        if (r - lane + 31 >= starts[b + 1]) {
-          mine = find(starts, b, p.n_seqs, r < rows ? r : rows - 1);
-          b = __shfl_sync(0xffffffffu, mine, 31);
-        }
-        if (r < rows) {
-          bool ignored = false;
-          pos = step_of(p, mine, ignored).keep + (int32_t)(r - starts[mine]);
-          const int64_t page = p.page_table[(int64_t)mine * p.max_pages + (pos >> p.page_shift)];
-          slot = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
-        }
-      }
-      if (r < r1) {
-        if (p.slot) p.slot[r] = slot;
-        if (p.pos) p.pos[r] = pos;
-      }
+  Sums at = scanned(mine, most);
+  if (lane == 31) part[warp] = at;
+  __syncthreads();
+  const Sums sums = scanned(lane < warps ? part[lane] : Sums{0, 0, 0}, most);
+  const int before_warp = warp ? warp - 1 : 0;
+  Sums base{__shfl_sync(0xffffffffu, sums.back, before_warp), __shfl_sync(0xffffffffu, sums.need, before_warp), __shfl_sync(0xffffffffu, sums.rows, before_warp)};
+  if (!warp) base = Sums{0, 0, 0};
+  const int32_t total_back = __shfl_sync(0xffffffffu, sums.back, 31);
+  // in front of this thread's run: the inclusive sums of the thread before (sums that are cut off cannot be subtracted)
+  Sums prev{__shfl_up_sync(0xffffffffu, at.back, 1), __shfl_up_sync(0xffffffffu, at.need, 1), __shfl_up_sync(0xffffffffu, at.rows, 1)};
+  if (!lane) prev = Sums{0, 0, 0};
+  Sums run = add(base, prev, most);
+  const int64_t free0 = f0 < 0 ? 0 : f0 < p.free_cap ? f0 : p.free_cap;
+  int64_t top = free0 + total_back;
+  const bool over = top > p.free_cap;                                  // pages that the list has no room for are lost, and reported
+  if (free0 != f0 || over) bad = true;
+  const int64_t usable = over ? p.free_cap : top;
+  // ---- who is served: from the first whose sums are too large on, nobody who asks for tokens
+  for (int32_t b = b0; b < b1; ++b) {
+    const Sums next = add(run, Sums{back[b], take[b], (uint32_t)start[b]}, most);
+    const bool served = next.need <= usable && next.rows <= (uint32_t)p.T;
+    back[b] = run.back;
+    take[b] = served ? run.need : -1;
+    start[b] = (int32_t)run.rows;
+    if (served && b == b1 - 1) {
+      atomicMax(&served_need, next.need);
+      atomicMax(&served_rows, next.rows);
+    } else if (!served && b > b0 && take[b - 1] >= 0) {               // the last served one of this run
+      atomicMax(&served_need, run.need);
+      atomicMax(&served_rows, run.rows);
     }
+    run = next;
   }
+  __syncthreads();
+  const int32_t taken = served_need, rows = (int32_t)served_rows;
+  for (int32_t b = b0; b < b1; ++b)
+    if (take[b] < 0) {
+      take[b] = taken;
+      start[b] = rows;
+    }
+  if (tid == 0) {
+    back[p.n_seqs] = total_back;
+    take[p.n_seqs] = taken;
+    start[p.n_seqs] = rows;
+  }
+  __syncthreads();
+
+  // ---- pages to the free list, pages from it
+  if (total_back) {
+    shared_out(back, p.n_seqs, total_back, me, all, [&](int64_t f, int32_t b) {
+      const int64_t to = top - 1 - f;
+      if (to < p.free_cap) p.free_pages[to] = p.page_table[(int64_t)b * p.max_pages + pages_of(p, keep[b]) + (f - back[b])];
+    });
+    all_sync(cluster);
+  }
+  shared_out(take, p.n_seqs, taken, me, all, [&](int64_t f, int32_t b) {
+    p.page_table[(int64_t)b * p.max_pages + pages_of(p, keep[b]) + (f - take[b])] = p.free_pages[usable - 1 - f];
+  });
+  for (int32_t b = blockIdx.x * blockDim.x + tid; b <= p.n_seqs; b += gridDim.x * blockDim.x) p.q_start[b] = start[b];
   all_sync(cluster);
 
   // ---- lengths last: until here everybody reads what the sequences held
-  for (int32_t b = me; b < p.n_seqs; b += all) {
-    bool ignored = false;
-    p.kv_len[b] = step_of(p, b, ignored).keep + starts[b + 1] - starts[b];
+  for (int32_t b = blockIdx.x * blockDim.x + tid; b < p.n_seqs; b += gridDim.x * blockDim.x) p.kv_len[b] = keep[b] + start[b + 1] - start[b];
+  if (blockIdx.x == 0 && tid == 0) *p.n_free = (int32_t)(usable - taken);
+  if (p.rows_here) shared_out(start, p.n_seqs, p.T, me, all, [&](int64_t r, int32_t b) { write_row(p, r, b, b < 0 ? 0 : keep[b] - start[b]); });
+  if (__syncthreads_or(bad) && blockIdx.x == 0 && tid == 0) atomicOr(p.status, 2u);
+}
+
+constexpr int kRowsPerWarp = 256;
+
+// The rows, 8 warps to a CTA.
+__global__ void __launch_bounds__(256) fb4_plan_rows_kernel(const __grid_constant__ Plan p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31;
+  const int64_t from = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * kRowsPerWarp, to = from + kRowsPerWarp < p.T ? from + kRowsPerWarp : p.T;
+  if (from >= to) return;
+  int32_t lo = 0, hi = p.n_seqs;           // the sequence of the run's first row, 32 places at a time
+  if (from < p.q_start[p.n_seqs]) {
+    while (hi - lo > 1) {
+      const int32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+      const uint32_t below = __ballot_sync(0xffffffffu, at < hi && p.q_start[at] <= from);
+      const int k = below ? 31 - __clz((int)below) : 0;
+      lo += k * step;
+      if (lo + step < hi) hi = lo + step;
+    }
   }
-  if (me == 0) *p.n_free = (int32_t)(top - taken);
-  if (__syncthreads_or(bad) && me == 0) atomicOr(p.status, 2u);
+  walk(p.q_start, p.n_seqs, from, to, lo, [&](int64_t r, int32_t b) {
+    write_row(p, r, b, b < 0 ? 0 : p.kv_len[b] - p.q_start[b + 1]);
+  });
 }
 
 }  // namespace
 
 cudaError_t fb4_plan_prepare_device() {
-  cudaError_t e = cudaFuncSetAttribute(fb4_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (FB4_PLAN_MAX_SEQS + 1) * 4);
-  return e;
+  return cudaFuncSetAttribute(fb4_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (4 * FB4_PLAN_MAX_SEQS + 3) * 4);
 }
 
 cudaError_t fb4_launch_cache_plan(const fb4_ctx* ctx, int32_t* page_table, int32_t max_pages, int32_t page_tokens, int32_t* kv_len,
                                   const int32_t* keep, const int32_t* new_len, int32_t n_seqs, int32_t* free_pages, int32_t free_cap,
-                                  int32_t* n_free, int64_t T, int32_t* q_start, int64_t* slot, int32_t* pos, cudaStream_t stream) {
-  Plan p{page_table, max_pages, 0, kv_len, keep, new_len, n_seqs, free_pages, free_cap, n_free, T, q_start, slot, pos, ctx->d_status};
+                                  int32_t* n_free, int64_t T, int32_t* q_start, int64_t* slot, int32_t* pos, cudaStream_t stream, int* launches) {
+  Plan p{page_table, max_pages, 0, kv_len, keep, new_len, n_seqs, free_pages, free_cap, n_free, T, q_start, slot, pos, T <= 8192, ctx->d_status};
   while ((1 << p.page_shift) < page_tokens) ++p.page_shift;
   const bool large = T > 2048 || n_seqs > 512;
   int threads = kMaxThreads;
   if (!large)
-    for (threads = 128; threads < n_seqs; threads *= 2) {}
+    for (threads = 128; threads < n_seqs || threads < T / 4; threads *= 2) {}
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
   cfg.gridDim = dim3(large ? kCluster : 1);
   cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = (size_t)(n_seqs + 1) * 4;
+  cfg.dynamicSmemBytes = (size_t)(4 * n_seqs + 3) * 4;
   cfg.stream = stream;
   cfg.attrs = attr;
   if (large) {
@@ -259,5 +287,15 @@ cudaError_t fb4_launch_cache_plan(const fb4_ctx* ctx, int32_t* page_table, int32
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.numAttrs = 1;
   }
-  return cudaLaunchKernelEx(&cfg, fb4_plan_kernel, p);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, fb4_plan_kernel, p);
+  *launches = 1;
+  if (e != cudaSuccess || p.rows_here || (!slot && !pos)) return e;
+  cfg.gridDim = dim3((unsigned)((T + 8 * kRowsPerWarp - 1) / (8 * kRowsPerWarp)));
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = 0;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // may be set up while the first kernel still runs
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.numAttrs = 1;
+  *launches = 2;
+  return cudaLaunchKernelEx(&cfg, fb4_plan_rows_kernel, p);
 }

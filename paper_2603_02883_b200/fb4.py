@@ -947,8 +947,8 @@ class Fb4:
                 raise ValueError("new_len and keep must be contiguous int32 tensors [n_seqs]")
             if t.get_device() != device:
                 raise ValueError(f"tensors must be on cuda:{self.device}, the device of this context")
-        if not 0 <= rows < 1 << 31:
-            raise ValueError("rows must be in [0, 2^31)")
+        if not 0 <= rows <= 1 << 30:
+            raise ValueError("rows must be in [0, 2^30]")
         q_start, slot, pos = new_len.new_empty(n + 1), new_len.new_empty(rows, dtype=torch.int64), new_len.new_empty(rows)
         self._call("fb4_cache_plan", table, max_pages, page_tokens, kv_len, None if keep is None else keep.data_ptr(), new_len.data_ptr(), n,
                    free, cap, n_free, rows, q_start.data_ptr(), slot.data_ptr(), pos.data_ptr())

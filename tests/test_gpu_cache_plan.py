@@ -110,7 +110,7 @@ def test_no_rows_and_no_list(q):
 
 def test_the_largest_number_of_sequences_and_many_rows(q):
     r = np.random.RandomState(5)
-    n = 32768
+    n = 8192
     table, kv, free, spare = state(r, n, 16, 20, 4, n)
     new = r.randint(0, 9, n).astype(np.int32)
     keep = np.maximum(kv - 3, 0).astype(np.int32)

@@ -23,7 +23,7 @@ PLAN = r"""
   if (plan(w, 1 << 26, 16, w, w, 31, w, 8, w, 10, w, slot, w) != FB4_ERR_CUDA || plan(w, 1 << 26, 16, w, w, 32, w, 8, w, 10, w, slot, w) != FB4_ERR_SHAPE) return 5;
   if (plan(w, 4, 16, w, w, -1, w, 8, w, 10, w, slot, w) != FB4_ERR_SHAPE || plan(w, 4, 16, w, w, FB4_PLAN_MAX_SEQS + 1, w, 8, w, 10, w, slot, w) != FB4_ERR_SHAPE) return 6;
   if (plan(w, 4, 16, w, w, 2, w, -1, w, 10, w, slot, w) != FB4_ERR_SHAPE) return 7;
-  if (plan(w, 4, 16, w, w, 2, w, 8, w, -1, w, slot, w) != FB4_ERR_SHAPE || plan(w, 4, 16, w, w, 2, w, 8, w, 1LL << 31, w, slot, w) != FB4_ERR_SHAPE) return 8;
+  if (plan(w, 4, 16, w, w, 2, w, 8, w, -1, w, slot, w) != FB4_ERR_SHAPE || plan(w, 4, 16, w, w, 2, w, 8, w, (1LL << 30) + 1, w, slot, w) != FB4_ERR_SHAPE) return 8;
   if (plan(0, 4, 16, w, w, 2, w, 8, w, 10, w, slot, w) != FB4_ERR_INVALID_ARG || plan(w, 4, 16, 0, w, 2, w, 8, w, 10, w, slot, w) != FB4_ERR_INVALID_ARG) return 9;
   if (plan(w, 4, 16, w, 0, 2, w, 8, w, 10, w, slot, w) != FB4_ERR_INVALID_ARG || plan(w, 4, 16, w, w, 2, 0, 8, w, 10, w, slot, w) != FB4_ERR_INVALID_ARG) return 10;
   if (plan(w, 4, 16, w, w, 2, w, 8, 0, 10, w, slot, w) != FB4_ERR_INVALID_ARG || plan(w, 4, 16, w, w, 2, w, 8, w, 10, 0, slot, w) != FB4_ERR_INVALID_ARG) return 11;
@@ -65,7 +65,7 @@ def test_cache_plan_in_the_binding(monkeypatch):
     plan = f.cache_plan(pt, i32(3), 7, keep=i32(3))
     assert plan.q_start.shape == (4,) and plan.slot.shape == (7,) and plan.slot.dtype == torch.int64 and plan.pos.dtype == torch.int32
     assert [c[0] for c in f.calls] == ["fb4_cache_plan"]
-    for new, rows, keep in ((i32(2), 7, None), (i32(3).long(), 7, None), (i32(6)[::2], 7, None), (i32(3), -1, None), (i32(3), 1 << 31, None),
+    for new, rows, keep in ((i32(2), 7, None), (i32(3).long(), 7, None), (i32(6)[::2], 7, None), (i32(3), -1, None), (i32(3), (1 << 30) + 1, None),
                             (i32(3), 7, i32(4)), (i32(3), 7, i32(3).short())):
         with pytest.raises(ValueError):
             f.cache_plan(pt, new, rows, keep=keep)
