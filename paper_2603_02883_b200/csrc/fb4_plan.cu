@@ -92,23 +92,35 @@ __device__ __forceinline__ int32_t find(const int32_t* at, int32_t lo, int32_t h
   return lo;
 }
 
-// Calls f(i, owner) for this lane's entries i of `count`, of which the first at[n] belong to owners 0 .. n - 1 (owner b has entries
-// at[b] .. at[b + 1] - 1) and the others to none (-1).  b: owner of the run's first entry.
-template <typename F>
-__device__ __forceinline__ void walk(const int32_t* at, int32_t n, int64_t from, int64_t to, int32_t b, F f) {
+// This lane's entries i of from .. to - 1, of which the first at[n] belong to owners 0 .. n - 1 (owner b has entries at[b] .. at[b + 1] - 1)
+// and the others to none (-1): store(i, owner, load(i, owner)), with the loads of K entries in flight.  b: owner of the run's first entry.
+template <int K, typename Load, typename Store>
+__device__ __forceinline__ void walk(const int32_t* at, int32_t n, int64_t from, int64_t to, int32_t b, Load load, Store store) {
   const int lane = threadIdx.x & 31;
   const int64_t owned = at[n];
-  for (int64_t i = from + lane; i - lane < to; i += 32) {
-    int32_t mine = -1;
-    if (i - lane < owned) {
-      mine = b;
-      if (i - lane + 31 >= at[b + 1]) {
-        mine = find(at, b, n, i < owned ? i : owned - 1);
-        b = __shfl_sync(0xffffffffu, mine, 31);
+  for (int64_t i0 = from; i0 < to; i0 += 32 * K) {
+    int32_t owner[K];
+    decltype(load(0, 0)) value[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t first = i0 + 32 * k, i = first + lane, last = first + 31 < owned ? first + 31 : owned - 1;
+      owner[k] = -1;
+      if (first < owned && first < to) {
+        int32_t mine = b;
+        if (last >= at[b + 1]) {                     // several owners, rarely more than these 32 and the next
+          const int32_t near = b + 33 < n && at[b + 33] > last ? b + 33 : n;
+          mine = find(at, b, near, i < owned ? i : owned - 1);
+          b = __shfl_sync(0xffffffffu, mine, 31);
+        }
+        if (i < owned) owner[k] = mine;
       }
-      if (i >= owned) mine = -1;
+      if (i < to) value[k] = load(i, owner[k]);
     }
-    if (i < to) f(i, mine);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t i = i0 + 32 * k + lane;
+      if (i < to) store(i, owner[k], value[k]);
+    }
   }
 }
 
@@ -119,24 +131,22 @@ __device__ __forceinline__ void run_of(int64_t count, int64_t warp, int64_t warp
   to = from + per < count ? from + per : count;
 }
 
-template <typename F>
-__device__ __forceinline__ void shared_out(const int32_t* at, int32_t n, int64_t count, int64_t warp, int64_t warps, F f) {
+template <typename Load, typename Store>
+__device__ __forceinline__ void shared_out(const int32_t* at, int32_t n, int64_t count, int64_t warp, int64_t warps, Load load, Store store) {
   int64_t from, to;
   run_of(count, warp, warps, from, to);
-  if (from < to) walk(at, n, from, to, from < at[n] ? find(at, 0, n, from) : 0, f);
+  if (from < to) walk<4>(at, n, from, to, from < at[n] ? find(at, 0, n, from) : 0, load, store);
 }
 
-// `first`: what the sequence had in front of its rows
-__device__ __forceinline__ void write_row(const Plan& p, int64_t r, int32_t b, int32_t first) {
-  int64_t slot = -1;
-  int32_t pos = 0;
-  if (b >= 0) {
-    pos = first + (int32_t)r;
-    const int64_t page = p.page_table[(int64_t)b * p.max_pages + (pos >> p.page_shift)];
-    slot = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
-  }
-  if (p.slot) p.slot[r] = slot;
-  if (p.pos) p.pos[r] = pos;
+// A row's position and page; `first` + r is its token's number.
+__device__ __forceinline__ int2 row_at(const Plan& p, int64_t r, int32_t b, int32_t first) {
+  if (b < 0) return make_int2(0, -1);
+  const int32_t pos = first + (int32_t)r;
+  return make_int2(pos, p.page_table[(int64_t)b * p.max_pages + (pos >> p.page_shift)]);
+}
+__device__ __forceinline__ void write_row(const Plan& p, int64_t r, int32_t b, int2 at) {
+  if (p.slot) p.slot[r] = b < 0 ? -1 : ((int64_t)at.y << p.page_shift) + (at.x & ((1 << p.page_shift) - 1));
+  if (p.pos) p.pos[r] = at.x;
 }
 
 __global__ void __launch_bounds__(kMaxThreads) fb4_plan_kernel(const __grid_constant__ Plan p) {
@@ -217,26 +227,26 @@ __global__ void __launch_bounds__(kMaxThreads) fb4_plan_kernel(const __grid_cons
 
   // ---- pages to the free list, pages from it
   if (total_back) {
-    shared_out(back, p.n_seqs, total_back, me, all, [&](int64_t f, int32_t b) {
-      const int64_t to = top - 1 - f;
-      if (to < p.free_cap) p.free_pages[to] = p.page_table[(int64_t)b * p.max_pages + pages_of(p, keep[b]) + (f - back[b])];
-    });
+    shared_out(back, p.n_seqs, total_back, me, all,
+               [&](int64_t f, int32_t b) { return p.page_table[(int64_t)b * p.max_pages + pages_of(p, keep[b]) + (f - back[b])]; },
+               [&](int64_t f, int32_t, int32_t page) { if (top - 1 - f < p.free_cap) p.free_pages[top - 1 - f] = page; });
     all_sync(cluster);
   }
-  shared_out(take, p.n_seqs, taken, me, all, [&](int64_t f, int32_t b) {
-    p.page_table[(int64_t)b * p.max_pages + pages_of(p, keep[b]) + (f - take[b])] = p.free_pages[usable - 1 - f];
-  });
+  shared_out(take, p.n_seqs, taken, me, all, [&](int64_t f, int32_t) { return p.free_pages[usable - 1 - f]; },
+             [&](int64_t f, int32_t b, int32_t page) { p.page_table[(int64_t)b * p.max_pages + pages_of(p, keep[b]) + (f - take[b])] = page; });
   for (int32_t b = blockIdx.x * blockDim.x + tid; b <= p.n_seqs; b += gridDim.x * blockDim.x) p.q_start[b] = start[b];
   all_sync(cluster);
 
   // ---- lengths last: until here everybody reads what the sequences held
   for (int32_t b = blockIdx.x * blockDim.x + tid; b < p.n_seqs; b += gridDim.x * blockDim.x) p.kv_len[b] = keep[b] + start[b + 1] - start[b];
   if (blockIdx.x == 0 && tid == 0) *p.n_free = (int32_t)(usable - taken);
-  if (p.rows_here) shared_out(start, p.n_seqs, p.T, me, all, [&](int64_t r, int32_t b) { write_row(p, r, b, b < 0 ? 0 : keep[b] - start[b]); });
+  if (p.rows_here)
+    shared_out(start, p.n_seqs, p.T, me, all, [&](int64_t r, int32_t b) { return row_at(p, r, b, b < 0 ? 0 : keep[b] - start[b]); },
+               [&](int64_t r, int32_t b, int2 at) { write_row(p, r, b, at); });
   if (__syncthreads_or(bad) && blockIdx.x == 0 && tid == 0) atomicOr(p.status, 2u);
 }
 
-constexpr int kRowsPerWarp = 256;
+constexpr int kRowsPerWarp = 64;
 
 // The rows, 8 warps to a CTA.
 __global__ void __launch_bounds__(256) fb4_plan_rows_kernel(const __grid_constant__ Plan p) {
@@ -254,9 +264,8 @@ __global__ void __launch_bounds__(256) fb4_plan_rows_kernel(const __grid_constan
       if (lo + step < hi) hi = lo + step;
     }
   }
-  walk(p.q_start, p.n_seqs, from, to, lo, [&](int64_t r, int32_t b) {
-    write_row(p, r, b, b < 0 ? 0 : p.kv_len[b] - p.q_start[b + 1]);
-  });
+  walk<kRowsPerWarp / 32>(p.q_start, p.n_seqs, from, to, lo, [&](int64_t r, int32_t b) { return row_at(p, r, b, b < 0 ? 0 : p.kv_len[b] - p.q_start[b + 1]); },
+                          [&](int64_t r, int32_t b, int2 at) { write_row(p, r, b, at); });
 }
 
 }  // namespace
