@@ -305,6 +305,7 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
     ctx->fast_ok = 1;
   ctx->append_error = fb4_rope_prepare_device();
   ctx->attend_error = fb4_attend_prepare_device();
+  ctx->append8_error = fb4_cache8_prepare_device();
   ctx->plan_error = fb4_plan_prepare_device();
   ctx->linear_error = fb4_linear_prepare_device(ctx->linear_slots);
   ctx->fast_table_bytes = fast_bytes;
@@ -830,6 +831,7 @@ int fb4_cache8_append(fb4_ctx* ctx, const fb4_cache8* cache, const int32_t* page
   if (rc != FB4_OK) return rc;
   if (q_heads > 0 && q == q_out && q_ld != q_out_ld) return FB4_ERR_INVALID_ARG;
   if (!aligned16(k_gain) || (q_heads > 0 && !aligned16(q_gain))) return FB4_ERR_ALIGN;
+  if (ctx->append8_error != cudaSuccess) return fb4_set_cuda_error(ctx->append8_error);
   const cudaError_t e = fb4_launch_cache8_append(ctx, cache, page_table, max_pages, kv_len, q_start, n_seqs, max_q, k, k_ld, v, v_ld, T, k_gain,
                                                  eps, rope, q, q_heads, q_ld, q_gain, q_out, q_out_ld, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fb4_set_cuda_error(e);

@@ -5,9 +5,10 @@
 // [-127, 127].  A power of two and not the maximum over 127: a block that is filled token by token grows its scale a few times, and codes that
 // are halved are off by at most one step of the last scale in all, while factors just above one would add half a step each time.
 //
-// Work: a CTA takes the new tokens of one block of one sequence, over all heads of K, V and Q (or one of `parts` shares of them).  The
-// tokens' cosines and sines go to shared memory once.  A warp takes a head of K or V at a time: the block's rows, norm and rotation, the
-// maximum over all of it, the codes.  Nobody else writes to a block, so there are no atomics, and the result is the same for every grid.
+// Work: a CTA takes the new tokens of a few blocks of one sequence, over all heads of K, V and Q (or one of `parts` shares of them).  The
+// tokens' cosines and sines go to shared memory once.  A warp takes one block of one head of K or V at a time (or 16 rows of Q): its rows, which
+// were requested while the unit before was rounded and stored, norm and rotation, the maximum over all of it, the codes.  Nobody else writes to
+// a block, so there are no atomics, and the result is the same for every grid.
 #include "fb4_attend.cuh"
 #include "fb4_rope.cuh"
 
@@ -17,6 +18,8 @@ using namespace fb4rope;
 
 constexpr int kWarps = 8;
 constexpr int kPlaces = 16;                // tokens of a block
+constexpr int kMaxBlocks = 8;              // of a CTA
+constexpr int kSmem = 100 * 1024;          // of a CTA; two are on an SM
 constexpr int kMinByte = 58, kMaxByte = 185;
 
 struct Append8 {
@@ -32,13 +35,14 @@ struct Append8 {
   const int32_t* q_start;
   int32_t n_seqs, max_q, max_kv;
   int64_t total_q;
-  int32_t blocks;           // > 0: CTAs per sequence; 0: the sequence is looked up (see owner)
+  int32_t blocks;           // blocks to a CTA
+  int32_t ctas;             // > 0: CTAs per sequence; 0: the sequence is looked up (see owner)
   uint32_t* status;
 };
 
-// Sequence b owns the CTAs from (q_start[b] >> 4) + 2 b on: the rows of a sequence touch at most rows / 16 + 2 blocks, so these
-// runs hold them, and together they are not many more than the blocks that there are.
-__device__ __forceinline__ int64_t first_cta(const Append8& p, int32_t b) { return (__ldg(p.q_start + b) >> 4) + 2 * (int64_t)b; }
+// Sequence b owns the CTAs from q_start[b] / (16 blocks) + 2 b on: its blocks, the first of which may hold tokens already, make at most
+// rows / (16 blocks) + 2 groups, so these runs hold them, and together they are not many more than the groups that there are.
+__device__ __forceinline__ int64_t first_cta(const Append8& p, int32_t b) { return __ldg(p.q_start + b) / (16 * p.blocks) + 2 * (int64_t)b; }
 
 __device__ __forceinline__ int32_t owner(const Append8& p, int64_t cta) {
   const int lane = threadIdx.x & 31;
@@ -118,38 +122,99 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float down) {
 
 __device__ __forceinline__ float two_to(int byte) { return __uint_as_float((uint32_t)byte << 23); }      // 2^(byte - 127), byte >= 1
 
+// 16 bytes to shared memory past L1
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// What a warp works on at a time.
+struct Unit {
+  int kind;                 // 0 K, 1 V, 2 Q
+  int32_t head, block;      // K, V
+  int32_t lo, hi;           // K, V: places of the block that are new; Q: rows from .. to of the group's (head-major: row r = head r / tokens)
+};
+
 template <int LG, bool INTER>
 __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const __grid_constant__ Append8 p) {
-  constexpr int RP = 32 / LG, NP = kPlaces / RP;      // rows of a pass, passes of a block
+  constexpr int RP = 32 / LG, NP = kPlaces / RP;      // rows of a pass, passes of a unit
   constexpr bool kHold = NP <= 4;                     // rows stay in registers between maximum and codes; else they are computed twice
-  extern __shared__ __align__(16) float4 cs_smem[];
+  extern __shared__ __align__(16) float4 smem4[];     // the warps' rows, then cosines and sines
   __shared__ __align__(16) uint8_t gain_smem[kGainBytes];
+  __shared__ int64_t page_of[kMaxBlocks];
   const uint32_t gains = fb4blk::smem_u32(gain_smem);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane % LG, g = lane / LG;
   const bool on = j < p.D / 16;
   const int half = p.D / 2, couples = p.D / 4;
+  const uint32_t stage = fb4blk::smem_u32(smem4) + (warp * NP * 2 * 32 + lane) * 16;      // this lane's pieces, 512 bytes apart
+  float4* cs_smem = smem4 + kWarps * NP * 2 * 32;
 
   // ---- which tokens
   int32_t b, nth;
-  if (p.blocks > 0) {
-    b = (int32_t)(blockIdx.x / p.blocks);
-    nth = (int32_t)(blockIdx.x - (int64_t)b * p.blocks);
+  if (p.ctas > 0) {
+    b = (int32_t)(blockIdx.x / p.ctas);
+    nth = (int32_t)(blockIdx.x - (int64_t)b * p.ctas);
   } else {
     b = owner(p, blockIdx.x);
     const int64_t d = blockIdx.x - first_cta(p, b);
-    nth = d < 0 || d > 0x7ffffff ? 0x7ffffff : (int32_t)d;
+    nth = d < 0 || d > 0x3ffffff ? 0x3ffffff : (int32_t)d;
   }
   const fb4att::Sequence sq = fb4att::sequence(p, b, nth == 0 && blockIdx.y == 0 && threadIdx.x == 0);
   const int32_t first = sq.kv - sq.n_q, from = first > 0 ? first : 0;
-  const int64_t base = ((int64_t)(from >> 4) + nth) << 4;                 // position of the block's first place
-  const int32_t lo = base > from ? 0 : from & 15;                         // places lo <= i < hi are new
+  const int64_t base = (((int64_t)(from >> 4) + (int64_t)nth * p.blocks) << 4);      // position of the group's first place
   if (base >= sq.kv || sq.n_q == 0) return;
-  const int32_t hi = sq.kv - base < kPlaces ? (int32_t)(sq.kv - base) : kPlaces, n_new = hi - lo;
+  const int32_t lo = base > from ? 0 : from & 15;                         // places lo <= i < hi of the group are new
+  const int32_t hi = sq.kv - base < kPlaces * p.blocks ? (int32_t)(sq.kv - base) : kPlaces * p.blocks, n_new = hi - lo;
   const int64_t row0 = sq.q0 + (base - first);                            // row of place 0 (which may be no row of the call)
   bool bad = false;
 
+  // ---- the units of this warp
+  const int32_t H = p.cache.n_heads, kv_units = (hi + kPlaces - 1) / kPlaces * 2 * H, q_rows = n_new * p.q.n;
+  const int32_t units = kv_units + (q_rows + kPlaces - 1) / kPlaces, step = gridDim.y * kWarps;
+  auto unit_at = [&](int32_t u) -> Unit {
+    if (u >= kv_units) return Unit{2, 0, 0, (u - kv_units) * kPlaces, q_rows};
+    const int32_t block = u / (2 * H), h = u - block * 2 * H;
+    return Unit{h >= H, h >= H ? h - H : h, block, max(lo - kPlaces * block, 0), min(hi - kPlaces * block, kPlaces)};
+  };
+  // place (in the group) and head of this lane's row of pass n; real: there is such a row
+  auto row_of = [&](const Unit& u, int n, int32_t& place, int32_t& head) -> bool {
+    const int32_t i = n * RP + g;
+    if (u.kind < 2) {
+      place = u.block * kPlaces + i;
+      head = u.head;
+      return on && i >= u.lo && i < u.hi;
+    }
+    const bool real = on && u.lo + i < u.hi;
+    head = real ? (u.lo + i) / n_new : 0;
+    place = lo + (real ? u.lo + i - head * n_new : 0);
+    return real;
+  };
+  auto any_row = [&](const Unit& u, int n) -> bool { return u.kind < 2 ? (n + 1) * RP > u.lo && n * RP < u.hi : u.lo + n * RP < u.hi; };
+  auto request = [&](int32_t at) {
+    if (at < units) {
+      const Unit u = unit_at(at);
+      const Heads& hd = u.kind == 0 ? p.k : u.kind == 1 ? p.v : p.q;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        int32_t place, head;
+        if (!row_of(u, n, place, head)) continue;
+        const uint16_t* x = hd.x + (row0 + place) * hd.ld + (int64_t)head * p.D + 8 * j;
+        copy16(stage + n * 1024, x);
+        copy16(stage + n * 1024 + 512, x + half);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  request(blockIdx.y * kWarps + warp);
+
   stage_gains<LG, INTER>(p, gains);
+  if (threadIdx.x < p.blocks && threadIdx.x * kPlaces < hi) {
+    const int64_t page = __ldg(p.page_table + (int64_t)b * p.max_pages + ((base + threadIdx.x * kPlaces) >> p.page_shift));
+    const bool there = page >= 0 && page < p.cache.n_pages;
+    if (!there) bad = true;
+    page_of[threadIdx.x] = there ? page : -1;
+  }
   if (p.rope.table) {
+#pragma unroll 4
     for (int x = threadIdx.x; x < n_new * couples; x += kWarps * 32) {
       const int i = lo + x / couples, c = x % couples;
       const int32_t* pos = p.rope.pos + (row0 + i) * p.rope.n_axes;
@@ -173,114 +238,93 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const
       cs_smem[cs_piece(couples, i, c)] = v;
     }
   }
-  int64_t page = __ldg(p.page_table + (int64_t)b * p.max_pages + (base >> p.page_shift));
-  if (page < 0 || page >= p.cache.n_pages) { bad = true; page = -1; }
   __syncthreads();
 
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  const int32_t H = p.cache.n_heads, q_units = (n_new * p.q.n + kPlaces - 1) / kPlaces;
-  for (int32_t unit = blockIdx.y * kWarps + warp; unit < 2 * H + q_units; unit += gridDim.y * kWarps) {
-    if (unit < 2 * H) {
-      // ------------------------------------------------ a head of K or V
-      if (page < 0) continue;
-      const bool is_v = unit >= H;
-      const int32_t h = is_v ? unit - H : unit;
-      const Heads& hd = is_v ? p.v : p.k;
-      const int64_t cell = (page * H + h) << p.page_shift;                // the head's tokens in the page
-      const int32_t in_page = (int32_t)(base & ((1 << p.page_shift) - 1));
-      uint8_t* codes = (is_v ? p.cache.v : p.cache.k) + (cell + in_page) * p.D;
-      uint8_t* scale = (is_v ? p.cache.v_scale : p.cache.k_scale) + ((cell + in_page) >> 4);
-      const int held = lo > 0 ? min(max((int)*scale, kMinByte), kMaxByte) : kMinByte;
-      const uint16_t* x = hd.x + row0 * hd.ld + (int64_t)h * p.D + 8 * j;
-      const uint32_t gain = gains + (4 * LG + j) * 16;
-      uint4 ra[NP], rb[NP];
-#pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        const int i = n * RP + g;
-        ra[n] = rb[n] = zero;
-        if (on && i >= lo && i < hi) {
-          ra[n] = __ldg(reinterpret_cast<const uint4*>(x + i * hd.ld));
-          rb[n] = __ldg(reinterpret_cast<const uint4*>(x + i * hd.ld + half));
-        }
-      }
-      auto row = [&](int n, Share& y) {
-        if (is_v) {
-          unpack<INTER>(ra[n], rb[n], y);
-        } else {
-          CosSin t;
-          const int i = n * RP + g;
-          if (p.rope.table) read_cs<INTER>(cs_smem, couples, on && i >= lo && i < hi ? i : lo, on ? j : 0, p.D, t);
-          norm_rotate<LG, INTER>(ra[n], rb[n], p.k.gain != nullptr, gain, p, t, y);
-        }
-      };
-      Share y[kHold ? NP : 1];
-      float top = 0.0f;
-#pragma unroll
-      for (int n = 0; n < NP; ++n)
-        if ((n + 1) * RP > lo && n * RP < hi) {
-          Share& z = y[kHold ? n : 0];
-          row(n, z);
-          const int i = n * RP + g;
-          if (on && i >= lo && i < hi) top = top_of(z, top);
-        }
-#pragma unroll
-      for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-      const int byte = max(byte_of(top), held);
-      const float inv = two_to(254 - byte);
-      const bool clamp = byte == kMaxByte;
-#pragma unroll
-      for (int n = 0; n < NP; ++n)
-        if ((n + 1) * RP > lo && n * RP < hi) {
-          Share& z = y[kHold ? n : 0];
-          if (!kHold) row(n, z);
-          const int i = n * RP + g;
-          uint2 ca, cb;
-          encode<INTER>(z, inv, clamp, ca, cb);
-          if (on && i >= lo && i < hi) {
-            *reinterpret_cast<uint2*>(codes + i * p.D + 8 * j) = ca;
-            *reinterpret_cast<uint2*>(codes + i * p.D + 8 * j + half) = cb;
-          }
-        }
-      if (lo > 0 && byte > held) {                                        // the tokens that the block holds take the new scale
-        const float down = two_to(127 + held - byte);
-        for (int x16 = lane; x16 < lo * p.D / 16; x16 += 32) {
-          uint4 w = *reinterpret_cast<const uint4*>(codes + 16 * x16);
-          w = make_uint4(rescaled(w.x, down), rescaled(w.y, down), rescaled(w.z, down), rescaled(w.w, down));
-          *reinterpret_cast<uint4*>(codes + 16 * x16) = w;
-        }
-      }
-      __syncwarp();
-      if (lane == 0) *scale = (uint8_t)byte;
-    } else {
-      // ------------------------------------------------ 16 rows of Q (head-major: row r = head r / n_new, token r mod n_new)
-      const int32_t r0 = (unit - 2 * H) * kPlaces;
-      const uint32_t gain = gains + j * 16;
-#pragma unroll 2
-      for (int n = 0; n < NP; ++n) {
-        const int32_t r = r0 + n * RP + g;
-        if (r0 + n * RP >= n_new * p.q.n) break;
-        const bool real = on && r < n_new * p.q.n;
-        const int32_t h = real ? r / n_new : 0, i = lo + (real ? r - h * n_new : 0);
-        const int64_t at = (int64_t)h * p.D + 8 * j;
-        uint4 qa = zero, qb = zero;
-        if (real) {
-          const uint16_t* x = p.q.x + (row0 + i) * p.q.ld + at;
-          qa = *reinterpret_cast<const uint4*>(x);
-          qb = *reinterpret_cast<const uint4*>(x + half);
-        }
+  for (int32_t at = blockIdx.y * kWarps + warp; at < units; at += step) {
+    const Unit u = unit_at(at);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");                  // a lane reads only what it has copied itself
+    // a row after norm and rotation, as far as it gets them
+    auto row = [&](int n, Share& y, int32_t& place, int32_t& head) -> bool {
+      const bool real = row_of(u, n, place, head);
+      const uint4 ra = real ? fb4blk::lds_v4(stage + n * 1024) : zero, rb = real ? fb4blk::lds_v4(stage + n * 1024 + 512) : zero;
+      if (u.kind == 1) {
+        unpack<INTER>(ra, rb, y);
+      } else {
         CosSin t;
-        if (p.rope.table) read_cs<INTER>(cs_smem, couples, i, on ? j : 0, p.D, t);
+        if (p.rope.table) read_cs<INTER>(cs_smem, couples, real ? place : lo, on ? j : 0, p.D, t);
+        norm_rotate<LG, INTER>(ra, rb, (u.kind ? p.q.gain : p.k.gain) != nullptr, gains + ((u.kind ? 0 : 4 * LG) + j) * 16, p, t, y);
+      }
+      return real;
+    };
+    if (u.kind == 2) {
+      // ------------------------------------------------ rows of Q
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        if (!any_row(u, n)) break;
         Share y;
-        norm_rotate<LG, INTER>(qa, qb, p.q.gain != nullptr, gain, p, t, y);
+        int32_t place, head;
+        const bool real = row(n, y, place, head);
+        uint4 qa, qb;
         pack<INTER>(y, pack_bf16, qa, qb);
         if (real) {
-          uint16_t* o = p.q.out + (row0 + i) * p.q.out_ld + at;
+          uint16_t* o = p.q.out + (row0 + place) * p.q.out_ld + (int64_t)head * p.D + 8 * j;
           *reinterpret_cast<uint4*>(o) = qa;
           *reinterpret_cast<uint4*>(o + half) = qb;
         }
       }
+      request(at + step);
+      continue;
     }
+    // -------------------------------------------------- a block of a head of K or V
+    const int64_t page = page_of[u.block];
+    const int64_t cell = ((page < 0 ? 0 : page) * H + u.head) << p.page_shift;                  // the head's tokens in the page
+    const int32_t in_page = (int32_t)((base + u.block * kPlaces) & ((1 << p.page_shift) - 1));
+    uint8_t* codes = (u.kind ? p.cache.v : p.cache.k) + (cell + in_page) * p.D;
+    uint8_t* scale = (u.kind ? p.cache.v_scale : p.cache.k_scale) + ((cell + in_page) >> 4);
+    const int held = u.lo > 0 && page >= 0 ? min(max((int)*scale, kMinByte), kMaxByte) : kMinByte;
+    Share y[kHold ? NP : 1];
+    float top = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+      if (any_row(u, n)) {
+        Share& z = y[kHold ? n : 0];
+        int32_t place, head;
+        if (row(n, z, place, head)) top = top_of(z, top);
+      }
+    if (kHold) request(at + step);
+#pragma unroll
+    for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    const int byte = max(byte_of(top), held);
+    const float inv = two_to(254 - byte);
+    const bool clamp = byte == kMaxByte;
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+      if (any_row(u, n)) {
+        Share& z = y[kHold ? n : 0];
+        int32_t place, head;
+        const bool real = kHold ? row_of(u, n, place, head) : row(n, z, place, head);
+        uint2 ca, cb;
+        encode<INTER>(z, inv, clamp, ca, cb);
+        if (real && page >= 0) {
+          uint8_t* o = codes + (n * RP + g) * p.D + 8 * j;
+          *reinterpret_cast<uint2*>(o) = ca;
+          *reinterpret_cast<uint2*>(o + half) = cb;
+        }
+      }
+    if (!kHold) request(at + step);
+    if (u.lo > 0 && byte > held && page >= 0) {                           // the tokens that the block holds take the new scale
+      const float down = two_to(127 + held - byte);
+      for (int x16 = lane; x16 < u.lo * p.D / 16; x16 += 32) {
+        uint4 w = *reinterpret_cast<const uint4*>(codes + 16 * x16);
+        w = make_uint4(rescaled(w.x, down), rescaled(w.y, down), rescaled(w.z, down), rescaled(w.w, down));
+        *reinterpret_cast<uint4*>(codes + 16 * x16) = w;
+      }
+    }
+    __syncwarp();
+    if (lane == 0 && page >= 0) *scale = (uint8_t)byte;
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
   if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, 2u);
 }
 
@@ -334,6 +378,20 @@ __global__ void __launch_bounds__(256) fb4_cache8_values_kernel(const uint8_t* _
 
 }  // namespace
 
+// Opt-in to the dynamic shared memory of the append kernels on the current device.
+cudaError_t fb4_cache8_prepare_device() {
+  cudaError_t e = cudaSuccess;
+#define FB4_OPT_IN(LG) \
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_cache8_append_kernel<LG, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); \
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_cache8_append_kernel<LG, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)
+  FB4_OPT_IN(2);
+  FB4_OPT_IN(4);
+  FB4_OPT_IN(8);
+  FB4_OPT_IN(16);
+#undef FB4_OPT_IN
+  return e;
+}
+
 cudaError_t fb4_launch_cache8_append(const fb4_ctx* ctx, const fb4_cache8* cache, const int32_t* page_table, int32_t max_pages,
                                      const int32_t* kv_len, const int32_t* q_start, int32_t n_seqs, int32_t max_q, const void* k,
                                      int64_t k_ld, const void* v, int64_t v_ld, int64_t T, const void* k_gain, float eps,
@@ -358,22 +416,28 @@ cudaError_t fb4_launch_cache8_append(const fb4_ctx* ctx, const fb4_cache8* cache
   p.max_kv = 0x7fffffff;
   p.total_q = T;
   p.status = ctx->d_status;
-  // CTAs by sequence where that is not many more of them than by rows (one row each: exactly as many as there are blocks)
-  const int64_t by_seq = ((int64_t)max_q + 30) / 16 * n_seqs, by_rows = (T >> 4) + 2 * (int64_t)n_seqs;
-  const int64_t grid = by_seq <= by_rows ? by_seq : by_rows;
-  p.blocks = by_seq <= by_rows ? (int32_t)(((int64_t)max_q + 30) / 16) : 0;
-  // few blocks: a block's heads are shared out until every warp has one unit
-  const int64_t units = 2 * cache->n_heads + q_heads, slots = (int64_t)ctx->sm_count * 2;
-  int64_t parts = (slots + grid - 1) / grid;
-  const int64_t most = (units + kWarps - 1) / kWarps;
+  // blocks to a CTA: as many as leave one CTA for every place (what a CTA begins with, its cosines and its first rows, is waited for), and
+  // as its shared memory holds
+  const int lg = lanes_of(p.D), rows = kWarps * (kPlaces * lg / 32) * 1024, per_block = kPlaces * p.D * 4;
+  const int64_t slots = (int64_t)ctx->sm_count * 2, all = T / kPlaces + n_seqs;
+  int64_t each = (all + slots - 1) / slots;
+  if (each > (kSmem - rows) / per_block) each = (kSmem - rows) / per_block;
+  p.blocks = (int32_t)(each < 1 ? 1 : each < kMaxBlocks ? each : kMaxBlocks);
+  // CTAs by sequence where they are not more than by rows
+  const int64_t wide = kPlaces * p.blocks, by_seq = ((int64_t)max_q + 15 + wide - 1) / wide, by_rows = T / wide + 2 * (int64_t)n_seqs;
+  p.ctas = by_seq * n_seqs <= by_rows ? (int32_t)by_seq : 0;
+  const int64_t grid = p.ctas ? by_seq * n_seqs : by_rows;
+  // few blocks: their heads are shared out until every warp has one unit
+  const int64_t units = 2 * cache->n_heads + q_heads, most = (units + kWarps - 1) / kWarps;
+  int64_t parts = p.blocks > 1 ? 1 : (slots + grid - 1) / grid;
   if (parts > most) parts = most;
   const dim3 dims((unsigned)grid, (unsigned)parts);
-  const size_t smem = rope ? (size_t)kPlaces * p.D * 4 : 0;
+  const size_t smem = (size_t)rows + (rope ? p.blocks * per_block : 0);
   const bool inter = rope && rope->interleaved;
 #define FB4_APPEND8(LG) \
   inter ? fb4_cache8_append_kernel<LG, true><<<dims, kWarps * 32, smem, stream>>>(p) \
         : fb4_cache8_append_kernel<LG, false><<<dims, kWarps * 32, smem, stream>>>(p)
-  switch (lanes_of(p.D)) {
+  switch (lg) {
     case 2: FB4_APPEND8(2); break;
     case 4: FB4_APPEND8(4); break;
     case 8: FB4_APPEND8(8); break;

@@ -53,6 +53,7 @@ struct fb4_ctx {
   int fast_ok;                   // formatbook/stage-1 table fit the fast kernel's packed layout
   cudaError_t append_error;      // why the append kernels cannot be launched on this device; their calls return it
   cudaError_t attend_error;      // the same for the tensor-core attention kernels
+  cudaError_t append8_error;     // the same for the append to the 8-bit cache
   cudaError_t plan_error;        // the same for the plan of a step
   cudaError_t linear_error;      // the same for the products with FB4 weights
   int32_t linear_slots[4][9];    // per kernel variant and cluster size: CTAs that are resident at a time
@@ -132,6 +133,7 @@ cudaError_t fb4_launch_cache_append(const fb4_ctx* ctx, const void* q, int32_t q
                                     const fb4_cache* cache, void* q_out, int64_t q_out_ld, cudaStream_t stream);
 
 // append to the 8-bit cache and its decode (fb4_cache8.cu)
+cudaError_t fb4_cache8_prepare_device();
 cudaError_t fb4_launch_cache8_append(const fb4_ctx* ctx, const fb4_cache8* cache, const int32_t* page_table, int32_t max_pages,
                                      const int32_t* kv_len, const int32_t* q_start, int32_t n_seqs, int32_t max_q, const void* k,
                                      int64_t k_ld, const void* v, int64_t v_ld, int64_t T, const void* k_gain, float eps,
