@@ -127,11 +127,12 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// What a warp works on at a time.
+// What a warp works on at a time: a block of a head of K, V or Q, or, where a group has few tokens, 16 rows of Q of several heads.
+enum Kind { kK, kV, kQ, kFewQ };
 struct Unit {
-  int kind;                 // 0 K, 1 V, 2 Q
-  int32_t head, block;      // K, V
-  int32_t lo, hi;           // K, V: places of the block that are new; Q: rows from .. to of the group's (head-major: row r = head r / tokens)
+  int kind;
+  int32_t head, block;
+  int32_t lo, hi;           // rows of the unit that there are: places of the block, or rows lo .. hi of the group's (head-major: row r = head r / tokens)
 };
 
 template <int LG, bool INTER>
@@ -168,38 +169,45 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const
   bool bad = false;
 
   // ---- the units of this warp
-  const int32_t H = p.cache.n_heads, kv_units = (hi + kPlaces - 1) / kPlaces * 2 * H, q_rows = n_new * p.q.n;
-  const int32_t units = kv_units + (q_rows + kPlaces - 1) / kPlaces, step = gridDim.y * kWarps;
+  const int32_t H = p.cache.n_heads, blocks = (hi + kPlaces - 1) / kPlaces, q_rows = n_new * p.q.n;
+  const bool few = n_new < kPlaces;
+  const int32_t heads = 2 * H + (few ? 0 : p.q.n), by_block = blocks * heads;
+  const int32_t units = by_block + (few ? (q_rows + kPlaces - 1) / kPlaces : 0), step = gridDim.y * kWarps;
   auto unit_at = [&](int32_t u) -> Unit {
-    if (u >= kv_units) return Unit{2, 0, 0, (u - kv_units) * kPlaces, q_rows};
-    const int32_t block = u / (2 * H), h = u - block * 2 * H;
-    return Unit{h >= H, h >= H ? h - H : h, block, max(lo - kPlaces * block, 0), min(hi - kPlaces * block, kPlaces)};
+    if (u >= by_block) return Unit{kFewQ, 0, 0, (u - by_block) * kPlaces, q_rows};
+    const int32_t block = u / heads, h = u - block * heads;
+    const int kind = h < H ? kK : h < 2 * H ? kV : kQ;
+    return Unit{kind, h - kind * H, block, max(lo - kPlaces * block, 0), min(hi - kPlaces * block, kPlaces)};
   };
-  // place (in the group) and head of this lane's row of pass n; real: there is such a row
-  auto row_of = [&](const Unit& u, int n, int32_t& place, int32_t& head) -> bool {
+  auto side_of = [&](const Unit& u) -> const Heads& { return u.kind == kK ? p.k : u.kind == kV ? p.v : p.q; };
+  // This lane's row of pass n: is there one, and where in the rows of K, V or Q it starts (`first` = first_row of the unit).
+  auto first_row = [&](const Unit& u, int64_t ld) -> int64_t { return (row0 + u.block * kPlaces + g) * ld + (int64_t)u.head * p.D + 8 * j; };
+  auto row_of = [&](const Unit& u, int n, int64_t ld, int64_t first, int32_t& place, int64_t& at) -> bool {
     const int32_t i = n * RP + g;
-    if (u.kind < 2) {
+    if (u.kind != kFewQ) {
       place = u.block * kPlaces + i;
-      head = u.head;
+      at = first + n * (RP * ld);
       return on && i >= u.lo && i < u.hi;
     }
     const bool real = on && u.lo + i < u.hi;
-    head = real ? (u.lo + i) / n_new : 0;
+    const int32_t head = real ? (u.lo + i) / n_new : 0;
     place = lo + (real ? u.lo + i - head * n_new : 0);
+    at = (row0 + place) * ld + (int64_t)head * p.D + 8 * j;
     return real;
   };
-  auto any_row = [&](const Unit& u, int n) -> bool { return u.kind < 2 ? (n + 1) * RP > u.lo && n * RP < u.hi : u.lo + n * RP < u.hi; };
+  auto any_row = [&](const Unit& u, int n) -> bool { return u.kind != kFewQ ? (n + 1) * RP > u.lo && n * RP < u.hi : u.lo + n * RP < u.hi; };
   auto request = [&](int32_t at) {
     if (at < units) {
       const Unit u = unit_at(at);
-      const Heads& hd = u.kind == 0 ? p.k : u.kind == 1 ? p.v : p.q;
+      const Heads& hd = side_of(u);
+      const int64_t first = first_row(u, hd.ld);
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
-        int32_t place, head;
-        if (!row_of(u, n, place, head)) continue;
-        const uint16_t* x = hd.x + (row0 + place) * hd.ld + (int64_t)head * p.D + 8 * j;
-        copy16(stage + n * 1024, x);
-        copy16(stage + n * 1024 + 512, x + half);
+        int32_t place;
+        int64_t x;
+        if (!row_of(u, n, hd.ld, first, place, x)) continue;
+        copy16(stage + n * 1024, hd.x + x);
+        copy16(stage + n * 1024 + 512, hd.x + x + half);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -245,32 +253,32 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const
     const Unit u = unit_at(at);
     asm volatile("cp.async.wait_group 0;" ::: "memory");                  // a lane reads only what it has copied itself
     // a row after norm and rotation, as far as it gets them
-    auto row = [&](int n, Share& y, int32_t& place, int32_t& head) -> bool {
-      const bool real = row_of(u, n, place, head);
+    auto row = [&](int n, bool real, int32_t place, Share& y) {
       const uint4 ra = real ? fb4blk::lds_v4(stage + n * 1024) : zero, rb = real ? fb4blk::lds_v4(stage + n * 1024 + 512) : zero;
-      if (u.kind == 1) {
+      if (u.kind == kV) {
         unpack<INTER>(ra, rb, y);
       } else {
         CosSin t;
         if (p.rope.table) read_cs<INTER>(cs_smem, couples, real ? place : lo, on ? j : 0, p.D, t);
-        norm_rotate<LG, INTER>(ra, rb, (u.kind ? p.q.gain : p.k.gain) != nullptr, gains + ((u.kind ? 0 : 4 * LG) + j) * 16, p, t, y);
+        norm_rotate<LG, INTER>(ra, rb, (u.kind == kK ? p.k.gain : p.q.gain) != nullptr, gains + ((u.kind == kK ? 4 * LG : 0) + j) * 16, p, t, y);
       }
-      return real;
     };
-    if (u.kind == 2) {
+    if (u.kind >= kQ) {
       // ------------------------------------------------ rows of Q
-#pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        if (!any_row(u, n)) break;
+      const int64_t first = first_row(u, p.q.out_ld);
+#pragma unroll 1
+      for (int n = 0; n < NP; ++n) {                  // rolled up: three kinds of units on the way at a time fill the instruction cache
+        if (!any_row(u, n)) continue;
         Share y;
-        int32_t place, head;
-        const bool real = row(n, y, place, head);
+        int32_t place;
+        int64_t o;
+        const bool real = row_of(u, n, p.q.out_ld, first, place, o);
+        row(n, real, place, y);
         uint4 qa, qb;
         pack<INTER>(y, pack_bf16, qa, qb);
         if (real) {
-          uint16_t* o = p.q.out + (row0 + place) * p.q.out_ld + (int64_t)head * p.D + 8 * j;
-          *reinterpret_cast<uint4*>(o) = qa;
-          *reinterpret_cast<uint4*>(o + half) = qb;
+          *reinterpret_cast<uint4*>(p.q.out + o) = qa;
+          *reinterpret_cast<uint4*>(p.q.out + o + half) = qb;
         }
       }
       request(at + step);
@@ -280,8 +288,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const
     const int64_t page = page_of[u.block];
     const int64_t cell = ((page < 0 ? 0 : page) * H + u.head) << p.page_shift;                  // the head's tokens in the page
     const int32_t in_page = (int32_t)((base + u.block * kPlaces) & ((1 << p.page_shift) - 1));
-    uint8_t* codes = (u.kind ? p.cache.v : p.cache.k) + (cell + in_page) * p.D;
-    uint8_t* scale = (u.kind ? p.cache.v_scale : p.cache.k_scale) + ((cell + in_page) >> 4);
+    uint8_t* codes = (u.kind == kV ? p.cache.v : p.cache.k) + (cell + in_page) * p.D;
+    uint8_t* scale = (u.kind == kV ? p.cache.v_scale : p.cache.k_scale) + ((cell + in_page) >> 4);
     const int held = u.lo > 0 && page >= 0 ? min(max((int)*scale, kMinByte), kMaxByte) : kMinByte;
     Share y[kHold ? NP : 1];
     float top = 0.0f;
@@ -289,8 +297,10 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const
     for (int n = 0; n < NP; ++n)
       if (any_row(u, n)) {
         Share& z = y[kHold ? n : 0];
-        int32_t place, head;
-        if (row(n, z, place, head)) top = top_of(z, top);
+        const int32_t i = n * RP + g;
+        const bool real = on && i >= u.lo && i < u.hi;
+        row(n, real, u.block * kPlaces + i, z);
+        if (real) top = top_of(z, top);
       }
     if (kHold) request(at + step);
 #pragma unroll
@@ -302,12 +312,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const
     for (int n = 0; n < NP; ++n)
       if (any_row(u, n)) {
         Share& z = y[kHold ? n : 0];
-        int32_t place, head;
-        const bool real = kHold ? row_of(u, n, place, head) : row(n, z, place, head);
+        const int32_t i = n * RP + g;
+        const bool real = on && i >= u.lo && i < u.hi;
+        if (!kHold) row(n, real, u.block * kPlaces + i, z);
         uint2 ca, cb;
         encode<INTER>(z, inv, clamp, ca, cb);
         if (real && page >= 0) {
-          uint8_t* o = codes + (n * RP + g) * p.D + 8 * j;
+          uint8_t* o = codes + i * p.D + 8 * j;
           *reinterpret_cast<uint2*>(o) = ca;
           *reinterpret_cast<uint2*>(o + half) = cb;
         }
