@@ -16,10 +16,10 @@ namespace {
 
 using namespace fb4rope;
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
 constexpr int kPlaces = 16;                // tokens of a block
 constexpr int kMaxBlocks = 8;              // of a CTA
-constexpr int kSmem = 100 * 1024;          // of a CTA; two are on an SM
+constexpr int kSmem = 100 * 1024;          // of a CTA at most
 constexpr int kMinByte = 58, kMaxByte = 185;
 
 struct Append8 {
@@ -122,11 +122,6 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float down) {
 
 __device__ __forceinline__ float two_to(int byte) { return __uint_as_float((uint32_t)byte << 23); }      // 2^(byte - 127), byte >= 1
 
-// 16 bytes to shared memory past L1
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-
 // What a warp works on at a time: a block of a head of K, V or Q, or, where a group has few tokens, 16 rows of Q of several heads.
 enum Kind { kK, kV, kQ, kFewQ };
 struct Unit {
@@ -135,19 +130,35 @@ struct Unit {
   int32_t lo, hi;           // rows of the unit that there are: places of the block, or rows lo .. hi of the group's (head-major: row r = head r / tokens)
 };
 
+// A lane's 16 values of a pass in shared memory, 512 bytes apart
+__device__ __forceinline__ void put(uint32_t at, const Share& x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at + i * 512), "f"(x.a[2 * i]), "f"(x.a[2 * i + 1]), "f"(x.b[2 * i]), "f"(x.b[2 * i + 1]) : "memory");
+}
+__device__ __forceinline__ void get(uint32_t at, Share& x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 v = fb4blk::lds_v4(at + i * 512);
+    x.a[2 * i] = __uint_as_float(v.x);
+    x.a[2 * i + 1] = __uint_as_float(v.y);
+    x.b[2 * i] = __uint_as_float(v.z);
+    x.b[2 * i + 1] = __uint_as_float(v.w);
+  }
+}
+
 template <int LG, bool INTER>
-__global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const __grid_constant__ Append8 p) {
+__global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_append_kernel(const __grid_constant__ Append8 p) {
   constexpr int RP = 32 / LG, NP = kPlaces / RP;      // rows of a pass, passes of a unit
-  constexpr bool kHold = NP <= 4;                     // rows stay in registers between maximum and codes; else they are computed twice
-  extern __shared__ __align__(16) float4 smem4[];     // the warps' rows, then cosines and sines
+  extern __shared__ __align__(16) float4 smem4[];     // the warps' values, then cosines and sines
   __shared__ __align__(16) uint8_t gain_smem[kGainBytes];
   __shared__ int64_t page_of[kMaxBlocks];
   const uint32_t gains = fb4blk::smem_u32(gain_smem);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane % LG, g = lane / LG;
   const bool on = j < p.D / 16;
   const int half = p.D / 2, couples = p.D / 4;
-  const uint32_t stage = fb4blk::smem_u32(smem4) + (warp * NP * 2 * 32 + lane) * 16;      // this lane's pieces, 512 bytes apart
-  float4* cs_smem = smem4 + kWarps * NP * 2 * 32;
+  const uint32_t stage = fb4blk::smem_u32(smem4) + (warp * NP * 4 * 32 + lane) * 16;      // this lane's pieces
+  float4* cs_smem = smem4 + kWarps * NP * 4 * 32;
 
   // ---- which tokens
   int32_t b, nth;
@@ -196,23 +207,24 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const
     return real;
   };
   auto any_row = [&](const Unit& u, int n) -> bool { return u.kind != kFewQ ? (n + 1) * RP > u.lo && n * RP < u.hi : u.lo + n * RP < u.hi; };
-  auto request = [&](int32_t at) {
-    if (at < units) {
-      const Unit u = unit_at(at);
-      const Heads& hd = side_of(u);
-      const int64_t first = first_row(u, hd.ld);
-#pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        int32_t place;
-        int64_t x;
-        if (!row_of(u, n, hd.ld, first, place, x)) continue;
-        copy16(stage + n * 1024, hd.x + x);
-        copy16(stage + n * 1024 + 512, hd.x + x + half);
-      }
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  uint4 ra = zero, rb = zero;                         // the row of the pass to come
+  auto fetch = [&](const Unit& u, int n) {
+    const Heads& hd = side_of(u);
+    int32_t place;
+    int64_t x;
+    ra = rb = zero;
+    if (row_of(u, n, hd.ld, first_row(u, hd.ld), place, x)) {
+      ra = *reinterpret_cast<const uint4*>(hd.x + x);                     // plain loads: q_out may be q
+      rb = *reinterpret_cast<const uint4*>(hd.x + x + half);
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  request(blockIdx.y * kWarps + warp);
+  int32_t at = blockIdx.y * kWarps + warp;
+  Unit u{};
+  if (at < units) {
+    u = unit_at(at);
+    fetch(u, 0);
+  }
 
   stage_gains<LG, INTER>(p, gains);
   if (threadIdx.x < p.blocks && threadIdx.x * kPlaces < hi) {
@@ -248,94 +260,81 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fb4_cache8_append_kernel(const
   }
   __syncthreads();
 
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-  for (int32_t at = blockIdx.y * kWarps + warp; at < units; at += step) {
-    const Unit u = unit_at(at);
-    asm volatile("cp.async.wait_group 0;" ::: "memory");                  // a lane reads only what it has copied itself
-    // a row after norm and rotation, as far as it gets them
-    auto row = [&](int n, bool real, int32_t place, Share& y) {
-      const uint4 ra = real ? fb4blk::lds_v4(stage + n * 1024) : zero, rb = real ? fb4blk::lds_v4(stage + n * 1024 + 512) : zero;
+  for (; at < units; at += step) {
+    const int64_t out_first = u.kind >= kQ ? first_row(u, p.q.out_ld) : 0;
+    const Unit next = at + step < units ? unit_at(at + step) : u;
+    float top = 0.0f;
+    // One pass at a time, not unrolled: the instructions of three kinds of units would not stay in the instruction cache.  The values of K
+    // and V wait in shared memory for the block's maximum.
+#pragma unroll 1
+    for (int n = 0; n < NP; ++n) {
+      const uint4 xa = ra, xb = rb;
+      if (n + 1 < NP) fetch(u, n + 1);
+      else if (at + step < units) fetch(next, 0);
+      if (!any_row(u, n)) continue;
+      int32_t place;
+      int64_t o;
+      const bool real = row_of(u, n, p.q.out_ld, out_first, place, o);
+      Share y;
       if (u.kind == kV) {
-        unpack<INTER>(ra, rb, y);
+        unpack<INTER>(xa, xb, y);
       } else {
         CosSin t;
         if (p.rope.table) read_cs<INTER>(cs_smem, couples, real ? place : lo, on ? j : 0, p.D, t);
-        norm_rotate<LG, INTER>(ra, rb, (u.kind == kK ? p.k.gain : p.q.gain) != nullptr, gains + ((u.kind == kK ? 4 * LG : 0) + j) * 16, p, t, y);
+        norm_rotate<LG, INTER>(xa, xb, (u.kind == kK ? p.k.gain : p.q.gain) != nullptr, gains + ((u.kind == kK ? 4 * LG : 0) + j) * 16, p, t, y);
       }
-    };
-    if (u.kind >= kQ) {
-      // ------------------------------------------------ rows of Q
-      const int64_t first = first_row(u, p.q.out_ld);
-#pragma unroll 1
-      for (int n = 0; n < NP; ++n) {                  // rolled up: three kinds of units on the way at a time fill the instruction cache
-        if (!any_row(u, n)) continue;
-        Share y;
-        int32_t place;
-        int64_t o;
-        const bool real = row_of(u, n, p.q.out_ld, first, place, o);
-        row(n, real, place, y);
+      if (u.kind >= kQ) {
         uint4 qa, qb;
         pack<INTER>(y, pack_bf16, qa, qb);
         if (real) {
           *reinterpret_cast<uint4*>(p.q.out + o) = qa;
           *reinterpret_cast<uint4*>(p.q.out + o + half) = qb;
         }
+      } else {
+        put(stage + n * 2048, y);
+        if (real) top = top_of(y, top);
       }
-      request(at + step);
-      continue;
     }
-    // -------------------------------------------------- a block of a head of K or V
-    const int64_t page = page_of[u.block];
-    const int64_t cell = ((page < 0 ? 0 : page) * H + u.head) << p.page_shift;                  // the head's tokens in the page
-    const int32_t in_page = (int32_t)((base + u.block * kPlaces) & ((1 << p.page_shift) - 1));
-    uint8_t* codes = (u.kind == kV ? p.cache.v : p.cache.k) + (cell + in_page) * p.D;
-    uint8_t* scale = (u.kind == kV ? p.cache.v_scale : p.cache.k_scale) + ((cell + in_page) >> 4);
-    const int held = u.lo > 0 && page >= 0 ? min(max((int)*scale, kMinByte), kMaxByte) : kMinByte;
-    Share y[kHold ? NP : 1];
-    float top = 0.0f;
-#pragma unroll
-    for (int n = 0; n < NP; ++n)
-      if (any_row(u, n)) {
-        Share& z = y[kHold ? n : 0];
-        const int32_t i = n * RP + g;
-        const bool real = on && i >= u.lo && i < u.hi;
-        row(n, real, u.block * kPlaces + i, z);
-        if (real) top = top_of(z, top);
-      }
-    if (kHold) request(at + step);
+    const Unit now = u;
+    u = next;
+    if (now.kind >= kQ) continue;
+    // -------------------------------------------------- a block of a head of K or V: its scale and its codes
+    const int64_t page = page_of[now.block];
+    if (page < 0) continue;
+    const int64_t cell = (page * H + now.head) << p.page_shift;                                // the head's tokens in the page
+    const int32_t in_page = (int32_t)((base + now.block * kPlaces) & ((1 << p.page_shift) - 1));
+    uint8_t* codes = (now.kind == kV ? p.cache.v : p.cache.k) + (cell + in_page) * p.D;
+    uint8_t* scale = (now.kind == kV ? p.cache.v_scale : p.cache.k_scale) + ((cell + in_page) >> 4);
+    const int held = now.lo > 0 ? min(max((int)*scale, kMinByte), kMaxByte) : kMinByte;
 #pragma unroll
     for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     const int byte = max(byte_of(top), held);
     const float inv = two_to(254 - byte);
     const bool clamp = byte == kMaxByte;
-#pragma unroll
-    for (int n = 0; n < NP; ++n)
-      if (any_row(u, n)) {
-        Share& z = y[kHold ? n : 0];
-        const int32_t i = n * RP + g;
-        const bool real = on && i >= u.lo && i < u.hi;
-        if (!kHold) row(n, real, u.block * kPlaces + i, z);
-        uint2 ca, cb;
-        encode<INTER>(z, inv, clamp, ca, cb);
-        if (real && page >= 0) {
-          uint8_t* o = codes + i * p.D + 8 * j;
-          *reinterpret_cast<uint2*>(o) = ca;
-          *reinterpret_cast<uint2*>(o + half) = cb;
-        }
+#pragma unroll 1
+    for (int n = now.lo / RP; n * RP < now.hi; ++n) {
+      const int32_t i = n * RP + g;
+      Share y;
+      get(stage + n * 2048, y);
+      uint2 ca, cb;
+      encode<INTER>(y, inv, clamp, ca, cb);
+      if (on && i >= now.lo && i < now.hi) {
+        uint8_t* c = codes + i * p.D + 8 * j;
+        *reinterpret_cast<uint2*>(c) = ca;
+        *reinterpret_cast<uint2*>(c + half) = cb;
       }
-    if (!kHold) request(at + step);
-    if (u.lo > 0 && byte > held && page >= 0) {                           // the tokens that the block holds take the new scale
+    }
+    if (now.lo > 0 && byte > held) {                                      // the tokens that the block holds take the new scale
       const float down = two_to(127 + held - byte);
-      for (int x16 = lane; x16 < u.lo * p.D / 16; x16 += 32) {
+      for (int x16 = lane; x16 < now.lo * p.D / 16; x16 += 32) {
         uint4 w = *reinterpret_cast<const uint4*>(codes + 16 * x16);
         w = make_uint4(rescaled(w.x, down), rescaled(w.y, down), rescaled(w.z, down), rescaled(w.w, down));
         *reinterpret_cast<uint4*>(codes + 16 * x16) = w;
       }
     }
     __syncwarp();
-    if (lane == 0 && page >= 0) *scale = (uint8_t)byte;
+    if (lane == 0) *scale = (uint8_t)byte;
   }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
   if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, 2u);
 }
 
@@ -427,13 +426,9 @@ cudaError_t fb4_launch_cache8_append(const fb4_ctx* ctx, const fb4_cache8* cache
   p.max_kv = 0x7fffffff;
   p.total_q = T;
   p.status = ctx->d_status;
-  // blocks to a CTA: as many as leave one CTA for every place (what a CTA begins with, its cosines and its first rows, is waited for), and
-  // as its shared memory holds
-  const int lg = lanes_of(p.D), rows = kWarps * (kPlaces * lg / 32) * 1024, per_block = kPlaces * p.D * 4;
-  const int64_t slots = (int64_t)ctx->sm_count * 2, all = T / kPlaces + n_seqs;
-  int64_t each = (all + slots - 1) / slots;
-  if (each > (kSmem - rows) / per_block) each = (kSmem - rows) / per_block;
-  p.blocks = (int32_t)(each < 1 ? 1 : each < kMaxBlocks ? each : kMaxBlocks);
+  const int lg = lanes_of(p.D), rows = kWarps * (kPlaces * lg / 32) * 2048, per_block = kPlaces * p.D * 4;
+  const int64_t slots = (int64_t)ctx->sm_count * (lg == 16 ? 2 : 5);
+  p.blocks = 1;
   // CTAs by sequence where they are not more than by rows
   const int64_t wide = kPlaces * p.blocks, by_seq = ((int64_t)max_q + 15 + wide - 1) / wide, by_rows = T / wide + 2 * (int64_t)n_seqs;
   p.ctas = by_seq * n_seqs <= by_rows ? (int32_t)by_seq : 0;
