@@ -57,19 +57,11 @@ __device__ __forceinline__ int32_t owner(const Append8& p, int64_t cta) {
   return lo;
 }
 
-// cos / sin of the block's tokens in shared memory: couple c (two pairs) of token i at this 16-byte piece, so that the lanes of a
-// pass meet in different banks
-__device__ __forceinline__ int cs_piece(int couples, int i, int c) { return i * couples + (c ^ ((c >> 3) & 3) ^ ((i & 1) << 1)); }
-
-template <bool INTER>
-__device__ __forceinline__ void read_cs(const float4* cs, int couples, int i, int j, int D, CosSin& t) {
-#pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int c = INTER ? 2 * j + (n & 1) + (n < 2 ? 0 : D / 8) : 4 * j + n;
-    const float4 v = cs[cs_piece(couples, i, c)];
-    t.c[2 * n] = v.x; t.s[2 * n] = v.y; t.c[2 * n + 1] = v.z; t.s[2 * n + 1] = v.w;
-  }
-}
+// cos / sin of the block's tokens in shared memory: couple c (two pairs) of a token at this 16-byte piece of its row, so that the lanes
+// that read together meet in different banks (eight lanes of one token; in heads of 64 and 32 channels the odd token's are turned by two)
+__device__ __forceinline__ int cs_piece(int c) { return c ^ ((c >> 3) & 3); }
+template <int LG>
+__device__ __forceinline__ int cs_turn(int i) { return LG <= 4 ? (i & 1) << 1 : 0; }
 
 __device__ __forceinline__ float top_of(const Share& x, float top) {
 #pragma unroll
@@ -184,45 +176,57 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
   const bool few = n_new < kPlaces;
   const int32_t heads = 2 * H + (few ? 0 : p.q.n), by_block = blocks * heads;
   const int32_t units = by_block + (few ? (q_rows + kPlaces - 1) / kPlaces : 0), step = gridDim.y * kWarps;
-  auto unit_at = [&](int32_t u) -> Unit {
-    if (u >= by_block) return Unit{kFewQ, 0, 0, (u - by_block) * kPlaces, q_rows};
-    const int32_t block = u / heads, h = u - block * heads;
-    const int kind = h < H ? kK : h < 2 * H ? kV : kQ;
-    return Unit{kind, h - kind * H, block, max(lo - kPlaces * block, 0), min(hi - kPlaces * block, kPlaces)};
+  // The units in order: (block, head) moved on without divisions.
+  int32_t next_block = 0, next_head = 0, at = blockIdx.y * kWarps + warp;
+  auto advance = [&](int32_t by) {
+    next_head += by;
+    while (next_head >= heads) {
+      next_head -= heads;
+      ++next_block;
+    }
   };
-  auto side_of = [&](const Unit& u) -> const Heads& { return u.kind == kK ? p.k : u.kind == kV ? p.v : p.q; };
-  // This lane's row of pass n: is there one, and where in the rows of K, V or Q it starts (`first` = first_row of the unit).
-  auto first_row = [&](const Unit& u, int64_t ld) -> int64_t { return (row0 + u.block * kPlaces + g) * ld + (int64_t)u.head * p.D + 8 * j; };
-  auto row_of = [&](const Unit& u, int n, int64_t ld, int64_t first, int32_t& place, int64_t& at) -> bool {
+  auto unit_at = [&](int32_t u) -> Unit {             // u in [0, units)
+    if (u >= by_block) return Unit{kFewQ, 0, 0, (u - by_block) * kPlaces, q_rows};
+    const int kind = next_head < H ? kK : next_head < 2 * H ? kV : kQ;
+    return Unit{kind, next_head - kind * H, next_block, max(lo - kPlaces * next_block, 0), min(hi - kPlaces * next_block, kPlaces)};
+  };
+  // Is there a row for this lane in pass n?  kFewQ: also its place in the group and its head.
+  auto row_of = [&](const Unit& u, int n, int32_t& place, int32_t& head) -> bool {
     const int32_t i = n * RP + g;
     if (u.kind != kFewQ) {
       place = u.block * kPlaces + i;
-      at = first + n * (RP * ld);
       return on && i >= u.lo && i < u.hi;
     }
     const bool real = on && u.lo + i < u.hi;
-    const int32_t head = real ? (u.lo + i) / n_new : 0;
+    head = real ? (u.lo + i) / n_new : 0;
     place = lo + (real ? u.lo + i - head * n_new : 0);
-    at = (row0 + place) * ld + (int64_t)head * p.D + 8 * j;
     return real;
   };
   auto any_row = [&](const Unit& u, int n) -> bool { return u.kind != kFewQ ? (n + 1) * RP > u.lo && n * RP < u.hi : u.lo + n * RP < u.hi; };
   const uint4 zero = make_uint4(0, 0, 0, 0);
   uint4 ra = zero, rb = zero;                         // the row of the pass to come
-  auto fetch = [&](const Unit& u, int n) {
-    const Heads& hd = side_of(u);
-    int32_t place;
-    int64_t x;
-    ra = rb = zero;
-    if (row_of(u, n, hd.ld, first_row(u, hd.ld), place, x)) {
-      ra = *reinterpret_cast<const uint4*>(hd.x + x);                     // plain loads: q_out may be q
-      rb = *reinterpret_cast<const uint4*>(hd.x + x + half);
-    }
+  const uint16_t* src = nullptr;                      // where it is, and how far the passes are apart
+  int64_t src_step = 0;
+  auto begin = [&](const Unit& u) {
+    const Heads& hd = u.kind == kK ? p.k : u.kind == kV ? p.v : p.q;
+    src = hd.x + (row0 + u.block * kPlaces + g) * hd.ld + (int64_t)u.head * p.D + 8 * j;
+    src_step = RP * hd.ld;
   };
-  int32_t at = blockIdx.y * kWarps + warp;
+  auto fetch = [&](const Unit& u, int n) {
+    int32_t place, head;
+    ra = rb = zero;
+    if (row_of(u, n, place, head)) {
+      const uint16_t* x = u.kind != kFewQ ? src : p.q.x + (row0 + place) * p.q.ld + (int64_t)head * p.D + 8 * j;
+      ra = *reinterpret_cast<const uint4*>(x);                            // plain loads: q_out may be q
+      rb = *reinterpret_cast<const uint4*>(x + half);
+    }
+    src += src_step;
+  };
+  advance(at);
   Unit u{};
   if (at < units) {
     u = unit_at(at);
+    begin(u);
     fetch(u, 0);
   }
 
@@ -255,40 +259,61 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
         v.z = w.x;
         v.w = w.y;
       }
-      cs_smem[cs_piece(couples, i, c)] = v;
+      cs_smem[i * couples + (cs_piece(c) ^ cs_turn<LG>(i))] = v;
     }
   }
   __syncthreads();
 
+  uint32_t cs_at[4];                                  // this lane's couples in a token's row
+#pragma unroll
+  for (int n = 0; n < 4; ++n) cs_at[n] = fb4blk::smem_u32(cs_smem) + cs_piece(INTER ? 2 * (on ? j : 0) + (n & 1) + (n < 2 ? 0 : p.D / 8) : 4 * (on ? j : 0) + n) * 16;
   for (; at < units; at += step) {
-    const int64_t out_first = u.kind >= kQ ? first_row(u, p.q.out_ld) : 0;
-    const Unit next = at + step < units ? unit_at(at + step) : u;
+    uint16_t* out = nullptr;
+    if (u.kind == kQ) out = p.q.out + (row0 + u.block * kPlaces + g) * p.q.out_ld + (int64_t)u.head * p.D + 8 * j;
+    const bool more = at + step < units;
+    Unit next = u;
+    if (more) {
+      advance(step);
+      next = unit_at(at + step);
+    }
     float top = 0.0f;
     // One pass at a time, not unrolled: the instructions of three kinds of units would not stay in the instruction cache.  The values of K
     // and V wait in shared memory for the block's maximum.
 #pragma unroll 1
     for (int n = 0; n < NP; ++n) {
       const uint4 xa = ra, xb = rb;
-      if (n + 1 < NP) fetch(u, n + 1);
-      else if (at + step < units) fetch(next, 0);
+      if (n + 1 < NP) {
+        fetch(u, n + 1);
+      } else if (more) {
+        begin(next);
+        fetch(next, 0);
+      }
       if (!any_row(u, n)) continue;
-      int32_t place;
-      int64_t o;
-      const bool real = row_of(u, n, p.q.out_ld, out_first, place, o);
+      int32_t place, head;
+      const bool real = row_of(u, n, place, head);
       Share y;
       if (u.kind == kV) {
         unpack<INTER>(xa, xb, y);
       } else {
         CosSin t;
-        if (p.rope.table) read_cs<INTER>(cs_smem, couples, real ? place : lo, on ? j : 0, p.D, t);
+        if (p.rope.table) {
+          const int32_t i = real ? place : lo;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint4 v = fb4blk::lds_v4((cs_at[k] ^ (cs_turn<LG>(i) * 16)) + i * couples * 16);
+            t.c[2 * k] = __uint_as_float(v.x); t.s[2 * k] = __uint_as_float(v.y);
+            t.c[2 * k + 1] = __uint_as_float(v.z); t.s[2 * k + 1] = __uint_as_float(v.w);
+          }
+        }
         norm_rotate<LG, INTER>(xa, xb, (u.kind == kK ? p.k.gain : p.q.gain) != nullptr, gains + ((u.kind == kK ? 4 * LG : 0) + j) * 16, p, t, y);
       }
       if (u.kind >= kQ) {
         uint4 qa, qb;
         pack<INTER>(y, pack_bf16, qa, qb);
+        uint16_t* o = u.kind == kQ ? out + n * (RP * p.q.out_ld) : p.q.out + (row0 + place) * p.q.out_ld + (int64_t)head * p.D + 8 * j;
         if (real) {
-          *reinterpret_cast<uint4*>(p.q.out + o) = qa;
-          *reinterpret_cast<uint4*>(p.q.out + o + half) = qb;
+          *reinterpret_cast<uint4*>(o) = qa;
+          *reinterpret_cast<uint4*>(o + half) = qb;
         }
       } else {
         put(stage + n * 2048, y);
