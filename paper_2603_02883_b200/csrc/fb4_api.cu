@@ -308,6 +308,7 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
   ctx->append8_error = fb4_cache8_prepare_device();
   ctx->plan_error = fb4_plan_prepare_device();
   ctx->linear_error = fb4_linear_prepare_device(ctx->linear_slots);
+  if (ctx->linear_error == cudaSuccess) ctx->linear_error = fb4_linear_tc_prepare_device(ctx->linear_tc_clusters);
   ctx->fast_table_bytes = fast_bytes;
   cudaGetLastError();
   *out = ctx;
@@ -701,7 +702,8 @@ int fb4_linear(fb4_ctx* ctx, const void* x, int64_t T, int64_t K, int64_t ld_ele
   if (!aligned16(x) || (ld_elems & 7) || !aligned16(codes) || !aligned16(meta) || !aligned16(out) || (reinterpret_cast<uintptr_t>(bias) & 1u))
     return FB4_ERR_ALIGN;
   if (ctx->linear_error != cudaSuccess) return fb4_set_cuda_error(ctx->linear_error);
-  const cudaError_t e = fb4_launch_linear(ctx, x, T, ld_elems, codes, meta, N, K, bias, out, out_ld, out_dtype, static_cast<cudaStream_t>(stream));
+  const auto launch = ctx->force_generic ? fb4_launch_linear : fb4_launch_linear_tc;
+  const cudaError_t e = launch(ctx, x, T, ld_elems, codes, meta, N, K, bias, out, out_ld, out_dtype, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
   ctx->launches += 1;
   return FB4_OK;

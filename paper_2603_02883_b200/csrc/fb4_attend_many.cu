@@ -32,16 +32,16 @@
 // the columns (2.2 to 2.9 us per tile).
 #include "fb4_attend.cuh"
 #include "fb4_staging.cuh"
+#include "fb4_tcgen05.cuh"
 
 namespace {
 
 using namespace fb4att;
+using namespace fb4tc;
 using fb4blk::smem_u32;
 using fb4stage::bulk_load;
-using fb4stage::kSpinLimit;
 using fb4stage::mbar_expect_tx;
 using fb4stage::mbar_init;
-using fb4stage::mbar_try_wait;
 
 constexpr int kKeys = 128;             // tokens of a tile
 constexpr int kSoftmaxWarps = 8, kDecodeWarps = 4;
@@ -68,81 +68,6 @@ struct Bars {
   uint64_t q_full, s_full[2], s_free, p_half[2], p_full[2], o_done[2], drained;
 };
 
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
-// Waits for a phase with a limit; a wait that runs out, here or anywhere in the CTA, ends every other one.  Eight bare tries
-// for each look at the limit: the roles that wait take issue slots from those that work (a fifth of all instructions went into
-// waiting with a look at every try).
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
-  for (uint32_t tries = 0; tries < kSpinLimit / 8; ++tries) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
-    if (*dead) break;
-  }
-  *dead = 1u;
-  return false;
-}
-
-// ---- tcgen05
-// Shared-memory descriptors, 128-byte swizzle, descriptor version of sm_100: the low word holds the address and the leading
-// offset, the high word the stride (1024 bytes between groups of 8 rows) and the layout; all in units of 16 bytes.
-__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lead) { return ((addr & 0x3ffffu) >> 4) | ((lead >> 4) << 16); }
-constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
-// bf16 x bf16 -> f32, M = 128; n_major: B is stored with its N side contiguous
-__host__ __device__ constexpr uint32_t instr_desc(int n, bool n_major) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | (n_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-}
-// The issuing warp runs warp-uniform code and only these instructions are one lane's: a lane that computes descriptors on its
-// own for every instruction takes longer than the tensor core for 128 x 128 x 16.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t idesc, bool add) {
-  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.u32 p, %4, 0;\n\t"
-               "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
-               ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(add ? 1u : 0u), "n"(kDescHigh) : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_low, uint32_t idesc, bool add) {
-  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.u32 p, %4, 0;\n\t"
-               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "r"(b_low), "r"(idesc), "r"(add ? 1u : 0u), "n"(kDescHigh) : "memory");
-}
-__device__ __forceinline__ bool elected() {
-  uint32_t e;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
-  return e != 0;
-}
-__device__ __forceinline__ void commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float* v) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
-        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
-        "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
-        "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
-      : "r"(addr));
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
-        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-      : "r"(addr));
-}
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
-}
 // two float32 operations in one instruction
 __device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
   float2 d;

@@ -1292,3 +1292,15 @@ cudaError_t fb4_flat_setup(const fb4_ctx* ctx, const void* x, int64_t T, int64_t
   return flat_setup(ctx, x, T, C, chunked, mx, map, p, grid_out);
 }
 bool fb4_flat_eligible(int64_t T, int64_t C, int64_t ld) { return flat_eligible(T, C, ld); }
+
+// Tensor map of a byte matrix [h][w] with rows `pitch` bytes apart, in boxes of box_w x box_h; what lies outside reads as zeros.
+cudaError_t fb4_encode_map_2d(CUtensorMap* map, const void* base, uint64_t w, uint64_t h, uint64_t pitch, uint32_t box_w, uint32_t box_h,
+                              CUtensorMapSwizzle swizzle) {
+  const EncodeTiledFn encode = encode_tiled_fn();
+  if (!encode) return cudaErrorNotSupported;
+  const cuuint64_t dims[2] = {w, h}, strides[1] = {pitch};
+  const cuuint32_t box[2] = {box_w, box_h}, elem[2] = {1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}

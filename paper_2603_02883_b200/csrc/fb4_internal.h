@@ -56,6 +56,7 @@ struct fb4_ctx {
   cudaError_t append8_error;     // the same for the append to the 8-bit cache
   cudaError_t plan_error;        // the same for the plan of a step
   cudaError_t linear_error;      // the same for the products with FB4 weights
+  int32_t linear_tc_clusters[9]; // tensor-core kernel, per cluster size: clusters that are resident at a time
   int32_t linear_slots[4][9];    // per kernel variant and cluster size: CTAs that are resident at a time
   int sm_count;
   void* d_topk_scratch;          // histograms and counters of the multi-CTA top-k selection (fb4_topk.cu)
@@ -187,6 +188,11 @@ cudaError_t fb4_launch_attend_generic(const fb4_ctx* ctx, const Fb4Attend& a, cu
 cudaError_t fb4_linear_prepare_device(int32_t (*slots)[9]);
 cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
                               int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream);
+
+// the same on the fifth-generation tensor cores (fb4_linear_tc.cu)
+cudaError_t fb4_linear_tc_prepare_device(int32_t* clusters);
+cudaError_t fb4_launch_linear_tc(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
+                                 int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream);
 
 // plan of a serving step (fb4_plan.cu)
 cudaError_t fb4_plan_prepare_device();

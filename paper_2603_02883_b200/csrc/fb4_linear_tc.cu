@@ -1,0 +1,423 @@
+// Products of rows with FB4 weights on the fifth-generation tensor cores: y[t][n] = sum_k x[t][k] w[n][k] + bias[n].
+//
+// The weights are the M side: 128 rows of W are a tile, their decoded values the A operand, which lies in tensor memory, a row to a lane, so
+// that a thread decodes a row of its own and nothing of the decoded weights passes through shared memory.  x, up to 128 rows at a time, is the
+// B operand in shared memory; channels stand in the order 0 2 1 3 4 6 5 7 of every eight on both sides, the decoder's.
+//
+// Work: one CTA per SM.  A cluster takes a run of rows of W (in quarters of a tile: 32 rows, a warp's), its CTAs a run of the channels each;
+// their sums are joined through distributed shared memory, always in the same order.  The warps of a CTA have fixed roles:
+//   decode   4 groups of 4 warps take the items (128 rows x 128 channels) in turn, each with a buffer of its own in tensor memory
+//   load     codes of the items into a ring (tensor copies of 32 rows x 64 bytes, 64-byte swizzle)
+//   product  one warp issues D_tile += A x
+//   x        4 warps bring x into shared memory, in chunks where it is too large for it
+#include "fb4_attend.cuh"
+#include "fb4_staging.cuh"
+#include "fb4_tcgen05.cuh"
+
+namespace {
+
+using namespace fb4att;
+using namespace fb4tc;
+using fb4blk::smem_u32;
+using fb4stage::mbar_expect_tx;
+using fb4stage::mbar_init;
+using fb4stage::tma_load_2d;
+
+constexpr int kGroups = 4, kDecodeWarps = 4 * kGroups, kLoadWarp = kDecodeWarps, kProductWarp = kLoadWarp + 1, kXWarp = kProductWarp + 1, kXWarps = 4;
+constexpr int kThreads = (kXWarp + kXWarps) * 32;
+constexpr int kStages = 8, kQuarter = 32 * 64, kStage = 4 * kQuarter;      // bytes of 32 and of 128 rows' codes of an item
+constexpr int kXBytes = 144 * 1024;
+constexpr int kBytes = 1024 + kStages * kStage + kXBytes;
+constexpr int kACols = 64, kDCol = kGroups * kACols, kDCols = 512 - kDCol; // tensor memory: A of each group, then D of each tile
+constexpr int kMaxRows = 128, kMaxSplits = 8;
+
+struct Linear {
+  const uint16_t* x;
+  int64_t ld;
+  const uint16_t* meta;
+  const uint16_t* bias;
+  void* out;
+  int64_t out_ld;
+  int64_t T, N;
+  int32_t nb;               // blocks of a row
+  int32_t rows;             // rows of x at a time, a multiple of 16
+  int32_t splits;           // CTAs of a cluster
+  int32_t quarters;         // quarters of a tile to a cluster
+  int32_t chunk, buffers;   // steps of 128 channels whose x is held at a time, and how often
+  int32_t out_dtype;
+  uint32_t m4, m16;         // 16 and 65536 (see decode_word_mul)
+  const Fb4DeviceTables* tables;
+  uint32_t* status;
+};
+
+struct Bars {
+  uint64_t ring_full[kStages], ring_empty[kStages];
+  uint64_t a_full[kGroups], a_empty[kGroups], x_full[2], x_empty[2], d_full, drained;
+};
+
+// decode_word with its shifts as multiplications by 16 and 2^16, which the compiler does not know and so leaves on the FMA pipe: the
+// ALU pipe, which has all the other operations, is what bounds this kernel
+__device__ __forceinline__ void decode_word_mul(uint32_t w, const BlockScale& s, uint32_t m4, uint32_t m16, uint32_t* o) {
+  const uint32_t sel = w & 0x77777777u;
+  uint32_t high, left;
+  asm("mul.hi.u32 %0, %1, %2;" : "=r"(high) : "r"(sel), "r"(m16));
+  asm("mul.lo.u32 %0, %1, %2;" : "=r"(left) : "r"(w), "r"(m4));
+  const uint32_t lo = prmt(s.t0, s.t1, sel), hi = prmt(s.t0, s.t1, high);
+  const uint32_t odd = w & 0x80808080u, even = left & 0x80808080u;
+  o[0] = mul_bf16x2(prmt(lo, even, 0x5240u), s.f);
+  o[1] = mul_bf16x2(prmt(lo, odd, 0x5341u), s.f);
+  o[2] = mul_bf16x2(prmt(hi, even, 0x7260u), s.f);
+  o[3] = mul_bf16x2(prmt(hi, odd, 0x7361u), s.f);
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]),
+      "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]),
+      "r"(v[30]), "r"(v[31]) : "memory");
+}
+
+// The items in order: chunk by chunk of x, in it tile by tile, in it step by step.
+struct Cursor {
+  int32_t item, tile, s, c0, c1, chunk_no;
+  __device__ __forceinline__ Cursor(int32_t begin, int32_t end, int32_t chunk) : item(0), tile(0), s(begin), c0(begin), c1(min(begin + chunk, end)), chunk_no(0) {}
+  __device__ __forceinline__ void advance(int32_t by, int32_t tiles, int32_t chunk, int32_t end) {
+    item += by;
+    s += by;
+    while (s >= c1 && c0 < end) {
+      int32_t over = s - c1;
+      if (++tile == tiles) {
+        tile = 0;
+        ++chunk_no;
+        c0 = c1;
+        c1 = min(c0 + chunk, end);
+      }
+      s = c0 + over;
+    }
+  }
+};
+
+__global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Linear p) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ Bars bars;
+  __shared__ uint32_t book[64];
+  __shared__ uint32_t tmem_at, dead_flag;
+  const uint32_t base_smem = (smem_u32(smem_raw) + 1023u) & ~1023u, ring_at = base_smem, x_at = base_smem + kStages * kStage;
+  float* sums = reinterpret_cast<float*>(smem_raw + (base_smem - smem_u32(smem_raw)));
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  volatile uint32_t* dead = &dead_flag;
+
+  // ---- which work
+  const int32_t split = (int32_t)(blockIdx.x % p.splits), rows = p.rows;
+  const int64_t row_base = (int64_t)(blockIdx.x / p.splits) * p.quarters * 32, t0 = (int64_t)blockIdx.y * rows;
+  const int32_t n_tok = (int32_t)(p.T - t0 < rows ? p.T - t0 : rows);
+  const int64_t left = (p.N - row_base + 31) / 32;
+  const int32_t quarters = (int32_t)(left < p.quarters ? left : p.quarters), tiles = (quarters + 3) / 4;
+  const int32_t steps = (p.nb + 3) / 4;
+  const int32_t s_begin = (int32_t)((int64_t)steps * split / p.splits), s_end = (int32_t)((int64_t)steps * (split + 1) / p.splits);
+  const int32_t items = (s_end - s_begin) * tiles;
+
+  // ---- set-up
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.ring_full[i]), 1); mbar_init(smem_u32(&bars.ring_empty[i]), 4); }
+    for (int i = 0; i < kGroups; ++i) { mbar_init(smem_u32(&bars.a_full[i]), 4); mbar_init(smem_u32(&bars.a_empty[i]), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.x_full[i]), kXWarps); mbar_init(smem_u32(&bars.x_empty[i]), 1); }
+    mbar_init(smem_u32(&bars.d_full), 1);
+    mbar_init(smem_u32(&bars.drained), 1);
+    dead_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kProductWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_at)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  if (threadIdx.x >= 64 && threadIdx.x < 128) fill_book(book, p.tables, threadIdx.x - 64);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
+
+  if (warp < kDecodeWarps) {
+    // =========================================================== decode
+    const int group = warp >> 2, quarter = warp & 3;
+    const uint32_t lanes = (uint32_t)quarter << 21, a_at = tmem + group * kACols + lanes, book_at = smem_u32(book);
+    const bool vec = p.nb % 4 == 0;        // a row's records of a step are 8 aligned bytes
+    auto fetch = [&](const Cursor& c) -> uint2 {
+      uint2 v = make_uint2(0, 0);
+      const int64_t row = row_base + (c.tile * 4 + quarter) * 32 + lane;
+      if (c.item >= items || row >= p.N) return v;
+      const uint16_t* m = p.meta + row * p.nb + 4 * c.s;
+      if (vec) return __ldg(reinterpret_cast<const uint2*>(m));
+      const int32_t n = p.nb - 4 * c.s;
+      v.x = __ldg(m);
+      if (n > 1) v.x |= (uint32_t)__ldg(m + 1) << 16;
+      if (n > 2) v.y = __ldg(m + 2);
+      if (n > 3) v.y |= (uint32_t)__ldg(m + 3) << 16;
+      return v;
+    };
+    Cursor c(s_begin, s_end, p.chunk);
+    c.advance(group, tiles, p.chunk, s_end);
+    uint2 next = fetch(c);
+    bool ok = true;
+    for (int32_t k = 0; c.item < items; ++k) {
+      const uint2 meta = next;
+      const int32_t item = c.item;
+      const bool there = c.tile * 4 + quarter < quarters;
+      c.advance(kGroups, tiles, p.chunk, s_end);
+      next = fetch(c);
+      const int st = item % kStages;
+      ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.ring_full[st]), (item / kStages) & 1, dead));
+      if (!ok) break;
+      uint32_t w[4][4];
+      if (there) {
+        const uint32_t codes = ring_at + st * kStage + quarter * kQuarter + lane * 64;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(codes + ((i ^ ((lane >> 1) & 3)) << 4)));
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.ring_empty[st]));
+      bool waited = k == 0;
+      if (there) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t o[32];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t m = h ? meta.y : meta.x;
+            const BlockScale sc = block_scale(i ? m >> 16 : m & 0xffffu, book_at, true);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) decode_word_mul(w[2 * h + i][q], sc, p.m4, p.m16, o + 16 * i + 4 * q);
+          }
+          if (!waited) {                   // the product of this group's item before has read the buffer
+            waited = true;
+            ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_empty[group]), (k - 1) & 1, dead));
+            if (!ok) break;
+            fence_after();
+          }
+          tmem_st32(a_at + 32 * h, o);
+        }
+        if (!ok) break;
+        tmem_wait_st();
+      } else if (!waited) {
+        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_empty[group]), (k - 1) & 1, dead));
+        if (!ok) break;
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.a_full[group]));
+    }
+    // ---- the sums, [row of x][row of W], to shared memory, which nobody uses any more once the last product is done
+    if (ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.d_full), 0, dead));
+    if (ok) {
+      fence_after();
+      const int32_t sums_ld = tiles * 128 + 4;
+      for (int32_t tile = group; tile < tiles; tile += kGroups) {
+        if (tile * 4 + quarter >= quarters) continue;
+        float* at = sums + tile * 128 + quarter * 32 + lane;
+        for (int32_t col = 0; col < rows; col += 16) {
+          uint32_t v[16];
+          tmem_ld16(tmem + kDCol + tile * rows + col + lanes, v);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) at[(col + i) * sums_ld] = __uint_as_float(v[i]);
+        }
+      }
+    }
+  } else if (warp == kLoadWarp) {
+    // =========================================================== load
+    bool ok = true;
+    for (Cursor c(s_begin, s_end, p.chunk); c.item < items && ok; c.advance(1, tiles, p.chunk, s_end)) {
+      const int st = c.item % kStages;
+      if (c.item >= kStages) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.ring_empty[st]), (c.item / kStages - 1) & 1, dead));
+      if (!ok) break;
+      const int32_t n = min(quarters - c.tile * 4, 4);
+      const uint32_t full = smem_u32(&bars.ring_full[st]);
+      if (lane == 0) {
+        mbar_expect_tx(full, (uint32_t)n * kQuarter);
+        for (int q = 0; q < n; ++q) tma_load_2d(ring_at + st * kStage + q * kQuarter, &map, full, c.s * 64, (int)(row_base + (c.tile * 4 + q) * 32));
+      }
+      __syncwarp();
+    }
+    // every copy has to have landed before the CTA ends
+    for (int32_t i = items > kStages ? items - kStages : 0; i < items && !*dead; ++i) wait(smem_u32(&bars.ring_full[i % kStages]), (i / kStages) & 1, dead);
+  } else if (warp == kProductWarp) {
+    // =========================================================== product: every lane waits, one issues
+    const uint32_t idesc = instr_desc(rows, false), x_low = desc_low(x_at, 16), x_buffer = (uint32_t)p.chunk * rows * 256;
+    bool ok = true;
+    int32_t chunk_no = -1;
+    for (Cursor c(s_begin, s_end, p.chunk); c.item < items && ok;) {
+      const Cursor now = c;
+      c.advance(1, tiles, p.chunk, s_end);
+      const int buf = now.chunk_no % p.buffers, group = now.item % kGroups;
+      if (now.chunk_no != chunk_no) {
+        chunk_no = now.chunk_no;
+        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_full[buf]), (chunk_no / p.buffers) & 1, dead));
+      }
+      if (ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_full[group]), (now.item / kGroups) & 1, dead));
+      if (!ok) break;
+      fence_after();
+      if (elected()) {
+        const uint32_t d = tmem + kDCol + now.tile * rows, a = tmem + group * kACols;
+        const uint32_t b = x_low + ((buf * x_buffer + (uint32_t)(now.s - now.c0) * rows * 256) >> 4);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) mma_ts(d, a + 8 * k, b + (((k >> 2) * rows * 128 + (k & 3) * 32) >> 4), idesc, k > 0 || now.s > s_begin);
+        commit(smem_u32(&bars.a_empty[group]));
+        if (c.item == items || c.chunk_no != chunk_no) commit(smem_u32(&bars.x_empty[buf]));
+        if (c.item == items) commit(smem_u32(&bars.d_full));
+      }
+      __syncwarp();
+    }
+    // nothing of this CTA may be on the tensor core when its tensor memory is given back
+    if (elected()) commit(smem_u32(&bars.drained));
+    uint32_t tries = 0;
+    while (!mbar_try_wait(smem_u32(&bars.drained), 0) && ++tries < kSpinLimit) {}
+  } else {
+    // =========================================================== x: [64 channels][row] with 128-byte swizzle, rows behind the last zero
+    const int xw = warp - kXWarp;
+    bool ok = true;
+    int32_t no = 0;
+    for (int32_t c0 = s_begin; c0 < s_end && ok; c0 += p.chunk, ++no) {
+      const int32_t n_steps = min(p.chunk, s_end - c0), buf = no % p.buffers;
+      if (no >= p.buffers) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_empty[buf]), (no / p.buffers - 1) & 1, dead));
+      if (!ok) break;
+      const uint32_t at = x_at + (uint32_t)buf * p.chunk * rows * 256;
+      for (int32_t r = xw; r < rows; r += kXWarps) {
+        const uint4* src = reinterpret_cast<const uint4*>(p.x + (t0 + r) * p.ld) + (int64_t)c0 * 16;
+        const uint32_t row_at = at + (r >> 3) * 1024 + (r & 7) * 128;
+#pragma unroll 4
+        for (int32_t run = lane; run < n_steps * 16; run += 32) {                       // 8 channels
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if (r < n_tok && 4 * c0 + (run >> 2) < p.nb) u = __ldg(src + run);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row_at + (run >> 3) * rows * 128 + (((run ^ r) & 7) << 4)), "r"(prmt(u.x, u.y, 0x5410u)),
+                       "r"(prmt(u.x, u.y, 0x7632u)), "r"(prmt(u.z, u.w, 0x5410u)), "r"(prmt(u.z, u.w, 0x7632u)) : "memory");
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.x_full[buf]));
+    }
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  const bool whole = !*dead;
+  if (threadIdx.x == 0 && !whole) atomicOr(p.status, 1u);
+  if (warp == kProductWarp) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  }
+  // ---- the CTAs of the cluster finish a part of the sums each
+  if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  const int32_t sums_ld = tiles * 128 + 4, out_rows = quarters * 32;
+  for (int32_t i = split * kThreads + threadIdx.x; i < n_tok * out_rows && whole; i += p.splits * kThreads) {
+    const int32_t tok = i / out_rows, r = i - tok * out_rows;
+    const int64_t n = row_base + r;
+    if (n >= p.N) continue;
+    float v = 0.0f;
+    if (p.splits > 1) {
+      const uint32_t at = smem_u32(sums + tok * sums_ld + r);
+#pragma unroll
+      for (int z = 0; z < kMaxSplits; ++z)
+        if (z < p.splits) {
+          float u;
+          asm volatile("{\n\t.reg .b32 q;\n\tmapa.shared::cluster.u32 q, %1, %2;\n\tld.shared::cluster.f32 %0, [q];\n\t}" : "=f"(u) : "r"(at), "r"(z));
+          v += u;
+        }
+    } else {
+      v = sums[tok * sums_ld + r];
+    }
+    v *= kUnshift;
+    if (p.bias) v += __uint_as_float((uint32_t)__ldg(p.bias + n) << 16);
+    const int64_t at = (t0 + tok) * p.out_ld + n;
+    if (p.out_dtype == 0) static_cast<float*>(p.out)[at] = v;
+    else if (p.out_dtype == 1) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
+    else static_cast<__half*>(p.out)[at] = __float2half_rn(v);
+  }
+  // nobody's shared memory goes away while another CTA reads it
+  if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+}  // namespace
+
+// Opt-in to the dynamic shared memory, and how many clusters of 1 to 8 CTAs are resident at a time (a cluster lies in one group of SMs).
+cudaError_t fb4_linear_tc_prepare_device(int32_t* clusters) {
+  cudaError_t e = cudaFuncSetAttribute(fb4_linear_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+  for (int s = 1; s <= kMaxSplits && e == cudaSuccess; ++s) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)s;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(s * 1024));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kBytes;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, fb4_linear_tc_kernel, &cfg);
+    clusters[s] = n > 1 ? n : 1;
+  }
+  return e;
+}
+
+cudaError_t fb4_launch_linear_tc(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
+                                 int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream) {
+  Linear p{};
+  p.x = static_cast<const uint16_t*>(x);
+  p.ld = ld;
+  p.meta = meta;
+  p.bias = static_cast<const uint16_t*>(bias);
+  p.out = out;
+  p.out_ld = out_ld;
+  p.T = T;
+  p.N = N;
+  p.nb = (int32_t)(K / 32);
+  p.out_dtype = out_dtype;
+  p.m4 = 16u;
+  p.m16 = 65536u;
+  p.tables = ctx->d_tables;
+  p.status = ctx->d_status;
+  // rows of x in passes of equal size
+  const int64_t z = (T + kMaxRows - 1) / kMaxRows, each = (T + z - 1) / z;
+  p.rows = (int32_t)((each + 15) / 16 * 16);
+  const int32_t steps = (p.nb + 3) / 4, most = kDCols / p.rows * 4;
+  const int64_t quarters = (N + 31) / 32;
+  // the cluster size with the fewest items for a CTA; a wave's start and join count as 6
+  double best = 1e300;
+  for (int c = 1; c <= kMaxSplits && (c == 1 || c <= steps); c *= 2) {
+    const int64_t at_once = ctx->linear_tc_clusters[c];
+    int64_t q = (quarters * z + at_once - 1) / at_once;
+    if (q > most) q = most;
+    const int64_t grid = (quarters + q - 1) / q * z, waves = (grid + at_once - 1) / at_once;
+    const double cost = (double)waves * ((q + 3) / 4 * ((steps + c - 1) / c) + 6);
+    if (cost < best) {
+      best = cost;
+      p.splits = c;
+      p.quarters = (int32_t)q;
+    }
+  }
+  const int32_t mine = (steps + p.splits - 1) / p.splits, step_bytes = p.rows * 256;
+  p.buffers = mine * step_bytes <= kXBytes ? 1 : 2;
+  p.chunk = p.buffers == 1 ? mine : kXBytes / 2 / step_bytes;
+  CUtensorMap map;
+  cudaError_t e = fb4_encode_map_2d(&map, codes, (uint64_t)K / 2, (uint64_t)N, (uint64_t)K / 2, 64, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  cfg.gridDim = dim3((unsigned)((quarters + p.quarters - 1) / p.quarters * p.splits), (unsigned)z);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kBytes;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  if (p.splits > 1) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.splits;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+  }
+  return cudaLaunchKernelEx(&cfg, fb4_linear_tc_kernel, map, p);
+}

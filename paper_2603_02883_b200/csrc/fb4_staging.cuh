@@ -125,5 +125,7 @@ cudaError_t fb4_fast_setup(const fb4_ctx* ctx, const void* x, int64_t T, int64_t
 cudaError_t fb4_flat_setup(const fb4_ctx* ctx, const void* x, int64_t T, int64_t C, bool chunked, bool mx,
                            CUtensorMap* map, fb4stage::FlatParams* p, int* grid_out);
 bool fb4_flat_eligible(int64_t T, int64_t C, int64_t ld);
+cudaError_t fb4_encode_map_2d(CUtensorMap* map, const void* base, uint64_t w, uint64_t h, uint64_t pitch, uint32_t box_w, uint32_t box_h,
+                              CUtensorMapSwizzle swizzle);
 // Opt-in to the dynamic shared memory of the producer kernels on the current device (fb4_producers.cu).
 cudaError_t fb4_producers_prepare_device();
