@@ -1,15 +1,18 @@
 // Products of rows with FB4 weights on the fifth-generation tensor cores: y[t][n] = sum_k x[t][k] w[n][k] + bias[n].
 //
 // The weights are the M side: 128 rows of W are a tile, their decoded values the A operand, which lies in tensor memory, a row to a lane, so
-// that a thread decodes a row of its own and nothing of the decoded weights passes through shared memory.  x, up to 128 rows at a time, is the
+// that a thread decodes a row of its own and nothing of the decoded weights passes through shared memory.  x, up to 96 rows at a time, is the
 // B operand in shared memory; channels stand in the order 0 2 1 3 4 6 5 7 of every eight on both sides, the decoder's.
 //
 // Work: one CTA per SM.  A cluster takes a run of rows of W (in quarters of a tile: 32 rows, a warp's), its CTAs a run of the channels each;
 // their sums are joined through distributed shared memory, always in the same order.  The warps of a CTA have fixed roles:
-//   decode   4 groups of 4 warps take the items (128 rows x 128 channels) in turn, each with a buffer of its own in tensor memory
-//   load     codes of the items into a ring (tensor copies of 32 rows x 64 bytes, 64-byte swizzle)
+//   decode   4 groups of 4 warps take the items (128 rows x 256 channels) in turn, half an item at a time into a ring of 4 to 7 buffers in
+//            tensor memory
+//   load     codes of the items into a ring (tensor copies of 32 rows x 128 bytes, 128-byte swizzle; with rows of 64 bytes the copies alone
+//            took 34 us where this takes 25)
 //   product  one warp issues D_tile += A x
-//   x        4 warps bring x into shared memory, in chunks where it is too large for it
+//   x        brought into shared memory at the start by all that have nothing to decode yet, where it is too large for it in chunks, the
+//            others by 6 warps
 #include "fb4_attend.cuh"
 #include "fb4_staging.cuh"
 #include "fb4_tcgen05.cuh"
@@ -23,13 +26,14 @@ using fb4stage::mbar_expect_tx;
 using fb4stage::mbar_init;
 using fb4stage::tma_load_2d;
 
-constexpr int kGroups = 4, kDecodeWarps = 4 * kGroups, kLoadWarp = kDecodeWarps, kProductWarp = kLoadWarp + 1, kXWarp = kProductWarp + 1, kXWarps = 4;
+constexpr int kGroups = 4, kDecodeWarps = 4 * kGroups, kLoadWarp = kDecodeWarps, kProductWarp = kLoadWarp + 1, kXWarp = kProductWarp + 1, kXWarps = 6;
 constexpr int kThreads = (kXWarp + kXWarps) * 32;
-constexpr int kStages = 8, kQuarter = 32 * 64, kStage = 4 * kQuarter;      // bytes of 32 and of 128 rows' codes of an item
-constexpr int kXBytes = 144 * 1024;
+constexpr int kStages = 7, kQuarter = 32 * 128, kStage = 4 * kQuarter;     // bytes of 32 and of 128 rows' codes of an item
+constexpr int kXBytes = 96 * 1024;
 constexpr int kBytes = 1024 + kStages * kStage + kXBytes;
-constexpr int kACols = 64, kDCol = kGroups * kACols, kDCols = 512 - kDCol; // tensor memory: A of each group, then D of each tile
-constexpr int kMaxRows = 128, kMaxSplits = 8;
+constexpr int kACols = 64, kMaxA = 7, kDCols = 512 - 4 * kACols;          // tensor memory: buffers for A, as many as D leaves, and D at its end
+constexpr int kMaxRows = 96, kMaxSplits = 8;
+static_assert(kXBytes / 2 >= kMaxRows * 512, "a chunk of x has at least one step");
 
 struct Linear {
   const uint16_t* x;
@@ -43,32 +47,16 @@ struct Linear {
   int32_t rows;             // rows of x at a time, a multiple of 16
   int32_t splits;           // CTAs of a cluster
   int32_t quarters;         // quarters of a tile to a cluster
-  int32_t chunk, buffers;   // steps of 128 channels whose x is held at a time, and how often
+  int32_t chunk, buffers;   // steps of 256 channels whose x is held at a time, and how often
   int32_t out_dtype;
-  uint32_t m4, m16;         // 16 and 65536 (see decode_word_mul)
   const Fb4DeviceTables* tables;
   uint32_t* status;
 };
 
 struct Bars {
   uint64_t ring_full[kStages], ring_empty[kStages];
-  uint64_t a_full[kGroups], a_empty[kGroups], x_full[2], x_empty[2], d_full, drained;
+  uint64_t a_full[kMaxA], a_empty[kMaxA], x_first, x_full[2], x_empty[2], d_full, drained;
 };
-
-// decode_word with its shifts as multiplications by 16 and 2^16, which the compiler does not know and so leaves on the FMA pipe: the
-// ALU pipe, which has all the other operations, is what bounds this kernel
-__device__ __forceinline__ void decode_word_mul(uint32_t w, const BlockScale& s, uint32_t m4, uint32_t m16, uint32_t* o) {
-  const uint32_t sel = w & 0x77777777u;
-  uint32_t high, left;
-  asm("mul.hi.u32 %0, %1, %2;" : "=r"(high) : "r"(sel), "r"(m16));
-  asm("mul.lo.u32 %0, %1, %2;" : "=r"(left) : "r"(w), "r"(m4));
-  const uint32_t lo = prmt(s.t0, s.t1, sel), hi = prmt(s.t0, s.t1, high);
-  const uint32_t odd = w & 0x80808080u, even = left & 0x80808080u;
-  o[0] = mul_bf16x2(prmt(lo, even, 0x5240u), s.f);
-  o[1] = mul_bf16x2(prmt(lo, odd, 0x5341u), s.f);
-  o[2] = mul_bf16x2(prmt(hi, even, 0x7260u), s.f);
-  o[3] = mul_bf16x2(prmt(hi, odd, 0x7361u), s.f);
-}
 
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* v) {
   asm volatile(
@@ -116,14 +104,15 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   const int32_t n_tok = (int32_t)(p.T - t0 < rows ? p.T - t0 : rows);
   const int64_t left = (p.N - row_base + 31) / 32;
   const int32_t quarters = (int32_t)(left < p.quarters ? left : p.quarters), tiles = (quarters + 3) / 4;
-  const int32_t steps = (p.nb + 3) / 4;
+  const int32_t steps = (p.nb + 7) / 8;
   const int32_t s_begin = (int32_t)((int64_t)steps * split / p.splits), s_end = (int32_t)((int64_t)steps * (split + 1) / p.splits);
   const int32_t items = (s_end - s_begin) * tiles;
 
   // ---- set-up
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.ring_full[i]), 1); mbar_init(smem_u32(&bars.ring_empty[i]), 4); }
-    for (int i = 0; i < kGroups; ++i) { mbar_init(smem_u32(&bars.a_full[i]), 4); mbar_init(smem_u32(&bars.a_empty[i]), 1); }
+    for (int i = 0; i < kMaxA; ++i) { mbar_init(smem_u32(&bars.a_full[i]), 4); mbar_init(smem_u32(&bars.a_empty[i]), 1); }
+    mbar_init(smem_u32(&bars.x_first), kDecodeWarps + kXWarps);
     for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.x_full[i]), kXWarps); mbar_init(smem_u32(&bars.x_empty[i]), 1); }
     mbar_init(smem_u32(&bars.d_full), 1);
     mbar_init(smem_u32(&bars.drained), 1);
@@ -138,32 +127,67 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0), d_col = tmem + 512 - tiles * rows;
+  const int n_a = min((512 - tiles * rows) / kACols, kMaxA);
+
+  // One step of x, 8 rows of it, by a warp: [64 channels][row] with 128-byte swizzle, rows behind the last zero.
+  auto bring = [&](uint32_t at, int32_t step, int32_t r0) {
+    const int32_t run = step * 32 + lane;                              // 8 channels, counted from the first of all
+    const uint4* src = reinterpret_cast<const uint4*>(p.x + (t0 + r0) * p.ld) + run;
+    uint4 u[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      u[r] = make_uint4(0, 0, 0, 0);
+      if ((run >> 2) < p.nb && r0 + r < n_tok) u[r] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(src) + r * p.ld));
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + (lane >> 3) * rows * 128 + (r0 >> 3) * 1024 + r * 128 + (((lane ^ r) & 7) << 4)),
+                   "r"(prmt(u[r].x, u[r].y, 0x5410u)), "r"(prmt(u[r].x, u[r].y, 0x7632u)), "r"(prmt(u[r].z, u[r].w, 0x5410u)),
+                   "r"(prmt(u[r].z, u[r].w, 0x7632u)) : "memory");
+  };
+  auto brought = [&](uint32_t bar) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+  };
+  if (warp != kLoadWarp && warp != kProductWarp) {
+    const int me = warp < kDecodeWarps ? warp : warp - 2, first_steps = min(p.chunk * p.buffers, s_end - s_begin);
+    for (int32_t i = me; i < first_steps * (rows >> 3); i += kDecodeWarps + kXWarps) {
+      const int32_t step = i / (rows >> 3);
+      bring(x_at + step * rows * 512, s_begin + step, (i - step * (rows >> 3)) * 8);
+    }
+    brought(smem_u32(&bars.x_first));
+  }
 
   if (warp < kDecodeWarps) {
     // =========================================================== decode
     const int group = warp >> 2, quarter = warp & 3;
-    const uint32_t lanes = (uint32_t)quarter << 21, a_at = tmem + group * kACols + lanes, book_at = smem_u32(book);
-    const bool vec = p.nb % 4 == 0;        // a row's records of a step are 8 aligned bytes
-    auto fetch = [&](const Cursor& c) -> uint2 {
-      uint2 v = make_uint2(0, 0);
+    const uint32_t lanes = (uint32_t)quarter << 21, book_at = smem_u32(book);
+    const int align = p.nb % 8 == 0 ? 8 : p.nb % 4 == 0 ? 4 : 1;      // records of a row that lie together in aligned words
+    auto fetch = [&](const Cursor& c) -> uint4 {
+      uint32_t v[4] = {0, 0, 0, 0};
       const int64_t row = row_base + (c.tile * 4 + quarter) * 32 + lane;
-      if (c.item >= items || row >= p.N) return v;
-      const uint16_t* m = p.meta + row * p.nb + 4 * c.s;
-      if (vec) return __ldg(reinterpret_cast<const uint2*>(m));
-      const int32_t n = p.nb - 4 * c.s;
-      v.x = __ldg(m);
-      if (n > 1) v.x |= (uint32_t)__ldg(m + 1) << 16;
-      if (n > 2) v.y = __ldg(m + 2);
-      if (n > 3) v.y |= (uint32_t)__ldg(m + 3) << 16;
-      return v;
+      if (c.item < items && row < p.N) {
+        const uint16_t* m = p.meta + row * p.nb + 8 * c.s;
+        const int32_t n = p.nb - 8 * c.s;                             // records there are; those behind read as zeros, as their codes do
+        if (align == 8) return __ldg(reinterpret_cast<const uint4*>(m));
+        if (align == 4) {
+          const uint2 lo = __ldg(reinterpret_cast<const uint2*>(m)), hi = n > 4 ? __ldg(reinterpret_cast<const uint2*>(m) + 1) : make_uint2(0, 0);
+          return make_uint4(lo.x, lo.y, hi.x, hi.y);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) v[i >> 1] |= (uint32_t)__ldg(m + i) << (16 * (i & 1));
+      }
+      return make_uint4(v[0], v[1], v[2], v[3]);
     };
     Cursor c(s_begin, s_end, p.chunk);
     c.advance(group, tiles, p.chunk, s_end);
-    uint2 next = fetch(c);
+    uint4 next = fetch(c);
     bool ok = true;
-    for (int32_t k = 0; c.item < items; ++k) {
-      const uint2 meta = next;
+    for (int32_t k = 0; c.item < items && ok; ++k) {
+      const uint32_t meta[4] = {next.x, next.y, next.z, next.w};
       const int32_t item = c.item;
       const bool there = c.tile * 4 + quarter < quarters;
       c.advance(kGroups, tiles, p.chunk, s_end);
@@ -171,44 +195,51 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
       const int st = item % kStages;
       ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.ring_full[st]), (item / kStages) & 1, dead));
       if (!ok) break;
-      uint32_t w[4][4];
+      // The whole item at once, so that its place in the ring is free for the next copy.  The fence: reads through the ordinary path are over
+      // before a copy, which takes another path, may overwrite them (without it some lanes read the item after).
+      uint32_t w[8][4];
       if (there) {
-        const uint32_t codes = ring_at + st * kStage + quarter * kQuarter + lane * 64;
+        const uint32_t codes = ring_at + st * kStage + quarter * kQuarter + lane * 128;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(codes + ((i ^ ((lane >> 1) & 3)) << 4)));
+        for (int i = 0; i < 8; ++i)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(codes + ((i ^ (lane & 7)) << 4)));
       }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars.ring_empty[st]));
-      bool waited = k == 0;
-      if (there) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t o[32];
+      for (int half = 0; half < 2; ++half) {
+        const int32_t turn = 2 * item + half, lap = turn / n_a, buf = turn - lap * n_a;
+        bool waited = lap == 0;
+        auto buffer_free = [&]() {           // the product that had the buffer before has read it
+          if (!waited) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_empty[buf]), (lap - 1) & 1, dead));
+          waited = true;
+          fence_after();
+        };
+        if (there) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t m = h ? meta.y : meta.x;
-            const BlockScale sc = block_scale(i ? m >> 16 : m & 0xffffu, book_at, true);
+          for (int h = 0; h < 2; ++h) {
+            uint32_t o[32];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) decode_word_mul(w[2 * h + i][q], sc, p.m4, p.m16, o + 16 * i + 4 * q);
-          }
-          if (!waited) {                   // the product of this group's item before has read the buffer
-            waited = true;
-            ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_empty[group]), (k - 1) & 1, dead));
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t m = meta[2 * half + h];
+              const BlockScale sc = block_scale(i ? m >> 16 : m & 0xffffu, book_at, true);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) decode_word(w[4 * half + 2 * h + i][q], sc, *reinterpret_cast<uint32_t(*)[4]>(o + 16 * i + 4 * q));
+            }
+            buffer_free();
             if (!ok) break;
-            fence_after();
+            tmem_st32(tmem + buf * kACols + lanes + 32 * h, o);
           }
-          tmem_st32(a_at + 32 * h, o);
+          tmem_wait_st();
+        } else {
+          buffer_free();
         }
         if (!ok) break;
-        tmem_wait_st();
-      } else if (!waited) {
-        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_empty[group]), (k - 1) & 1, dead));
-        if (!ok) break;
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.a_full[buf]));
       }
-      fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars.a_full[group]));
     }
     // ---- the sums, [row of x][row of W], to shared memory, which nobody uses any more once the last product is done
     if (ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.d_full), 0, dead));
@@ -220,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
         float* at = sums + tile * 128 + quarter * 32 + lane;
         for (int32_t col = 0; col < rows; col += 16) {
           uint32_t v[16];
-          tmem_ld16(tmem + kDCol + tile * rows + col + lanes, v);
+          tmem_ld16(d_col + tile * rows + col + lanes, v);
           tmem_wait_ld();
 #pragma unroll
           for (int i = 0; i < 16; ++i) at[(col + i) * sums_ld] = __uint_as_float(v[i]);
@@ -238,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
       const uint32_t full = smem_u32(&bars.ring_full[st]);
       if (lane == 0) {
         mbar_expect_tx(full, (uint32_t)n * kQuarter);
-        for (int q = 0; q < n; ++q) tma_load_2d(ring_at + st * kStage + q * kQuarter, &map, full, c.s * 64, (int)(row_base + (c.tile * 4 + q) * 32));
+        for (int q = 0; q < n; ++q) tma_load_2d(ring_at + st * kStage + q * kQuarter, &map, full, c.s * 128, (int)(row_base + (c.tile * 4 + q) * 32));
       }
       __syncwarp();
     }
@@ -246,59 +277,61 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
     for (int32_t i = items > kStages ? items - kStages : 0; i < items && !*dead; ++i) wait(smem_u32(&bars.ring_full[i % kStages]), (i / kStages) & 1, dead);
   } else if (warp == kProductWarp) {
     // =========================================================== product: every lane waits, one issues
-    const uint32_t idesc = instr_desc(rows, false), x_low = desc_low(x_at, 16), x_buffer = (uint32_t)p.chunk * rows * 256;
-    bool ok = true;
-    int32_t chunk_no = -1;
+    const uint32_t idesc = instr_desc(rows, false), x_low = desc_low(x_at, 16), x_buffer = (uint32_t)p.chunk * rows * 512;
+    bool ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_first), 0, dead));
+    int32_t chunk_no = 0;
+    int turn_buf = 0;                        // buffer of A, and how often it has been used, mod 2
+    uint32_t turn_lap = 0;
     for (Cursor c(s_begin, s_end, p.chunk); c.item < items && ok;) {
-      const Cursor now = c;
+      const int32_t tile = c.tile, s = c.s, c0 = c.c0;
+      const int xb = c.chunk_no & (p.buffers - 1);
+      if (c.chunk_no != chunk_no) {
+        chunk_no = c.chunk_no;
+        if (chunk_no >= p.buffers) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_full[xb]), (chunk_no / p.buffers - 1) & 1, dead));
+      }
       c.advance(1, tiles, p.chunk, s_end);
-      const int buf = now.chunk_no % p.buffers, group = now.item % kGroups;
-      if (now.chunk_no != chunk_no) {
-        chunk_no = now.chunk_no;
-        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_full[buf]), (chunk_no / p.buffers) & 1, dead));
-      }
-      if (ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_full[group]), (now.item / kGroups) & 1, dead));
-      if (!ok) break;
-      fence_after();
-      if (elected()) {
-        const uint32_t d = tmem + kDCol + now.tile * rows, a = tmem + group * kACols;
-        const uint32_t b = x_low + ((buf * x_buffer + (uint32_t)(now.s - now.c0) * rows * 256) >> 4);
+      const bool end = c.item >= items, chunk_end = end || c.chunk_no != chunk_no;
+      const uint32_t d = d_col + tile * rows;
+      uint32_t b = x_low + ((xb * x_buffer + (uint32_t)(s - c0) * rows * 512) >> 4);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) mma_ts(d, a + 8 * k, b + (((k >> 2) * rows * 128 + (k & 3) * 32) >> 4), idesc, k > 0 || now.s > s_begin);
-        commit(smem_u32(&bars.a_empty[group]));
-        if (c.item == items || c.chunk_no != chunk_no) commit(smem_u32(&bars.x_empty[buf]));
-        if (c.item == items) commit(smem_u32(&bars.d_full));
+      for (int half = 0; half < 2; ++half, b += rows * 16) {
+        if (ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_full[turn_buf]), turn_lap, dead));
+        if (!ok) break;
+        fence_after();
+        if (elected()) {
+          const uint32_t a = tmem + turn_buf * kACols;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) mma_ts(d, a + 8 * k, b + (k >> 2) * rows * 8 + (k & 3) * 2, idesc, k > 0 || half > 0 || s > s_begin);
+          commit(smem_u32(&bars.a_empty[turn_buf]));
+          if (half && chunk_end) commit(smem_u32(&bars.x_empty[xb]));
+          if (half && end) commit(smem_u32(&bars.d_full));
+        }
+        __syncwarp();
+        if (++turn_buf == n_a) {
+          turn_buf = 0;
+          turn_lap ^= 1u;
+        }
       }
-      __syncwarp();
     }
     // nothing of this CTA may be on the tensor core when its tensor memory is given back
     if (elected()) commit(smem_u32(&bars.drained));
     uint32_t tries = 0;
     while (!mbar_try_wait(smem_u32(&bars.drained), 0) && ++tries < kSpinLimit) {}
   } else {
-    // =========================================================== x: [64 channels][row] with 128-byte swizzle, rows behind the last zero
+    // =========================================================== x: the chunks behind the first ones
     const int xw = warp - kXWarp;
     bool ok = true;
-    int32_t no = 0;
-    for (int32_t c0 = s_begin; c0 < s_end && ok; c0 += p.chunk, ++no) {
+    int32_t no = p.buffers;
+    for (int32_t c0 = s_begin + p.chunk * p.buffers; c0 < s_end; c0 += p.chunk, ++no) {
       const int32_t n_steps = min(p.chunk, s_end - c0), buf = no % p.buffers;
-      if (no >= p.buffers) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_empty[buf]), (no / p.buffers - 1) & 1, dead));
+      ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_empty[buf]), (no / p.buffers - 1) & 1, dead));
       if (!ok) break;
-      const uint32_t at = x_at + (uint32_t)buf * p.chunk * rows * 256;
-      for (int32_t r = xw; r < rows; r += kXWarps) {
-        const uint4* src = reinterpret_cast<const uint4*>(p.x + (t0 + r) * p.ld) + (int64_t)c0 * 16;
-        const uint32_t row_at = at + (r >> 3) * 1024 + (r & 7) * 128;
-#pragma unroll 4
-        for (int32_t run = lane; run < n_steps * 16; run += 32) {                       // 8 channels
-          uint4 u = make_uint4(0, 0, 0, 0);
-          if (r < n_tok && 4 * c0 + (run >> 2) < p.nb) u = __ldg(src + run);
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row_at + (run >> 3) * rows * 128 + (((run ^ r) & 7) << 4)), "r"(prmt(u.x, u.y, 0x5410u)),
-                       "r"(prmt(u.x, u.y, 0x7632u)), "r"(prmt(u.z, u.w, 0x5410u)), "r"(prmt(u.z, u.w, 0x7632u)) : "memory");
-        }
+      const uint32_t at = x_at + (uint32_t)buf * p.chunk * rows * 512;
+      for (int32_t i = xw; i < n_steps * (rows >> 3); i += kXWarps) {
+        const int32_t step = i / (rows >> 3);
+        bring(at + step * rows * 512, c0 + step, (i - step * (rows >> 3)) * 8);
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars.x_full[buf]));
+      brought(smem_u32(&bars.x_full[buf]));
     }
   }
   __syncwarp();
@@ -377,34 +410,32 @@ cudaError_t fb4_launch_linear_tc(const fb4_ctx* ctx, const void* x, int64_t T, i
   p.N = N;
   p.nb = (int32_t)(K / 32);
   p.out_dtype = out_dtype;
-  p.m4 = 16u;
-  p.m16 = 65536u;
   p.tables = ctx->d_tables;
   p.status = ctx->d_status;
   // rows of x in passes of equal size
   const int64_t z = (T + kMaxRows - 1) / kMaxRows, each = (T + z - 1) / z;
   p.rows = (int32_t)((each + 15) / 16 * 16);
-  const int32_t steps = (p.nb + 3) / 4, most = kDCols / p.rows * 4;
+  const int32_t steps = (p.nb + 7) / 8, most = kDCols / p.rows * 4;
   const int64_t quarters = (N + 31) / 32;
-  // the cluster size with the fewest items for a CTA; a wave's start and join count as 6
+  // the cluster size with the fewest items for a CTA; a wave's start and join count as 3
   double best = 1e300;
   for (int c = 1; c <= kMaxSplits && (c == 1 || c <= steps); c *= 2) {
     const int64_t at_once = ctx->linear_tc_clusters[c];
     int64_t q = (quarters * z + at_once - 1) / at_once;
     if (q > most) q = most;
     const int64_t grid = (quarters + q - 1) / q * z, waves = (grid + at_once - 1) / at_once;
-    const double cost = (double)waves * ((q + 3) / 4 * ((steps + c - 1) / c) + 6);
+    const double cost = (double)waves * ((q + 3) / 4 * ((steps + c - 1) / c) + 3);
     if (cost < best) {
       best = cost;
       p.splits = c;
       p.quarters = (int32_t)q;
     }
   }
-  const int32_t mine = (steps + p.splits - 1) / p.splits, step_bytes = p.rows * 256;
+  const int32_t mine = (steps + p.splits - 1) / p.splits, step_bytes = p.rows * 512;
   p.buffers = mine * step_bytes <= kXBytes ? 1 : 2;
   p.chunk = p.buffers == 1 ? mine : kXBytes / 2 / step_bytes;
   CUtensorMap map;
-  cudaError_t e = fb4_encode_map_2d(&map, codes, (uint64_t)K / 2, (uint64_t)N, (uint64_t)K / 2, 64, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  cudaError_t e = fb4_encode_map_2d(&map, codes, (uint64_t)K / 2, (uint64_t)N, (uint64_t)K / 2, 128, 32, CU_TENSOR_MAP_SWIZZLE_128B);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
