@@ -702,8 +702,7 @@ int fb4_linear(fb4_ctx* ctx, const void* x, int64_t T, int64_t K, int64_t ld_ele
   if (!aligned16(x) || (ld_elems & 7) || !aligned16(codes) || !aligned16(meta) || !aligned16(out) || (reinterpret_cast<uintptr_t>(bias) & 1u))
     return FB4_ERR_ALIGN;
   if (ctx->linear_error != cudaSuccess) return fb4_set_cuda_error(ctx->linear_error);
-  const auto launch = ctx->force_generic ? fb4_launch_linear : fb4_launch_linear_tc;
-  const cudaError_t e = launch(ctx, x, T, ld_elems, codes, meta, N, K, bias, out, out_ld, out_dtype, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = fb4_launch_linear(ctx, x, T, ld_elems, codes, meta, N, K, bias, out, out_ld, out_dtype, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fb4_set_cuda_error(e);
   ctx->launches += 1;
   return FB4_OK;

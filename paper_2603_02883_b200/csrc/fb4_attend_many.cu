@@ -439,6 +439,8 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         for (int k = 0; k < kTasks; ++k)
           asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cw[k][0]), "=r"(cw[k][1]), "=r"(cw[k][2]), "=r"(cw[k][3]) : "r"(codes + row * D + (k ^ mix) * 16));
         const Int8Scale sc = int8_scale(is_v ? v_byte : k_byte, true);          // whatever a slot that no token fills holds is finite
+        // reads through the ordinary path are over before the next copy, which takes another path, may overwrite what they read
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars.ring_empty[st]));
         if (t >= 2) ok = __all_sync(0xffffffffu, wait(smem_u32(is_v ? &bars.v_empty[buf] : &bars.k_empty[buf]), ((t >> 1) - 1) & 1, dead));

@@ -57,7 +57,7 @@ struct fb4_ctx {
   cudaError_t plan_error;        // the same for the plan of a step
   cudaError_t linear_error;      // the same for the products with FB4 weights
   int32_t linear_tc_clusters[9]; // tensor-core kernel, per cluster size: clusters that are resident at a time
-  int32_t linear_slots[4][9];    // per kernel variant and cluster size: CTAs that are resident at a time
+  int32_t linear_slots[9];       // kernel of few rows, per cluster size: CTAs that are resident at a time
   int sm_count;
   void* d_topk_scratch;          // histograms and counters of the multi-CTA top-k selection (fb4_topk.cu)
   uint32_t* d_status;            // device status word (bit 0: a TMA wait ran out of tries; bit 1: an index argument out of range)
@@ -184,8 +184,8 @@ cudaError_t fb4_launch_attend_join(const Fb4Attend& a, cudaStream_t stream);
 cudaError_t fb4_launch_attend_few(const Fb4Attend& a, cudaStream_t stream);
 cudaError_t fb4_launch_attend_generic(const fb4_ctx* ctx, const Fb4Attend& a, cudaStream_t stream);
 
-// products with FB4 weights (fb4_linear.cu)
-cudaError_t fb4_linear_prepare_device(int32_t (*slots)[9]);
+// products with FB4 weights (fb4_linear.cu: few rows, and the choice)
+cudaError_t fb4_linear_prepare_device(int32_t* slots);
 cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
                               int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream);
 

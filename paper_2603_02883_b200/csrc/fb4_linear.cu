@@ -1,12 +1,16 @@
-// Products of few rows with FB4 weights: y[t][n] = sum_k x[t][k] w[n][k] + bias[n].
+// Products of up to 8 rows with FB4 weights: y[t][n] = sum_k x[t][k] w[n][k] + bias[n].  More rows: fb4_linear_tc.cu.
 //
-// The weights are the long side, so their rows are the M side of mma.sync m16n8k16 and up to 64 rows of x its N side: a warp reads a
-// weight once for all of them.  A lane decodes a block of 32 channels of two rows at a time from two 16-byte words of codes, straight into
+// The weights are the long side, so their rows are the M side of mma.sync m16n8k16 and the rows of x its N side: a warp reads a weight once
+// for all of them.  A lane decodes a block of 32 channels of two rows at a time from two 16-byte words of codes, straight into
 // the A fragments (which channel sits at which k is free, as long as x agrees).  x lies in shared memory in the order in which the
 // lanes read it, 16 bytes for 8 channels.
 //
-// Work: a CTA of 8 warps takes 128 rows of W (256 in warps of 32 rows, where more than 8 rows of x share the fragments) and one run of the
-// channels, the CTAs of a row tile are a cluster, which joins their sums through distributed shared memory, always in the same order.
+// Work: a CTA of 8 warps takes 128 rows of W and one run of the channels; the CTAs of a row tile are a cluster, which joins their sums through
+// distributed shared memory, always in the same order.
+//
+// Bound: the ALU pipe (decode: 10 operations per 8 weights, two thirds of all of its) while all warps are at work, and CTAs that are two or three to
+// an SM; 12288 x 12288 in 31.5 us, 2.7 TB/s, the same out of L2 (28.5).  One CTA per SM with its rows dealt out evenly came out slower (39.6),
+// and so did clusters of three (41.7: they are not spread evenly) and 16 warps an SM with loads four steps ahead (49.8 in two waves).
 #include "fb4_attend.cuh"
 #include "fb4_block.cuh"
 
@@ -15,8 +19,9 @@ namespace {
 using namespace fb4att;
 
 constexpr int kWarps = 8;                       // a step of a warp is 128 channels: 4 blocks, one to each lane of a quad
-__host__ __device__ constexpr int ahead(int MT) { return 2; }      // steps that are loaded ahead
-__host__ __device__ constexpr int resident(int MT) { return MT == 1 ? 3 : 2; }      // CTAs per SM
+constexpr int kAhead = 2;                        // steps that are loaded ahead
+constexpr int kResident = 3;                     // CTAs per SM
+constexpr int kRows = kWarps * 16;               // rows of W to a CTA
 constexpr int kMaxSplits = 8;                    // portable cluster size
 constexpr int kXBytes = 64 * 1024;               // most of x that a CTA holds at a time
 
@@ -42,130 +47,97 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// MT: tiles of 16 rows of W to a warp; NT: tiles of 8 rows of x
-template <int MT, int NT>
-__global__ void __launch_bounds__(kWarps * 32, resident(MT)) fb4_linear_kernel(const __grid_constant__ Linear p) {
-  constexpr int kRows = kWarps * 16 * MT, kAhead = ahead(MT);      // rows of W to a CTA
+__global__ void __launch_bounds__(kWarps * 32, kResident) fb4_linear_kernel(const __grid_constant__ Linear p) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t book[64];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int32_t split = (int32_t)(blockIdx.x % p.splits);
   const int64_t tile = blockIdx.x / p.splits;
-  const int64_t n0 = tile * kRows + warp * (16 * MT), t0 = (int64_t)blockIdx.y * (8 * NT);
-  const int32_t n_tok = (int32_t)(p.T - t0 < 8 * NT ? p.T - t0 : 8 * NT);
+  const int64_t n0 = tile * kRows + warp * 16;
+  const int32_t n_tok = (int32_t)p.T;
   const int32_t steps = (p.nb + 3) / 4;
   const int32_t s_begin = (int32_t)((int64_t)steps * split / p.splits), s_end = (int32_t)((int64_t)steps * (split + 1) / p.splits);
   const uint32_t x_at = fb4blk::smem_u32(smem), book_at = fb4blk::smem_u32(book);
   if (threadIdx.x < 64) fill_book(book, p.tables, threadIdx.x);
 
   // this lane's rows of W, from the run's first block on; rows behind the last are computed like it and not stored
-  const uint8_t* codes[MT][2];
-  const uint16_t* meta[MT][2];
+  const uint8_t* codes[2];
+  const uint16_t* meta[2];
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int64_t n = n0 + 16 * m + 8 * r + g, at = (n < p.N ? n : p.N - 1) * p.nb + 4 * (int64_t)s_begin + t;
-      codes[m][r] = p.codes + at * 16;
-      meta[m][r] = p.meta + at;
-    }
-  float acc[MT][NT][4];
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) acc[m][n][k] = 0.0f;
-
-  uint4 cw[kAhead][MT][2];
-  uint16_t mt[kAhead][MT][2];                       // joined only when used: that would wait for the load
+  for (int r = 0; r < 2; ++r) {
+    const int64_t n = n0 + 8 * r + g, at = (n < p.N ? n : p.N - 1) * p.nb + 4 * (int64_t)s_begin + t;
+    codes[r] = p.codes + at * 16;
+    meta[r] = p.meta + at;
+  }
+  float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  uint4 cw[kAhead][2];
+  uint16_t mt[kAhead][2];                           // joined only when used: that would wait for the load
   const int32_t whole = p.nb / 4;                   // steps whose four blocks all exist; there is at most one more
   // loads step s, which lies i steps behind the pointers, into ring place `at`
   auto load = [&](int32_t s, int i, int at) {
     const bool there = s < whole || 4 * s + t < p.nb;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        cw[at][m][r] = make_uint4(0, 0, 0, 0);
-        mt[at][m][r] = 0;                           // scale byte 0 and codes 0: zeros
-        if (there) {
-          cw[at][m][r] = __ldg(reinterpret_cast<const uint4*>(codes[m][r] + 64 * i));
-          mt[at][m][r] = __ldg(meta[m][r] + 4 * i);
-        }
+    for (int r = 0; r < 2; ++r) {
+      cw[at][r] = make_uint4(0, 0, 0, 0);
+      mt[at][r] = 0;                                // scale byte 0 and codes 0: zeros
+      if (there) {
+        cw[at][r] = __ldg(reinterpret_cast<const uint4*>(codes[r] + 64 * i));
+        mt[at][r] = __ldg(meta[r] + 4 * i);
       }
+    }
   };
 #pragma unroll
   for (int i = 0; i < kAhead; ++i)
     if (s_begin + i < s_end) load(s_begin + i, i, i);
 
-  // x of a chunk, piece (s, w, n, g, t): channels 8 w .. 8 w + 7 of block 4 s + t of row 8 n + g, in the order 0 2 1 3 4 6 5 7 of the
-  // decoder; with one tile of rows only `wide` of them (a power of two) have room, and the lanes behind read zeros
-  const int wide = NT > 1 ? 8 : p.wide;
-  const uint32_t x_lane = NT > 1 ? lane << 4 : (lane & (4 * wide - 1)) << 4;
-  const uint32_t x_piece = NT > 1 ? NT * 512 : wide * 64;
-  const bool x_there = NT > 1 || lane < 4 * wide;
+  // x of a chunk, piece (s, w, g, t): channels 8 w .. 8 w + 7 of block 4 s + t of row g, in the order 0 2 1 3 4 6 5 7 of the decoder; only
+  // `wide` rows (a power of two) have room, and the lanes behind them read zeros
+  const uint32_t x_piece = p.wide * 64;
+  const bool x_there = lane < 4 * p.wide;
   for (int32_t c0 = s_begin; c0 < s_end; c0 += p.chunk) {
     const int32_t c1 = c0 + p.chunk < s_end ? c0 + p.chunk : s_end;
     __syncthreads();                                // nobody reads the x of the chunk before any more
-    for (int32_t tok = warp; tok < (NT > 1 ? 8 * NT : wide); tok += kWarps) {
-      const uint4* src = reinterpret_cast<const uint4*>(p.x + (t0 + tok) * p.ld) + (int64_t)c0 * 16;
-      const uint32_t row_at = x_at + (NT > 1 ? (tok >> 3) * 512 : 0) + (tok & 7) * 64;
-#pragma unroll 4
-      for (int32_t k16 = lane; k16 < (c1 - c0) * 16; k16 += 32) {                       // 16-byte pieces of the chunk's row
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (tok < n_tok && 4 * c0 + (k16 >> 2) < p.nb) u = __ldg(src + k16);
-        const uint32_t dst = row_at + ((k16 >> 4) * 4 + (k16 & 3)) * x_piece + ((k16 >> 2) & 3) * 16;
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(prmt(u.x, u.y, 0x5410u)), "r"(prmt(u.x, u.y, 0x7632u)),
-                     "r"(prmt(u.z, u.w, 0x5410u)), "r"(prmt(u.z, u.w, 0x7632u)) : "memory");
-      }
+    for (int32_t i = warp; i < p.wide * ((c1 - c0 + 1) / 2); i += kWarps) {               // 2 steps of a row to a warp
+      const int32_t tok = i % p.wide, k16 = i / p.wide * 32 + lane;                     // 16-byte piece of the chunk's row
+      if (k16 >= (c1 - c0) * 16) continue;
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (tok < n_tok && 4 * c0 + (k16 >> 2) < p.nb) u = __ldg(reinterpret_cast<const uint4*>(p.x + tok * p.ld) + (int64_t)c0 * 16 + k16);
+      const uint32_t dst = x_at + tok * 64 + ((k16 >> 4) * 4 + (k16 & 3)) * x_piece + ((k16 >> 2) & 3) * 16;
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(prmt(u.x, u.y, 0x5410u)), "r"(prmt(u.x, u.y, 0x7632u)),
+                   "r"(prmt(u.z, u.w, 0x5410u)), "r"(prmt(u.z, u.w, 0x7632u)) : "memory");
     }
     __syncthreads();
-    uint32_t x_step = x_at + x_lane;
+    uint32_t x_step = x_at + (lane & (4 * p.wide - 1)) * 16;
     for (int32_t s0 = c0; s0 < c1; s0 += kAhead) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int32_t s = s0 + i;
         if (s >= c1) break;
-        BlockScale sc[MT][2];
-        uint32_t words[MT][2][4];
+        BlockScale sc[2];
+        uint32_t words[2][4];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            sc[m][r] = block_scale(mt[i][m][r], book_at, true);
-            words[m][r][0] = cw[i][m][r].x; words[m][r][1] = cw[i][m][r].y; words[m][r][2] = cw[i][m][r].z; words[m][r][3] = cw[i][m][r].w;
-          }
+        for (int r = 0; r < 2; ++r) {
+          sc[r] = block_scale(mt[i][r], book_at, true);
+          words[r][0] = cw[i][r].x; words[r][1] = cw[i][r].y; words[r][2] = cw[i][r].z; words[r][3] = cw[i][r].w;
         }
         if (s + kAhead < s_end) load(s + kAhead, i + kAhead, i);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          uint32_t a[MT][2][4];
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            decode_word(words[m][0][w], sc[m][0], a[m][0]);
-            decode_word(words[m][1][w], sc[m][1], a[m][1]);
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            uint4 b = make_uint4(0, 0, 0, 0);
-            if (x_there) b = fb4blk::lds_v4(x_step + (i * 4 + w) * x_piece + n * 512);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-              mma_bf16(acc[m][n], a[m][0][0], a[m][1][0], a[m][0][1], a[m][1][1], b.x, b.y);
-              mma_bf16(acc[m][n], a[m][0][2], a[m][1][2], a[m][0][3], a[m][1][3], b.z, b.w);
-            }
-          }
+          uint32_t a[2][4];
+          decode_word(words[0][w], sc[0], a[0]);
+          decode_word(words[1][w], sc[1], a[1]);
+          uint4 b = make_uint4(0, 0, 0, 0);
+          if (x_there) b = fb4blk::lds_v4(x_step + (i * 4 + w) * x_piece);
+          mma_bf16(acc, a[0][0], a[1][0], a[0][1], a[1][1], b.x, b.y);
+          mma_bf16(acc, a[0][2], a[1][2], a[0][3], a[1][3], b.z, b.w);
         }
       }
       x_step += kAhead * 4 * x_piece;
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          codes[m][r] += 64 * kAhead;
-          meta[m][r] += 4 * kAhead;
-        }
+      for (int r = 0; r < 2; ++r) {
+        codes[r] += 64 * kAhead;
+        meta[r] += 4 * kAhead;
+      }
     }
   }
 
@@ -174,11 +146,7 @@ __global__ void __launch_bounds__(kWarps * 32, resident(MT)) fb4_linear_kernel(c
   float* sums = reinterpret_cast<float*>(smem);
   constexpr int kLd = kRows + 4;                    // the quads' rows of x fall into different banks
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) sums[(8 * n + 2 * t + (k & 1)) * kLd + warp * 16 * MT + 16 * m + g + 8 * (k >> 1)] = acc[m][n][k];
+  for (int k = 0; k < 4; ++k) sums[(2 * t + (k & 1)) * kLd + warp * 16 + g + 8 * (k >> 1)] = acc[k];
   if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   else __syncthreads();
   for (int32_t i = split * (kWarps * 32) + threadIdx.x; i < n_tok * kRows; i += p.splits * (kWarps * 32)) {
@@ -200,7 +168,7 @@ __global__ void __launch_bounds__(kWarps * 32, resident(MT)) fb4_linear_kernel(c
     }
     v *= kUnshift;
     if (p.bias) v += __uint_as_float((uint32_t)__ldg(p.bias + n) << 16);
-    const int64_t at = (t0 + tok) * p.out_ld + n;
+    const int64_t at = tok * p.out_ld + n;
     if (p.out_dtype == 0) static_cast<float*>(p.out)[at] = v;
     else if (p.out_dtype == 1) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
     else static_cast<__half*>(p.out)[at] = __float2half_rn(v);
@@ -209,19 +177,56 @@ __global__ void __launch_bounds__(kWarps * 32, resident(MT)) fb4_linear_kernel(c
   if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int MT, int NT>
-constexpr int join_bytes() { return 8 * NT * (kWarps * 16 * MT + 4) * 4; }
+constexpr int kJoinBytes = 8 * (kRows + 4) * 4;
 
-template <int MT, int NT>
-cudaError_t launch(const fb4_ctx* ctx, const int32_t* slots, Linear p, cudaStream_t stream) {
-  constexpr int kRows = kWarps * 16 * MT, kAhead = ahead(MT);
-  const int64_t tiles = (p.N + kRows - 1) / kRows, z = (p.T + 8 * NT - 1) / (8 * NT);
+}  // namespace
+
+// Opt-in to the dynamic shared memory, and how many CTAs are resident at a time in clusters of 1 to 8 (fewer than without clusters: a
+// cluster lies in one group of SMs).
+cudaError_t fb4_linear_prepare_device(int32_t* slots) {
+  cudaError_t e = cudaFuncSetAttribute(fb4_linear_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
+  for (int s = 1; s <= kMaxSplits && e == cudaSuccess; ++s) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)s;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(s * 1024));
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = kXBytes;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, fb4_linear_kernel, &cfg);
+    slots[s] = n * s > 1 ? n * s : 1;
+  }
+  return e;
+}
+
+cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
+                              int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream) {
+  if (T > 8) return fb4_launch_linear_tc(ctx, x, T, ld, codes, meta, N, K, bias, out, out_ld, out_dtype, stream);
+  Linear p{};
+  p.x = static_cast<const uint16_t*>(x);
+  p.ld = ld;
+  p.codes = codes;
+  p.meta = meta;
+  p.bias = static_cast<const uint16_t*>(bias);
+  p.out = out;
+  p.out_ld = out_ld;
+  p.T = T;
+  p.N = N;
+  p.nb = (int32_t)(K / 32);
+  p.out_dtype = out_dtype;
+  p.tables = ctx->d_tables;
+  const int32_t* slots = ctx->linear_slots;
+  const int64_t tiles = (N + kRows - 1) / kRows;
   const int32_t steps = (p.nb + 3) / 4;
   // splits: the least of waves x work of a CTA, its start and its part of the join counted as 4 steps
   double best = 1e300;
   p.splits = 1;
   for (int s = 1; s <= kMaxSplits && (s == 1 || steps / s >= 2); ++s) {
-    const int64_t waves = (tiles * z * s + slots[s] - 1) / slots[s];
+    const int64_t waves = (tiles * s + slots[s] - 1) / slots[s];
     const double cost = (double)waves * ((steps + s - 1) / s + 4);
     if (cost < best * 0.97) {
       best = cost;
@@ -229,15 +234,15 @@ cudaError_t launch(const fb4_ctx* ctx, const int32_t* slots, Linear p, cudaStrea
     }
   }
   const int32_t mine = (steps + p.splits - 1) / p.splits;
-  for (p.wide = 1; p.wide < 8 && p.wide < p.T; p.wide *= 2) {}
-  const int per_step = NT > 1 ? 2048 * NT : 256 * p.wide;
+  for (p.wide = 1; p.wide < 8 && p.wide < T; p.wide *= 2) {}
+  const int per_step = 256 * p.wide;
   const int32_t most = kXBytes / per_step / kAhead * kAhead;
   p.chunk = mine < most ? (mine + kAhead - 1) / kAhead * kAhead : most;
   int smem = p.chunk * per_step;
-  if (smem < join_bytes<MT, NT>()) smem = join_bytes<MT, NT>();
+  if (smem < kJoinBytes) smem = kJoinBytes;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
-  cfg.gridDim = dim3((unsigned)(tiles * p.splits), (unsigned)z);
+  cfg.gridDim = dim3((unsigned)(tiles * p.splits));
   cfg.blockDim = dim3(kWarps * 32);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = stream;
@@ -248,48 +253,5 @@ cudaError_t launch(const fb4_ctx* ctx, const int32_t* slots, Linear p, cudaStrea
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.numAttrs = 1;
   }
-  return cudaLaunchKernelEx(&cfg, fb4_linear_kernel<MT, NT>, p);
-}
-
-}  // namespace
-
-// Opt-in to the dynamic shared memory, and how many CTAs are resident at a time in clusters of 1 to 8 (fewer than without clusters: a
-// cluster lies in one group of SMs).
-cudaError_t fb4_linear_prepare_device(int32_t (*slots)[kMaxSplits + 1]) {
-  cudaError_t e = cudaSuccess;
-  auto prepare = [&](void (*kernel)(Linear), int smem, int32_t* of) {
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    for (int s = 1; s <= kMaxSplits && e == cudaSuccess; ++s) {
-      cudaLaunchConfig_t cfg{};
-      cudaLaunchAttribute attr[1];
-      attr[0].id = cudaLaunchAttributeClusterDimension;
-      attr[0].val.clusterDim.x = (unsigned)s;
-      attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-      cfg.gridDim = dim3((unsigned)(s * 1024));
-      cfg.blockDim = dim3(kWarps * 32);
-      cfg.dynamicSmemBytes = (size_t)smem;
-      cfg.attrs = attr;
-      cfg.numAttrs = 1;
-      int n = 0;
-      e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
-      of[s] = n * s > 1 ? n * s : 1;
-    }
-  };
-#define FB4_PREPARE(MT, NT, i) prepare(fb4_linear_kernel<MT, NT>, kXBytes > join_bytes<MT, NT>() ? kXBytes : join_bytes<MT, NT>(), slots[i])
-  FB4_PREPARE(1, 1, 0);
-  FB4_PREPARE(2, 2, 1);
-  FB4_PREPARE(2, 4, 2);
-  FB4_PREPARE(2, 8, 3);
-#undef FB4_PREPARE
-  return e;
-}
-
-cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
-                              int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream) {
-  Linear p{static_cast<const uint16_t*>(x), ld, codes, meta, static_cast<const uint16_t*>(bias), out, out_ld, T, N, (int32_t)(K / 32), 1, 1, 8,
-           out_dtype, ctx->d_tables};
-  if (T <= 8) return launch<1, 1>(ctx, ctx->linear_slots[0], p, stream);
-  if (T <= 16) return launch<2, 2>(ctx, ctx->linear_slots[1], p, stream);
-  if (T <= 32) return launch<2, 4>(ctx, ctx->linear_slots[2], p, stream);
-  return launch<2, 8>(ctx, ctx->linear_slots[3], p, stream);
+  return cudaLaunchKernelEx(&cfg, fb4_linear_kernel, p);
 }
