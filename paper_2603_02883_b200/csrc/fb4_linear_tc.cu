@@ -53,9 +53,13 @@ struct Linear {
   uint32_t* status;
 };
 
+// A wait tells only whether the phase before the present one has ended, so a waiter must never be two phases ahead.  Buffers of A go round the
+// groups, and a group that begins turn q (half an item) knows of the products of turns up to q - n - 7 only (n buffers: its own turn before
+// was q - 7 or later, and it had a buffer).  With a barrier for the odd and one for the even uses of a buffer it waits for turn q - n where
+// q - 3 n must have ended, which is so from 4 buffers on; with one barrier, q - 2 n, from 7 on.
 struct Bars {
   uint64_t ring_full[kStages], ring_empty[kStages];
-  uint64_t a_full[kMaxA], a_empty[kMaxA], x_first, x_full[2], x_empty[2], d_full, drained;
+  uint64_t a_full[kMaxA], a_empty[2][kMaxA], x_first, x_full[2], x_empty[2], d_full, drained;
 };
 
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* v) {
@@ -111,7 +115,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   // ---- set-up
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.ring_full[i]), 1); mbar_init(smem_u32(&bars.ring_empty[i]), 4); }
-    for (int i = 0; i < kMaxA; ++i) { mbar_init(smem_u32(&bars.a_full[i]), 4); mbar_init(smem_u32(&bars.a_empty[i]), 1); }
+    for (int i = 0; i < kMaxA; ++i) { mbar_init(smem_u32(&bars.a_full[i]), 4); mbar_init(smem_u32(&bars.a_empty[0][i]), 1); mbar_init(smem_u32(&bars.a_empty[1][i]), 1); }
     mbar_init(smem_u32(&bars.x_first), kDecodeWarps + kXWarps);
     for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.x_full[i]), kXWarps); mbar_init(smem_u32(&bars.x_empty[i]), 1); }
     mbar_init(smem_u32(&bars.d_full), 1);
@@ -212,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
         const int32_t turn = 2 * item + half, lap = turn / n_a, buf = turn - lap * n_a;
         bool waited = lap == 0;
         auto buffer_free = [&]() {           // the product that had the buffer before has read it
-          if (!waited) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_empty[buf]), (lap - 1) & 1, dead));
+          if (!waited) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_empty[(lap - 1) & 1][buf]), ((lap - 1) >> 1) & 1, dead));
           waited = true;
           fence_after();
         };
@@ -302,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
           const uint32_t a = tmem + turn_buf * kACols;
 #pragma unroll
           for (int k = 0; k < 8; ++k) mma_ts(d, a + 8 * k, b + (k >> 2) * rows * 8 + (k & 3) * 2, idesc, k > 0 || half > 0 || s > s_begin);
-          commit(smem_u32(&bars.a_empty[turn_buf]));
+          commit(smem_u32(&bars.a_empty[turn_lap][turn_buf]));
           if (half && chunk_end) commit(smem_u32(&bars.x_empty[xb]));
           if (half && end) commit(smem_u32(&bars.d_full));
         }

@@ -157,6 +157,21 @@ def test_captured_on_another_stream_and_strided_output(f, T):
     assert torch.equal(o[:, :500], f.linear(x, w))
 
 
+@pytest.mark.parametrize("size", [(12, 9000, 8192), (32, 12288, 8192), (64, 7000, 8192), (96, 9500, 2048)], ids=lambda s: ".".join(map(str, s)))
+def test_many_items_again_and_again(f, size):
+    """several tiles, chunks and laps of every ring, with other traffic in memory between: each run gives the same bits"""
+    T, N, K = size
+    x, w = rows(T, K, seed=T), weights(N, K, seed=N)
+    first = f.linear(x, w, dtype=torch.float32)
+    agree(first, x, w, None, torch.float32)
+    other = torch.ones(48 << 20, device="cuda")
+    for i in range(60):
+        if i % 3 == 0:
+            other.mul_(1.0001)
+        assert torch.equal(f.linear(x, w, dtype=torch.float32), first), f"run {i}"
+    assert f.device_status == 0
+
+
 def test_two_calls_at_once(f):
     args = [(rows(1, 4096, seed=1), weights(3000, 4096, seed=1)), (rows(40, 4096, seed=2), weights(1000, 4096, seed=2))]
     want = [f.linear(*a) for a in args]
