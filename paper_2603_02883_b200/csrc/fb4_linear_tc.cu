@@ -11,8 +11,7 @@
 //   load     codes of the items into a ring (tensor copies of 32 rows x 128 bytes, 128-byte swizzle; with rows of 64 bytes the copies alone
 //            took 34 us where this takes 25)
 //   product  one warp issues D_tile += A x
-//   x        brought into shared memory at the start by all that have nothing to decode yet, where it is too large for it in chunks, the
-//            others by 6 warps
+//   x        6 warps bring x into shared memory, in chunks where it is too large for it
 #include "fb4_attend.cuh"
 #include "fb4_staging.cuh"
 #include "fb4_tcgen05.cuh"
@@ -49,6 +48,7 @@ struct Linear {
   int32_t quarters;         // quarters of a tile to a cluster
   int32_t chunk, buffers;   // steps of 256 channels whose x is held at a time, and how often
   int32_t out_dtype;
+  int32_t wide_out;         // 4 neighbouring results are stored at once
   const Fb4DeviceTables* tables;
   uint32_t* status;
 };
@@ -59,7 +59,7 @@ struct Linear {
 // q - 3 n must have ended, which is so from 4 buffers on; with one barrier, q - 2 n, from 7 on.
 struct Bars {
   uint64_t ring_full[kStages], ring_empty[kStages];
-  uint64_t a_full[kMaxA], a_empty[2][kMaxA], x_first, x_full[2], x_empty[2], d_full, drained;
+  uint64_t a_full[kMaxA], a_empty[2][kMaxA], x_full[2], x_empty[2], d_full, drained;
 };
 
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* v) {
@@ -116,7 +116,6 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.ring_full[i]), 1); mbar_init(smem_u32(&bars.ring_empty[i]), 4); }
     for (int i = 0; i < kMaxA; ++i) { mbar_init(smem_u32(&bars.a_full[i]), 4); mbar_init(smem_u32(&bars.a_empty[0][i]), 1); mbar_init(smem_u32(&bars.a_empty[1][i]), 1); }
-    mbar_init(smem_u32(&bars.x_first), kDecodeWarps + kXWarps);
     for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.x_full[i]), kXWarps); mbar_init(smem_u32(&bars.x_empty[i]), 1); }
     mbar_init(smem_u32(&bars.d_full), 1);
     mbar_init(smem_u32(&bars.drained), 1);
@@ -133,36 +132,6 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0), d_col = tmem + 512 - tiles * rows;
   const int n_a = min((512 - tiles * rows) / kACols, kMaxA);
-
-  // One step of x, 8 rows of it, by a warp: [64 channels][row] with 128-byte swizzle, rows behind the last zero.
-  auto bring = [&](uint32_t at, int32_t step, int32_t r0) {
-    const int32_t run = step * 32 + lane;                              // 8 channels, counted from the first of all
-    const uint4* src = reinterpret_cast<const uint4*>(p.x + (t0 + r0) * p.ld) + run;
-    uint4 u[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      u[r] = make_uint4(0, 0, 0, 0);
-      if ((run >> 2) < p.nb && r0 + r < n_tok) u[r] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(src) + r * p.ld));
-    }
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + (lane >> 3) * rows * 128 + (r0 >> 3) * 1024 + r * 128 + (((lane ^ r) & 7) << 4)),
-                   "r"(prmt(u[r].x, u[r].y, 0x5410u)), "r"(prmt(u[r].x, u[r].y, 0x7632u)), "r"(prmt(u[r].z, u[r].w, 0x5410u)),
-                   "r"(prmt(u[r].z, u[r].w, 0x7632u)) : "memory");
-  };
-  auto brought = [&](uint32_t bar) {
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar);
-  };
-  if (warp != kLoadWarp && warp != kProductWarp) {
-    const int me = warp < kDecodeWarps ? warp : warp - 2, first_steps = min(p.chunk * p.buffers, s_end - s_begin);
-    for (int32_t i = me; i < first_steps * (rows >> 3); i += kDecodeWarps + kXWarps) {
-      const int32_t step = i / (rows >> 3);
-      bring(x_at + step * rows * 512, s_begin + step, (i - step * (rows >> 3)) * 8);
-    }
-    brought(smem_u32(&bars.x_first));
-  }
 
   if (warp < kDecodeWarps) {
     // =========================================================== decode
@@ -190,14 +159,16 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
     c.advance(group, tiles, p.chunk, s_end);
     uint4 next = fetch(c);
     bool ok = true;
-    for (int32_t k = 0; c.item < items && ok; ++k) {
+    // place in the ring and buffer of A of the item's first half, and how often they have been used, moved on without divisions
+    int st = group, buf = 2 * group;
+    uint32_t st_lap = 0, lap = 0;
+    for (; buf >= n_a; buf -= n_a) ++lap;
+    while (c.item < items && ok) {
       const uint32_t meta[4] = {next.x, next.y, next.z, next.w};
-      const int32_t item = c.item;
       const bool there = c.tile * 4 + quarter < quarters;
       c.advance(kGroups, tiles, p.chunk, s_end);
       next = fetch(c);
-      const int st = item % kStages;
-      ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.ring_full[st]), (item / kStages) & 1, dead));
+      ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.ring_full[st]), st_lap & 1, dead));
       if (!ok) break;
       // The whole item at once, so that its place in the ring is free for the next copy.  The fence: reads through the ordinary path are over
       // before a copy, which takes another path, may overwrite them (without it some lanes read the item after).
@@ -211,9 +182,10 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars.ring_empty[st]));
+      st += kGroups;
+      if (st >= kStages) { st -= kStages; ++st_lap; }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const int32_t turn = 2 * item + half, lap = turn / n_a, buf = turn - lap * n_a;
         bool waited = lap == 0;
         auto buffer_free = [&]() {           // the product that had the buffer before has read it
           if (!waited) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_empty[(lap - 1) & 1][buf]), ((lap - 1) >> 1) & 1, dead));
@@ -243,6 +215,8 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars.a_full[buf]));
+        buf += half ? 2 * kGroups - 1 : 1;
+        for (; buf >= n_a; buf -= n_a) ++lap;
       }
     }
     // ---- the sums, [row of x][row of W], to shared memory, which nobody uses any more once the last product is done
@@ -282,8 +256,8 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   } else if (warp == kProductWarp) {
     // =========================================================== product: every lane waits, one issues
     const uint32_t idesc = instr_desc(rows, false), x_low = desc_low(x_at, 16), x_buffer = (uint32_t)p.chunk * rows * 512;
-    bool ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_first), 0, dead));
-    int32_t chunk_no = 0;
+    bool ok = true;
+    int32_t chunk_no = -1;
     int turn_buf = 0;                        // buffer of A, and how often it has been used, mod 2
     uint32_t turn_lap = 0;
     for (Cursor c(s_begin, s_end, p.chunk); c.item < items && ok;) {
@@ -291,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
       const int xb = c.chunk_no & (p.buffers - 1);
       if (c.chunk_no != chunk_no) {
         chunk_no = c.chunk_no;
-        if (chunk_no >= p.buffers) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_full[xb]), (chunk_no / p.buffers - 1) & 1, dead));
+        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_full[xb]), (chunk_no / p.buffers) & 1, dead));
       }
       c.advance(1, tiles, p.chunk, s_end);
       const bool end = c.item >= items, chunk_end = end || c.chunk_no != chunk_no;
@@ -322,20 +296,37 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
     uint32_t tries = 0;
     while (!mbar_try_wait(smem_u32(&bars.drained), 0) && ++tries < kSpinLimit) {}
   } else {
-    // =========================================================== x: the chunks behind the first ones
+    // =========================================================== x
     const int xw = warp - kXWarp;
     bool ok = true;
-    int32_t no = p.buffers;
-    for (int32_t c0 = s_begin + p.chunk * p.buffers; c0 < s_end; c0 += p.chunk, ++no) {
+    int32_t no = 0;
+    for (int32_t c0 = s_begin; c0 < s_end; c0 += p.chunk, ++no) {
       const int32_t n_steps = min(p.chunk, s_end - c0), buf = no % p.buffers;
-      ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_empty[buf]), (no / p.buffers - 1) & 1, dead));
+      if (no >= p.buffers) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_empty[buf]), (no / p.buffers - 1) & 1, dead));
       if (!ok) break;
       const uint32_t at = x_at + (uint32_t)buf * p.chunk * rows * 512;
-      for (int32_t i = xw; i < n_steps * (rows >> 3); i += kXWarps) {
-        const int32_t step = i / (rows >> 3);
-        bring(at + step * rows * 512, c0 + step, (i - step * (rows >> 3)) * 8);
+      // [64 channels][row] with 128-byte swizzle, rows behind the last zero; one step of 8 rows to a warp at a time
+      const int32_t groups = rows >> 3;
+      for (int32_t i = xw, step = xw / groups, r8 = xw - step * groups; i < n_steps * groups; i += kXWarps) {
+        const int32_t run = (c0 + step) * 32 + lane;                   // 8 channels, counted from the first of all
+        const bool real = (run >> 2) < p.nb;
+        const uint16_t* src = p.x + (t0 + r8 * 8) * p.ld + (int64_t)run * 8;
+        const uint32_t to = at + step * rows * 512 + (lane >> 3) * rows * 128 + r8 * 1024;
+        uint4 u[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r, src += p.ld) {
+          u[r] = make_uint4(0, 0, 0, 0);
+          if (real && r8 * 8 + r < n_tok) u[r] = __ldg(reinterpret_cast<const uint4*>(src));
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + r * 128 + (((lane ^ r) & 7) << 4)), "r"(prmt(u[r].x, u[r].y, 0x5410u)),
+                       "r"(prmt(u[r].x, u[r].y, 0x7632u)), "r"(prmt(u[r].z, u[r].w, 0x5410u)), "r"(prmt(u[r].z, u[r].w, 0x7632u)) : "memory");
+        for (r8 += kXWarps; r8 >= groups; r8 -= groups) ++step;
       }
-      brought(smem_u32(&bars.x_full[buf]));
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.x_full[buf]));
     }
   }
   __syncwarp();
@@ -350,29 +341,48 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   // ---- the CTAs of the cluster finish a part of the sums each
   if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   const int32_t sums_ld = tiles * 128 + 4, out_rows = quarters * 32;
-  for (int32_t i = split * kThreads + threadIdx.x; i < n_tok * out_rows && whole; i += p.splits * kThreads) {
-    const int32_t tok = i / out_rows, r = i - tok * out_rows;
-    const int64_t n = row_base + r;
-    if (n >= p.N) continue;
-    float v = 0.0f;
+  for (int32_t i = split * kThreads + threadIdx.x; i < n_tok * (out_rows / 4) && whole; i += p.splits * kThreads) {
+    const int32_t tok = i / (out_rows / 4), r = (i - tok * (out_rows / 4)) * 4;        // 4 neighbouring rows of W
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (p.splits > 1) {
       const uint32_t at = smem_u32(sums + tok * sums_ld + r);
 #pragma unroll
       for (int z = 0; z < kMaxSplits; ++z)
         if (z < p.splits) {
-          float u;
-          asm volatile("{\n\t.reg .b32 q;\n\tmapa.shared::cluster.u32 q, %1, %2;\n\tld.shared::cluster.f32 %0, [q];\n\t}" : "=f"(u) : "r"(at), "r"(z));
-          v += u;
+          float4 u;
+          asm volatile("{\n\t.reg .b32 q;\n\tmapa.shared::cluster.u32 q, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [q];\n\t}"
+                       : "=f"(u.x), "=f"(u.y), "=f"(u.z), "=f"(u.w) : "r"(at), "r"(z));
+          v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
         }
     } else {
-      v = sums[tok * sums_ld + r];
+      v = *reinterpret_cast<const float4*>(sums + tok * sums_ld + r);
     }
-    v *= kUnshift;
-    if (p.bias) v += __uint_as_float((uint32_t)__ldg(p.bias + n) << 16);
-    const int64_t at = (t0 + tok) * p.out_ld + n;
-    if (p.out_dtype == 0) static_cast<float*>(p.out)[at] = v;
-    else if (p.out_dtype == 1) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
-    else static_cast<__half*>(p.out)[at] = __float2half_rn(v);
+    const int64_t n = row_base + r, at = (t0 + tok) * p.out_ld + n;
+    float y[4] = {v.x * kUnshift, v.y * kUnshift, v.z * kUnshift, v.w * kUnshift};
+    if (p.bias) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (n + k < p.N) y[k] += __uint_as_float((uint32_t)__ldg(p.bias + n + k) << 16);
+    }
+    if (p.wide_out && n + 4 <= p.N) {
+      if (p.out_dtype == 0) {
+        *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
+      } else if (p.out_dtype == 1) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(y[0], y[1]), hi = __floats2bfloat162_rn(y[2], y[3]);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      } else {
+        const __half2 lo = __floats2half2_rn(y[0], y[1]), hi = __floats2half2_rn(y[2], y[3]);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (n + k >= p.N) break;
+        if (p.out_dtype == 0) static_cast<float*>(p.out)[at + k] = y[k];
+        else if (p.out_dtype == 1) static_cast<__nv_bfloat16*>(p.out)[at + k] = __float2bfloat16_rn(y[k]);
+        else static_cast<__half*>(p.out)[at + k] = __float2half_rn(y[k]);
+      }
+    }
   }
   // nobody's shared memory goes away while another CTA reads it
   if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -414,6 +424,8 @@ cudaError_t fb4_launch_linear_tc(const fb4_ctx* ctx, const void* x, int64_t T, i
   p.N = N;
   p.nb = (int32_t)(K / 32);
   p.out_dtype = out_dtype;
+  const int64_t item_bytes = out_dtype == 0 ? 4 : 2;
+  p.wide_out = reinterpret_cast<uintptr_t>(out) % (4 * item_bytes) == 0 && out_ld % 4 == 0;
   p.tables = ctx->d_tables;
   p.status = ctx->d_status;
   // rows of x in passes of equal size
