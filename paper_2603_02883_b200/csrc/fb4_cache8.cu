@@ -5,10 +5,10 @@
 // [-127, 127].  A power of two and not the maximum over 127: a block that is filled token by token grows its scale a few times, and codes that
 // are halved are off by at most one step of the last scale in all, while factors just above one would add half a step each time.
 //
-// Work: a CTA takes the new tokens of a few blocks of one sequence, over all heads of K, V and Q (or one of `parts` shares of them).  The
-// tokens' cosines and sines go to shared memory once.  A warp takes one block of one head of K or V at a time (or 16 rows of Q): its rows, which
-// were requested while the unit before was rounded and stored, norm and rotation, the maximum over all of it, the codes.  Nobody else writes to
-// a block, so there are no atomics, and the result is the same for every grid.
+// Work: a CTA takes the new tokens of one block of one sequence, over all heads of K, V and Q (or a share of them, where there are few blocks).
+// The tokens' cosines and sines go to shared memory once.  A warp takes the block of one head of K or V at a time (or 16 rows of Q), a few rows in
+// a pass: norm and rotation, the maximum over all of them, the codes; the rows of a pass are requested during the one before.  Nobody else
+// writes to a block, so there are no atomics, and the result is the same for every grid.
 #include "fb4_attend.cuh"
 #include "fb4_rope.cuh"
 
@@ -18,7 +18,6 @@ using namespace fb4rope;
 
 constexpr int kWarps = 4;
 constexpr int kPlaces = 16;                // tokens of a block
-constexpr int kMaxBlocks = 8;              // of a CTA
 constexpr int kSmem = 100 * 1024;          // of a CTA at most
 constexpr int kMinByte = 58, kMaxByte = 185;
 
@@ -35,14 +34,13 @@ struct Append8 {
   const int32_t* q_start;
   int32_t n_seqs, max_q, max_kv;
   int64_t total_q;
-  int32_t blocks;           // blocks to a CTA
   int32_t ctas;             // > 0: CTAs per sequence; 0: the sequence is looked up (see owner)
   uint32_t* status;
 };
 
-// Sequence b owns the CTAs from q_start[b] / (16 blocks) + 2 b on: its blocks, the first of which may hold tokens already, make at most
-// rows / (16 blocks) + 2 groups, so these runs hold them, and together they are not many more than the groups that there are.
-__device__ __forceinline__ int64_t first_cta(const Append8& p, int32_t b) { return __ldg(p.q_start + b) / (16 * p.blocks) + 2 * (int64_t)b; }
+// Sequence b owns the CTAs from q_start[b] / 16 + 2 b on: its blocks, the first of which may hold tokens already, are at most rows / 16 + 2, so
+// these runs hold them, and together they are not many more than the blocks that there are.
+__device__ __forceinline__ int64_t first_cta(const Append8& p, int32_t b) { return __ldg(p.q_start + b) / kPlaces + 2 * (int64_t)b; }
 
 __device__ __forceinline__ int32_t owner(const Append8& p, int64_t cta) {
   const int lane = threadIdx.x & 31;
@@ -114,12 +112,12 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float down) {
 
 __device__ __forceinline__ float two_to(int byte) { return __uint_as_float((uint32_t)byte << 23); }      // 2^(byte - 127), byte >= 1
 
-// What a warp works on at a time: a block of a head of K, V or Q, or, where a group has few tokens, 16 rows of Q of several heads.
+// What a warp works on at a time: the block of a head of K, V or Q, or, where fewer than 16 tokens of it are new, 16 rows of Q of several heads.
 enum Kind { kK, kV, kQ, kFewQ };
 struct Unit {
   int kind;
-  int32_t head, block;
-  int32_t lo, hi;           // rows of the unit that there are: places of the block, or rows lo .. hi of the group's (head-major: row r = head r / tokens)
+  int32_t head;
+  int32_t lo, hi;           // rows of the unit that there are: places of the block, or rows lo .. hi of all (head-major: row r = head r / tokens)
 };
 
 // A lane's 16 values of a pass in shared memory, 512 bytes apart
@@ -144,7 +142,6 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
   constexpr int RP = 32 / LG, NP = kPlaces / RP;      // rows of a pass, passes of a unit
   extern __shared__ __align__(16) float4 smem4[];     // the warps' values, then cosines and sines
   __shared__ __align__(16) uint8_t gain_smem[kGainBytes];
-  __shared__ int64_t page_of[kMaxBlocks];
   const uint32_t gains = fb4blk::smem_u32(gain_smem);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane % LG, g = lane / LG;
   const bool on = j < p.D / 16;
@@ -164,37 +161,29 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
   }
   const fb4att::Sequence sq = fb4att::sequence(p, b, nth == 0 && blockIdx.y == 0 && threadIdx.x == 0);
   const int32_t first = sq.kv - sq.n_q, from = first > 0 ? first : 0;
-  const int64_t base = (((int64_t)(from >> 4) + (int64_t)nth * p.blocks) << 4);      // position of the group's first place
+  const int64_t base = ((int64_t)(from >> 4) + nth) << 4;                 // position of the block's first place
   if (base >= sq.kv || sq.n_q == 0) return;
-  const int32_t lo = base > from ? 0 : from & 15;                         // places lo <= i < hi of the group are new
-  const int32_t hi = sq.kv - base < kPlaces * p.blocks ? (int32_t)(sq.kv - base) : kPlaces * p.blocks, n_new = hi - lo;
+  const int32_t lo = base > from ? 0 : from & 15;                         // places lo <= i < hi of the block are new
+  const int32_t hi = sq.kv - base < kPlaces ? (int32_t)(sq.kv - base) : kPlaces, n_new = hi - lo;
   const int64_t row0 = sq.q0 + (base - first);                            // row of place 0 (which may be no row of the call)
   bool bad = false;
 
   // ---- the units of this warp
-  const int32_t H = p.cache.n_heads, blocks = (hi + kPlaces - 1) / kPlaces, q_rows = n_new * p.q.n;
+  const int32_t H = p.cache.n_heads, q_rows = n_new * p.q.n;
   const bool few = n_new < kPlaces;
-  const int32_t heads = 2 * H + (few ? 0 : p.q.n), by_block = blocks * heads;
-  const int32_t units = by_block + (few ? (q_rows + kPlaces - 1) / kPlaces : 0), step = gridDim.y * kWarps;
-  // The units in order: (block, head) moved on without divisions.
-  int32_t next_block = 0, next_head = 0, at = blockIdx.y * kWarps + warp;
-  auto advance = [&](int32_t by) {
-    next_head += by;
-    while (next_head >= heads) {
-      next_head -= heads;
-      ++next_block;
-    }
-  };
+  const int32_t heads = 2 * H + (few ? 0 : p.q.n);
+  const int32_t units = heads + (few ? (q_rows + kPlaces - 1) / kPlaces : 0), step = gridDim.y * kWarps;
+  int32_t at = blockIdx.y * kWarps + warp;
   auto unit_at = [&](int32_t u) -> Unit {             // u in [0, units)
-    if (u >= by_block) return Unit{kFewQ, 0, 0, (u - by_block) * kPlaces, q_rows};
-    const int kind = next_head < H ? kK : next_head < 2 * H ? kV : kQ;
-    return Unit{kind, next_head - kind * H, next_block, max(lo - kPlaces * next_block, 0), min(hi - kPlaces * next_block, kPlaces)};
+    if (u >= heads) return Unit{kFewQ, 0, (u - heads) * kPlaces, q_rows};
+    const int kind = u < H ? kK : u < 2 * H ? kV : kQ;
+    return Unit{kind, u - kind * H, lo, hi};
   };
-  // Is there a row for this lane in pass n?  kFewQ: also its place in the group and its head.
+  // Is there a row for this lane in pass n?  Also its place in the block, and for kFewQ its head.
   auto row_of = [&](const Unit& u, int n, int32_t& place, int32_t& head) -> bool {
     const int32_t i = n * RP + g;
     if (u.kind != kFewQ) {
-      place = u.block * kPlaces + i;
+      place = i;
       return on && i >= u.lo && i < u.hi;
     }
     const bool real = on && u.lo + i < u.hi;
@@ -209,7 +198,7 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
   int64_t src_step = 0;
   auto begin = [&](const Unit& u) {
     const Heads& hd = u.kind == kK ? p.k : u.kind == kV ? p.v : p.q;
-    src = hd.x + (row0 + u.block * kPlaces + g) * hd.ld + (int64_t)u.head * p.D + 8 * j;
+    src = hd.x + (row0 + g) * hd.ld + (int64_t)u.head * p.D + 8 * j;
     src_step = RP * hd.ld;
   };
   auto fetch = [&](const Unit& u, int n) {
@@ -222,7 +211,6 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
     }
     src += src_step;
   };
-  advance(at);
   Unit u{};
   if (at < units) {
     u = unit_at(at);
@@ -231,11 +219,10 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
   }
 
   stage_gains<LG, INTER>(p, gains);
-  if (threadIdx.x < p.blocks && threadIdx.x * kPlaces < hi) {
-    const int64_t page = __ldg(p.page_table + (int64_t)b * p.max_pages + ((base + threadIdx.x * kPlaces) >> p.page_shift));
-    const bool there = page >= 0 && page < p.cache.n_pages;
-    if (!there) bad = true;
-    page_of[threadIdx.x] = there ? page : -1;
+  int64_t page = __ldg(p.page_table + (int64_t)b * p.max_pages + (base >> p.page_shift));
+  if (page < 0 || page >= p.cache.n_pages) {
+    bad = true;
+    page = -1;
   }
   if (p.rope.table) {
 #pragma unroll 4
@@ -269,13 +256,10 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
   for (int n = 0; n < 4; ++n) cs_at[n] = fb4blk::smem_u32(cs_smem) + cs_piece(INTER ? 2 * (on ? j : 0) + (n & 1) + (n < 2 ? 0 : p.D / 8) : 4 * (on ? j : 0) + n) * 16;
   for (; at < units; at += step) {
     uint16_t* out = nullptr;
-    if (u.kind == kQ) out = p.q.out + (row0 + u.block * kPlaces + g) * p.q.out_ld + (int64_t)u.head * p.D + 8 * j;
+    if (u.kind == kQ) out = p.q.out + (row0 + g) * p.q.out_ld + (int64_t)u.head * p.D + 8 * j;
     const bool more = at + step < units;
     Unit next = u;
-    if (more) {
-      advance(step);
-      next = unit_at(at + step);
-    }
+    if (more) next = unit_at(at + step);
     float top = 0.0f;
     // One pass at a time, not unrolled: the instructions of three kinds of units would not stay in the instruction cache.  The values of K
     // and V wait in shared memory for the block's maximum.
@@ -322,12 +306,10 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
     }
     const Unit now = u;
     u = next;
-    if (now.kind >= kQ) continue;
-    // -------------------------------------------------- a block of a head of K or V: its scale and its codes
-    const int64_t page = page_of[now.block];
-    if (page < 0) continue;
+    if (now.kind >= kQ || page < 0) continue;
+    // -------------------------------------------------- the block of a head of K or V: its scale and its codes
     const int64_t cell = (page * H + now.head) << p.page_shift;                                // the head's tokens in the page
-    const int32_t in_page = (int32_t)((base + now.block * kPlaces) & ((1 << p.page_shift) - 1));
+    const int32_t in_page = (int32_t)(base & ((1 << p.page_shift) - 1));
     uint8_t* codes = (now.kind == kV ? p.cache.v : p.cache.k) + (cell + in_page) * p.D;
     uint8_t* scale = (now.kind == kV ? p.cache.v_scale : p.cache.k_scale) + ((cell + in_page) >> 4);
     const int held = now.lo > 0 ? min(max((int)*scale, kMinByte), kMaxByte) : kMinByte;
@@ -453,17 +435,16 @@ cudaError_t fb4_launch_cache8_append(const fb4_ctx* ctx, const fb4_cache8* cache
   p.status = ctx->d_status;
   const int lg = lanes_of(p.D), rows = kWarps * (kPlaces * lg / 32) * 2048, per_block = kPlaces * p.D * 4;
   const int64_t slots = (int64_t)ctx->sm_count * (lg == 16 ? 2 : 5);
-  p.blocks = 1;
   // CTAs by sequence where they are not more than by rows
-  const int64_t wide = kPlaces * p.blocks, by_seq = ((int64_t)max_q + 15 + wide - 1) / wide, by_rows = T / wide + 2 * (int64_t)n_seqs;
+  const int64_t by_seq = ((int64_t)max_q + 2 * kPlaces - 2) / kPlaces, by_rows = T / kPlaces + 2 * (int64_t)n_seqs;
   p.ctas = by_seq * n_seqs <= by_rows ? (int32_t)by_seq : 0;
   const int64_t grid = p.ctas ? by_seq * n_seqs : by_rows;
   // few blocks: their heads are shared out until every warp has one unit
   const int64_t units = 2 * cache->n_heads + q_heads, most = (units + kWarps - 1) / kWarps;
-  int64_t parts = p.blocks > 1 ? 1 : (slots + grid - 1) / grid;
+  int64_t parts = (slots + grid - 1) / grid;
   if (parts > most) parts = most;
   const dim3 dims((unsigned)grid, (unsigned)parts);
-  const size_t smem = (size_t)rows + (rope ? p.blocks * per_block : 0);
+  const size_t smem = (size_t)rows + (rope ? per_block : 0);
   const bool inter = rope && rope->interleaved;
 #define FB4_APPEND8(LG) \
   inter ? fb4_cache8_append_kernel<LG, true><<<dims, kWarps * 32, smem, stream>>>(p) \
