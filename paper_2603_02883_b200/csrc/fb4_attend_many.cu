@@ -439,10 +439,6 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         for (int k = 0; k < kTasks; ++k)
           asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cw[k][0]), "=r"(cw[k][1]), "=r"(cw[k][2]), "=r"(cw[k][3]) : "r"(codes + row * D + (k ^ mix) * 16));
         const Int8Scale sc = int8_scale(is_v ? v_byte : k_byte, true);          // whatever a slot that no token fills holds is finite
-        // reads through the ordinary path are over before the next copy, which takes another path, may overwrite what they read
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars.ring_empty[st]));
         if (t >= 2) ok = __all_sync(0xffffffffu, wait(smem_u32(is_v ? &bars.v_empty[buf] : &bars.k_empty[buf]), ((t >> 1) - 1) & 1, dead));
         if (!ok) break;
 #pragma unroll
@@ -475,8 +471,6 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
         const bool use = !is_v || (j0 + row_of(k) < sq.kv && ((here >> (row_of(k) >> 4)) & 1u));
         sc[k] = block_scale(use ? mt[k] : 0u, book_at, use);
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars.ring_empty[st]));
       if (t >= 2) ok = __all_sync(0xffffffffu, wait(smem_u32(is_v ? &bars.v_empty[buf] : &bars.k_empty[buf]), ((t >> 1) - 1) & 1, dead));
       if (!ok) break;
 #pragma unroll
@@ -488,9 +482,14 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_attend_many_kernel(const __gr
           asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + swizzled(row_of(k), 4 * block_of(k) + q)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
         }
       }
+      // The fence stands between what has been written and the tensor core's reads, and between what has been read and the next copy, which
+      // takes another path than the reads
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(is_v ? &bars.v_full[buf] : &bars.k_full[buf]));
+      if (lane == 0) {
+        mbar_arrive(smem_u32(is_v ? &bars.v_full[buf] : &bars.k_full[buf]));
+        mbar_arrive(smem_u32(&bars.ring_empty[st]));
+      }
     }
   } else {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
