@@ -345,50 +345,57 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
   if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, 2u);
 }
 
-// ---- decode: 8 codes per thread and step, K then V
-__global__ void __launch_bounds__(256) fb4_cache8_values_kernel(const uint8_t* __restrict__ k, const uint8_t* __restrict__ k_scale, const uint8_t* __restrict__ v,
-                                                                const uint8_t* __restrict__ v_scale, void* __restrict__ k_out, void* __restrict__ v_out,
-                                                                int64_t pieces, int32_t per_block, int out_dtype) {
+// ---- decode: 8 codes per thread and step, K then V.  A CTA takes whole blocks, as many as 1024 pieces of 8 codes hold, so that a piece's block is
+// found without a division.  A code in the last byte of 2^23 is the number 2^23 + code, and one fused multiply-add takes it to
+// (code - 128) 2^e, exactly; in bfloat16 that is the upper half of it (8 bits are enough for every code).
+constexpr int kValuesThreads = 256, kValuesSteps = 4;
+
+template <int DTYPE>
+__global__ void __launch_bounds__(kValuesThreads) fb4_cache8_values_kernel(const uint8_t* __restrict__ k, const uint8_t* __restrict__ k_scale,
+                                                                           const uint8_t* __restrict__ v, const uint8_t* __restrict__ v_scale,
+                                                                           void* __restrict__ k_out, void* __restrict__ v_out, int64_t blocks,
+                                                                           int32_t per_block, int32_t at_once, uint32_t inverse) {
   const bool is_v = blockIdx.y != 0;
-  const uint2* src = reinterpret_cast<const uint2*>(is_v ? v : k);
-  const uint8_t* scale = is_v ? v_scale : k_scale;
+  const int64_t block0 = (int64_t)blockIdx.x * at_once;
+  const int32_t pieces = (int32_t)(blocks - block0 < at_once ? blocks - block0 : at_once) * per_block;
+  const uint2* src = reinterpret_cast<const uint2*>(is_v ? v : k) + block0 * per_block;
+  const uint8_t* scale = (is_v ? v_scale : k_scale) + block0;
   void* out = is_v ? v_out : k_out;
-  constexpr int kStep = 4;                 // pieces of a thread, 256 apart
-  const int64_t p0 = (int64_t)blockIdx.x * (256 * kStep) + threadIdx.x;
-  uint2 c[kStep];
-  int s[kStep];
+  uint2 c[kValuesSteps];
+  int s[kValuesSteps];
 #pragma unroll
-  for (int n = 0; n < kStep; ++n) {
-    const int64_t at = p0 + n * 256;
+  for (int n = 0; n < kValuesSteps; ++n) {
+    const int32_t at = threadIdx.x + n * kValuesThreads;
     if (at < pieces) {
-      c[n] = __ldg(src + at);
-      s[n] = __ldg(scale + at / per_block);
+      c[n] = __ldcs(src + at);
+      s[n] = __ldg(scale + __umulhi((uint32_t)at, inverse));
     }
   }
 #pragma unroll
-  for (int n = 0; n < kStep; ++n) {
-    const int64_t at = p0 + n * 256;
+  for (int n = 0; n < kValuesSteps; ++n) {
+    const int32_t at = threadIdx.x + n * kValuesThreads;
     if (at >= pieces) continue;
-    const float f = two_to(min(max(s[n], kMinByte), kMaxByte));
+    const float f = two_to(min(max(s[n], kMinByte), kMaxByte)), offset = -(0x1p23f + 128.0f) * f;
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = ((float)((i < 4 ? c[n].x : c[n].y) >> (8 * (i & 3)) & 255u) - 128.0f) * f;
-    if (out_dtype == 0) {
-      float4* o = static_cast<float4*>(out) + 2 * at;
+    for (int i = 0; i < 8; ++i) x[i] = fmaf(__uint_as_float(__byte_perm(i < 4 ? c[n].x : c[n].y, 0x4b000000u, 0x7650 + (i & 3))), f, offset);
+    const int64_t to = block0 * per_block + at;
+    if (DTYPE == 0) {
+      float4* o = static_cast<float4*>(out) + 2 * to;
       o[0] = make_float4(x[0], x[1], x[2], x[3]);
       o[1] = make_float4(x[4], x[5], x[6], x[7]);
     } else {
       uint32_t w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (out_dtype == 1) {
-          w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+        if (DTYPE == 1) {
+          w[i] = __byte_perm(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), 0x7632);
         } else {
           const __half2 y = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
           w[i] = *reinterpret_cast<const uint32_t*>(&y);
         }
       }
-      static_cast<uint4*>(out)[at] = make_uint4(w[0], w[1], w[2], w[3]);
+      static_cast<uint4*>(out)[to] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
@@ -460,8 +467,15 @@ cudaError_t fb4_launch_cache8_append(const fb4_ctx* ctx, const fb4_cache8* cache
 }
 
 cudaError_t fb4_launch_cache8_values(const fb4_cache8* cache, void* k_out, void* v_out, int out_dtype, cudaStream_t stream) {
-  const int64_t pieces = cache->n_pages * cache->n_heads * cache->page_tokens * (cache->head_dim / 8);
-  const dim3 grid((unsigned)((pieces + 1023) / 1024), 2);
-  fb4_cache8_values_kernel<<<grid, 256, 0, stream>>>(cache->k, cache->k_scale, cache->v, cache->v_scale, k_out, v_out, pieces, 2 * cache->head_dim, out_dtype);
+  const int64_t blocks = cache->n_pages * cache->n_heads * (cache->page_tokens / kPlaces);
+  const int32_t per_block = 2 * cache->head_dim, at_once = kValuesThreads * kValuesSteps / per_block;       // 64 to 512 pieces to a block
+  const dim3 grid((unsigned)((blocks + at_once - 1) / at_once), 2);
+  const uint32_t inverse = (uint32_t)(0x100000000ull / per_block) + 1;         // its product's upper half is the quotient, up to 2^16
+#define FB4_VALUES8(DTYPE) \
+  fb4_cache8_values_kernel<DTYPE><<<grid, kValuesThreads, 0, stream>>>(cache->k, cache->k_scale, cache->v, cache->v_scale, k_out, v_out, blocks, per_block, at_once, inverse)
+  if (out_dtype == 0) FB4_VALUES8(0);
+  else if (out_dtype == 1) FB4_VALUES8(1);
+  else FB4_VALUES8(2);
+#undef FB4_VALUES8
   return cudaGetLastError();
 }
