@@ -35,9 +35,9 @@
  *     different contexts may run concurrently.
  *   - Device code has no unbounded wait loops: waits for asynchronous loads into shared memory and between the
  *     warps of a CTA give up after a fixed number of tries and raise a status bit (fb4_device_status).
- *     fb4_cache_attention also waits in hardware, where no limit can be set: for the other CTAs of a cluster
- *     (scheduled together), for tensor memory (until kernels on the same SM that hold it have ended) and, in
- *     its second launch, for the end of its first.
+ *     fb4_cache_attention, fb4_cache8_attention, fb4_linear and fb4_cache_plan also wait in hardware, where no limit can
+ *     be set: for the other CTAs of a cluster (scheduled together), the first three for tensor memory (until kernels on
+ *     the same SM that hold it have ended) and, in their second launch, all but fb4_linear for the end of the first.
  *
  * Output layout
  *   codes : uint8 [T][C/2].  Byte j of a row holds element 2j in its low nibble
@@ -337,7 +337,7 @@ int fb4_quantize_weights(fb4_ctx* ctx, const void* w_bf16, int64_t N, int64_t K,
  * Products of rows of x with FB4 weights (App. D.2: 4-bit codes are decoded on the fly with the block scale applied):
  *     out[t][n] = sum_k x[t][k] * w[n][k] + bias[n],   w = value(codes, meta) of fb4_quantize_weights (or fb4_quantize)
  * without the weights ever being written out: 4.5 bits of memory traffic per weight.  Made for few rows (single and drafted tokens of a decoding
- * batch); any number is taken, and every 64 rows read the weights again.  Products are exact, sums float32 in an order that depends on
+ * batch); any number is taken, and every 96 rows read the weights again.  Products are exact, sums float32 in an order that depends on
  * the sizes alone, the result is rounded once to the type of out.  A row of x that holds an infinity or NaN affects its own row of out only.
  *   x       : device bfloat16 [T][ld_elems], T at most 2^22, 16-byte aligned, ld_elems a multiple of 8 (>= K)
  *   codes, meta : device [N][K/2], [N][K/32], 16-byte aligned; K a multiple of 32, at least 32.  An element scale above 2^61 is read as

@@ -12,6 +12,14 @@
 //            took 34 us where this takes 25)
 //   product  one warp issues D_tile += A x
 //   x        6 warps bring x into shared memory, in chunks where it is too large for it
+//
+// Bound: for large weights the decode (12288 x 12288, 16 rows, of 64 000 cycles: 45 000; the ALU pipe is busy 57 % and the issue slots 61 % of the
+// time), then start and end (11 000 until x and the first codes are there, 10 000 from the last decoded value to the last result: the last
+// products, the cluster's slowest CTA, the join).  For small ones the latter alone.  16 rows with 24576 x 12288 weights take 57 us (3.0 TB/s), 12288 x 12288
+// takes 30.7 for one row, 36.5 for 32, 43 for 64 (450 TFLOP/s), 6152 x 1568 12.4 for 61.
+// On the way (12288 x 12288): A through shared memory 61 us for 32 rows, against 49 with a row to a thread in tensor memory; x brought in by 4 warps 89 for 64
+// rows; 4 buffers of A, one a group, 36.9 for one row.  Leaving out the decode gives 28.9 for one row, the metadata's loads too 26.1, the stores to tensor
+// memory 25.3, the products 21.5: copies, start and end alone.  First copies before the set-up: 32.9.
 #include "fb4_attend.cuh"
 #include "fb4_staging.cuh"
 #include "fb4_tcgen05.cuh"
@@ -239,7 +247,8 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   } else if (warp == kLoadWarp) {
     // =========================================================== load
     bool ok = true;
-    for (Cursor c(s_begin, s_end, p.chunk); c.item < items && ok; c.advance(1, tiles, p.chunk, s_end)) {
+    Cursor c(s_begin, s_end, p.chunk);
+    for (; c.item < items; c.advance(1, tiles, p.chunk, s_end)) {
       const int st = c.item % kStages;
       if (c.item >= kStages) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.ring_empty[st]), (c.item / kStages - 1) & 1, dead));
       if (!ok) break;
@@ -252,7 +261,10 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
       __syncwarp();
     }
     // every copy has to have landed before the CTA ends
-    for (int32_t i = items > kStages ? items - kStages : 0; i < items && !*dead; ++i) wait(smem_u32(&bars.ring_full[i % kStages]), (i / kStages) & 1, dead);
+    for (int32_t i = c.item > kStages ? c.item - kStages : 0; i < c.item; ++i) {
+      uint32_t tries = 0;
+      while (!mbar_try_wait(smem_u32(&bars.ring_full[i % kStages]), (i / kStages) & 1) && ++tries < kSpinLimit) {}
+    }
   } else if (warp == kProductWarp) {
     // =========================================================== product: every lane waits, one issues
     const uint32_t idesc = instr_desc(rows, false), x_low = desc_low(x_at, 16), x_buffer = (uint32_t)p.chunk * rows * 512;
