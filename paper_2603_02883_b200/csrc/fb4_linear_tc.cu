@@ -202,18 +202,15 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
         };
         if (there) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t o[32];
+          for (int h = 0; h < 4; ++h) {
+            uint32_t o[16];
+            const uint32_t m = meta[2 * half + (h >> 1)];
+            const BlockScale sc = block_scale((h & 1) ? m >> 16 : m & 0xffffu, book_at, true);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t m = meta[2 * half + h];
-              const BlockScale sc = block_scale(i ? m >> 16 : m & 0xffffu, book_at, true);
-#pragma unroll
-              for (int q = 0; q < 4; ++q) decode_word(w[4 * half + 2 * h + i][q], sc, *reinterpret_cast<uint32_t(*)[4]>(o + 16 * i + 4 * q));
-            }
+            for (int q = 0; q < 4; ++q) decode_word(w[4 * half + h][q], sc, *reinterpret_cast<uint32_t(*)[4]>(o + 4 * q));
             buffer_free();
             if (!ok) break;
-            tmem_st32(tmem + buf * kACols + lanes + 32 * h, o);
+            tmem_st16(tmem + buf * kACols + lanes + 16 * h, o);
           }
           tmem_wait_st();
         } else {
