@@ -264,41 +264,46 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
     }
   } else if (warp == kProductWarp) {
     // =========================================================== product: every lane waits, one issues
-    const uint32_t idesc = instr_desc(rows, false), x_low = desc_low(x_at, 16), x_buffer = (uint32_t)p.chunk * rows * 512;
+    const uint32_t idesc = instr_desc(rows, false), x_low = desc_low(x_at, 16), x_half = rows * 16, a_end = tmem + n_a * kACols;
+    const uint32_t full0 = smem_u32(&bars.a_full[0]), empty0 = smem_u32(&bars.a_empty[0][0]);
     bool ok = true;
-    int32_t chunk_no = -1;
-    int turn_buf = 0;                        // buffer of A, and how often it has been used, mod 2
-    uint32_t turn_lap = 0;
-    for (Cursor c(s_begin, s_end, p.chunk); c.item < items && ok;) {
-      const int32_t tile = c.tile, s = c.s, c0 = c.c0;
-      const int xb = c.chunk_no & (p.buffers - 1);
-      if (c.chunk_no != chunk_no) {
-        chunk_no = c.chunk_no;
-        ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_full[xb]), (chunk_no / p.buffers) & 1, dead));
-      }
-      c.advance(1, tiles, p.chunk, s_end);
-      const bool end = c.item >= items, chunk_end = end || c.chunk_no != chunk_no;
-      const uint32_t d = d_col + tile * rows;
-      uint32_t b = x_low + ((xb * x_buffer + (uint32_t)(s - c0) * rows * 512) >> 4);
+    uint32_t a = tmem, full = full0, empty = empty0, lap = 0;      // buffer of A, its barriers, and how often it has been used, mod 2
+    int32_t chunk_no = 0;
+    for (int32_t c0 = s_begin; c0 < s_end && ok; ++chunk_no) {
+      const int32_t c1 = min(c0 + p.chunk, s_end);
+      const int xb = chunk_no & (p.buffers - 1);
+      ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.x_full[xb]), (chunk_no / p.buffers) & 1, dead));
+      const uint32_t b0 = x_low + ((xb * (uint32_t)p.chunk * rows * 512) >> 4);
+      uint32_t d = d_col;
+      for (int32_t tile = 0; tile < tiles && ok; ++tile, d += rows) {
+        uint32_t b = b0;
+        for (int32_t half = 2 * c0; half < 2 * c1; ++half, b += x_half) {
+          ok = __all_sync(0xffffffffu, wait(full, lap, dead));
+          if (!ok) break;
+          fence_after();
+          if (elected()) {
+            mma_ts(d, a, b, idesc, half > 2 * s_begin);
 #pragma unroll
-      for (int half = 0; half < 2; ++half, b += rows * 16) {
-        if (ok) ok = __all_sync(0xffffffffu, wait(smem_u32(&bars.a_full[turn_buf]), turn_lap, dead));
-        if (!ok) break;
-        fence_after();
-        if (elected()) {
-          const uint32_t a = tmem + turn_buf * kACols;
+            for (int k = 1; k < 4; ++k) mma_ts(d, a + 8 * k, b + 2 * k, idesc, true);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) mma_ts(d, a + 8 * k, b + (k >> 2) * rows * 8 + (k & 3) * 2, idesc, k > 0 || half > 0 || s > s_begin);
-          commit(smem_u32(&bars.a_empty[turn_lap][turn_buf]));
-          if (half && chunk_end) commit(smem_u32(&bars.x_empty[xb]));
-          if (half && end) commit(smem_u32(&bars.d_full));
-        }
-        __syncwarp();
-        if (++turn_buf == n_a) {
-          turn_buf = 0;
-          turn_lap ^= 1u;
+            for (int k = 4; k < 8; ++k) mma_ts(d, a + 8 * k, b + (x_half >> 1) + 2 * k - 8, idesc, true);
+            commit(empty);
+          }
+          __syncwarp();
+          a += kACols;
+          full += 8;
+          empty += 8;
+          if (a == a_end) {
+            a = tmem;
+            lap ^= 1u;
+            full = full0;
+            empty = empty0 + lap * (kMaxA * 8);
+          }
         }
       }
+      c0 = c1;
+      if (ok && elected()) commit(smem_u32(c0 < s_end ? &bars.x_empty[xb] : &bars.d_full));
+      __syncwarp();
     }
     // nothing of this CTA may be on the tensor core when its tensor memory is given back
     if (elected()) commit(smem_u32(&bars.drained));
