@@ -1,4 +1,4 @@
-// Attention of few query rows per cache head (single tokens, drafted tokens, small groups) over the paged FB4 cache.
+// Attention of few query rows per cache head (single tokens, drafted tokens, small groups) over the paged caches, FB4 and 8-bit.
 //
 // Work: a CTA of 4 warps takes one sequence, one cache head, up to 8 * NT query rows (query-major: row r = query r / group,
 // head r mod group) and one run of the cached tokens (a "split"); its warps take that run's tiles of 32 tokens in turn.  Each warp
@@ -17,6 +17,10 @@
 // decode and the products), 60 % of the issue slots and of the ALU pipe's.  75600 tokens of 12 heads take 51 us, 2.55 TB/s of the cache's
 // 4.5 bits per value, 39 % of the copy bandwidth.  More warps at fewer registers (20 or 24 instead of 16 per SM) came out slower, and so
 // did the same work on tcgen05 (K decoded into tensor memory, V into a swizzled tile, roles by warp: 61 us).
+//
+// Over 8 bits a tile's codes are twice as many bytes and their decode is 8 instructions per 8 values instead of 14, without metadata in the ring (a tile has two
+// scale bytes for each of K and V): 75600 tokens of 12 heads take 48 us, 4.8 TB/s, 64 sequences of 131 to 8191 tokens 101 us, 5.4 TB/s (74 and 83 % of the copy
+// bandwidth; issue 44 to 49 %, 12 warps an SM at 156 registers).
 #include "fb4_attend.cuh"
 #include "fb4_block.cuh"
 

@@ -1,4 +1,4 @@
-// Attention of many query rows per cache head (prompts in chunks, frames, large groups) over the paged FB4 cache, on the
+// Attention of many query rows per cache head (prompts in chunks, frames, large groups) over the paged caches, FB4 and 8-bit, on the
 // fifth-generation tensor cores.
 //
 // Work: a CTA takes one sequence, one cache head, up to 256 query rows (two tiles of 128; row r = query r / group, head
@@ -30,6 +30,10 @@
 // every lane of a half-warp, which ends the bank conflicts (349 / 133); the first tile's Q in TMEM and P in half the columns
 // (388 / 141); two threads to a row (16 softmax warps: 507 / 171); a polynomial in place of the special function for a part of
 // the columns (2.2 to 2.9 us per tile).
+//
+// Over 8 bits the decode is cheaper (a thread takes a token's row, its scale bytes straight from memory a tile ahead) and the same frame takes 313 us, 1005
+// TFLOP/s, 62 % of the product rate; heads of 64 are bound by exponentials and the chain of a tile (four causal prompts of up to 1024 tokens, 16 heads over 4, 61
+// us, 388 TFLOP/s; the longest CTA's 32 tiles are 54 of them).  A ring stage of 128 channels holds 16 KB, so there is room for two.
 #include "fb4_attend.cuh"
 #include "fb4_staging.cuh"
 #include "fb4_tcgen05.cuh"
