@@ -52,12 +52,12 @@ __global__ void __launch_bounds__(kWarps * 32, kResident) fb4_linear_kernel(cons
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t book[64];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int32_t split = (int32_t)(blockIdx.x % p.splits);
-  const int64_t tile = blockIdx.x / p.splits;
+  const int64_t tile = blockIdx.x / (uint32_t)p.splits;
+  const int32_t split = (int32_t)(blockIdx.x - (uint32_t)tile * p.splits);
   const int64_t n0 = tile * kRows + warp * 16;
   const int32_t n_tok = (int32_t)p.T;
   const int32_t steps = (p.nb + 3) / 4;
-  const int32_t s_begin = (int32_t)((int64_t)steps * split / p.splits), s_end = (int32_t)((int64_t)steps * (split + 1) / p.splits);
+  const int32_t s_begin = steps * split / p.splits, s_end = steps * (split + 1) / p.splits;      // 2^24 steps, 8 CTAs at most
   const uint32_t x_at = fb4blk::smem_u32(smem), book_at = fb4blk::smem_u32(book);
   if (threadIdx.x < 64) fill_book(book, p.tables, threadIdx.x);
 

@@ -38,7 +38,7 @@ using fb4stage::tma_load_2d;
 constexpr int kGroups = 4, kDecodeWarps = 4 * kGroups, kLoadWarp = kDecodeWarps, kProductWarp = kLoadWarp + 1, kXWarp = kProductWarp + 1, kXWarps = 6;
 constexpr int kThreads = (kXWarp + kXWarps) * 32;
 constexpr int kStages = 7, kQuarter = 32 * 128, kStage = 4 * kQuarter;     // bytes of 32 and of 128 rows' codes of an item
-constexpr int kXBytes = 96 * 1024;
+constexpr int kXBytes = 96 * 1024;                                       // of x, and the stages that a CTA of few items does not need
 constexpr int kBytes = 1024 + kStages * kStage + kXBytes;
 constexpr int kACols = 64, kMaxA = 7, kDCols = 512 - 4 * kACols;          // tensor memory: buffers for A, as many as D leaves, and D at its end
 constexpr int kMaxRows = 96, kMaxSplits = 8;
@@ -56,6 +56,7 @@ struct Linear {
   int32_t rows;             // rows of x at a time, a multiple of 16
   int32_t splits;           // CTAs of a cluster
   int32_t quarters;         // quarters of a tile to a cluster
+  int32_t stages;           // of the ring: kStages, or as many as there are items, which then do not come round
   int32_t chunk, buffers;   // steps of 256 channels whose x is held at a time, and how often
   int32_t out_dtype;
   int32_t wide_out;         // 4 neighbouring results are stored at once
@@ -107,19 +108,19 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   __shared__ Bars bars;
   __shared__ uint32_t book[64];
   __shared__ uint32_t tmem_at, dead_flag;
-  const uint32_t base_smem = (smem_u32(smem_raw) + 1023u) & ~1023u, ring_at = base_smem, x_at = base_smem + kStages * kStage;
+  const uint32_t base_smem = (smem_u32(smem_raw) + 1023u) & ~1023u, ring_at = base_smem, x_at = base_smem + p.stages * kStage;
   float* sums = reinterpret_cast<float*>(smem_raw + (base_smem - smem_u32(smem_raw)));
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   volatile uint32_t* dead = &dead_flag;
 
   // ---- which work
-  const int32_t split = (int32_t)(blockIdx.x % p.splits), rows = p.rows;
-  const int64_t row_base = (int64_t)(blockIdx.x / p.splits) * p.quarters * 32, t0 = (int64_t)blockIdx.y * rows;
+  const int32_t cluster = (int32_t)(blockIdx.x / (uint32_t)p.splits), split = (int32_t)blockIdx.x - cluster * p.splits, rows = p.rows;
+  const int64_t row_base = (int64_t)cluster * p.quarters * 32, t0 = (int64_t)blockIdx.y * rows;
   const int32_t n_tok = (int32_t)(p.T - t0 < rows ? p.T - t0 : rows);
-  const int64_t left = (p.N - row_base + 31) / 32;
+  const int64_t left = (p.N - row_base + 31) >> 5;
   const int32_t quarters = (int32_t)(left < p.quarters ? left : p.quarters), tiles = (quarters + 3) / 4;
   const int32_t steps = (p.nb + 7) / 8;
-  const int32_t s_begin = (int32_t)((int64_t)steps * split / p.splits), s_end = (int32_t)((int64_t)steps * (split + 1) / p.splits);
+  const int32_t s_begin = steps * split / p.splits, s_end = steps * (split + 1) / p.splits;      // 2^23 steps, 8 CTAs at most
   const int32_t items = (s_end - s_begin) * tiles;
 
   // ---- set-up
@@ -464,8 +465,11 @@ cudaError_t fb4_launch_linear_tc(const fb4_ctx* ctx, const void* x, int64_t T, i
     }
   }
   const int32_t mine = (steps + p.splits - 1) / p.splits, step_bytes = p.rows * 512;
-  p.buffers = mine * step_bytes <= kXBytes ? 1 : 2;
-  p.chunk = p.buffers == 1 ? mine : kXBytes / 2 / step_bytes;
+  const int32_t tiles = (p.quarters + 3) / 4;
+  p.stages = (int64_t)mine * tiles < kStages ? mine * tiles : kStages;
+  const int32_t x_bytes = kXBytes + (kStages - p.stages) * kStage;
+  p.buffers = (int64_t)mine * step_bytes <= x_bytes ? 1 : 2;
+  p.chunk = p.buffers == 1 ? mine : x_bytes / 2 / step_bytes;
   CUtensorMap map;
   cudaError_t e = fb4_encode_map_2d(&map, codes, (uint64_t)K / 2, (uint64_t)N, (uint64_t)K / 2, 128, 32, CU_TENSOR_MAP_SWIZZLE_128B);
   if (e != cudaSuccess) return e;
