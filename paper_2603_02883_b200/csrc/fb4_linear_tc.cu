@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
   // ---- the CTAs of the cluster finish a part of the sums each
   if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   const int32_t sums_ld = tiles * 128 + 4, out_rows = quarters * 32;
-  for (int32_t i = split * kThreads + threadIdx.x; i < n_tok * (out_rows / 4) && whole; i += p.splits * kThreads) {
+  for (int32_t i = (warp * p.splits + split) * 32 + lane; i < n_tok * (out_rows / 4) && whole; i += p.splits * kThreads) {       // a warp of each CTA in turn
     const int32_t tok = i / (out_rows / 4), r = (i - tok * (out_rows / 4)) * 4;        // 4 neighbouring rows of W
     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (p.splits > 1) {
