@@ -9,7 +9,7 @@
 // distributed shared memory, always in the same order.
 //
 // Bound: the ALU pipe (decode: 10 operations per 8 weights, two thirds of all of its) while all warps are at work, CTAs that are two or three to
-// an SM, and for small weights the start.  One row with 4096 x 4096 weights takes 6.0 us, 8192 x 8192 16.0 (2.4 TB/s), 12288 x 12288 31.1 (2.7 TB/s, and
+// an SM, and for small weights the start.  One row with 4096 x 4096 weights takes 5.8 us, 8192 x 8192 16.3 (2.4 TB/s), 12288 x 12288 31.1 (2.7 TB/s, and
 // 28.5 out of L2).  For the last, one CTA per SM with its rows dealt out evenly came out slower (39.6), and so did clusters of three
 // (41.7: they are not spread evenly) and 16 warps an SM with loads four steps ahead (49.8 in two waves).
 #include "fb4_attend.cuh"
@@ -207,8 +207,8 @@ cudaError_t fb4_linear_prepare_device(int32_t* slots) {
 cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
                               int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream) {
   // The tensor-memory kernel starts 3 us later, but takes less for a weight, and next to nothing for another row.  This against that one, us:
-  // 4096 x 4096 weights 6.0 / 9.0 (1 row), 7.1 / 9.4 (8 rows); 16384 x 4096 16.3 / 17.3 (1), 17.6 / 17.3 (4), 19.2 / 17.4 (8); 8192 x 12288 22.4 / 23.8 (1),
-  // 24.1 / 24.0 (4), 26.0 / 24.4 (8); 32768 x 4096 30.5 / 28.1 (1), 36.6 / 28.6 (8).
+  // 4096 x 4096 weights 5.8 / 8.6 (1 row), 7.2 / 8.9 (8 rows); 12288 x 4096 11.7 / 14.4 (1), 13.1 / 14.7 (8); 16384 x 4096 16.1 / 16.4 (1), 17.3 / 16.5 (4),
+  // 18.9 / 16.7 (8); 8192 x 12288 22.2 / 22.9 (1), 23.9 / 23.1 (4), 25.9 / 23.6 (8); 32768 x 4096 30.3 / 27.1 (1), 36.1 / 27.7 (8).
   if (T > 8 || (double)N * (double)K * (double)(T + 4) >= 640e6) return fb4_launch_linear_tc(ctx, x, T, ld, codes, meta, N, K, bias, out, out_ld, out_dtype, stream);
   Linear p{};
   p.x = static_cast<const uint16_t*>(x);

@@ -13,10 +13,10 @@
 //   product  one warp issues D_tile += A x
 //   x        6 warps bring x into shared memory, in chunks where it is too large for it
 //
-// Bound: for large weights the decode (12288 x 12288, 16 rows, of 64 000 cycles: 45 000; the ALU pipe is busy 57 % and the issue slots 61 % of the
+// Bound: for large weights the decode (12288 x 12288, 16 rows, of 62 000 cycles: 43 000; the ALU pipe is busy 59 % and the issue slots 62 % of the
 // time), then start and end (11 000 until x and the first codes are there, 10 000 from the last decoded value to the last result: the last
 // products, the cluster's slowest CTA, the join).  For small ones the latter alone.  16 rows with 24576 x 12288 weights take 55 us (3.1 TB/s), 12288 x 12288
-// takes 29.7 for one row, 36 for 32, 41 for 64 (470 TFLOP/s), 6152 x 1568 12.3 for 61.  The products of half an item leave every 500 to 640 cycles, at most
+// takes 29.6 for one row, 32 for 16, 40.6 for 64 (475 TFLOP/s), 6152 x 1568 11.7 for 61.  The products of half an item leave every 500 to 640 cycles, at most
 // 200 of which are the tensor core's: instructions of one warp among those that decode.
 // On the way (12288 x 12288): A through shared memory 61 us for 32 rows, against 49 with a row to a thread in tensor memory; x brought in by 4 warps 89 for 64
 // rows; 4 buffers of A, one a group, 36.9 for one row.  Leaving out the decode gives 28.9 for one row, the metadata's loads too 26.1, the stores to tensor
