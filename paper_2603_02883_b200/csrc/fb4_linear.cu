@@ -1,4 +1,4 @@
-// Products of up to 8 rows with FB4 weights: y[t][n] = sum_k x[t][k] w[n][k] + bias[n].  More rows, and large weights: fb4_linear_tc.cu.
+// Products of up to 16 rows with FB4 weights: y[t][n] = sum_k x[t][k] w[n][k] + bias[n].  More rows, and large weights: fb4_linear_tc.cu.
 //
 // The weights are the long side, so their rows are the M side of mma.sync m16n8k16 and the rows of x its N side: a warp reads a weight once
 // for all of them.  A lane decodes a block of 32 channels of two rows at a time from two 16-byte words of codes, straight into
@@ -48,6 +48,8 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// NT: groups of 8 rows of x
+template <int NT>
 __global__ void __launch_bounds__(kWarps * 32, kResident) fb4_linear_kernel(const __grid_constant__ Linear p) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t book[64];
@@ -70,7 +72,9 @@ __global__ void __launch_bounds__(kWarps * 32, kResident) fb4_linear_kernel(cons
     codes[r] = p.codes + at * 16;
     meta[r] = p.meta + at;
   }
-  float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  float acc[NT][4];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
   uint4 cw[kAhead][2];
   uint16_t mt[kAhead][2];                           // joined only when used: that would wait for the load
   const int32_t whole = p.nb / 4;                   // steps whose four blocks all exist; there is at most one more
@@ -108,7 +112,7 @@ __global__ void __launch_bounds__(kWarps * 32, kResident) fb4_linear_kernel(cons
                    "r"(prmt(u.z, u.w, 0x5410u)), "r"(prmt(u.z, u.w, 0x7632u)) : "memory");
     }
     __syncthreads();
-    uint32_t x_step = x_at + (lane & (4 * p.wide - 1)) * 16;
+    uint32_t x_step = x_at + (NT > 1 ? lane : lane & (4 * p.wide - 1)) * 16;
     for (int32_t s0 = c0; s0 < c1; s0 += kAhead) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
@@ -127,10 +131,13 @@ __global__ void __launch_bounds__(kWarps * 32, kResident) fb4_linear_kernel(cons
           uint32_t a[2][4];
           decode_word(words[0][w], sc[0], a[0]);
           decode_word(words[1][w], sc[1], a[1]);
-          uint4 b = make_uint4(0, 0, 0, 0);
-          if (x_there) b = fb4blk::lds_v4(x_step + (i * 4 + w) * x_piece);
-          mma_bf16(acc, a[0][0], a[1][0], a[0][1], a[1][1], b.x, b.y);
-          mma_bf16(acc, a[0][2], a[1][2], a[0][3], a[1][3], b.z, b.w);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            uint4 b = make_uint4(0, 0, 0, 0);
+            if (NT > 1 || x_there) b = fb4blk::lds_v4(x_step + (i * 4 + w) * x_piece + n * 512);
+            mma_bf16(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], b.x, b.y);
+            mma_bf16(acc[n], a[0][2], a[1][2], a[0][3], a[1][3], b.z, b.w);
+          }
         }
       }
       x_step += kAhead * 4 * x_piece;
@@ -147,7 +154,9 @@ __global__ void __launch_bounds__(kWarps * 32, kResident) fb4_linear_kernel(cons
   float* sums = reinterpret_cast<float*>(smem);
   constexpr int kLd = kRows + 4;                    // the quads' rows of x fall into different banks
 #pragma unroll
-  for (int k = 0; k < 4; ++k) sums[(2 * t + (k & 1)) * kLd + warp * 16 + g + 8 * (k >> 1)] = acc[k];
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sums[(8 * n + 2 * t + (k & 1)) * kLd + warp * 16 + g + 8 * (k >> 1)] = acc[n][k];
   if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   else __syncthreads();
   for (int32_t i = split * (kWarps * 32) + threadIdx.x; i < n_tok * kRows; i += p.splits * (kWarps * 32)) {
@@ -178,14 +187,15 @@ __global__ void __launch_bounds__(kWarps * 32, kResident) fb4_linear_kernel(cons
   if (p.splits > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-constexpr int kJoinBytes = 8 * (kRows + 4) * 4;
+constexpr int kJoinBytes = 8 * (kRows + 4) * 4;                 // for 8 rows of x
 
 }  // namespace
 
 // Opt-in to the dynamic shared memory, and how many CTAs are resident at a time in clusters of 1 to 8 (fewer than without clusters: a
 // cluster lies in one group of SMs).
 cudaError_t fb4_linear_prepare_device(int32_t* slots) {
-  cudaError_t e = cudaFuncSetAttribute(fb4_linear_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
+  cudaError_t e = cudaFuncSetAttribute(fb4_linear_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_linear_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
   for (int s = 1; s <= kMaxSplits && e == cudaSuccess; ++s) {
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[1];
@@ -198,7 +208,7 @@ cudaError_t fb4_linear_prepare_device(int32_t* slots) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, fb4_linear_kernel, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&n, fb4_linear_kernel<2>, &cfg);
     slots[s] = n * s > 1 ? n * s : 1;
   }
   return e;
@@ -209,7 +219,10 @@ cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int6
   // The tensor-memory kernel starts 3 us later, but takes less for a weight, and next to nothing for another row.  This against that one, us:
   // 4096 x 4096 weights 5.8 / 8.6 (1 row), 7.2 / 8.9 (8 rows); 12288 x 4096 11.7 / 14.4 (1), 13.1 / 14.7 (8); 16384 x 4096 16.1 / 16.4 (1), 17.3 / 16.5 (4),
   // 18.9 / 16.7 (8); 8192 x 12288 22.2 / 22.9 (1), 23.9 / 23.1 (4), 25.9 / 23.6 (8); 32768 x 4096 30.3 / 27.1 (1), 36.1 / 27.7 (8).
-  if (T > 8 || (double)N * (double)K * (double)(T + 4) >= 640e6) return fb4_launch_linear_tc(ctx, x, T, ld, codes, meta, N, K, bias, out, out_ld, out_dtype, stream);
+  // Of 9 to 16 rows this one takes small weights only: 2048 x 2048 6.1 / 7.6, 6152 x 1568 8.0 / 9.2, 6144 x 2048 7.9 / 8.7, but 4096 x 4096 8.8 / 8.9, 8192 x 4096
+  // 13.7 / 11.6, and 1536 x 8960, few rows of many channels, 10.7 / 9.6.
+  const double size = (double)N * (double)K;
+  if (T > 16 || (T > 8 && (size > 13e6 || K > 4096)) || size * (double)(T + 4) >= 640e6) return fb4_launch_linear_tc(ctx, x, T, ld, codes, meta, N, K, bias, out, out_ld, out_dtype, stream);
   Linear p{};
   p.x = static_cast<const uint16_t*>(x);
   p.ld = ld;
@@ -238,12 +251,13 @@ cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int6
     }
   }
   const int32_t mine = (steps + p.splits - 1) / p.splits;
-  for (p.wide = 1; p.wide < 8 && p.wide < T; p.wide *= 2) {}
+  for (p.wide = 1; p.wide < 16 && p.wide < T; p.wide *= 2) {}
   const int per_step = 256 * p.wide;
   const int32_t most = kXBytes / per_step / kAhead * kAhead;
   p.chunk = mine < most ? (mine + kAhead - 1) / kAhead * kAhead : most;
   int smem = p.chunk * per_step;
-  if (smem < kJoinBytes) smem = kJoinBytes;
+  const int join = T > 8 ? 2 * kJoinBytes : kJoinBytes;
+  if (smem < join) smem = join;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
   cfg.gridDim = dim3((unsigned)(tiles * p.splits));
@@ -257,5 +271,5 @@ cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int6
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.numAttrs = 1;
   }
-  return cudaLaunchKernelEx(&cfg, fb4_linear_kernel, p);
+  return T > 8 ? cudaLaunchKernelEx(&cfg, fb4_linear_kernel<2>, p) : cudaLaunchKernelEx(&cfg, fb4_linear_kernel<1>, p);
 }

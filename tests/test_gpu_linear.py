@@ -157,7 +157,7 @@ def test_captured_on_another_stream_and_strided_output(f, T):
     assert torch.equal(o[:, :500], f.linear(x, w))
 
 
-@pytest.mark.parametrize("size", [(1, 12288, 12288), (5, 9000, 8192), (12, 9000, 8192), (32, 12288, 8192), (64, 7000, 8192), (96, 9500, 2048)], ids=lambda s: ".".join(map(str, s)))
+@pytest.mark.parametrize("size", [(1, 12288, 12288), (5, 9000, 8192), (12, 9000, 8192), (16, 3000, 4096), (14, 1500, 8192), (32, 12288, 8192), (64, 7000, 8192), (96, 9500, 2048)], ids=lambda s: ".".join(map(str, s)))
 def test_many_items_again_and_again(f, size):
     """several tiles, chunks and laps of every ring, with other traffic in memory between: each run gives the same bits"""
     T, N, K = size
