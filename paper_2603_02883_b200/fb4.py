@@ -680,8 +680,11 @@ class Fb4:
         return Quantized(codes, meta)
 
     def linear(self, x, w: Quantized, bias=None, dtype=torch.bfloat16):
-        """x [T][K] (bfloat16) times FB4 weights w [N][K], plus bias [N]: [T][N].  Made for few rows; w as quantize_weights gives it"""
+        """x [T][K] (bfloat16) times FB4 weights w [N][K], plus bias [N]: [T][N].  Made for few rows; w as quantize_weights gives it
+        (a tensor with a residual is refused: its salient rows are more than their codes)"""
         codes, meta = w.codes, w.meta
+        if w.res_codes is not None:
+            raise ValueError("weights with a residual are not supported")
         code = _out_dtype(dtype)
         if x.dtype is not torch.bfloat16 or x.dim() != 2 or codes.dim() != 2 or meta.dim() != 2:
             raise ValueError("expected x bfloat16 [T][K] and weights [N][K]")

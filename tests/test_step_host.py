@@ -223,7 +223,8 @@ def test_linear_in_the_binding(monkeypatch):
     assert f.linear(x, w).shape == (4, 10) and f.linear(x, w, bias=x[0, :10], dtype=torch.float32).dtype == torch.float32 and len(f.calls) == 2
     swap = lambda **k: fb4.Quantized(**{**dict(codes=w.codes, meta=w.meta), **k})  # noqa: E731
     for bad in ((x.float(), w), (x[0], w), (x[:, :32], w), (x.t().contiguous().t(), w), (x, swap(codes=w.codes.short())), (x, swap(meta=w.meta[:9])), (x, swap(meta=w.meta.int())),
-                (x, swap(codes=torch.zeros(32, 10, dtype=torch.uint8).t())), (x, w, x[0, :9]), (x, w, x[0, :10].float()), (x, w, x[:, 0]), (x, w, None, torch.float64)):
+                (x, swap(codes=torch.zeros(32, 10, dtype=torch.uint8).t())), (x, w, x[0, :9]), (x, w, x[0, :10].float()), (x, w, x[:, 0]), (x, w, None, torch.float64),
+                (x, swap(salient_idx=torch.zeros(1, dtype=torch.int32), res_codes=w.codes[:1], res_meta=w.meta[:1]))):
         with pytest.raises(ValueError):
             f.linear(*bad)
     assert len(f.calls) == 2
