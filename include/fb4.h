@@ -571,8 +571,10 @@ typedef struct {
  * exponent at most, half a step otherwise.  Codes behind the new tokens are left alone.
  *   page_table, max_pages, kv_len, q_start, n_seqs, max_q : as in fb4_cache_attention (clamped and reported alike; a page outside
  *            [0, n_pages) gets no tokens and raises bit 1 of the status word); n_seqs <= 2^28.  The pages that are written to belong to one
- *            sequence each (precondition).  Positions below 0 (n_q above kv_len) are left out
- *   T      : rows of q, k and v; rows of no sequence are left out, and so are their rows of q_out
+ *            sequence each (precondition).  Positions below 0 (n_q above kv_len) are left out; where q_start falls, which is reported,
+ *            so may rows of the sequences around be
+ *   T      : rows of q, k and v; rows of no sequence are left out, and so are their rows of q_out.  With T, n_seqs, max_q or max_pages 0 nothing is
+ *            done, and nothing reported
  *   q_heads: 0 = no q (q, q_gain and q_out are ignored)
  *   other arguments as in fb4_qk_norm_rope; k and v have cache->n_heads heads.  Works with every context configuration
  */

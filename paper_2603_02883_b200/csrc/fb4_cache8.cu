@@ -44,8 +44,11 @@ struct Append8 {
 };
 
 // Sequence b owns the CTAs from q_start[b] / 16 + 2 b on: its blocks, the first of which may hold tokens already, are at most rows / 16 + 2, so
-// these runs hold them, and together they are not many more than the blocks that there are.
-__device__ __forceinline__ int64_t first_cta(const Append8& p, int32_t b) { return __ldg(p.q_start + b) / kPlaces + 2 * (int64_t)b; }
+// these runs hold them, and together they are not many more than the blocks that there are.  q_start is clamped as its rows are.
+__device__ __forceinline__ int64_t first_cta(const Append8& p, int32_t b) {
+  const int32_t at = __ldg(p.q_start + b);
+  return (at < 0 ? 0 : at < p.total_q ? at : p.total_q) / kPlaces + 2 * (int64_t)b;
+}
 
 __device__ __forceinline__ int32_t owner(const Append8& p, int64_t cta) {
   const int lane = threadIdx.x & 31;
@@ -163,8 +166,10 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
     b = owner(p, blockIdx.x);
     const int64_t d = blockIdx.x - first_cta(p, b);
     nth = d < 0 || d > 0x3ffffff ? 0x3ffffff : (int32_t)d;
+    // where q_start falls a sequence may have no CTA, so that the reports are dealt out by number (there are two CTAs a sequence at least)
+    if (blockIdx.x < (uint32_t)p.n_seqs && blockIdx.y == 0 && threadIdx.x == 0) fb4att::sequence(p, (int32_t)blockIdx.x, true);
   }
-  const fb4att::Sequence sq = fb4att::sequence(p, b, nth == 0 && blockIdx.y == 0 && threadIdx.x == 0);
+  const fb4att::Sequence sq = fb4att::sequence(p, b, p.ctas > 0 && nth == 0 && blockIdx.y == 0 && threadIdx.x == 0);
   const int32_t first = sq.kv - sq.n_q, from = first > 0 ? first : 0;
   const int64_t base = ((int64_t)(from >> 4) + nth) << 4;                 // position of the block's first place
   if (base >= sq.kv || sq.n_q == 0) return;
