@@ -261,9 +261,10 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
   }
   __syncthreads();
 
-  uint32_t cs_at[4];                                  // this lane's couples in a token's row
+  const uint32_t cs_base = fb4blk::smem_u32(cs_smem);
+  uint32_t cs_at[4];                                  // this lane's couples in a token's row, counted from its start: turns exchange pieces of a row
 #pragma unroll
-  for (int n = 0; n < 4; ++n) cs_at[n] = fb4blk::smem_u32(cs_smem) + cs_piece(INTER ? 2 * (on ? j : 0) + (n & 1) + (n < 2 ? 0 : p.D / 8) : 4 * (on ? j : 0) + n) * 16;
+  for (int n = 0; n < 4; ++n) cs_at[n] = cs_piece(INTER ? 2 * (on ? j : 0) + (n & 1) + (n < 2 ? 0 : p.D / 8) : 4 * (on ? j : 0) + n) * 16;
   for (; at < units; at += step) {
     uint16_t* out = nullptr;
     if (u.kind == kQ) out = p.q.out + (row0 + g) * p.q.out_ld + (int64_t)u.head * p.D + 8 * j;
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(kWarps * 32, LG == 16 ? 2 : 5) fb4_cache8_appe
           const int32_t i = real ? place : lo;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint4 v = fb4blk::lds_v4((cs_at[k] ^ (cs_turn<LG>(i) * 16)) + i * couples * 16);
+            const uint4 v = fb4blk::lds_v4((cs_at[k] ^ (cs_turn<LG>(i) * 16)) + (cs_base + i * couples * 16));
             t.c[2 * k] = __uint_as_float(v.x); t.s[2 * k] = __uint_as_float(v.y);
             t.c[2 * k + 1] = __uint_as_float(v.z); t.s[2 * k + 1] = __uint_as_float(v.w);
           }
