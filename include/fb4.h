@@ -569,6 +569,9 @@ typedef struct {
  *     code = 128 + x / 2^s rounded to the nearest integer, ties to even (beyond 127 * 2^58: saturated)
  * Tokens in front are rounded in the same way to the new exponent; a block that is filled token by token is off by one step of its last
  * exponent at most, half a step otherwise.  Codes behind the new tokens are left alone.
+ * A block's exponent never falls while it holds tokens in front of the new ones, and it is not known which tokens it came from: drafted tokens
+ * of large values that are rejected afterwards (fb4_cache_plan, keep) cost the block's kept and later tokens their lower bits, within the
+ * bounds above, until its first place is written anew.
  *   page_table, max_pages, kv_len, q_start, n_seqs, max_q : as in fb4_cache_attention (clamped and reported alike; a page outside
  *            [0, n_pages) gets no tokens and raises bit 1 of the status word); n_seqs <= 2^28.  The pages that are written to belong to one
  *            sequence each (precondition).  Positions below 0 (n_q above kv_len) are left out; where q_start falls, which is reported,
