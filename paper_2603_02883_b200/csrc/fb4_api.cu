@@ -307,7 +307,7 @@ int fb4_init(fb4_ctx** out, int device, const uint8_t* formatbook, const uint32_
   ctx->attend_error = fb4_attend_prepare_device();
   ctx->append8_error = fb4_cache8_prepare_device();
   ctx->plan_error = fb4_plan_prepare_device();
-  ctx->linear_error = fb4_linear_prepare_device(ctx->linear_slots);
+  ctx->linear_error = fb4_linear_prepare_device(ctx->linear_clusters);
   if (ctx->linear_error == cudaSuccess) ctx->linear_error = fb4_linear_tc_prepare_device(ctx->linear_tc_clusters);
   ctx->fast_table_bytes = fast_bytes;
   cudaGetLastError();

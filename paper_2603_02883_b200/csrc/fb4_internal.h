@@ -56,8 +56,8 @@ struct fb4_ctx {
   cudaError_t append8_error;     // the same for the append to the 8-bit cache
   cudaError_t plan_error;        // the same for the plan of a step
   cudaError_t linear_error;      // the same for the products with FB4 weights
-  int32_t linear_tc_clusters[9]; // tensor-core kernel, per cluster size: clusters that are resident at a time
-  int32_t linear_slots[9];       // kernel of few rows, per cluster size: CTAs that are resident at a time
+  int32_t linear_tc_clusters[9]; // tensor-core kernel, per cluster size: clusters that are resident at a time, 0 where the size does not fit
+  int32_t linear_clusters[9];    // the same for the kernel of few rows
   int sm_count;
   void* d_topk_scratch;          // histograms and counters of the multi-CTA top-k selection (fb4_topk.cu)
   uint32_t* d_status;            // device status word (bit 0: a TMA wait ran out of tries; bit 1: an index argument out of range)
@@ -185,12 +185,23 @@ cudaError_t fb4_launch_attend_few(const Fb4Attend& a, cudaStream_t stream);
 cudaError_t fb4_launch_attend_generic(const fb4_ctx* ctx, const Fb4Attend& a, cudaStream_t stream);
 
 // products with FB4 weights (fb4_linear.cu: few rows, and the choice)
-cudaError_t fb4_linear_prepare_device(int32_t* slots);
+cudaError_t fb4_linear_prepare_device(int32_t* clusters);
+// Per cluster size from 1 to 8: how many clusters of a kernel are resident at a time (a cluster lies in one group of SMs), 0 where the size does not
+// fit this device or the part of it that the process has.  An error if CTAs on their own do not fit.
+cudaError_t fb4_clusters_at_once(const void* kernel, int threads, int smem, int32_t* clusters);
+// CTAs that share the channels of a row tile: one of the cluster sizes that fit
+int32_t fb4_linear_splits(const int32_t* clusters, int64_t N, int64_t K);
 cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
                               int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream);
 
 // the same on the fifth-generation tensor cores (fb4_linear_tc.cu)
 cudaError_t fb4_linear_tc_prepare_device(int32_t* clusters);
+struct Fb4LinearTcPlan {
+  int32_t rows;             // rows of x at a time, a multiple of 16
+  int32_t splits;           // CTAs of a cluster: one of the sizes that fit
+  int32_t quarters;         // 32 rows of W each, to a cluster
+};
+Fb4LinearTcPlan fb4_linear_tc_plan(const int32_t* clusters, int64_t T, int64_t N, int64_t K);
 cudaError_t fb4_launch_linear_tc(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
                                  int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream);
 

@@ -191,27 +191,49 @@ constexpr int kJoinBytes = 8 * (kRows + 4) * 4;                 // for 8 rows of
 
 }  // namespace
 
-// Opt-in to the dynamic shared memory, and how many CTAs are resident at a time in clusters of 1 to 8 (fewer than without clusters: a
-// cluster lies in one group of SMs).
-cudaError_t fb4_linear_prepare_device(int32_t* slots) {
-  cudaError_t e = cudaFuncSetAttribute(fb4_linear_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_linear_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
-  for (int s = 1; s <= kMaxSplits && e == cudaSuccess; ++s) {
+cudaError_t fb4_clusters_at_once(const void* kernel, int threads, int smem, int32_t* clusters) {
+  for (int s = 1; s <= kMaxSplits; ++s) {
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)s;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)(s * 1024));
-    cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = kXBytes;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, fb4_linear_kernel<2>, &cfg);
-    slots[s] = n * s > 1 ? n * s : 1;
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+    clusters[s] = e == cudaSuccess && n > 0 ? n : 0;
+    if (s == 1 && clusters[s] == 0) return e != cudaSuccess ? e : cudaErrorInvalidConfiguration;
   }
+  return cudaSuccess;
+}
+
+// Opt-in to the dynamic shared memory, and the clusters that are resident at a time.
+cudaError_t fb4_linear_prepare_device(int32_t* clusters) {
+  cudaError_t e = cudaFuncSetAttribute(fb4_linear_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fb4_linear_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
+  if (e == cudaSuccess) e = fb4_clusters_at_once(reinterpret_cast<const void*>(fb4_linear_kernel<2>), kWarps * 32, kXBytes, clusters);
   return e;
+}
+
+// The least of waves x work of a CTA, its start and its part of the join counted as 4 steps.
+int32_t fb4_linear_splits(const int32_t* clusters, int64_t N, int64_t K) {
+  const int64_t tiles = (N + kRows - 1) / kRows, steps = (K / 32 + 3) / 4;
+  double best = 1e300;
+  int32_t splits = 1;
+  for (int s = 1; s <= kMaxSplits && (s == 1 || steps / s >= 2); ++s) {
+    if (clusters[s] == 0) continue;
+    const int64_t waves = (tiles + clusters[s] - 1) / clusters[s];
+    const double cost = (double)waves * (double)((steps + s - 1) / s + 4);
+    if (cost < best * 0.97) {
+      best = cost;
+      splits = s;
+    }
+  }
+  return splits;
 }
 
 cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
@@ -236,20 +258,9 @@ cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int6
   p.nb = (int32_t)(K / 32);
   p.out_dtype = out_dtype;
   p.tables = ctx->d_tables;
-  const int32_t* slots = ctx->linear_slots;
+  p.splits = fb4_linear_splits(ctx->linear_clusters, N, K);
   const int64_t tiles = (N + kRows - 1) / kRows;
   const int32_t steps = (p.nb + 3) / 4;
-  // splits: the least of waves x work of a CTA, its start and its part of the join counted as 4 steps
-  double best = 1e300;
-  p.splits = 1;
-  for (int s = 1; s <= kMaxSplits && (s == 1 || steps / s >= 2); ++s) {
-    const int64_t waves = (tiles * s + slots[s] - 1) / slots[s];
-    const double cost = (double)waves * ((steps + s - 1) / s + 4);
-    if (cost < best * 0.97) {
-      best = cost;
-      p.splits = s;
-    }
-  }
   const int32_t mine = (steps + p.splits - 1) / p.splits;
   for (p.wide = 1; p.wide < 16 && p.wide < T; p.wide *= 2) {}
   const int per_step = 256 * p.wide;

@@ -407,25 +407,34 @@ __global__ void __launch_bounds__(kThreads, 1) fb4_linear_tc_kernel(const __grid
 
 }  // namespace
 
-// Opt-in to the dynamic shared memory, and how many clusters of 1 to 8 CTAs are resident at a time (a cluster lies in one group of SMs).
+// Opt-in to the dynamic shared memory, and the clusters that are resident at a time.
 cudaError_t fb4_linear_tc_prepare_device(int32_t* clusters) {
   cudaError_t e = cudaFuncSetAttribute(fb4_linear_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-  for (int s = 1; s <= kMaxSplits && e == cudaSuccess; ++s) {
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)s;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(s * 1024));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kBytes;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, fb4_linear_tc_kernel, &cfg);
-    clusters[s] = n > 1 ? n : 1;
-  }
+  if (e == cudaSuccess) e = fb4_clusters_at_once(reinterpret_cast<const void*>(fb4_linear_tc_kernel), kThreads, kBytes, clusters);
   return e;
+}
+
+// Rows of x in passes of equal size; of the cluster sizes that fit, the one with the fewest items for a CTA, a wave's start and join counted as 3.
+Fb4LinearTcPlan fb4_linear_tc_plan(const int32_t* clusters, int64_t T, int64_t N, int64_t K) {
+  Fb4LinearTcPlan p{0, 1, 1};
+  const int64_t z = (T + kMaxRows - 1) / kMaxRows, each = (T + z - 1) / z;
+  p.rows = (int32_t)((each + 15) / 16 * 16);
+  const int64_t steps = (K / 32 + 7) / 8, most = kDCols / p.rows * 4, quarters = (N + 31) / 32;
+  double best = 1e300;
+  for (int c = 1; c <= kMaxSplits && (c == 1 || c <= steps); c *= 2) {
+    const int64_t at_once = clusters[c];
+    if (at_once == 0) continue;
+    int64_t q = (quarters * z + at_once - 1) / at_once;
+    if (q > most) q = most;
+    const int64_t grid = (quarters + q - 1) / q * z, waves = (grid + at_once - 1) / at_once;
+    const double cost = (double)waves * (double)((q + 3) / 4 * ((steps + c - 1) / c) + 3);
+    if (cost < best) {
+      best = cost;
+      p.splits = c;
+      p.quarters = (int32_t)q;
+    }
+  }
+  return p;
 }
 
 cudaError_t fb4_launch_linear_tc(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
@@ -445,25 +454,12 @@ cudaError_t fb4_launch_linear_tc(const fb4_ctx* ctx, const void* x, int64_t T, i
   p.wide_out = reinterpret_cast<uintptr_t>(out) % (4 * item_bytes) == 0 && out_ld % 4 == 0;
   p.tables = ctx->d_tables;
   p.status = ctx->d_status;
-  // rows of x in passes of equal size
-  const int64_t z = (T + kMaxRows - 1) / kMaxRows, each = (T + z - 1) / z;
-  p.rows = (int32_t)((each + 15) / 16 * 16);
-  const int32_t steps = (p.nb + 7) / 8, most = kDCols / p.rows * 4;
-  const int64_t quarters = (N + 31) / 32;
-  // the cluster size with the fewest items for a CTA; a wave's start and join count as 3
-  double best = 1e300;
-  for (int c = 1; c <= kMaxSplits && (c == 1 || c <= steps); c *= 2) {
-    const int64_t at_once = ctx->linear_tc_clusters[c];
-    int64_t q = (quarters * z + at_once - 1) / at_once;
-    if (q > most) q = most;
-    const int64_t grid = (quarters + q - 1) / q * z, waves = (grid + at_once - 1) / at_once;
-    const double cost = (double)waves * ((q + 3) / 4 * ((steps + c - 1) / c) + 3);
-    if (cost < best) {
-      best = cost;
-      p.splits = c;
-      p.quarters = (int32_t)q;
-    }
-  }
+  const Fb4LinearTcPlan plan = fb4_linear_tc_plan(ctx->linear_tc_clusters, T, N, K);
+  p.rows = plan.rows;
+  p.splits = plan.splits;
+  p.quarters = plan.quarters;
+  const int32_t steps = (p.nb + 7) / 8;
+  const int64_t quarters = (N + 31) / 32, z = (T + kMaxRows - 1) / kMaxRows;
   const int32_t mine = (steps + p.splits - 1) / p.splits, step_bytes = p.rows * 512;
   const int32_t tiles = (p.quarters + 3) / 4;
   p.stages = (int64_t)mine * tiles < kStages ? mine * tiles : kStages;
