@@ -337,8 +337,10 @@ int fb4_quantize_weights(fb4_ctx* ctx, const void* w_bf16, int64_t N, int64_t K,
  * Products of rows of x with FB4 weights (App. D.2: 4-bit codes are decoded on the fly with the block scale applied):
  *     out[t][n] = sum_k x[t][k] * w[n][k] + bias[n],   w = value(codes, meta) of fb4_quantize_weights (or fb4_quantize)
  * without the weights ever being written out: 4.5 bits of memory traffic per weight.  Made for few rows (single and drafted tokens of a decoding
- * batch); any number is taken, and every 96 rows read the weights again.  Products are exact, sums float32 in an order that depends on
- * the sizes alone, the result is rounded once to the type of out.  A row of x that holds an infinity or NaN affects its own row of out only.
+ * batch); any number is taken, and every 96 rows read the weights again.  Products are exact, sums float32, the result is rounded
+ * once to the type of out.  The order of the sums depends on the sizes, T among them (a row may get other bits when other rows stand beside it),
+ * and on how many CTAs the device holds at a time: the same sizes on the same device give the same bits.  A row of x that holds an infinity or NaN
+ * affects its own row of out only.
  *   x       : device bfloat16 [T][ld_elems], T at most 2^22, 16-byte aligned, ld_elems a multiple of 8 (>= K)
  *   codes, meta : device [N][K/2], [N][K/32], 16-byte aligned; K a multiple of 32, at least 32.  An element scale above 2^61 is read as
  *             2^61, a weight to within 2^-70, and the sums are in steps of 2^-85 where they are smaller than float32 steps
