@@ -523,6 +523,8 @@ class PageTables:
         for t in (pt, kv, fp, nf):
             if t.dtype is not torch.int32 or not t.is_contiguous():
                 raise ValueError("page_table, kv_len, free_pages and n_free must be contiguous int32")
+        if self.page_tokens >> 31 or any(size >> 31 for size in (*pt.shape, *fp.shape)):        # passed as 32 bits
+            raise ValueError("page_tokens and the sizes of the tables must be in [0, 2^31)")
         c = (pt.data_ptr(), pt.shape[1], self.page_tokens, kv.data_ptr()), (fp.data_ptr(), fp.shape[0], nf.data_ptr()), pt.shape[0]
         object.__setattr__(self, "_c", (c, _device_of(pt, kv, fp, nf)))
 
