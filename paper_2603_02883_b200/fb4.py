@@ -798,6 +798,8 @@ class Fb4:
         n = kv_len.numel()
         if page_table.dim() != 2 or page_table.shape[0] != n or kv_len.dim() != 1 or q_start.dim() != 1 or q_start.numel() != n + 1:
             raise ValueError("expected page_table [n_seqs][max_pages], kv_len [n_seqs] and q_start [n_seqs + 1]")
+        if n >> 31 or page_table.shape[1] >> 31:                    # passed as 32 bits
+            raise ValueError("n_seqs and max_pages must be below 2^31")
         for t in (page_table, kv_len, q_start):
             if t.dtype is not torch.int32 or not t.is_contiguous():
                 raise ValueError("page_table, kv_len and q_start must be contiguous int32")

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2603_02883_b200 import fb4
+from test_attention_binding import context
 
 
 def i32(*shape):
@@ -33,3 +34,11 @@ def test_sizes_of_the_tables(monkeypatch, which):
     monkeypatch.setattr(torch.Tensor, "data_ptr", lambda self: 0)
     with pytest.raises(ValueError):
         fb4.PageTables(*args, 16)
+
+
+def test_a_page_table_wider_than_32_bits(monkeypatch):
+    """as the appends and the attention read it"""
+    f = context(monkeypatch)
+    with pytest.raises(ValueError):
+        f._sequences(torch.empty((3, (1 << 32) + 8), dtype=torch.int32, device="meta"), i32(3), i32(4))
+    assert f._sequences(i32(3, 8), i32(3), i32(4)) == 3
