@@ -1,4 +1,4 @@
-// What the attention kernels over the paged caches share: the sequence and mask arithmetic and the output store.
+// What the kernels over the paged caches and those of the products with FB4 weights share: sequences and masks, decoders, softmax, the output store.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -127,6 +127,12 @@ __device__ __forceinline__ void decode_bytes(uint32_t w0, uint32_t w1, const Int
   o[1] = fma_bf16x2(prmt(w0, 0u, 0x4341u), s.f, s.c);
   o[2] = fma_bf16x2(w1 & 0x00ff00ffu, s.f, s.c);
   o[3] = fma_bf16x2(prmt(w1, 0u, 0x4341u), s.f, s.c);
+}
+
+// the warp-wide product of the kernels of few rows: 16 x 16 by 16 x 8
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 __device__ __forceinline__ float exp2_approx(float x) {
