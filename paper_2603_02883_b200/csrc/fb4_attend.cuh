@@ -147,6 +147,10 @@ __device__ __forceinline__ float exp2_approx(float x) {
 // two operands of a product have one type; in two bf16 pieces p would keep 16 bits, at twice the second product's instructions and twice P's
 // room.  Each weight is off by at most 2^-8 of itself, as much as the rounding of a bf16 result, and the errors of a row's weights
 // mostly cancel; the sum that divides is that of the unrounded ones, so lse does not see it.
+// Over 8 bits the codes alone are half-precision numbers, so p could keep 11 bits with the block's power of two multiplied into it.  But these powers lie up to
+// 2^127 apart, side by side, and half precision holds 2^40: with one reference for all rows, a row whose weight lies on blocks of small scales would get
+// zeros.  Each row would need a second running maximum, of score plus exponent, and another multiplication for each weight for the sum that divides.
+// As it is, the relative error of causal prompts in bf16 is 0.0019 against 0.0016 with weights in float32, nearly all of which is the result's rounding.
 //
 // The running maximum is a rounded product, score * scale; a probability takes the exact one, in one operation with the
 // subtraction of the maximum.  The two differ by half a step of the maximum, which cancels between numerator and denominator as long

@@ -652,8 +652,10 @@ Fb4AttendPlan fb4_attend_plan(const fb4_ctx* ctx, int int8, int32_t q_heads, int
     const int64_t tiles = (span + kTile - 1) / kTile + 1;
     const int64_t most = (tiles + 2 * kWarpsFew - 1) / (2 * kWarpsFew);
     int64_t s = slots / units;                                      // one wave
-    // sequences of unlike lengths: pieces of 1024 tokens even them out, of 96 tiles in 8 bits (64 of 131 to 8191 tokens: 142 us in pieces of
-    // 1024, 103 of 2048, 101 as it is, 107 of 8192)
+    // Sequences of unlike lengths: pieces of 1024 tokens even them out, of 96 tiles in 8 bits.  us in pieces of 32, 64, 96, 128, 256 tiles, 8 heads of
+    // 128 where nothing else is said: 64 sequences of 131 to 8191 tokens 141, 103, 100, 100, 107 (heads of 64: 79, 63, 59, 60, 73); 96 of 50 to 8000 183, 135, 133, 148, 148;
+    // 16 of 200 to 32000 97, 97, 97, 101, 118; 128 of 100 to 2000 69, 57, 57, 56, 56; 256 of 16 to 4000, 2 heads, 63, 58, 58, 58, 58; 32 of 1000 to 16000, 4 heads of 64, 39, 40, 37,
+    // 39, 39.  64 of 4096 each, where nothing is to be evened out, are 1.15 waves: 110, 105, 116, 116, 116.
     const int64_t piece = int8 ? 96 : 32, fine = tiles / piece < 8 ? tiles / piece : 8;
     if (s < fine) s = fine;
     if (s > most) s = most;

@@ -9,9 +9,11 @@
 // distributed shared memory, always in the same order.
 //
 // Bound: the ALU pipe (decode: 10 operations per 8 weights, two thirds of all of its) while all warps are at work, CTAs that are two or three to
-// an SM, and for small weights the start.  One row with 4096 x 4096 weights takes 5.8 us, 8192 x 8192 16.3 (2.4 TB/s), 12288 x 12288 31.1 (2.7 TB/s, and
-// 28.5 out of L2).  For the last, one CTA per SM with its rows dealt out evenly came out slower (39.6), and so did clusters of three
-// (41.7: they are not spread evenly) and 16 warps an SM with loads four steps ahead (49.8 in two waves).
+// an SM, and for small weights the start.  Weights out of memory, one row: 4096 x 4096 take 6.6 us, 12288 x 4096 12.9, 8192 x 8192 16.5 to 17.0 (2.2
+// TB/s), 16384 x 4096 16.9, the largest; 16 rows with 6144 x 2048 8.5.  For 12288 x 4096 and 8192 x 8192, one row: 2 CTAs an SM take 16.0 and 16.4, 4 (which spill)
+// 13.8 and 17.7; steps loaded one ahead 13.2 and 16.6, four ahead (spills) 14.9 and 18.8.  8192 x 8192 in clusters of 1, 2, 3, 4, 6 (the rule's choice), 8: 39.7,
+// 21.9, 20.2, 15.8, 16.7, 19.3.  Of an older form, for weights that are the other kernel's now (12288 x 12288, 31.1): one CTA per SM with its rows dealt out
+// evenly 39.6, 16 warps an SM with loads four steps ahead 49.8 in two waves.
 #include "fb4_attend.cuh"
 #include "fb4_block.cuh"
 
@@ -233,11 +235,13 @@ int32_t fb4_linear_splits(const int32_t* clusters, int64_t N, int64_t K) {
 
 cudaError_t fb4_launch_linear(const fb4_ctx* ctx, const void* x, int64_t T, int64_t ld, const uint8_t* codes, const uint16_t* meta, int64_t N,
                               int64_t K, const void* bias, void* out, int64_t out_ld, int out_dtype, cudaStream_t stream) {
-  // The tensor-memory kernel starts 3 us later, but takes less for a weight, and next to nothing for another row.  This against that one, us:
-  // 4096 x 4096 weights 5.8 / 8.6 (1 row), 7.2 / 8.9 (8 rows); 12288 x 4096 11.7 / 14.4 (1), 13.1 / 14.7 (8); 16384 x 4096 16.1 / 16.4 (1), 17.3 / 16.5 (4),
-  // 18.9 / 16.7 (8); 8192 x 12288 22.2 / 22.9 (1), 23.9 / 23.1 (4), 25.9 / 23.6 (8); 32768 x 4096 30.3 / 27.1 (1), 36.1 / 27.7 (8).
-  // Of 9 to 16 rows this one takes small weights only: 2048 x 2048 6.1 / 7.6, 6152 x 1568 8.0 / 9.2, 6144 x 2048 7.9 / 8.7, but 4096 x 4096 8.8 / 8.9, 8192 x 4096
-  // 13.7 / 11.6, and 1536 x 8960, few rows of many channels, 10.7 / 9.6.
+  // The tensor-memory kernel starts 2.5 us later, but takes less for a weight, and next to nothing for another row.  This against that one, us, weights out of
+  // memory: 4096 x 4096 6.6 / 9.1 (1 row), 7.8 / 9.3 (8 rows); 12288 x 4096 12.9 / 14.9 (1), 15.1 / 15.5 (8); 16384 x 4096 16.9 / 16.8 (1), 18.1 / 16.9 (4),
+  // 19.7 / 17.2 (8); 8192 x 8192 17.0 / 17.9 (1), 19.5 / 18.1 (8); 8192 x 12288 22.4 / 23.0 (1), 23.9 / 23.2 (4), 26.0 / 23.8 (8); 32768 x 4096 30.3 / 27.1 (1),
+  // 36.1 / 27.7 (8).  Of 9 to 16 rows this one takes small weights only.  16 rows: 640 x 640 6.3 / 6.6, 2048 x 2048 6.4 / 8.0, 4096 x 2048 7.2 / 8.4, 8192 x 1536 8.5 /
+  // 9.0, 12288 x 1024 8.4 / 9.8, 6152 x 1568 9.1 / 9.9, 6144 x 2048 8.5 / 9.5, 256 x 4096 6.4 / 7.0, 1024 x 4096 7.7 / 8.0, 3200 x 4096 9.6 / 9.6 (9 rows 9.2 / 9.4), 3200 x
+  // 3200 9.4 / 9.4; beyond, 4096 x 4096 9.8 / 9.8, 14000 x 1536 12.2 / 10.1, 8192 x 4096 15.5 / 12.8, and few rows of many channels, 1536 x 6144 10.0 / 9.0, 1024 x 8192
+  // 12.0 / 9.5, 512 x 12288 16.4 / 10.6.
   const double size = (double)N * (double)K;
   if (T > 16 || (T > 8 && (size > 13e6 || K > 4096)) || size * (double)(T + 4) >= 640e6) return fb4_launch_linear_tc(ctx, x, T, ld, codes, meta, N, K, bias, out, out_ld, out_dtype, stream);
   Linear p{};

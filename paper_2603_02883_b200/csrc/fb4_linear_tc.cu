@@ -13,15 +13,18 @@
 //   product  one warp issues D_tile += A x
 //   x        6 warps bring x into shared memory, in chunks where it is too large for it
 //
-// Bound: for large weights the decode (12288 x 12288, 16 rows, of 62 000 cycles: 43 000; the ALU pipe is busy 59 % and the issue slots 62 % of the
-// time), then start and end (11 000 until x and the first codes are there, 10 000 from the last decoded value to the last result: the last
-// products, the cluster's slowest CTA, the join).  For small ones the latter alone.  16 rows with 24576 x 12288 weights take 55 us (3.1 TB/s), 12288 x 12288
-// takes 29.6 for one row, 32 for 16, 40.6 for 64 (475 TFLOP/s), 6152 x 1568 11.7 for 61.  The products of half an item leave every 500 to 640 cycles, at most
-// 200 of which are the tensor core's: instructions of one warp among those that decode.
-// On the way (12288 x 12288): A through shared memory 61 us for 32 rows, against 49 with a row to a thread in tensor memory; x brought in by 4 warps 89 for 64
-// rows; 4 buffers of A, one a group, 36.9 for one row.  Leaving out the decode gives 28.9 for one row, the metadata's loads too 26.1, the stores to tensor
-// memory 25.3, the products 21.5: copies, start and end alone.  First copies before the set-up: 32.9.  x earlier gives nothing, though the products wait 11 000
-// cycles for it: in parts with a barrier each +0.5 us, its first pieces by all warps before the set-up +0.5, by asynchronous copies and reordered in place +3.
+// Bound: for large weights no part alone, but the issue slots that decode, metadata and products share (62 % of them are taken, the ALU pipe is busy 59 %
+// of the time), then start and end; for small weights these two alone.  12288 x 12288 with one row takes 29.5 us, with 64 40.3 (479 TFLOP/s), 24576 x 12288 with 16
+// 55.1 (3.1 TB/s), 6152 x 1568 with 61 11.7.  Copies of the kernel that leave parts out (wrong results), for the first three:
+//   decode's arithmetic 26.0 / 36.1 / 46.9; the metadata's loads too 22.3 / 33.8 / 38.4; the stores to tensor memory too 20.8 / 32.7 / 35.1; the
+//   products too 17.8 / 31.5 / 29.9: copies, x, start and end alone.  Metadata alone 28.8 / 36.6 / 52.1, products alone 27.5 / 38.1 / 51.1.
+// The decoding warps are at work, waits among it, for 43 000 of 62 000 cycles (12288 x 12288, 16 rows); 11 000 pass until x and the first codes are there, 10 000 from
+// the last decoded value to the last result: the last products, the cluster's slowest CTA, the join.  The products of half an item leave every 500 to 640 cycles,
+// at most 200 of which are the tensor core's: instructions of one warp among those that decode.
+// On the way (12288 x 12288), each against the kernel of its time: A through shared memory 61 us for 32 rows, 49 with a row to a thread in tensor memory; x brought
+// in by 4 warps 89 for 64 rows; 4 buffers of A, one a group, 36.9 for one row, 31.9 with 7; first copies before the set-up 32.9.  x earlier gives nothing, though
+// the products wait 11 000 cycles for it: in parts with a barrier each +0.5 us, its first pieces by all warps before the set-up +0.5, by asynchronous
+// copies and reordered in place +3.
 #include "fb4_attend.cuh"
 #include "fb4_staging.cuh"
 #include "fb4_tcgen05.cuh"
